@@ -641,6 +641,104 @@ edb_status edb_probe_copy(const void* src, void* dst, int64_t bytes, int32_t n_w
 
 void edb_exec_free(edb_exec_t* e);
 
+/* ---- token operators: words into vectors, logits into answers and losses ---- */
+/* What stands before and behind the cells of a model over words: the input
+ * rows x come from a table by token ids, the states' vocabulary logits (a
+ * product with an output matrix) become log probabilities, alternatives or a
+ * loss, and gradients go back.
+ *
+ * Common to these calls:
+ *   - all arrays are device memory; matrices are row-major with a row stride
+ *     in elements (>= the row's length) and need only be aligned to their
+ *     elements; dtype is EDB_F32 or EDB_BF16 and every sum is fp32 (a bf16
+ *     result is rounded to nearest even once);
+ *   - a token id outside [0, vocab) stands for no token (-1 by convention):
+ *     nothing is read for it;
+ *   - the work is enqueued on `stream` on the current device; no call waits,
+ *     allocates or keeps anything, so all may be captured into a HIP graph.  A
+ *     workspace (device, 16-byte aligned, of at least the bytes that the
+ *     matching *_bytes call gives; NULL where that is 0) is written before it
+ *     is read and must not be shared by calls that can overlap;
+ *   - results do not depend on timing: the same inputs give the same bits;
+ *   - n == 0 rows are allowed.
+ * Errors: EDB_ERR_INVALID (NULL, sizes, strides, alignment, dtype, overlapping
+ * input and output, a workspace that is too small), EDB_ERR_UNSUPPORTED (a
+ * size beyond the stated limits), EDB_ERR_HIP. */
+
+/* out[i][:] = scale * table[ids[i]][:], a zero row where there is no token.
+ * table [vocab x dim], out [n x dim], each of its own dtype; vocab <= 2^30,
+ * dim <= 2^20, n * dim <= 2^38. */
+edb_status edb_embed(const int32_t* ids, int32_t n, const void* table, int32_t table_dtype, int32_t vocab,
+                     int32_t dim, int64_t table_stride, float scale, void* out, int32_t out_dtype,
+                     int64_t out_stride, void* stream);
+
+/* The gradient of edb_embed with respect to its table:
+ *   dtable[v][:] = scale * sum over the i with ids[i] == v of dout[i][:],
+ * zero rows for words that do not occur.  With accumulate != 0 the sums are
+ * added to the rows of dtable instead and the other rows are left alone. */
+edb_status edb_embed_grad_bytes(int32_t n, int32_t vocab, int32_t dim, int64_t* bytes);
+edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* dout, int32_t dout_dtype, int32_t vocab,
+                          int32_t dim, int64_t dout_stride, float scale, int32_t accumulate, void* dtable,
+                          int32_t dtable_dtype, int64_t dtable_stride, void* workspace, int64_t workspace_bytes,
+                          void* stream);
+
+#define EDB_LOGPROBS_MAX_TOP 64
+
+/* Log probabilities of given tokens under softmax(logits / temperature), with
+ * the entropy and the best alternatives of every row, in one pass.
+ *   logits   [n x vocab], vocab <= 2^30; a token is masked out by -inf
+ *   ids      int32[n], or NULL: no given tokens (logprob must be NULL then)
+ *   logprob  float[n] or NULL: ln p of the given token (-inf if masked out)
+ *   entropy  float[n] or NULL: -sum p ln p
+ *   stats    float[n][2] or NULL: the largest logit m and
+ *            ln sum exp((x - m) / temperature), for edb_logprobs_grad
+ *   top_ids, top_logprobs  int32 and float [n][top], 0 <= top <=
+ *            EDB_LOGPROBS_MAX_TOP: the largest logits, the lowest id first
+ *            among equal ones; without masked ones, -1 and -inf past the end
+ * A row whose id (where ids are given) is no token is not read: 0 everywhere,
+ * no alternatives.  A row that is masked out whole has log probability -inf,
+ * entropy 0, stats (-inf, 0) and no alternatives.  A row with a NaN or +inf has
+ * no distribution: NaN, stats (NaN, NaN); its alternatives are listed by value,
+ * NaN left out, with log probabilities of NaN. */
+edb_status edb_logprobs_bytes(int32_t n, int32_t vocab, int32_t dtype, int32_t top, int64_t* bytes);
+edb_status edb_logprobs(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
+                        const int32_t* ids, float temperature, int32_t top, float* logprob, float* entropy,
+                        float* stats, int32_t* top_ids, float* top_logprobs, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/* The logits' gradient of sum_i g_logprob[i] logprob[i] + g_entropy[i] entropy[i]:
+ *   dlogits[i][j] = (g_logprob (1[j == id] - p_j) - g_entropy p_j (ln p_j + entropy)) / temperature,
+ * with the stats and entropy that edb_logprobs gave for the same logits, ids
+ * and temperature.  g_logprob and g_entropy are float[n] or NULL (zero);
+ * entropy may be NULL with g_entropy.  dlogits has the logits' dtype; it may be
+ * the logits themselves (same address and stride).  A row without a token,
+ * with both gradients 0 or masked out whole gives zeros. */
+edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
+                             const int32_t* ids, float temperature, const float* stats, const float* entropy,
+                             const float* g_logprob, const float* g_entropy, void* dlogits, int64_t dlogits_stride,
+                             void* stream);
+
+#define EDB_DISTILL_MAX_TOP 256
+
+/* Distillation from a teacher of which only the best logits are kept.  Per row,
+ * q = softmax(top_logits / temperature) over the listed tokens (entries that
+ * are no token left out, equal ids counted as one with their masses added),
+ * p = softmax(logits / temperature) over the vocabulary, and
+ *   loss[i]       = temperature^2 sum_v q_v (ln q_v - ln p_v),
+ *   dlogits[i][v] = weight[i] temperature (p_v - q_v),
+ * the gradient of sum_i weight[i] loss[i].
+ *   top_ids, top_logits  int32 and float [n][top], 1 <= top <= EDB_DISTILL_MAX_TOP
+ *   weight   float[n] or NULL (1)
+ *   loss     float[n] (without the weight)
+ *   dlogits  the logits' dtype, or NULL (the loss alone); it may be the logits
+ *            themselves (same address and stride)
+ * A row of weight 0 or without a listed token is not read: loss 0, zero
+ * gradient.  A listed token that the student masks out (-inf) makes the loss
+ * +inf; a row that the student masks out whole has a zero gradient besides. */
+edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
+                       const int32_t* top_ids, const float* top_logits, int32_t top, float temperature,
+                       const float* weight, float* loss, void* dlogits, int64_t dlogits_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,6 +35,7 @@ FLOW_VARIANT = 100
 SPLIT_VARIANTS = (18, 19, 20)            # split tile (fp32 through bf16 pieces)
 TEAM_VARIANT = 101                        # team launch (the tail of the schedule in one launch)
 NOALLOC_SCRATCH_BYTES = 32 << 20   # EDB_NOALLOC_SCRATCH_BYTES
+LOGPROBS_MAX_TOP, DISTILL_MAX_TOP = 64, 256
 
 # every symbol include/edb.h declares
 EXPORTS = [
@@ -48,6 +49,8 @@ EXPORTS = [
     "edb_exec_check", "edb_exec_validate", "edb_exec_free", "edb_forward", "edb_stream_release",
     "edb_forward_noalloc",
     "edb_split_phase_bytes", "edb_split_phase", "edb_probe_mfma", "edb_probe_copy",
+    "edb_embed", "edb_embed_grad_bytes", "edb_embed_grad",
+    "edb_logprobs_bytes", "edb_logprobs", "edb_logprobs_grad", "edb_distill",
 ]
 
 
@@ -159,6 +162,18 @@ def load():
         "edb_split_phase": (C.c_int32, [vp, vp, vp, vp, vp, C.c_int64, vp, P(C.c_float), C.c_int32]),
         "edb_probe_mfma": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, P(C.c_float), vp, P(C.c_float)]),
         "edb_probe_copy": (C.c_int32, [vp, vp, C.c_int64, C.c_int32, vp, P(C.c_float)]),
+        "edb_embed": (C.c_int32, [vp, C.c_int32, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_float, vp,
+                                  C.c_int32, C.c_int64, vp]),
+        "edb_embed_grad_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, P(C.c_int64)]),
+        "edb_embed_grad": (C.c_int32, [vp, C.c_int32, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_float,
+                                       C.c_int32, vp, C.c_int32, C.c_int64, vp, C.c_int64, vp]),
+        "edb_logprobs_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, P(C.c_int64)]),
+        "edb_logprobs": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, C.c_float, C.c_int32, vp, vp,
+                                     vp, vp, vp, vp, C.c_int64, vp]),
+        "edb_logprobs_grad": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, C.c_float, vp, vp, vp,
+                                          vp, vp, C.c_int64, vp]),
+        "edb_distill": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, vp, C.c_int32, C.c_float, vp,
+                                    vp, vp, C.c_int64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

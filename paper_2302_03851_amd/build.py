@@ -21,7 +21,7 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 
 HOST_SRC = ["graph.cpp", "schedule.cpp", "learn.cpp", "plan.cpp", "pqplan.cpp", "team.cpp", "forward.cpp"]
-HIP_SRC = ["exec.hip", "team_f32.hip", "team_bf16.hip", "diag.hip"]
+HIP_SRC = ["exec.hip", "team_f32.hip", "team_bf16.hip", "diag.hip", "embed.hip", "logits.hip"]
 
 # -ffp-contract=off: the policy learner's floating-point updates round as written
 CXXFLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-ffp-contract=off", "-I", os.path.join(ROOT, "include")]

@@ -1,0 +1,742 @@
+"""Token operators (embedding and its gradient, log probabilities and theirs,
+distillation) against the definitions in 64 bits, and their refusals.
+
+Tolerances.  u = 2^-24 is fp32's rounding unit; a bf16 result adds half a unit
+in its last place, at most 2^-8 of the value (8 significant bits).
+* An fp32 sum of k terms, in any order, is off by at most k u sum |term|.
+* ln sum exp: each exponent (x - m) / T is off by 4 u of itself, the
+  exponential by 4 u more, the sum (every thread adds at most V / 64 terms, then a tree) by
+  (V / 64 + 16) u, the logarithm by 4 u of its own value.  So l is off by at
+  most LSE = (V / 64 + 24 + 4 w) u + 4 u l, w being the p-weighted mean of |x - m| / T;
+  a log probability by LSE + 4 u (|x - m| / T + |lp|); the entropy by
+  LSE + (V / 64 + 16) u H plus, per term p |y|, 8 u (1 + |y|).
+* p is off by LSE + 8 u (1 + |lp|) of itself.
+"""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from paper_2302_03851_amd import _lib as L
+
+torch = pytest.importorskip("torch")
+gpu = pytest.mark.gpu
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+INF = math.inf
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _half_ulp(ref, dtype):
+    return ref.abs() * (2.0 ** -8 if dtype == BF16 else U)
+
+
+def _close(got, ref, tol):
+    """Equal where not finite, within tol elsewhere."""
+    got = got.double()
+    fine = torch.isfinite(ref)
+    assert torch.equal(torch.isnan(got), torch.isnan(ref))
+    assert torch.equal(torch.isfinite(got), fine)
+    assert torch.equal(got[~fine & ~torch.isnan(ref)], ref[~fine & ~torch.isnan(ref)])
+    tol = torch.as_tensor(tol, device=ref.device, dtype=torch.float64).nan_to_num(0.0)
+    off = (got - ref).abs()[fine] - torch.broadcast_to(tol, ref.shape)[fine]
+    assert off.numel() == 0 or float(off.max()) <= 0, (float(off.max()), float((got - ref).abs()[fine].max()))
+
+
+def _view(t, pad, shift):
+    """The same matrix as a view with `pad` more elements a row, starting
+    `shift` elements into its memory; what lies between is NaN."""
+    n, m = t.shape
+    mem = torch.full((n * (m + pad) + shift + 16,), float("nan"), dtype=t.dtype, device=t.device)
+    v = mem[shift:shift + n * (m + pad)].view(n, m + pad)[:, :m]
+    v.copy_(t)
+    return v, mem
+
+
+# ---- embedding ---------------------------------------------------------------
+
+EMBED = [(1, 5, 1), (7, 3, 7), (64, 100, 8), (112, 50, 64), (33, 1000, 100), (1000, 77, 256), (300, 9, 513), (65, 40, 1032)]
+
+
+def _some_ids(n, V, g, spread):
+    """Ids in range, with ones outside on both sides among them."""
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    if spread:
+        ids = (ids.double() / V).pow(3).mul(V).to(torch.int32)
+        for k, bad in enumerate((-1, V, -2 ** 31, 2 ** 31 - 1)):
+            ids[k + 2::11] = bad
+    return ids
+
+
+@gpu
+@pytest.mark.parametrize("table,out", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n,V,E", EMBED)
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 0), (3, 1)])
+def test_embed(n, V, E, table, out, pad, shift):
+    """One fp32 product and one rounding: the same bits as torch's."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(n + E)
+    w, _ = _view(torch.randn((V, E), generator=g, device="cuda").to(table), pad, shift)
+    ids = _some_ids(n, V, g, True)
+    there = (ids >= 0) & (ids < V)
+    ref = torch.where(there[:, None], w[torch.where(there, ids, 0).long()].float() * 1.7, 0.0).to(out)
+    dst, mem = _view(torch.zeros((n, E), dtype=out, device="cuda"), pad, shift)
+    before = mem.clone()
+    got = tokens.embed(ids, w, 1.7, out=dst)
+    assert torch.equal(got, ref)
+    dst.copy_(before[shift:shift + n * (E + pad)].view(n, E + pad)[:, :E])
+    assert torch.equal(mem.view(torch.uint8), before.view(torch.uint8))     # nothing beside the rows
+
+
+@gpu
+def test_embed_empty_and_values():
+    from paper_2302_03851_amd import tokens
+    w = torch.tensor([[1.0, -INF], [float("nan"), 3.0]], device="cuda")
+    ids = torch.tensor([1, 0, -1], dtype=torch.int32, device="cuda")
+    got = tokens.embed(ids, w, 2.0)
+    assert torch.isnan(got[0, 0]) and got[0, 1] == 6 and got[1, 0] == 2 and got[1, 1] == -INF and not got[2].any()
+    assert tokens.embed(ids[:0], w).shape == (0, 2)
+
+
+@gpu
+def test_embed_offsets_past_32_bits():
+    """Rows beyond 2^31 and 2^32 elements, read, written and summed into."""
+    from paper_2302_03851_amd import tokens
+    E, far = 8, 1 << 31
+    mem = torch.empty(2 * far + E, dtype=BF16, device="cuda")
+    w = mem.as_strided((3, E), (far, 1))
+    w.copy_(torch.arange(24, device="cuda").view(3, E))
+    ids = torch.tensor([2, 0, 1, 2], dtype=torch.int32, device="cuda")
+    assert torch.equal(tokens.embed(ids, w), w[ids.long()])
+    x = tokens.embed(ids, w, dtype=F32)
+    tokens.embed_grad(ids, x, 3, 0.5, out=w)
+    ref = torch.stack([x[1] * 0.5, x[2] * 0.5, x[0]]).to(BF16)
+    assert torch.equal(w, ref)
+    tokens.embed(ids[:3], x[:3].contiguous(), 1.0, out=w)     # three rows of x, far apart
+    assert torch.equal(w, x[ids[:3].long().clamp(max=2)].to(BF16))
+
+
+def _grad_check(ids, dout, V, scale, out_dtype, got, old=None):
+    """Any order of the terms, the scale, the addition and the rounding."""
+    there = (ids >= 0) & (ids < V)
+    at, d = ids[there].long(), dout[there].double()
+    ref = torch.zeros((V, dout.shape[1]), dtype=torch.float64, device="cuda").index_add_(0, at, d) * scale
+    mag = torch.zeros_like(ref).index_add_(0, at, d.abs()) * abs(scale)
+    k = torch.zeros(V, dtype=torch.float64, device="cuda").index_add_(0, at, torch.ones(len(at), dtype=torch.float64, device="cuda"))
+    if old is not None:
+        ref += old.double()
+    _close(got, ref, (k[:, None] + 2) * U * mag + 2 * U * ref.abs() + _half_ulp(ref, out_dtype) * 1.01 + 1e-40)
+    return k
+
+
+GRADS = [(0, 5, 8), (1, 1, 1), (3, 2, 7), (112, 50, 64), (700, 1000, 100), (1627, 300, 128), (4097, 33, 40),
+         (9000, 70000, 16), (20000, 513, 33), (33000, 2, 264)]
+
+
+@gpu
+@pytest.mark.parametrize("src,dst", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n,V,E", GRADS)
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_grad(n, V, E, src, dst, accumulate):
+    from paper_2302_03851_amd import tokens
+    g = _gen(n + V)
+    ids = _some_ids(n, V, g, n > 3)
+    dout = torch.randn((n, E), generator=g, device="cuda").to(src)
+    old = torch.randn((V, E), generator=g, device="cuda").to(dst)
+    runs = []
+    for _ in range(2):
+        out = old.clone() if accumulate else torch.full((V, E), float("nan"), dtype=dst, device="cuda")
+        runs.append(tokens.embed_grad(ids, dout, V, -1.3, out=out, accumulate=accumulate))
+    assert torch.equal(runs[0].view(torch.uint8), runs[1].view(torch.uint8))
+    k = _grad_check(ids, dout, V, -1.3, dst, runs[0], old if accumulate else None)
+    if accumulate:
+        assert torch.equal(runs[0][k == 0], old[k == 0])
+
+
+@gpu
+@pytest.mark.parametrize("n", [1, 64, 3000, 5000, 70000])
+@pytest.mark.parametrize("kind", ["same", "two", "none", "ordered", "falling"])
+def test_embed_grad_runs(n, kind):
+    """Words with all the rows, with half of them, no words, and one row each."""
+    from paper_2302_03851_amd import tokens
+    V, E = 70001, 24
+    i = torch.arange(n, device="cuda", dtype=torch.int32)
+    ids = {"same": i * 0 + 69999, "two": (i % 2) * 70000, "none": i * 0 - 1, "ordered": i, "falling": 70000 - i}[kind]
+    dout = torch.randn((n, E), generator=_gen(n), device="cuda")
+    got = tokens.embed_grad(ids, dout, V)
+    _grad_check(ids, dout, V, 1.0, F32, got)
+
+
+@gpu
+@pytest.mark.parametrize("n,V,E,pad,shift", [(500, 60, 64, 8, 0), (500, 60, 65, 3, 1), (6000, 900, 64, 8, 8), (6000, 900, 7, 1, 1)])
+def test_embed_grad_strides(n, V, E, pad, shift):
+    """Padded and shifted rows on both sides; NaN between them stays out and stays there."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(5)
+    ids = _some_ids(n, V, g, True)
+    dout, _ = _view(torch.randn((n, E), generator=g, device="cuda"), pad, shift)
+    out, mem = _view(torch.zeros((V, E), device="cuda"), pad, shift)
+    before = mem.clone()
+    tokens.embed_grad(ids, dout, V, out=out)
+    _grad_check(ids, dout, V, 1.0, F32, out)
+    out.copy_(before[shift:shift + V * (E + pad)].view(V, E + pad)[:, :E])
+    assert torch.equal(mem.view(torch.uint8), before.view(torch.uint8))
+
+
+@gpu
+def test_embed_grad_differences():
+    """sum(dout * embed(W)) is linear in W: its differences are the gradient's products."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(9)
+    V, E, n = 40, 24, 300
+    ids = _some_ids(n, V, g, True)
+    w = torch.randn((V, E), generator=g, device="cuda")
+    dout = torch.randn((n, E), generator=g, device="cuda")
+    d = tokens.embed_grad(ids, dout, V, 0.7).double()
+    for _ in range(5):
+        step = torch.randn((V, E), generator=g, device="cuda")
+        f = [(tokens.embed(ids, w + s * step, 0.7).double() * dout.double()).sum() for s in (1, -1)]
+        mag = (dout.double().abs() * 4).sum() * 0.7 * 8 * U      # the two lookups' roundings, |w| + |step| below 4 + 4 on the whole
+        assert abs(float((f[0] - f[1]) / 2 - (d * step.double()).sum())) <= float(mag) + 1e-5 * float(d.abs().max())
+
+
+# ---- log probabilities -------------------------------------------------------
+
+
+def _rows(kind, n, V, dtype, g):
+    x = 3 * torch.randn((n, V), generator=g, device="cuda")
+    if kind == "masked":
+        x[torch.rand((n, V), generator=g, device="cuda") < 0.6] = -INF
+        x[0] = -INF                                    # nothing left
+        if n > 1:
+            x[1] = -INF
+            x[1, V // 2] = 1.5                         # one left
+        if n > 2:
+            x[2, V // 3:] = -INF
+    elif kind == "ties":
+        x = x.div(3).round()
+        x[0] = 0.25
+        if n > 1:
+            x[1] = torch.where(torch.arange(V, device="cuda") % 2 == 0, 0.0, -0.0)
+    elif kind == "lowest":
+        x[:] = torch.finfo(dtype).min
+        x[n // 2:, V // 2] = torch.finfo(dtype).max
+    elif kind == "rising":
+        x = torch.arange(V, device="cuda", dtype=F32).mul(8.0 / V).repeat(n, 1)
+    elif kind == "falling":
+        x = torch.arange(V, 0, -1, device="cuda", dtype=F32).mul(8.0 / V).repeat(n, 1)
+    elif kind == "broken":
+        x[0, V // 2] = float("nan")
+        if n > 1:
+            x[1, V - 1] = INF
+        if n > 2:
+            x[2] = float("nan")
+        if n > 3:
+            x[3, ::3] = float("nan")
+            x[3, 1::3] = -INF
+    return x.to(dtype)
+
+
+def _reference(x, ids, T):
+    """Per row in 64 bits: lp, entropy, m, l and the tolerance of l."""
+    x = x.double()
+    m = x.amax(1, keepdim=True)
+    ref = torch.where(m == -INF, 0.0, m)
+    y = (x - ref) / T
+    e = torch.exp(y)
+    S = e.sum(1, keepdim=True)
+    empty = S == 0
+    l = torch.where(empty, 0.0, torch.log(S))
+    lp = torch.where(empty, -INF, y - l)
+    p = torch.exp(lp)
+    h = -torch.where(p > 0, p * lp, torch.where(torch.isnan(p), p, 0.0)).sum(1)
+    w = torch.where(p > 0, p * y.abs(), 0.0).sum(1, keepdim=True)
+    V = x.shape[1]
+    tol_l = (V / 64 + 24 + 4 * w) * U + 4 * U * l.abs()
+    tol_h = tol_l[:, 0] + (V / 64 + 16) * U * h.abs() + (torch.where(p > 0, p * 8 * U * (1 + y.abs()) * (1 + y.abs()), 0.0)).sum(1)
+    return lp, p, y, h, m, l, tol_l, tol_h
+
+
+def _check_logprobs(x, ids, T, top, r):
+    n, V = x.shape
+    lp, p, y, h, m, l, tol_l, tol_h = _reference(x, ids, T)
+    there = torch.ones(n, dtype=torch.bool, device="cuda") if ids is None else (ids >= 0) & (ids < V)
+    broken = torch.isnan(l[:, 0])
+    tol_lp = tol_l + 4 * U * (torch.where(torch.isfinite(y), y.abs(), 0.0) + torch.where(torch.isfinite(lp), lp.abs(), 0.0))
+    lp = lp.float().double()       # -inf past fp32's range
+    if ids is not None:
+        at = torch.where(there, ids, 0).long()[:, None]
+        _close(r.logprob, torch.where(there, lp.gather(1, at)[:, 0], 0.0), tol_lp.gather(1, at)[:, 0])
+    else:
+        assert r.logprob is None
+    _close(r.entropy, torch.where(there, h, 0.0), tol_h)
+    stats = torch.cat([torch.where(broken[:, None], float("nan"), m), l], 1)
+    _close(r.stats, torch.where(there[:, None], stats, 0.0), torch.cat([0 * tol_l, tol_l], 1))
+    # the list: by value, then by index; no NaN, nothing masked out
+    xs = x.float() + 0.0
+    key = torch.where(torch.isnan(xs), -INF, xs)
+    order = torch.sort(key, dim=1, descending=True, stable=True)
+    k = min(top, V)
+    want = torch.full((n, top), -1, dtype=torch.int64, device="cuda")
+    want[:, :k] = torch.where((order.values[:, :k] > -INF) & there[:, None], order.indices[:, :k], -1)
+    assert torch.equal(r.top_ids.long(), want)
+    _close(r.top_logprobs, torch.where(want < 0, -INF, lp.gather(1, want.clamp(min=0))), tol_lp.gather(1, want.clamp(min=0)))
+
+
+def _given(n, V, g):
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    for k, bad in enumerate((-1, V, -2 ** 31, 2 ** 31 - 1)):
+        ids[k + 4::9] = bad
+    return ids
+
+
+SIZES = [(1, 1), (3, 2), (5, 7), (4, 64), (9, 65), (6, 513), (30, 1000), (4, 4099), (5, 20000), (3, 70001)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", SIZES)
+@pytest.mark.parametrize("kind,top,T", [("plain", 0, 1.0), ("plain", 5, 0.7), ("masked", 20, 1.0), ("ties", 64, 2.0),
+                                        ("ties", 1, 1.0), ("lowest", 3, 1.0), ("rising", 64, 1.0), ("falling", 33, 1.0),
+                                        ("broken", 8, 1.0)])
+def test_logprobs(n, V, dtype, kind, top, T):
+    from paper_2302_03851_amd import tokens
+    g = _gen(V + top)
+    x = _rows(kind, n, V, dtype, g)
+    ids = _given(n, V, g)
+    runs = [tokens.logprobs(x, ids, T, top) for _ in range(2)]
+    for a, b in zip(*runs):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    _check_logprobs(x, ids, T, top, runs[0])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(1, 131072), (2, 131071), (70, 33000), (600, 9001), (1, 300007)])
+@pytest.mark.parametrize("top", [0, 50])
+def test_logprobs_split_rows(n, V, dtype, top):
+    """Few long rows and many, without given tokens, in views with odd strides."""
+    from paper_2302_03851_amd import tokens
+    x, _ = _view(_rows("plain", n, V, dtype, _gen(V)), 5, 3)
+    _check_logprobs(x, None, 1.3, top, tokens.logprobs(x, None, 1.3, top))
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["masked", "ties", "rising", "falling", "broken", "lowest"])
+def test_logprobs_split_kinds(kind):
+    """The odd rows of above where a row is long."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(3)
+    x = _rows(kind, 4, 131072, BF16, g)
+    ids = torch.tensor([5, 131071, 0, 70000], dtype=torch.int32, device="cuda")
+    _check_logprobs(x, ids, 1.0, 64, tokens.logprobs(x, ids, 1.0, 64))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logprobs_offsets_past_32_bits(dtype):
+    """Rows 2^31 elements apart: forward, gradient and distillation."""
+    from paper_2302_03851_amd import tokens
+    V, far = 1001, 1 << 31
+    x = torch.empty(2 * far + V, dtype=dtype, device="cuda").as_strided((3, V), (far, 1))
+    dense = _rows("plain", 3, V, dtype, _gen(1))
+    x.copy_(dense)
+    ids = torch.tensor([7, 1000, 3], dtype=torch.int32, device="cuda")
+    a, b = tokens.logprobs(x, ids, top=4), tokens.logprobs(dense, ids, top=4)
+    for s, t in zip(a, b):
+        assert torch.equal(s, t)
+    one = torch.ones(3, device="cuda")
+    q = torch.tensor([[1, 2], [3, -1], [1000, 0]], dtype=torch.int32, device="cuda"), torch.zeros((3, 2), device="cuda")
+    ref = tokens.distill(dense, *q)
+    got = tokens.distill(x, *q)
+    assert torch.equal(got.loss, ref.loss) and torch.equal(got.dlogits, ref.dlogits)
+    ref = tokens.logprobs_grad(dense, ids, b.stats, b.entropy, one, one)
+    assert tokens.logprobs_grad(x, ids, a.stats, a.entropy, one, one, out=x) is x
+    assert torch.equal(x, ref)
+
+
+def _grad_reference(x, ids, T, g1, g2):
+    lp, p, y, h, m, l, tol_l, tol_h = _reference(x, ids, T)
+    n, V = x.shape
+    there = (ids >= 0) & (ids < V)
+    out = ~there | ((g1 == 0) & (g2 == 0)) | (m[:, 0] == -INF)
+    one = torch.zeros_like(p).scatter_(1, torch.where(there, ids, 0).long()[:, None], 1.0)
+    g1, g2 = g1.double()[:, None], g2.double()[:, None]
+    plp = torch.where(p > 0, p * lp, torch.where(torch.isnan(p), p, 0.0))
+    d = (g1 * (one - p) - g2 * (plp + p * h[:, None])) / T
+    lpa = torch.where(p > 0, lp.abs(), 0.0)
+    rel = tol_l + 8 * U * (1 + lpa)
+    tol = p * (g1.abs() + g2.abs() * (lpa + h[:, None])) * (rel + 8 * U) + p * g2.abs() * (tol_h[:, None] + tol_l + 8 * U * (1 + lpa)) + 4 * U * g1.abs() * one
+    return torch.where(out[:, None], 0.0, d), tol / T
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", SIZES + [(300, 10007), (2, 131071)])
+@pytest.mark.parametrize("kind,T", [("plain", 0.7), ("masked", 1.0), ("lowest", 1.0), ("broken", 1.0), ("ties", 2.0)])
+def test_logprobs_grad(n, V, dtype, kind, T):
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = _rows(kind, n, V, dtype, g)
+    ids = _given(n, V, g)
+    r = tokens.logprobs(x, ids, T)
+    g1 = torch.randn(n, generator=g, device="cuda")
+    g2 = torch.randn(n, generator=g, device="cuda")
+    g1[2::5] = 0
+    g2[2::10] = 0
+    zero = torch.zeros_like(g1)
+    for a, b in ((g1, g2), (g1, None), (None, g2)):
+        ref, tol = _grad_reference(x, ids, T, zero if a is None else a, zero if b is None else b)
+        got = tokens.logprobs_grad(x, ids, r.stats, r.entropy, a, b, T)
+        _close(got, ref, tol + 1.01 * _half_ulp(ref, dtype) + 1e-38)
+    # odd strides on both sides, and in place
+    xv, _ = _view(x, 3, 1)
+    ov, mem = _view(torch.zeros_like(x), 5, 2)
+    before = mem.clone()
+    full = tokens.logprobs_grad(x, ids, r.stats, r.entropy, g1, g2, T)
+    tokens.logprobs_grad(xv, ids, r.stats, r.entropy, g1, g2, T, out=ov)
+    assert torch.equal(ov.contiguous().view(torch.uint8), full.view(torch.uint8))
+    ov.zero_()
+    before[2:2 + n * (V + 5)].view(n, V + 5)[:, :V] = 0
+    assert torch.equal(mem.view(torch.uint8), before.view(torch.uint8))
+    tokens.logprobs_grad(x, ids, r.stats, r.entropy, g1, g2, T, out=x)
+    assert torch.equal(x.view(torch.uint8), full.view(torch.uint8))
+
+
+@gpu
+def test_logprobs_grad_differences():
+    """Central differences of the 64-bit definition, step 1e-4: their own error
+    is below 1e-7, fp32's below 1e-5 of the gradients' scale."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(2)
+    n, V, T = 3, 40, 0.8
+    x = _rows("plain", n, V, F32, g)
+    ids = torch.tensor([3, 0, 39], dtype=torch.int32, device="cuda")
+    g1, g2 = torch.randn(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    r = tokens.logprobs(x, ids, T)
+    d = tokens.logprobs_grad(x, ids, r.stats, r.entropy, g1, g2, T).double()
+
+    def f(z):
+        lp = torch.log_softmax(z / T, 1)
+        given = lp.gather(1, ids.long()[:, None])[:, 0]
+        return (g1.double() * given - g2.double() * (lp.exp() * lp).sum(1)).sum()
+
+    for j in range(V):
+        step = torch.zeros((n, V), dtype=torch.float64, device="cuda")
+        step[:, j] = 1e-4
+        for i in range(n):
+            one = step.clone()
+            one[torch.arange(n) != i] = 0
+            diff = (f(x.double() + one) - f(x.double() - one)) / 2e-4
+            assert abs(float(diff - d[i, j])) <= 1e-5 * (1 + float(g1.abs().max() + 5 * g2.abs().max())) / T
+
+
+# ---- distillation ------------------------------------------------------------
+
+
+def _teacher(n, V, K, g, kind):
+    ids = torch.randint(0, V, (n, K), generator=g, device="cuda", dtype=torch.int32)      # equal ids among them
+    u = 4 * torch.randn((n, K), generator=g, device="cuda")
+    if kind == "distinct":
+        ids = torch.stack([torch.randperm(V, generator=g, device="cuda")[:K] if V >= K else
+                           torch.arange(K, device="cuda") % V for _ in range(n)]).to(torch.int32)
+    if kind == "short":
+        ids[:, K // 2:] = -1
+        u[:, K // 2:] = float("nan")                   # behind a masked entry
+        ids[::5, 0] = V
+        u[1::5, 0] = -INF                              # no mass
+        ids[2::5] = -1                                 # nothing listed
+        u[3::5] = -INF                                 # nothing left
+        u[4::5] = torch.finfo(F32).min
+    return ids, u
+
+
+def _distill_reference(x, ids, u, T, w):
+    n, V = x.shape
+    lp, p, y, h, m, l, tol_l, tol_h = _reference(x, None, T)
+    there = (ids >= 0) & (ids < V)
+    v = torch.where(there, u.double(), -INF)
+    tm = v.amax(1, keepdim=True)
+    e = torch.exp((v - torch.where(tm == -INF, 0.0, tm)) / T)
+    S = e.sum(1, keepdim=True)
+    out = (S[:, 0] == 0) | (w == 0)
+    q = torch.zeros_like(p).scatter_add_(1, torch.where(there, ids, 0).long(), e / torch.where(S == 0, 1.0, S))
+    lq = torch.where(q > 0, torch.log(torch.where(q > 0, q, 1.0)), 0.0)
+    loss = torch.where(out, 0.0, T * T * torch.where(q > 0, q * (lq - lp), torch.where(torch.isnan(q), q, 0.0)).sum(1))
+    loss = loss.float().double()   # inf past fp32's range
+    empty = m[:, 0] == -INF
+    w = w.double()[:, None]
+    d = torch.where((out | empty)[:, None], 0.0, w * T * (p - q))
+    lpa = torch.where((q > 0) & torch.isfinite(lp), lp.abs(), 0.0)
+    ya = torch.where((q > 0) & torch.isfinite(y), y.abs(), 0.0)
+    K = ids.shape[1]
+    spread = torch.where(torch.isfinite(v), (v - tm).abs() / T, 0.0)
+    q_rel = (K + 24) * U + (e / torch.where(S == 0, 1.0, S) * spread).sum(1, keepdim=True) * 8 * U
+    dense_spread = torch.zeros_like(p).scatter_reduce_(1, torch.where(there, ids, 0).long(), torch.where(e > 0, spread, 0.0), "amax")
+    q_rel = q_rel + 8 * U * dense_spread
+    tol_loss = T * T * torch.where(q > 0, q * ((q_rel + 8 * U) * (lq.abs() + lpa + 1) + tol_l + 8 * U * (1 + ya + lpa)), 0.0).sum(1) * 1.01
+    lpp = torch.where(p > 0, lp.abs(), 0.0)
+    tol_d = w.abs() * T * (p * (tol_l + 8 * U * (2 + lpp)) + q * (q_rel + 8 * U))
+    return loss, d, tol_loss + U * K * loss.abs(), tol_d
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", SIZES + [(40, 33000), (6, 131072), (3, 150001), (2, 300007)])
+@pytest.mark.parametrize("kind,teacher,K,T", [("plain", "distinct", 16, 2.0), ("masked", "short", 9, 1.0),
+                                              ("plain", "equal", 256, 0.7), ("lowest", "equal", 1, 1.0),
+                                              ("broken", "distinct", 5, 1.0)])
+def test_distill(n, V, dtype, kind, teacher, K, T):
+    from paper_2302_03851_amd import tokens
+    g = _gen(V + K)
+    x = _rows(kind, n, V, dtype, g)
+    ids, u = _teacher(n, V, K, g, teacher)
+    w = torch.rand(n, generator=g, device="cuda") - 0.3
+    w[3::7] = 0
+    for weight in (None, w):
+        ww = torch.ones_like(w) if weight is None else weight
+        loss, d, tol_loss, tol_d = _distill_reference(x, ids, u, T, ww)
+        runs = [tokens.distill(x, ids, u, T, weight) for _ in range(2)]
+        for a, b in zip(*runs):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        _close(runs[0].loss, loss, tol_loss)
+        _close(runs[0].dlogits, d, tol_d + 1.01 * _half_ulp(d, dtype) + 1e-38)
+        alone = tokens.distill(x, ids, u, T, weight, grad=False)
+        assert alone.dlogits is None and torch.equal(alone.loss.view(torch.uint8), runs[0].loss.view(torch.uint8))
+    # odd strides on both sides, and in place
+    xv, _ = _view(x, 3, 1)
+    ov, mem = _view(torch.zeros_like(x), 5, 2)
+    before = mem.clone()
+    full = runs[0]
+    got = tokens.distill(xv, ids, u, T, w, out=tokens.Distilled(torch.empty_like(loss, dtype=F32), ov))
+    assert torch.equal(got.loss.view(torch.uint8), full.loss.view(torch.uint8))
+    assert torch.equal(ov.contiguous().view(torch.uint8), full.dlogits.view(torch.uint8))
+    ov.zero_()
+    before[2:2 + n * (V + 5)].view(n, V + 5)[:, :V] = 0
+    assert torch.equal(mem.view(torch.uint8), before.view(torch.uint8))
+    tokens.distill(x, ids, u, T, w, out=tokens.Distilled(full.loss, x))
+    assert torch.equal(x.view(torch.uint8), full.dlogits.view(torch.uint8))
+
+
+@gpu
+def test_distill_differences():
+    """Central differences of the 64-bit loss (as for the log probabilities)."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(4)
+    n, V, T = 2, 30, 1.5
+    x = _rows("plain", n, V, F32, g)
+    ids, u = _teacher(n, V, 6, g, "equal")
+    w = torch.tensor([0.4, -1.1], device="cuda")
+    d = tokens.distill(x, ids, u, T, w).dlogits.double()
+
+    def f(z):
+        q = torch.zeros((n, V), dtype=torch.float64, device="cuda").scatter_add_(1, ids.long(), torch.softmax(u.double() / T, 1))
+        return (w.double() * T * T * (torch.xlogy(q, q) - q * torch.log_softmax(z / T, 1)).sum(1)).sum()
+
+    for i in range(n):
+        for j in range(V):
+            step = torch.zeros((n, V), dtype=torch.float64, device="cuda")
+            step[i, j] = 1e-4
+            assert abs(float((f(x.double() + step) - f(x.double() - step)) / 2e-4 - d[i, j])) <= 1e-5
+
+
+# ---- streams and graphs ------------------------------------------------------
+
+
+def _everything(seed):
+    """Inputs of each operator and a function that runs them into fixed outputs."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(seed)
+    n, V, E, K = 700, 9001, 72, 12
+    ids = _some_ids(n, V, g, True)
+    w = torch.randn((V, E), generator=g, device="cuda")
+    x = _rows("masked", n, V, BF16, g)
+    q = _teacher(n, V, K, g, "short")
+    g1 = torch.randn(n, generator=g, device="cuda")
+    # a few long rows, and enough rows for every path of the table's gradient
+    long = _rows("plain", 2, 100003, F32, g)
+    many = torch.randint(0, V, (30000,), generator=g, device="cuda", dtype=torch.int32)
+    dy = torch.randn((30000, 40), generator=g, device="cuda")
+
+    def go():
+        y = tokens.embed(ids, w, 0.3)
+        dw = tokens.embed_grad(ids, y, V, 0.3)
+        r = tokens.logprobs(x, ids, 0.9, 10)
+        dx = tokens.logprobs_grad(x, ids, r.stats, r.entropy, g1, g1, 0.9)
+        t = tokens.distill(x, *q, 1.4, g1)
+        s = tokens.logprobs(long, None, 1.0, 7)
+        dm = tokens.embed_grad(many, dy, V)
+        return [y, dw, *r, dx, *t, *s[1:], dm]
+
+    return go
+
+
+def _same(a, b):
+    return all(torch.equal(s.view(torch.uint8), t.view(torch.uint8)) for s, t in zip(a, b))
+
+
+@gpu
+def test_tokens_streams():
+    """The current stream's work, several streams at once."""
+    runs = [_everything(s) for s in range(3)]
+    ref = [go() for go in runs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in runs]
+    for _ in range(3):
+        got = []
+        for go, st in zip(runs, streams):
+            with torch.cuda.stream(st):
+                got.append(go())
+        torch.cuda.synchronize()
+        assert all(_same(a, b) for a, b in zip(got, ref))
+
+
+@gpu
+def test_tokens_captured():
+    """All calls in one HIP graph, replayed between eager calls."""
+    go = _everything(7)
+    ref = go()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = go()
+    for _ in range(4):
+        for t in held:
+            t.view(torch.uint8).fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert _same(held, ref)
+        assert _same(go(), ref)
+        torch.cuda.synchronize()
+
+
+# ---- refusals ----------------------------------------------------------------
+
+A = 1 << 20      # addresses that are never read: every call below is refused first
+
+
+def _embed(**k):
+    a = dict(ids=A, n=4, table=2 * A, td=L.F32, V=10, E=8, ts=8, scale=1.0, out=3 * A, od=L.F32, os=8)
+    a.update(k)
+    return L.load().edb_embed(*a.values(), None)
+
+
+def _embed_grad(**k):
+    a = dict(ids=A, n=4, dout=2 * A, dd=L.F32, V=10, E=8, ds=8, scale=1.0, acc=0, out=3 * A, od=L.F32, os=8, ws=4 * A, wb=1 << 40)
+    a.update(k)
+    return L.load().edb_embed_grad(*a.values(), None)
+
+
+def _logprobs(**k):
+    a = dict(x=A, d=L.F32, n=4, V=10, s=10, ids=2 * A, T=1.0, top=2, lp=3 * A, h=3 * A, st=3 * A, ti=3 * A, tl=3 * A, ws=4 * A, wb=1 << 40)
+    a.update(k)
+    return L.load().edb_logprobs(*a.values(), None)
+
+
+def _lp_grad(**k):
+    a = dict(x=A, d=L.F32, n=4, V=10, s=10, ids=2 * A, T=1.0, st=3 * A, h=3 * A, g1=3 * A, g2=3 * A, out=4 * A, os=10)
+    a.update(k)
+    return L.load().edb_logprobs_grad(*a.values(), None)
+
+
+def _distill(**k):
+    a = dict(x=A, d=L.F32, n=4, V=10, s=10, ti=2 * A, tl=3 * A, top=2, T=1.0, w=3 * A, loss=3 * A, out=4 * A, os=10)
+    a.update(k)
+    return L.load().edb_distill(*a.values(), None)
+
+
+INVALID, UNSUPPORTED = L.EDB_ERR_INVALID, L.EDB_ERR_UNSUPPORTED
+ROWS_BAD = [(dict(x=None), INVALID), (dict(d=7), INVALID), (dict(n=-1), INVALID), (dict(V=0), INVALID), (dict(s=9), INVALID),
+            (dict(s=1 << 47), INVALID), (dict(V=(1 << 30) + 1, s=1 << 31, os=1 << 31), UNSUPPORTED), (dict(T=0.0), INVALID),
+            (dict(T=-1.0), INVALID), (dict(T=INF), INVALID), (dict(T=float("nan")), INVALID), (dict(T=1e-45), INVALID),
+            (dict(x=A + 2), INVALID), (dict(d=L.BF16, x=A + 1), INVALID)]
+REFUSED = (
+    [(_embed, k, e) for k, e in [
+        (dict(ids=None), INVALID), (dict(table=None), INVALID), (dict(out=None), INVALID), (dict(td=2), INVALID),
+        (dict(od=-1), INVALID), (dict(n=-1), INVALID), (dict(V=0), INVALID), (dict(E=0), INVALID), (dict(ts=7), INVALID),
+        (dict(os=7), INVALID), (dict(scale=INF), INVALID), (dict(V=(1 << 30) + 1), UNSUPPORTED),
+        (dict(E=(1 << 20) + 1, ts=1 << 21, os=1 << 21), UNSUPPORTED), (dict(table=2 * A + 2), INVALID), (dict(out=3 * A + 1), INVALID),
+        (dict(out=2 * A + 64), INVALID), (dict(n=1 << 30, E=1 << 10, ts=1 << 10, os=1 << 10, out=1 << 45), UNSUPPORTED)]]
+    + [(_embed_grad, k, e) for k, e in [
+        (dict(ids=None), INVALID), (dict(dout=None), INVALID), (dict(out=None), INVALID), (dict(out=None, n=0), INVALID),
+        (dict(dd=3), INVALID), (dict(od=3), INVALID), (dict(n=-1), INVALID), (dict(V=0), INVALID), (dict(E=0), INVALID),
+        (dict(ds=7), INVALID), (dict(os=7), INVALID), (dict(scale=float("nan")), INVALID), (dict(out=2 * A + 64), INVALID),
+        (dict(dout=2 * A + 2), INVALID)]]
+    + [(_logprobs, k, e) for k, e in [(q, e) for q, e in ROWS_BAD if "os" not in q] + [
+        (dict(top=-1), UNSUPPORTED), (dict(top=65), UNSUPPORTED), (dict(ids=None), INVALID), (dict(ti=None), INVALID),
+        (dict(tl=None), INVALID)]]
+    + [(_lp_grad, k, e) for k, e in ROWS_BAD + [
+        (dict(ids=None), INVALID), (dict(st=None), INVALID), (dict(h=None), INVALID), (dict(out=None), INVALID), (dict(os=9), INVALID),
+        (dict(out=A + 4), INVALID), (dict(out=A, os=12), INVALID), (dict(out=4 * A + 2), INVALID)]]
+    + [(_distill, k, e) for k, e in ROWS_BAD + [
+        (dict(ti=None), INVALID), (dict(tl=None), INVALID), (dict(loss=None), INVALID), (dict(top=0), UNSUPPORTED),
+        (dict(top=257), UNSUPPORTED), (dict(os=9), INVALID), (dict(out=A + 4), INVALID), (dict(out=A, os=12), INVALID)]])
+
+
+@pytest.mark.parametrize("call,changed,status", REFUSED, ids=[f"{f.__name__[1:]}-{i}" for i, (f, _, _) in enumerate(REFUSED)])
+def test_refusals(call, changed, status):
+    """Refused on the host, with a message, before any launch (no GPU needed)."""
+    assert call(**changed) == status
+    assert L.load().edb_last_error()
+
+
+@pytest.mark.parametrize("call", [_embed, _logprobs, _lp_grad, _distill])
+def test_nothing_to_do(call):
+    assert call(n=0) == L.EDB_OK
+
+
+def test_workspace_sizes():
+    lib, nb = L.load(), C.c_int64(-1)
+    assert lib.edb_logprobs_bytes(5, 1000, L.BF16, 3, C.byref(nb)) == L.EDB_OK and nb.value >= 0
+    assert lib.edb_embed_grad_bytes(1000, 500, 64, C.byref(nb)) == L.EDB_OK and nb.value >= 0
+    assert lib.edb_logprobs_bytes(5, 1000, L.BF16, 65, C.byref(nb)) == UNSUPPORTED
+    assert lib.edb_logprobs_bytes(5, 1000, 9, 3, C.byref(nb)) == INVALID
+    assert lib.edb_logprobs_bytes(5, 1000, L.F32, 3, None) == INVALID
+    assert lib.edb_embed_grad_bytes(-1, 500, 64, C.byref(nb)) == INVALID
+    assert lib.edb_embed_grad_bytes(1, 500, 64, None) == INVALID
+
+
+def test_python_checks():
+    """Tensors that no call may take (CPU tensors, wrong types and shapes)."""
+    from paper_2302_03851_amd import tokens
+    w, ids = torch.zeros((4, 8)), torch.zeros(3, dtype=torch.int32)
+    for bad in (w, w.double(), w.view(-1), w.t()):
+        with pytest.raises(ValueError):
+            tokens.embed(ids, bad)
+        with pytest.raises(ValueError):
+            tokens.embed_grad(ids, bad, 5)
+        with pytest.raises(ValueError):
+            tokens.logprobs(bad, ids)
+        with pytest.raises(ValueError):
+            tokens.logprobs_grad(bad, ids, torch.zeros((4, 2)))
+        with pytest.raises(ValueError):
+            tokens.distill(bad, ids.view(1, 3), torch.zeros((1, 3)))
+
+
+@gpu
+def test_python_checks_gpu():
+    from paper_2302_03851_amd import tokens
+    w = torch.zeros((4, 8), device="cuda")
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    two = torch.zeros((4, 2), device="cuda")
+    bad = [lambda: tokens.embed(ids.long(), w), lambda: tokens.embed(ids.cpu(), w), lambda: tokens.embed(ids[::2], w),
+           lambda: tokens.embed(ids, w, out=w[:3]), lambda: tokens.embed(ids, w, dtype=F32, out=w.to(BF16)),
+           lambda: tokens.embed(ids, w.t()), lambda: tokens.embed(ids, w[:1].expand(4, 8)),
+           lambda: tokens.embed_grad(ids, w, 5, accumulate=True), lambda: tokens.embed_grad(ids[:3], w, 5),
+           lambda: tokens.embed_grad(ids, w, 5, out=w), lambda: tokens.logprobs(w, ids[:3]),
+           lambda: tokens.logprobs(w, ids, out=tokens.logprobs(w)), lambda: tokens.logprobs(w, ids, top=2, out=tokens.logprobs(w, ids)),
+           lambda: tokens.logprobs_grad(w, ids, two[:3]), lambda: tokens.logprobs_grad(w, ids, two.double()),
+           lambda: tokens.logprobs_grad(w, ids, two, out=w.to(BF16)), lambda: tokens.distill(w, ids, two),
+           lambda: tokens.distill(w, ids.view(4, 1), two), lambda: tokens.distill(w, ids.view(4, 1), two[:, :1].to(BF16)),
+           lambda: tokens.distill(w, ids.view(4, 1), two[:, :1].contiguous(), weight=ids)]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: tokens.logprobs(w, ids, temperature=0.0), lambda: tokens.logprobs(w, ids, top=65),
+              lambda: tokens.embed(ids, w, out=w)):
+        with pytest.raises(L.EdbError):
+            f()
