@@ -18,6 +18,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
+
 struct bf16 {
     uint16_t bits;
 };
@@ -79,15 +82,27 @@ struct Elem<bf16> {
             x[2 * i + 1] = __builtin_bit_cast(float, (uint32_t)v[i] & 0xffff0000u);
         }
     }
-    static __device__ __forceinline__ u32x4 pack(const float* x) {
+    static __device__ __forceinline__ u32x2 load_half(const bf16* p) { return *reinterpret_cast<const u32x2_a2*>(p); }
+    static __device__ __forceinline__ void unpack_half(u32x2 v, float* x) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            x[2 * i] = __builtin_bit_cast(float, (uint32_t)v[i] << 16);
+            x[2 * i + 1] = __builtin_bit_cast(float, (uint32_t)v[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ void store_half(bf16* p, const float* x) {
+        *reinterpret_cast<u32x2_a2*>(p) = u32x2{pack_pair(x[0], x[1]), pack_pair(x[2], x[3])};
+    }
+    // one conversion instruction a pair
+    static __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
         typedef float f2 __attribute__((ext_vector_type(2)));
         typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), b2));
+    }
+    static __device__ __forceinline__ u32x4 pack(const float* x) {
         u32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {  // one conversion instruction a pair
-            const f2 pair = {x[2 * i], x[2 * i + 1]};
-            v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, b2));
-        }
+        for (int i = 0; i < 4; ++i) v[i] = pack_pair(x[2 * i], x[2 * i + 1]);
         return v;
     }
 };

@@ -665,7 +665,7 @@ REFUSED = (
         (dict(ids=None), INVALID), (dict(dout=None), INVALID), (dict(out=None), INVALID), (dict(out=None, n=0), INVALID),
         (dict(dd=3), INVALID), (dict(od=3), INVALID), (dict(n=-1), INVALID), (dict(V=0), INVALID), (dict(E=0), INVALID),
         (dict(ds=7), INVALID), (dict(os=7), INVALID), (dict(scale=float("nan")), INVALID), (dict(out=2 * A + 64), INVALID),
-        (dict(dout=2 * A + 2), INVALID)]]
+        (dict(dout=2 * A + 2), INVALID), (dict(wb=0), INVALID), (dict(ws=None), INVALID), (dict(ws=4 * A + 8), INVALID)]]
     + [(_logprobs, k, e) for k, e in [(q, e) for q, e in ROWS_BAD if "os" not in q] + [
         (dict(top=-1), UNSUPPORTED), (dict(top=65), UNSUPPORTED), (dict(ids=None), INVALID), (dict(ti=None), INVALID),
         (dict(tl=None), INVALID)]]
