@@ -368,52 +368,94 @@ __device__ __forceinline__ void put_word(const SumArgs& a, uint32_t word, int co
     store_k<O, K>(d, v);
 }
 
+// Eight neighbouring entries of the sorted lists.  WAVE: the same ones in every
+// lane of the wave, kept in scalar registers.
+template <bool WAVE>
+struct Eight {
+    uint32_t key[8], pos[8];
+
+    __device__ __forceinline__ void load(const SumArgs& a, int i) {
+        u32x4 v[4];
+        v[0] = *reinterpret_cast<const u32x4*>(a.keys + i);
+        v[1] = *reinterpret_cast<const u32x4*>(a.keys + i + 4);
+        v[2] = *reinterpret_cast<const u32x4*>(a.pos + i);
+        v[3] = *reinterpret_cast<const u32x4*>(a.pos + i + 4);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            key[u] = v[u >> 2][u & 3];
+            pos[u] = v[2 + (u >> 2)][u & 3];
+        }
+    }
+    __device__ __forceinline__ void settle() {
+        if constexpr (WAVE)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                key[u] = __builtin_amdgcn_readfirstlane(key[u]);
+                pos[u] = __builtin_amdgcn_readfirstlane(pos[u]);
+            }
+    }
+};
+
 // A group of lanes adds up the runs of one chunk of the sorted positions, K
 // columns a lane, eight rows in flight.  A run that lies inside the chunk is
 // final; the part of one that came in from the chunk before goes to the
 // chunk's first partial row, of one that only goes on to the next to the second.
-template <class T, class O, int K>
+// All eight entries are there before the first row is asked for (loads return
+// in order: a wait for a later entry would wait for the rows before it too),
+// and a place without a row reads its chunk's first one, without a branch.
+template <class T, class O, int K, bool WAVE>
 __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
-    const int64_t chunk = ((int64_t)blockIdx.x * 256 + threadIdx.x) / a.lanes;
-    const int col = (blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1))) * K;
-    const int64_t begin64 = chunk * a.chunk;
+    int chunk;
+    if constexpr (WAVE) chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    else chunk = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) / a.lanes);
+    const int lanes = WAVE ? 64 : a.lanes;
+    const int col = (blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * K;
+    const int64_t begin64 = (int64_t)chunk * a.chunk;
     if (begin64 >= a.n || col >= a.dim) return;
     const int begin = (int)begin64, end = (int)min((int64_t)a.n, begin64 + a.chunk);
     const T* rows = static_cast<const T*>(a.dout) + col;
-    uint32_t cur = a.keys[begin];
-    bool from_before = begin > 0 && a.keys[begin - 1] == cur;
+    float* partial = a.partial + 2 * (int64_t)chunk * a.dim + col;
+    Eight<WAVE> at;
+    at.load(a, begin);
+    const uint32_t before = begin > 0 ? a.keys[begin - 1] : a.vocab, after = end < a.n ? a.keys[end] : a.vocab;
+    at.settle();
+    uint32_t cur = at.key[0];
+    if (cur >= a.vocab) return;  // only ids that are no token
+    bool from_before = before == cur;
+    const uint32_t some = at.pos[0];
     float sum[K] = {};
     for (int i = begin; i < end; i += 8) {
-        uint32_t key[8];
         float v[8][K];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            key[u] = a.keys[i + u];
-            const uint32_t p = a.pos[i + u];
-            if (i + u < end && key[u] < a.vocab) load_k<T, K>(rows + p * a.dout_stride, v[u]);
+            const uint32_t p = i + u < end ? at.pos[u] : some;
+            load_k<T, K>(rows + p * a.dout_stride, v[u]);
         }
+        const Eight<WAVE> now = at;
+        if (i + 8 < end) at.load(a, i + 8);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             if (i + u >= end) break;
-            if (key[u] != cur) {
-                if (from_before) store_k<float, K>(a.partial + (2 * chunk) * a.dim + col, sum);
+            if (now.key[u] != cur) {
+                if (from_before) store_k<float, K>(partial, sum);
                 else put_word<O, K>(a, cur, col, sum);
                 from_before = false;
-                cur = key[u];
+                cur = now.key[u];
+                if (cur >= a.vocab) return;
 #pragma unroll
                 for (int k = 0; k < K; ++k) sum[k] = 0.f;
             }
-            if (cur >= a.vocab) return;  // only ids that are no token follow
 #pragma unroll
             for (int k = 0; k < K; ++k) sum[k] += v[u][k];
         }
+        at.settle();
     }
-    if (from_before) store_k<float, K>(a.partial + (2 * chunk) * a.dim + col, sum);
-    else if (end < a.n && a.keys[end] == cur) store_k<float, K>(a.partial + (2 * chunk + 1) * a.dim + col, sum);
+    if (from_before) store_k<float, K>(partial, sum);
+    else if (after == cur) store_k<float, K>(partial + a.dim, sum);
     else put_word<O, K>(a, cur, col, sum);
 }
 
-constexpr int kJoinThreads = 512;
+constexpr int kJoinThreads = 256;
 
 // A work-group a chunk: where a run begins in the chunk and goes on after it,
 // adds the run's partial rows, a contiguous part of them for each group of lanes.
@@ -561,7 +603,8 @@ GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
 template <class T, class O, int K>
 void launch_sums(const GradPlan& g, const SumArgs& a, hipStream_t st) {
     const dim3 grid((unsigned)(((int64_t)g.chunks * g.lanes + 255) / 256), g.tiles_y);
-    sum_chunks<T, O, K><<<grid, 256, 0, st>>>(a);
+    if (g.lanes == 64) sum_chunks<T, O, K, true><<<grid, 256, 0, st>>>(a);
+    else sum_chunks<T, O, K, false><<<grid, 256, 0, st>>>(a);
     if (g.chunks > 1) join_chunks<O, K><<<dim3(g.chunks, g.tiles_y), kJoinThreads, 0, st>>>(a);
 }
 
