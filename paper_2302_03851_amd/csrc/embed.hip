@@ -17,15 +17,17 @@ namespace {
 
 // K consecutive elements of a row as fp32: 8 or 4 where rows hold whole groups
 // of so many (at any alignment), else 1.
-template <class T, int K>
+// ONCE: read once only, not worth a place in the caches.
+template <class T, int K, bool ONCE = false>
 __device__ __forceinline__ void load_k(const T* p, float* v) {
     if constexpr (K == 1) {
         v[0] = Elem<T>::get(p);
     } else if constexpr (K < Elem<T>::kVec) {
-        Elem<T>::unpack_half(Elem<T>::load_half(p), v);
+        Elem<T>::unpack_half(ONCE ? Elem<T>::load_half_nt(p) : Elem<T>::load_half(p), v);
     } else {
 #pragma unroll
-        for (int i = 0; i < K; i += Elem<T>::kVec) Elem<T>::unpack(Elem<T>::load(p + i), v + i);
+        for (int i = 0; i < K; i += Elem<T>::kVec)
+            Elem<T>::unpack(ONCE ? Elem<T>::load_nt(p + i) : Elem<T>::load(p + i), v + i);
     }
 }
 template <class T, int K>
@@ -76,43 +78,13 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
 // that are no token get the word V and sort to the end.  Up to kBlockSort ids
 // are sorted by one work-group in LDS; more by passes over digits of up to
 // kMaxDigit bits, three launches each (counts per tile, their prefix sums, the
-// scatter).  The zero rows of the result are written by further work-groups of
-// the sorting launches, which leave the memory idle.
+// scatter).  The zero rows of the other words are written in the launch of the
+// sums, by further work-groups.
 
 constexpr int kBlockSort = 8192;   // ids of the one-work-group sort: keys, positions and counts fill 56 KB of LDS
 constexpr int kMaxDigit = 10;
-constexpr int kTile = 2048;        // ids a work-group of the large sort ranks: 4 waves of 8 rounds
-constexpr int kRounds = 8;
-
-struct FillArgs {  // rows to zero: `share` of `shares` equal parts, by the work-groups from `first` on
-    void* rows;
-    int64_t stride_bytes, row_bytes, n_rows;
-    int32_t share, shares, first;
-};
-
-// Zeroes its part of the rows: as one range of 16-byte pieces where the rows
-// are dense, otherwise row by row in 2-byte units.
-__device__ __forceinline__ void fill_share(const FillArgs& f, int threads) {
-    const int64_t r0 = f.n_rows * f.share / f.shares, r1 = f.n_rows * (f.share + 1) / f.shares;
-    const int64_t step = (int64_t)(gridDim.x - f.first) * threads;
-    const int64_t me = (int64_t)(blockIdx.x - f.first) * threads + threadIdx.x;
-    char* base = static_cast<char*>(f.rows);
-    if (f.stride_bytes == f.row_bytes) {
-        char* p = base + r0 * f.row_bytes;
-        const int64_t bytes = (r1 - r0) * f.row_bytes, whole = bytes >> 4;
-        for (int64_t i = me; i < whole; i += step) *reinterpret_cast<u32x4_a2*>(p + (i << 4)) = u32x4{0u, 0u, 0u, 0u};
-        const int64_t rest = (bytes - (whole << 4)) >> 1;
-        if (me < rest) *reinterpret_cast<uint16_t*>(p + (whole << 4) + 2 * me) = 0;
-    } else {
-        const int64_t units = f.row_bytes >> 1;
-        for (int64_t r = r0 + me / units, c = me % units; r < r1;) {
-            *reinterpret_cast<uint16_t*>(base + r * f.stride_bytes + 2 * c) = 0;
-            c += step;
-            r += c / units;
-            c %= units;
-        }
-    }
-}
+constexpr int kTile = 1024;        // ids a work-group of the large sort ranks: 4 waves of 4 rounds
+constexpr int kRounds = 4;
 
 __device__ __forceinline__ uint32_t word_of(int32_t id, uint32_t vocab) {
     return (uint32_t)id < vocab ? (uint32_t)id : vocab;
@@ -139,25 +111,24 @@ __device__ __forceinline__ uint32_t wave_scan_inclusive(uint32_t v) {
     return v;
 }
 
+struct alignas(8) Pair {
+    uint32_t word, pos;
+};
+
 struct SortArgs {
-    const int32_t* ids;          // pass 0 reads the ids
-    const uint32_t *keys, *pos;  // later passes read these
-    uint32_t *keys_out, *pos_out;
-    uint32_t* counts;            // [bin][tile]; their prefix sums after sort_scan
-    uint32_t* totals;            // [bin]
+    const int32_t* ids;  // pass 0 reads the ids
+    const Pair* in;      // later passes read these
+    Pair* out;
+    uint32_t* counts;    // [tile][bin]; their prefix sums over the tiles after sort_scan
+    uint32_t* totals;    // [bin]
     int32_t n, tiles, shift, bits;
     uint32_t vocab;
-    FillArgs fill;
 };
 
 // One work-group, everything in LDS: passes of 8 bits.  Each of the 16 waves
 // ranks a contiguous eighth-kilo of ids, so the order (digit, wave, round,
 // lane) is the stable one.
 __global__ __launch_bounds__(1024) void sort_block(SortArgs a) {
-    if (blockIdx.x) {
-        fill_share(a.fill, 1024);
-        return;
-    }
     constexpr int kWaves = 16, kBins = 256, kPer = kBlockSort / 1024;
     __shared__ uint32_t keys[kBlockSort];
     __shared__ uint16_t pos[kBlockSort];
@@ -225,88 +196,93 @@ __global__ __launch_bounds__(1024) void sort_block(SortArgs a) {
             }
         }
     }
-    for (int i = tid; i < a.n; i += 1024) {
-        a.keys_out[i] = keys[i];
-        a.pos_out[i] = pos[i];
-    }
+    for (int i = tid; i < a.n; i += 1024) a.out[i] = Pair{keys[i], pos[i]};
 }
 
-__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int i) {
-    return a.ids ? word_of(a.ids[i], a.vocab) : a.keys[i];
+__device__ __forceinline__ Pair sort_pair(const SortArgs& a, int64_t i) {
+    return a.ids ? Pair{word_of(a.ids[i], a.vocab), (uint32_t)i} : a.in[i];
 }
 
-// counts[bin][tile] of one digit.
+// counts[tile][bin] of one digit.
 __global__ __launch_bounds__(256) void sort_count(SortArgs a) {
-    if ((int)blockIdx.x >= a.tiles) {
-        fill_share(a.fill, 256);
-        return;
-    }
     __shared__ uint32_t count[1 << kMaxDigit];
     const int bins = 1 << a.bits, tile = blockIdx.x;
     for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
-    __syncthreads();
+    uint32_t k[kTile / 256];
 #pragma unroll
     for (int r = 0; r < kTile / 256; ++r) {
         const int64_t i = (int64_t)tile * kTile + r * 256 + threadIdx.x;
-        if (i < a.n) atomicAdd(&count[(sort_key(a, (int)i) >> a.shift) & (bins - 1)], 1u);
+        k[r] = i < a.n ? sort_pair(a, i).word : 0;
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += 256) a.counts[(int64_t)b * a.tiles + tile] = count[b];
+#pragma unroll
+    for (int r = 0; r < kTile / 256; ++r)
+        if ((int64_t)tile * kTile + r * 256 + threadIdx.x < a.n) atomicAdd(&count[(k[r] >> a.shift) & (bins - 1)], 1u);
+    __syncthreads();
+    for (int b = threadIdx.x; b < bins; b += 256) a.counts[(int64_t)tile * bins + b] = count[b];
 }
 
-// Prefix sums of a bin's counts over the tiles: a wave a bin.
+// Prefix sums of every bin's counts over the tiles: a work-group takes 16 bins,
+// each of its 16 x 16 threads a bin's counts of a sixteenth of the tiles.
+constexpr int kScanBins = 16;
 __global__ __launch_bounds__(256) void sort_scan(SortArgs a) {
-    const int scanners = ((1 << a.bits) + 3) / 4;
-    if ((int)blockIdx.x >= scanners) {
-        fill_share(a.fill, 256);
-        return;
+    const int bins = 1 << a.bits;
+    __shared__ uint32_t part[16][kScanBins];
+    const int mine = threadIdx.x >> 4, bin = blockIdx.x * kScanBins + (threadIdx.x & 15);
+    const int per = (a.tiles + 15) / 16, t0 = min(a.tiles, mine * per), t1 = min(a.tiles, t0 + per);
+    uint32_t* c = a.counts + bin;
+    uint32_t sum = 0;
+    if (bin < bins) {
+#pragma unroll 8
+        for (int t = t0; t < t1; ++t) sum += c[(int64_t)t * bins];
     }
-    const int bin = blockIdx.x * 4 + (threadIdx.x >> 6), lane = lane_id();
-    if (bin >= 1 << a.bits) return;
-    uint32_t* c = a.counts + (int64_t)bin * a.tiles;
+    part[mine][threadIdx.x & 15] = sum;
+    __syncthreads();
     uint32_t base = 0;
-    for (int t = 0; t < a.tiles; t += 64) {
-        const uint32_t v = t + lane < a.tiles ? c[t + lane] : 0, upto = wave_scan_inclusive(v);
-        if (t + lane < a.tiles) c[t + lane] = base + upto - v;
-        base += __shfl(upto, 63);
+    for (int i = 0; i < mine; ++i) base += part[i][threadIdx.x & 15];
+    if (bin >= bins) return;
+#pragma unroll 8
+    for (int t = t0; t < t1; ++t) {
+        const uint32_t v = c[(int64_t)t * bins];
+        c[(int64_t)t * bins] = base;
+        base += v;
     }
-    if (lane == 0) a.totals[bin] = base;
+    if (mine == 15) a.totals[bin] = base;
 }
 
 // Ranks a tile's ids and writes them to their places.
 __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
-    if ((int)blockIdx.x >= a.tiles) {
-        fill_share(a.fill, 256);
-        return;
-    }
     constexpr int kBins = 1 << kMaxDigit;
     __shared__ uint32_t at[4][kBins];  // per wave: counts, then the next place of a digit
     __shared__ uint32_t wave_sum[4];
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, tile = blockIdx.x, bins = 1 << a.bits;
-    for (int b = lane; b < bins; b += 64) at[wave][b] = 0;
     // each thread owns four neighbouring bins
-    uint32_t total[kBins / 256], sum = 0;
+    constexpr int kOwn = kBins / 256;
+    uint32_t total[kOwn], prior[kOwn], sum = 0;
 #pragma unroll
-    for (int i = 0; i < kBins / 256; ++i) {
-        const int b = tid * (kBins / 256) + i;
+    for (int i = 0; i < kOwn; ++i) {
+        const int b = tid * kOwn + i;
         total[i] = b < bins ? a.totals[b] : 0;
-        sum += total[i];
+        prior[i] = b < bins ? a.counts[(int64_t)tile * bins + b] : 0;
     }
-    const uint32_t upto = wave_scan_inclusive(sum);
-    if (lane == 63) wave_sum[wave] = upto;
     const int64_t first = (int64_t)tile * kTile + wave * (kTile / 4);
-    uint32_t k[kRounds], p[kRounds], rank[kRounds];
+    Pair k[kRounds];
+    uint32_t rank[kRounds];
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
         const int64_t i = first + r * 64 + lane;
-        k[r] = i < a.n ? sort_key(a, (int)i) : 0;
-        p[r] = i < a.n ? (a.ids ? (uint32_t)i : a.pos[i]) : 0;
+        k[r] = i < a.n ? sort_pair(a, i) : Pair{0, 0};
     }
+    for (int b = lane; b < bins; b += 64) at[wave][b] = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) sum += total[i];
+    const uint32_t upto = wave_scan_inclusive(sum);
+    if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
         const bool valid = first + r * 64 + lane < a.n;
-        const uint32_t d = (k[r] >> a.shift) & (bins - 1);
+        const uint32_t d = (k[r].word >> a.shift) & (bins - 1);
         const uint64_t m = same_digit(d, a.bits, __ballot(valid));
         if (valid) rank[r] = at[wave][d] + __popcll(m & ((1ull << lane) - 1));
         __builtin_amdgcn_wave_barrier();
@@ -317,10 +293,10 @@ __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
     uint32_t base = upto - sum;
     for (int w = 0; w < wave; ++w) base += wave_sum[w];
 #pragma unroll
-    for (int i = 0; i < kBins / 256; ++i) {
-        const int b = tid * (kBins / 256) + i;
+    for (int i = 0; i < kOwn; ++i) {
+        const int b = tid * kOwn + i;
         if (b < bins) {
-            uint32_t next = base + a.counts[(int64_t)b * a.tiles + tile];
+            uint32_t next = base + prior[i];
             for (int w = 0; w < 4; ++w) {
                 const uint32_t c = at[w][b];
                 at[w][b] = next;
@@ -332,29 +308,73 @@ __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kRounds; ++r)
-        if (first + r * 64 + lane < a.n) {
-            const uint32_t to = at[wave][(k[r] >> a.shift) & (bins - 1)] + rank[r];
-            a.keys_out[to] = k[r];
-            a.pos_out[to] = p[r];
-        }
+        if (first + r * 64 + lane < a.n) a.out[at[wave][(k[r].word >> a.shift) & (bins - 1)] + rank[r]] = k[r];
 }
 
 struct SumArgs {
-    const uint32_t *keys, *pos;  // sorted; readable to a multiple of 8
-    int32_t n, chunk;            // chunk: a multiple of 8
+    const Pair* sorted;  // readable to a multiple of 8
+    int32_t n, chunk;    // chunk: a multiple of 8
     uint32_t vocab;
-    int32_t dim, lanes;          // lanes: a power of two up to 64 that share a row
+    int32_t dim, lanes;  // lanes: a power of two up to 64 that share a row
     const void* dout;
     int64_t dout_stride;
     float scale;
     int32_t accumulate;
     void* dtable;
     int64_t dtable_stride;
-    float* partial;              // [chunks][2][dim]
+    float* partial;      // [chunks][2][dim]
+    int32_t sum_groups;  // work-groups of the sums (per column tile); the others zero rows
+    int32_t fill_rows;   // rows that one of those looks at, at most kFillRows
 };
 
-template <class O, int K>
-__device__ __forceinline__ void put_word(const SumArgs& a, uint32_t word, int col, const float* sum) {
+constexpr int kFillRows = 256;
+
+// Zeroes the rows first .. first + rows of the table's gradient but those marked in `there`.
+template <class O>
+__device__ __forceinline__ void zero_rows(void* dtable, int64_t stride, int32_t dim, uint32_t first, uint32_t rows,
+                                          const uint8_t* there, uint32_t threads) {
+    constexpr int kPer = 16 / (int)sizeof(O);
+    const uint32_t pieces = (dim + kPer - 1) / kPer, items = rows * pieces;
+    O* base = static_cast<O*>(dtable) + first * stride;
+    for (uint32_t i = threadIdx.x; i < items; i += threads) {
+        const uint32_t r = i / pieces, c = (i - r * pieces) * kPer;
+        if (there[r]) continue;
+        O* d = base + r * stride + c;
+        if ((int)c + kPer <= dim) Elem<O>::store_nt(d, u32x4{0u, 0u, 0u, 0u});
+        else
+            for (int k = c; k < dim; ++k) Elem<O>::put(d + (k - c), 0.f);
+    }
+}
+
+// Zeroes those of a group's fill_rows rows whose words do not occur.
+template <class O>
+__device__ __forceinline__ void fill_absent(const SumArgs& a, int group) {
+    __shared__ uint8_t there[kFillRows];
+    const uint32_t first = (uint32_t)group * a.fill_rows, rows = min((uint32_t)a.fill_rows, a.vocab - first);
+    if (threadIdx.x < rows) {
+        const uint32_t word = first + threadIdx.x;
+        int lo = 0, hi = a.n;  // the first place whose word is not below
+        while (lo < hi) {
+            const int mid = lo + (hi - lo) / 2;
+            if (a.sorted[mid].word < word) lo = mid + 1;
+            else hi = mid;
+        }
+        there[threadIdx.x] = lo < a.n && a.sorted[lo].word == word;
+    }
+    __syncthreads();
+    zero_rows<O>(a.dtable, a.dtable_stride, a.dim, first, rows, there, 256);
+}
+
+// The sums over the groups of `lanes` lanes of a wave, in every group.
+template <int K>
+__device__ __forceinline__ void add_groups(float* sum, int lanes) {
+    for (int d = lanes; d < 64; d <<= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) sum[k] += __shfl_xor(sum[k], d);
+}
+
+template <class O, int K, class A>
+__device__ __forceinline__ void put_word(const A& a, uint32_t word, int col, const float* sum) {
     O* d = static_cast<O*>(a.dtable) + word * a.dtable_stride + col;
     float v[K];
     if (a.accumulate) {
@@ -376,14 +396,12 @@ struct Eight {
 
     __device__ __forceinline__ void load(const SumArgs& a, int i) {
         u32x4 v[4];
-        v[0] = *reinterpret_cast<const u32x4*>(a.keys + i);
-        v[1] = *reinterpret_cast<const u32x4*>(a.keys + i + 4);
-        v[2] = *reinterpret_cast<const u32x4*>(a.pos + i);
-        v[3] = *reinterpret_cast<const u32x4*>(a.pos + i + 4);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const u32x4*>(a.sorted + i + 2 * u);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            key[u] = v[u >> 2][u & 3];
-            pos[u] = v[2 + (u >> 2)][u & 3];
+            key[u] = v[u >> 1][2 * (u & 1)];
+            pos[u] = v[u >> 1][2 * (u & 1) + 1];
         }
     }
     __device__ __forceinline__ void settle() {
@@ -405,6 +423,10 @@ struct Eight {
 // and a place without a row reads its chunk's first one, without a branch.
 template <class T, class O, int K, bool WAVE>
 __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
+    if ((int)blockIdx.x >= a.sum_groups) {
+        if (blockIdx.y == 0) fill_absent<O>(a, blockIdx.x - a.sum_groups);
+        return;
+    }
     int chunk;
     if constexpr (WAVE) chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     else chunk = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) / a.lanes);
@@ -417,7 +439,7 @@ __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
     float* partial = a.partial + 2 * (int64_t)chunk * a.dim + col;
     Eight<WAVE> at;
     at.load(a, begin);
-    const uint32_t before = begin > 0 ? a.keys[begin - 1] : a.vocab, after = end < a.n ? a.keys[end] : a.vocab;
+    const uint32_t before = begin > 0 ? a.sorted[begin - 1].word : a.vocab, after = end < a.n ? a.sorted[end].word : a.vocab;
     at.settle();
     uint32_t cur = at.key[0];
     if (cur >= a.vocab) return;  // only ids that are no token
@@ -429,7 +451,7 @@ __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             const uint32_t p = i + u < end ? at.pos[u] : some;
-            load_k<T, K>(rows + p * a.dout_stride, v[u]);
+            load_k<T, K, true>(rows + p * a.dout_stride, v[u]);
         }
         const Eight<WAVE> now = at;
         if (i + 8 < end) at.load(a, i + 8);
@@ -455,55 +477,205 @@ __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
     else put_word<O, K>(a, cur, col, sum);
 }
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinWaves = 16;
+constexpr int kJoinAlone = 32;  // partial rows that a wave adds up by itself
 
-// A work-group a chunk: where a run begins in the chunk and goes on after it,
-// adds the run's partial rows, a contiguous part of them for each group of lanes.
-template <class O, int K>
-__global__ __launch_bounds__(kJoinThreads) void join_chunks(SumArgs a) {
-    const int64_t chunk = blockIdx.x, begin = chunk * a.chunk, end = begin + a.chunk;
-    if (end >= a.n) return;
-    const uint32_t word = a.keys[end - 1];
-    if (word >= a.vocab || a.keys[end] != word) return;
-    if (begin > 0 && a.keys[begin] == word && a.keys[begin - 1] == word) return;
-    // the chunks after this one that begin with the word
-    int64_t more = 0;
-    const int lane = lane_id();
-    for (;;) {
-        const int64_t at = end + (more + lane) * a.chunk;
-        const uint64_t m = __ballot(at < a.n && a.keys[at < a.n ? at : 0] == word);
-        const int run = m == ~0ull ? 64 : __ffsll((unsigned long long)~m) - 1;
-        more += run;
-        if (run < 64) break;
+// The sum of the partial rows i0 .. i1 of the run that begins in `chunk`: the
+// chunk's second row, then the first rows of the chunks after it.
+template <int K>
+__device__ __forceinline__ void add_partial(const SumArgs& a, int64_t chunk, int64_t i0, int64_t i1, int col, float* sum) {
+    for (int64_t i = i0; i < i1; i += 8) {
+        float v[8][K];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {  // a place past the end reads the part's last row
+            const int64_t j = min(i + u, i1 - 1);
+            load_k<float, K>(a.partial + (2 * (chunk + j) + (j == 0 ? 1 : 0)) * a.dim + col, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u < i1)
+#pragma unroll
+                for (int k = 0; k < K; ++k) sum[k] += v[u][k];
     }
-    const int64_t n = more + 1;  // partial rows: this chunk's second, then the others' first ones
-    const int group = threadIdx.x / a.lanes, groups = kJoinThreads / a.lanes;
-    const int col = (blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1))) * K;
-    const int64_t per = (n + groups - 1) / groups, i0 = group * per, i1 = min(n, i0 + per);
-    float sum[K] = {};
-    if (col < a.dim) {
-        for (int64_t i = i0; i < i1; i += 8) {
-            float v[8][K];
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (i + u < i1) load_k<float, K>(a.partial + (2 * (chunk + i + u) + (i + u == 0 ? 1 : 0)) * a.dim + col, v[u]);
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (i + u < i1)
-#pragma unroll
-                    for (int k = 0; k < K; ++k) sum[k] += v[u][k];
+}
+
+// A wave a chunk: where a run begins in the chunk and goes on after it, its
+// partial rows are added up, by the wave or, of a run over more than kJoinAlone
+// chunks (at most one begins in a work-group's), by all waves together, each
+// group of lanes a contiguous part.
+template <class O, int K>
+__global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
+    static_assert(kJoinAlone >= kJoinWaves, "one long run a work-group");
+    __shared__ float part[kJoinWaves][64][K];
+    __shared__ int64_t long_chunk, long_rows;
+    __shared__ uint32_t long_word;
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    const int64_t chunk = (int64_t)blockIdx.x * kJoinWaves + wave, begin = chunk * a.chunk, end = begin + a.chunk;
+    const int col = (blockIdx.y * a.lanes + (lane & (a.lanes - 1))) * K, groups = 64 / a.lanes;
+    if (threadIdx.x == 0) long_rows = 0;
+    int64_t rows = 0;
+    uint32_t word = a.vocab;
+    if (end < a.n) {
+        word = a.sorted[end - 1].word;
+        const uint32_t after = a.sorted[end].word, head = a.sorted[begin].word,
+                       before = begin > 0 ? a.sorted[begin - 1].word : a.vocab;
+        if (word < a.vocab && after == word && !(head == word && before == word)) {
+            // the chunks after this one that begin with the word: the first 64 looked at one by one, then 64
+            // places of what is left at a time
+            int64_t step = 1, limit = (a.n - end + a.chunk - 1) / a.chunk;
+            while (rows < limit) {
+                const int64_t at = rows + lane * step;
+                const uint64_t m = __ballot(at < limit && a.sorted[end + min(at, limit - 1) * a.chunk].word == word);
+                const int run = m == ~0ull ? 64 : __ffsll((unsigned long long)~m) - 1;
+                if (run < 64) limit = min(limit, rows + run * step);
+                if (run) rows += (run - 1) * step + 1;
+                step = (limit - rows + 63) / 64;
+            }
+            ++rows;  // and its own second row
         }
     }
-    __shared__ float part[kJoinThreads][K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) part[threadIdx.x][k] = sum[k];
     __syncthreads();
-    if (group || col >= a.dim) return;
-    const int used = (int)((n + per - 1) / per);
-    for (int g = 1; g < used; ++g)
+    if (rows > kJoinAlone) {
+        if (lane == 0) {
+            long_chunk = chunk;
+            long_rows = rows;
+            long_word = word;
+        }
+    } else if (rows) {
+        const int64_t per = (rows + groups - 1) / groups, i0 = min(rows, (lane / a.lanes) * per), i1 = min(rows, i0 + per);
+        float sum[K] = {};
+        if (col < a.dim) add_partial<K>(a, chunk, i0, i1, col, sum);
+        add_groups<K>(sum, a.lanes);
+        if (lane < a.lanes && col < a.dim) put_word<O, K>(a, word, col, sum);
+    }
+    __syncthreads();
+    if (!long_rows) return;
+    const int64_t n = long_rows, all = kJoinWaves * groups, per = (n + all - 1) / all;
+    const int64_t i0 = min(n, (threadIdx.x / a.lanes) * per), i1 = min(n, i0 + per);
+    float sum[K] = {};
+    if (col < a.dim) add_partial<K>(a, long_chunk, i0, i1, col, sum);
+    add_groups<K>(sum, a.lanes);
 #pragma unroll
-        for (int k = 0; k < K; ++k) sum[k] += part[g * a.lanes + threadIdx.x][k];
-    put_word<O, K>(a, word, col, sum);
+    for (int k = 0; k < K; ++k) part[wave][lane][k] = sum[k];
+    __syncthreads();
+    if ((int)threadIdx.x >= a.lanes || col >= a.dim) return;
+    for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+        for (int k = 0; k < K; ++k) sum[k] += part[w][lane][k];
+    put_word<O, K>(a, long_word, col, sum);
+}
+
+// ---- a few ids: one launch, without a sort
+//
+// A work-group an id looks through all ids.  The one at a word's first place
+// adds up the word's rows (a contiguous part of them for each group of lanes),
+// the others end; further work-groups zero the rows of the other words.
+constexpr int kSmall = 2048;
+constexpr int kSmallThreads = 512, kSmallWaves = kSmallThreads / 64;
+
+struct SmallArgs {
+    const int32_t* ids;
+    int32_t n;
+    uint32_t vocab;
+    int32_t dim, lanes, tiles;
+    const void* dout;
+    int64_t dout_stride;
+    float scale;
+    int32_t accumulate;
+    void* dtable;
+    int64_t dtable_stride;
+    int32_t fill_rows;
+};
+
+template <class T, class O, int K>
+__global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
+    __shared__ uint8_t there[kFillRows];
+    __shared__ uint16_t list[kSmall];
+    __shared__ int count[kSmallWaves], early[kSmallWaves];
+    __shared__ float part[kSmallWaves][64][K];
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+    constexpr int kLook = kSmall / kSmallThreads;  // ids a thread looks at
+    int32_t id[kLook];
+    if ((int)blockIdx.x >= a.n) {
+        const uint32_t first = (blockIdx.x - a.n) * (uint32_t)a.fill_rows, rows = min((uint32_t)a.fill_rows, a.vocab - first);
+#pragma unroll
+        for (int r = 0; r < kLook; ++r) id[r] = r * kSmallThreads + tid < a.n ? a.ids[r * kSmallThreads + tid] : -1;
+        if (tid < kFillRows) there[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kLook; ++r)
+            if (id[r] >= 0 && (uint32_t)id[r] - first < rows) there[(uint32_t)id[r] - first] = 1;
+        __syncthreads();
+        zero_rows<O>(a.dtable, a.dtable_stride, a.dim, first, rows, there, kSmallThreads);
+        return;
+    }
+    const int me = blockIdx.x, span = (a.n + kSmallThreads - 1) / kSmallThreads * 64, first = wave * span;
+    const uint32_t word = word_of(a.ids[me], a.vocab);
+#pragma unroll
+    for (int r = 0; r < kLook; ++r) {
+        const int i = first + r * 64 + lane;
+        id[r] = r * 64 < span && i < a.n ? a.ids[i] : -1;
+    }
+    if (word >= a.vocab) return;
+    uint64_t same[kLook];
+    int mine = 0;
+    bool before = false;
+#pragma unroll
+    for (int r = 0; r < kLook; ++r) {
+        same[r] = __ballot((uint32_t)id[r] == word);
+        mine += __popcll(same[r]);
+        before |= same[r] && first + r * 64 + __ffsll((unsigned long long)same[r]) - 1 < me;
+    }
+    if (lane == 0) {
+        count[wave] = mine;
+        early[wave] = before;
+    }
+    __syncthreads();
+    int at = 0, n = 0;
+    for (int w = 0; w < kSmallWaves; ++w) {
+        if (early[w]) return;
+        if (w < wave) at += count[w];
+        n += count[w];
+    }
+#pragma unroll
+    for (int r = 0; r < kLook; ++r) {
+        if ((same[r] >> lane) & 1) list[at + __popcll(same[r] & ((1ull << lane) - 1))] = (uint16_t)(first + r * 64 + lane);
+        at += __popcll(same[r]);
+    }
+    __syncthreads();
+    const int per = (n * a.lanes + kSmallThreads - 1) / kSmallThreads;  // rows a group of lanes
+    const int i0 = min(n, (tid / a.lanes) * per), i1 = min(n, i0 + per);
+    const int used = (n * a.lanes + 64 * per - 1) / (64 * per);         // waves with rows
+    for (int t = 0; t < a.tiles; ++t) {
+        const int col = (t * a.lanes + (tid & (a.lanes - 1))) * K;
+        float sum[K] = {};
+        if (col < a.dim) {
+            const T* rows = static_cast<const T*>(a.dout) + col;
+            for (int i = i0; i < i1; i += 8) {
+                float v[8][K];
+#pragma unroll
+                for (int u = 0; u < 8; ++u)  // a place past the end reads its part's last row
+                    load_k<T, K>(rows + list[min(i + u, i1 - 1)] * a.dout_stride, v[u]);
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (i + u < i1)
+#pragma unroll
+                        for (int k = 0; k < K; ++k) sum[k] += v[u][k];
+            }
+        }
+        add_groups<K>(sum, a.lanes);
+        if (used > 1) {
+            if (t) __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) part[wave][lane][k] = sum[k];
+            __syncthreads();
+            if (wave == 0)
+                for (int w = 1; w < used; ++w)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) sum[k] += part[w][lane][k];
+        }
+        if (tid < a.lanes && col < a.dim) put_word<O, K>(a, word, col, sum);
+    }
 }
 
 int64_t elem_bytes(int32_t dtype) { return dtype == EDB_BF16 ? 2 : 4; }
@@ -556,7 +728,7 @@ void launch_embed(const EmbedArgs& a, hipStream_t st) {
 struct GradPlan {
     int32_t piece, lanes, tiles_y, chunk, chunks;
     int32_t passes, digit, sort_tiles;
-    int64_t keys[2], pos[2], counts, totals, partial, bytes;  // offsets
+    int64_t sorted[2], counts, totals, partial, bytes;  // offsets
 };
 
 GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
@@ -566,8 +738,8 @@ GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
     g.lanes = 1;
     while (g.lanes < 64 && g.lanes < pieces) g.lanes *= 2;
     g.tiles_y = (pieces + g.lanes - 1) / g.lanes;
-    // enough chunks for every SIMD to hold several waves, and long ones where there are more than that
-    int64_t chunk = (int64_t)n * g.lanes * g.tiles_y / (64 * 4096) / 8 * 8;
+    // two waves a SIMD, more where chunks would pass 64 rows: short chunks cost partial rows
+    int64_t chunk = (int64_t)n * g.lanes * g.tiles_y / (64 * 2048) / 8 * 8;
     g.chunk = (int32_t)(chunk < 8 ? 8 : chunk > 64 ? 64 : chunk);
     g.chunks = (int32_t)(((int64_t)n + g.chunk - 1) / g.chunk);
     int bits = 1;
@@ -578,34 +750,47 @@ GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    const int64_t list = ((int64_t)n + 7) / 8 * 8 * 4;
+    const int64_t list = ((int64_t)n + 7) / 8 * 8 * (int64_t)sizeof(Pair);
     if (n <= kBlockSort) {
         g.passes = 0;
         g.digit = bits;
-        g.keys[0] = take(list);
-        g.pos[0] = take(list);
+        g.sorted[0] = take(list);
     } else {
         g.passes = (bits + kMaxDigit - 1) / kMaxDigit;
         g.digit = (bits + g.passes - 1) / g.passes;
         g.sort_tiles = (int32_t)(((int64_t)n + kTile - 1) / kTile);
-        for (int i = 0; i < 2; ++i) {
-            g.keys[i] = take(list);
-            g.pos[i] = take(list);
-        }
+        g.sorted[0] = take(list);
+        g.sorted[1] = take(list);
         g.counts = take((int64_t)g.sort_tiles * 4 << g.digit);
         g.totals = take(INT64_C(4) << g.digit);
     }
     g.partial = take((int64_t)g.chunks * 2 * dim * 4);
-    g.bytes = n ? at : 0;
+    g.bytes = n > kSmall ? at : 0;
     return g;
 }
 
 template <class T, class O, int K>
+void launch_small(const SmallArgs& a, hipStream_t st) {
+    const int64_t fill = a.accumulate ? 0 : ((int64_t)a.vocab + a.fill_rows - 1) / a.fill_rows;
+    if (a.n + fill) sum_small<T, O, K><<<(unsigned)(a.n + fill), kSmallThreads, 0, st>>>(a);
+}
+
+template <class T, class O>
+void launch_small(int piece, const SmallArgs& a, hipStream_t st) {
+    if (piece == 8) launch_small<T, O, 8>(a, st);
+    else if (piece == 4) launch_small<T, O, 4>(a, st);
+    else launch_small<T, O, 1>(a, st);
+}
+
+template <class T, class O, int K>
 void launch_sums(const GradPlan& g, const SumArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)(((int64_t)g.chunks * g.lanes + 255) / 256), g.tiles_y);
+    const dim3 grid((unsigned)(a.sum_groups + (a.accumulate ? 0 : ((int64_t)a.vocab + a.fill_rows - 1) / a.fill_rows)),
+                    g.tiles_y);
+    if (grid.x == 0) return;
     if (g.lanes == 64) sum_chunks<T, O, K, true><<<grid, 256, 0, st>>>(a);
     else sum_chunks<T, O, K, false><<<grid, 256, 0, st>>>(a);
-    if (g.chunks > 1) join_chunks<O, K><<<dim3(g.chunks, g.tiles_y), kJoinThreads, 0, st>>>(a);
+    if (g.chunks > 1)
+        join_chunks<O, K><<<dim3((g.chunks + kJoinWaves - 1) / kJoinWaves, g.tiles_y), 64 * kJoinWaves, 0, st>>>(a);
 }
 
 template <class T, class O>
@@ -613,12 +798,6 @@ void launch_sums(const GradPlan& g, const SumArgs& a, hipStream_t st) {
     if (g.piece == 8) launch_sums<T, O, 8>(g, a, st);
     else if (g.piece == 4) launch_sums<T, O, 4>(g, a, st);
     else launch_sums<T, O, 1>(g, a, st);
-}
-
-// Work-groups that fill, beside the sorting ones of a launch.
-int fill_groups(int64_t bytes, int threads) {
-    const int64_t n = (bytes + 64 * threads - 1) / (64 * threads);
-    return (int)(n > 2048 ? 2048 : n);
 }
 
 }  // namespace
@@ -676,58 +855,56 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
         return fail(EDB_ERR_INVALID, "edb_embed_grad: a 16-byte aligned workspace of " + std::to_string(g.bytes) +
                                          " bytes is needed");
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const int64_t row_bytes = dim * elem_bytes(dtable_dtype);
-    FillArgs fill{dtable, dtable_stride * elem_bytes(dtable_dtype), row_bytes, accumulate ? 0 : vocab, 0, 1, 1};
+    const int64_t row_bytes = dim * elem_bytes(dtable_dtype), rows64k = 65536 / row_bytes;
+    const int fill_rows = (int)(rows64k < 1 ? 1 : rows64k > kFillRows ? kFillRows : rows64k);
+    if (n <= kSmall) {
+        const SmallArgs a{ids,         n,     (uint32_t)vocab, dim,    g.lanes,       g.tiles_y, dout,
+                          dout_stride, scale, accumulate,      dtable, dtable_stride, fill_rows};
+        if (dout_dtype == EDB_F32) {
+            if (dtable_dtype == EDB_F32) launch_small<float, float>(g.piece, a, st);
+            else launch_small<float, bf16>(g.piece, a, st);
+        } else {
+            if (dtable_dtype == EDB_F32) launch_small<bf16, float>(g.piece, a, st);
+            else launch_small<bf16, bf16>(g.piece, a, st);
+        }
+        return launched(who);
+    }
     char* ws = static_cast<char*>(workspace);
-    auto at = [&](int64_t off) { return reinterpret_cast<uint32_t*>(ws + off); };
+    auto sorted = [&](int i) { return reinterpret_cast<Pair*>(ws + g.sorted[i]); };
     SortArgs s{};
     s.n = n;
     s.vocab = (uint32_t)vocab;
     int last = 0;
     if (g.passes == 0) {
         s.ids = ids;
-        s.keys_out = at(g.keys[0]);
-        s.pos_out = at(g.pos[0]);
+        s.out = sorted(0);
         s.bits = g.digit;
-        s.fill = fill;
-        sort_block<<<1 + fill_groups(fill.n_rows * row_bytes, 1024), 1024, 0, st>>>(s);
+        sort_block<<<1, 1024, 0, st>>>(s);
     } else {
         s.tiles = g.sort_tiles;
-        s.counts = at(g.counts);
-        s.totals = at(g.totals);
+        s.counts = reinterpret_cast<uint32_t*>(ws + g.counts);
+        s.totals = reinterpret_cast<uint32_t*>(ws + g.totals);
         s.bits = g.digit;
-        fill.shares = 3 * g.passes;
-        const int beside = fill_groups(fill.n_rows * row_bytes / fill.shares, 256), scanners = ((1 << g.digit) + 3) / 4;
         for (int p = 0; p < g.passes; ++p) {
             s.ids = p ? nullptr : ids;
-            s.keys = at(g.keys[(p + 1) & 1]);
-            s.pos = at(g.pos[(p + 1) & 1]);
-            s.keys_out = at(g.keys[p & 1]);
-            s.pos_out = at(g.pos[p & 1]);
+            s.in = sorted((p + 1) & 1);
+            s.out = sorted(p & 1);
             s.shift = p * g.digit;
             last = p & 1;
-            s.fill = fill;
-            s.fill.first = g.sort_tiles;
-            s.fill.share = 3 * p;
-            sort_count<<<g.sort_tiles + beside, 256, 0, st>>>(s);
-            s.fill.first = scanners;
-            s.fill.share = 3 * p + 1;
-            sort_scan<<<scanners + beside, 256, 0, st>>>(s);
-            s.fill.first = g.sort_tiles;
-            s.fill.share = 3 * p + 2;
-            sort_scatter<<<g.sort_tiles + beside, 256, 0, st>>>(s);
+            sort_count<<<g.sort_tiles, 256, 0, st>>>(s);
+            sort_scan<<<((1 << g.digit) + kScanBins - 1) / kScanBins, 256, 0, st>>>(s);
+            sort_scatter<<<g.sort_tiles, 256, 0, st>>>(s);
         }
     }
-    if (n) {
-        const SumArgs a{at(g.keys[last]), at(g.pos[last]), n, g.chunk, (uint32_t)vocab, dim, g.lanes, dout, dout_stride,
-                        scale, accumulate, dtable, dtable_stride, reinterpret_cast<float*>(ws + g.partial)};
-        if (dout_dtype == EDB_F32) {
-            if (dtable_dtype == EDB_F32) launch_sums<float, float>(g, a, st);
-            else launch_sums<float, bf16>(g, a, st);
-        } else {
-            if (dtable_dtype == EDB_F32) launch_sums<bf16, float>(g, a, st);
-            else launch_sums<bf16, bf16>(g, a, st);
-        }
+    const int sum_groups = (int)(((int64_t)g.chunks * g.lanes + 255) / 256);
+    const SumArgs a{sorted(last), n, g.chunk, (uint32_t)vocab, dim, g.lanes, dout, dout_stride, scale,
+                    accumulate, dtable, dtable_stride, reinterpret_cast<float*>(ws + g.partial), sum_groups, fill_rows};
+    if (dout_dtype == EDB_F32) {
+        if (dtable_dtype == EDB_F32) launch_sums<float, float>(g, a, st);
+        else launch_sums<float, bf16>(g, a, st);
+    } else {
+        if (dtable_dtype == EDB_F32) launch_sums<bf16, float>(g, a, st);
+        else launch_sums<bf16, bf16>(g, a, st);
     }
     return launched(who);
 }

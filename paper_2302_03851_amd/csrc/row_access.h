@@ -83,6 +83,9 @@ struct Elem<bf16> {
         }
     }
     static __device__ __forceinline__ u32x2 load_half(const bf16* p) { return *reinterpret_cast<const u32x2_a2*>(p); }
+    static __device__ __forceinline__ u32x2 load_half_nt(const bf16* p) {
+        return __builtin_nontemporal_load(reinterpret_cast<const u32x2_a2*>(p));
+    }
     static __device__ __forceinline__ void unpack_half(u32x2 v, float* x) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {

@@ -665,7 +665,8 @@ REFUSED = (
         (dict(ids=None), INVALID), (dict(dout=None), INVALID), (dict(out=None), INVALID), (dict(out=None, n=0), INVALID),
         (dict(dd=3), INVALID), (dict(od=3), INVALID), (dict(n=-1), INVALID), (dict(V=0), INVALID), (dict(E=0), INVALID),
         (dict(ds=7), INVALID), (dict(os=7), INVALID), (dict(scale=float("nan")), INVALID), (dict(out=2 * A + 64), INVALID),
-        (dict(dout=2 * A + 2), INVALID), (dict(wb=0), INVALID), (dict(ws=None), INVALID), (dict(ws=4 * A + 8), INVALID)]]
+        (dict(dout=2 * A + 2), INVALID), (dict(n=5000, wb=0), INVALID), (dict(n=5000, ws=None), INVALID),
+        (dict(n=5000, ws=4 * A + 8), INVALID)]]
     + [(_logprobs, k, e) for k, e in [(q, e) for q, e in ROWS_BAD if "os" not in q] + [
         (dict(top=-1), UNSUPPORTED), (dict(top=65), UNSUPPORTED), (dict(ids=None), INVALID), (dict(ti=None), INVALID),
         (dict(tl=None), INVALID)]]
@@ -692,7 +693,7 @@ def test_nothing_to_do(call):
 def test_workspace_sizes():
     lib, nb = L.load(), C.c_int64(-1)
     assert lib.edb_logprobs_bytes(5, 1000, L.BF16, 3, C.byref(nb)) == L.EDB_OK and nb.value >= 0
-    assert lib.edb_embed_grad_bytes(1000, 500, 64, C.byref(nb)) == L.EDB_OK and nb.value >= 0
+    assert lib.edb_embed_grad_bytes(9000, 500, 64, C.byref(nb)) == L.EDB_OK and nb.value > 0
     assert lib.edb_logprobs_bytes(5, 1000, L.BF16, 65, C.byref(nb)) == UNSUPPORTED
     assert lib.edb_logprobs_bytes(5, 1000, 9, 3, C.byref(nb)) == INVALID
     assert lib.edb_logprobs_bytes(5, 1000, L.F32, 3, None) == INVALID
