@@ -43,14 +43,14 @@ struct Stats {
         t = (t + s * d) * f;
         s = s * f;
     }
-    __device__ __forceinline__ void add(const float* x, int n, float c) {
-        float top = x[0];
-        for (int i = 1; i < n; ++i) top = fmaxf(top, x[i]);
+    // N values, with `top` their largest
+    template <int N>
+    __device__ __forceinline__ void add(const float* x, float top, float c) {
         const float nm = fmaxf(m, top), ref = nm == -kInf ? 0.f : nm;
         rescale(ref, c);
         m = nm;
 #pragma unroll
-        for (int i = 0; i < n; ++i) {
+        for (int i = 0; i < N; ++i) {
             const float y = (x[i] - ref) * c, e = exp2_hw(y);
             s += e;
             t = __builtin_fmaf(fmaxf(y, kLow), e, t);
@@ -80,32 +80,74 @@ __device__ __forceinline__ Stats wave_join(Stats a, float c) {
     return a;
 }
 
+template <int N>
+__device__ __forceinline__ float largest(const float* x) {
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+    return top;
+}
+
+__device__ __forceinline__ float lane_value(float v, int lane) {  // lane: the same in every lane
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
 // The best entries seen by a wave, lane i holding the i-th best: larger
-// values first, the lowest index first among equal ones.
+// values first, the lowest index first among equal ones.  -inf and NaN are no
+// entries.
 struct Best {
     float v = -kInf;
     int j = kNoIndex;
 
     __device__ __forceinline__ static bool better(float v, int j, float w, int k) { return v > w || (v == w && j < k); }
-    // v, j: the same in every lane
+    // nv, nj: the same in every lane
     __device__ __forceinline__ void insert(float nv, int nj, int lane) {
+        constexpr int kUp = 0x138;  // DPP: every lane takes the value of the one before it
         const int at = __popcll(__ballot(better(v, j, nv, nj)));
-        const float pv = __shfl_up(v, 1);
-        const int pj = __shfl_up(j, 1);
+        const float pv = __builtin_bit_cast(
+            float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kUp, 0xf, 0xf, false));
+        const int pj = __builtin_amdgcn_update_dpp(0, j, kUp, 0xf, 0xf, false);
         v = lane < at ? v : lane == at ? nv : pv;
         j = lane < at ? j : lane == at ? nj : pj;
     }
     // takes one candidate per lane; `top`: entries that count
     __device__ __forceinline__ void offer(float nv, int nj, int top, int lane) {
         for (;;) {
-            const float wv = __shfl(v, top - 1);
-            const int wj = __shfl(j, top - 1);
+            const float wv = lane_value(v, top - 1);
+            const int wj = lane_value(j, top - 1);
             const uint64_t who = __ballot(nv > -kInf && better(nv, nj, wv, wj));
             if (!who) return;
             const int src = __ffsll((unsigned long long)who) - 1;
-            insert(__shfl(nv, src), __shfl(nj, src), lane);
+            insert(lane_value(nv, src), lane_value(nj, src), lane);
             if (lane == src) nv = -kInf;
         }
+    }
+    // The best `top` of n candidates, get(i) giving value and index.  The lanes'
+    // own largest values come first: the top-th of these is a bound that at
+    // least `top` candidates reach, and only few more do, so that there are
+    // about `top` insertions whatever the candidates' order.
+    template <class Get>
+    __device__ __forceinline__ static Best of(int n, int top, int lane, Get get) {
+        float own = -kInf;
+        int j;
+        for (int i = lane; i < n; i += 64) {
+            float w;
+            get(i, w, j);
+            own = fmaxf(own, w);
+        }
+        int above = 0;
+#pragma unroll
+        for (int k = 0; k < 64; ++k) above += better(lane_value(own, k), k, own, lane);
+        const float bound = lane_value(own, __ffsll((unsigned long long)__ballot(above == top - 1)) - 1);
+        Best b;
+        for (int i = lane; i - lane < n; i += 64) {
+            float w = -kInf;
+            j = kNoIndex;
+            if (i < n) get(i, w, j);
+            b.offer(w >= bound ? w : -kInf, j, top, lane);
+        }
+        return b;
     }
 };
 
@@ -119,6 +161,10 @@ struct LogprobArgs {
     float *logprob, *entropy, *stats;
     int32_t* top_ids;
     float* top_logprobs;
+    int32_t part, parts;  // a row is split into `parts` parts of `part` logits
+    Stats* part_stats;    // [n][parts]
+    float* part_v;        // [n][parts][top]
+    int32_t* part_j;
 };
 
 __device__ __forceinline__ void put_left_out(const LogprobArgs& a, int64_t row, int lane) {
@@ -154,52 +200,136 @@ __device__ __forceinline__ void put_row(const LogprobArgs& a, int64_t row, const
     }
 }
 
-// One work-group a row, one pass: 16 bytes a thread and step.
+// A quad is four neighbouring lanes: together they load 64 bytes of the row.
+__device__ __forceinline__ float quad_max(float v) {
+    constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e;  // DPP quad permutations 1,0,3,2 and 2,3,0,1
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kSwap1, 0xf, 0xf, false)));
+    return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kSwap2, 0xf, 0xf, false)));
+}
+
+constexpr int kLogThreads = 256, kLogWaves = kLogThreads / 64;
+constexpr int kLoads = 4;  // 16-byte loads of a thread in flight
+
+// A work-group takes a part of a row (mostly all of it) in one pass, 16 bytes a
+// load.  For the alternatives each quad of lanes leaves the largest of its 64
+// bytes in LDS: the best `top` logits lie in the best `top` of these groups (a
+// group that does not belong to them has `top` groups with a better logit
+// before it), so at the end one wave looks for those groups and reads them again.
 template <class T, bool TOP>
-__global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a) {
-    constexpr int N = Elem<T>::kVec;
-    const int64_t row = blockIdx.x;
+__global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
+    constexpr int N = Elem<T>::kVec, kStep = kLogThreads * N;
+    extern __shared__ float group_max[];
+    __shared__ float part_m[kLogWaves], part_s[kLogWaves], part_t[kLogWaves];
+    const int64_t row = blockIdx.x / a.parts;
+    const int which = blockIdx.x - (int)row * a.parts;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* x = static_cast<const T*>(a.logits) + row * a.stride;
-    const int V = a.vocab;
+    const int V = a.vocab, begin = which * a.part, end = min(V, begin + a.part);
     const int id = a.ids ? a.ids[row] : 0;
     if (id < 0 || id >= V) {
-        if (wave == 0) put_left_out(a, row, lane);
+        if (a.parts == 1 && wave == 0) put_left_out(a, row, lane);
         return;
     }
     Stats st = Stats::none();
-    Best best;
-    for (int j0 = wave * 64 * N; j0 < V; j0 += 256 * N) {
-        const int j = j0 + lane * N;
-        float v[N];
-        if (j + N <= V) {
-            Elem<T>::unpack(Elem<T>::load(x + j), v);
+    for (int j0 = begin; j0 < end; j0 += kLoads * kStep) {
+        const int j = j0 + tid * N;
+        float v[kLoads][N];
+        if (j0 + kLoads * kStep <= end) {
+            u32x4 raw[kLoads];
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + u * kStep);
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) Elem<T>::unpack(raw[u], v[u]);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
+            for (int u = 0; u < kLoads; ++u) {
+                const int k = j + u * kStep;
+                if (k + N <= end) {
+                    Elem<T>::unpack(Elem<T>::load(x + k), v[u]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[u][i] = k + i < end ? Elem<T>::get(x + k + i) : -kInf;
+                }
+            }
         }
-        st.add(v, N, a.c);
+        float top[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) top[u] = largest<N>(v[u]);
+        st.add<kLoads * N>(&v[0][0], largest<kLoads>(top), a.c);
         if constexpr (TOP) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) best.offer(v[i], j + i, a.top, lane);
+            for (int u = 0; u < kLoads; ++u) {
+                const float q = quad_max(top[u]);
+                if ((lane & 3) == 0 && j + u * kStep < end) group_max[(j + u * kStep - begin) / (4 * N)] = q;
+            }
         }
     }
     st = wave_join(st, a.c);
-    __shared__ Stats part[4];
-    __shared__ float best_v[4][64];
-    __shared__ int best_j[4][64];
-    if (lane == 0) part[wave] = st;
-    if constexpr (TOP) {
-        best_v[wave][lane] = best.v;
-        best_j[wave][lane] = best.j;
+    if (lane == 0) {
+        part_m[wave] = st.m;
+        part_s[wave] = st.s;
+        part_t[wave] = st.t;
     }
     __syncthreads();
     if (wave) return;
-    for (int w = 1; w < 4; ++w) {
-        st.join(part[w], a.c);
-        if constexpr (TOP) best.offer(best_v[w][lane], best_j[w][lane], a.top, lane);
+    for (int w = 1; w < kLogWaves; ++w) st.join(Stats{part_m[w], part_s[w], part_t[w]}, a.c);
+    Best best;
+    if constexpr (TOP) {
+        constexpr int kGroup = 4 * N, kAtOnce = 64 / kGroup;
+        const Best groups = Best::of((end - begin + kGroup - 1) / kGroup, a.top, lane, [&](int i, float& w, int& j) {
+            w = group_max[i];
+            j = i;
+        });
+        const int there = __popcll(__ballot(lane < a.top && groups.v > -kInf));
+        const float bound = lane_value(groups.v, a.top - 1);
+        for (int g0 = 0; g0 < there; g0 += 4 * kAtOnce) {
+            float w[4];
+            int j[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int g = g0 + u * kAtOnce + lane / kGroup;
+                j[u] = begin + __shfl(groups.j, g & 63) * kGroup + lane % kGroup;
+                w[u] = g < there && j[u] < end ? Elem<T>::get(x + j[u]) : -kInf;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) best.offer(w[u] >= bound ? w[u] : -kInf, j[u], a.top, lane);
+        }
     }
-    put_row(a, row, st, best, a.ids ? Elem<T>::get(x + id) : 0.f, lane);
+    if (a.parts == 1) {
+        put_row(a, row, st, best, a.ids ? Elem<T>::get(x + id) : 0.f, lane);
+    } else {
+        const int64_t at = row * a.parts + which;
+        if (lane == 0) a.part_stats[at] = st;
+        if (lane < a.top) {
+            a.part_v[at * a.top + lane] = best.v;
+            a.part_j[at * a.top + lane] = best.j;
+        }
+    }
+}
+
+// Joins the parts of split rows: a wave a row.
+template <class T>
+__global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const int id = a.ids ? a.ids[row] : 0;
+    if (id < 0 || id >= a.vocab) {
+        put_left_out(a, row, lane);
+        return;
+    }
+    Stats st = Stats::none();
+    for (int i = lane; i < a.parts; i += 64) st.join(a.part_stats[row * a.parts + i], a.c);
+    st = wave_join(st, a.c);
+    Best best;
+    if (a.top) {
+        const float* v = a.part_v + row * a.parts * a.top;
+        const int32_t* idx = a.part_j + row * a.parts * a.top;
+        best = Best::of(a.parts * a.top, a.top, lane, [&](int i, float& w, int& j) {
+            w = v[i];
+            j = idx[i];
+        });
+    }
+    put_row(a, row, st, best, a.ids ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.stride + id) : 0.f, lane);
 }
 
 struct GradArgs {
@@ -338,7 +468,7 @@ __global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
             }
-            st.add(v, N, a.c);
+            st.add<N>(v, largest<N>(v), a.c);
         }
     st = wave_join(st, a.c);
     if (lane == 0) part[wave] = st;
@@ -434,6 +564,33 @@ edb_status launched(const char* who) {
     return EDB_OK;
 }
 
+// How a forward call splits its rows, and its scratch memory.
+struct RowPlan {
+    int32_t part, parts;
+    int64_t stats, v, j, bytes;  // offsets
+};
+
+// A row is split where there are too few rows for the card, and where a part's
+// group maxima would pass 32 KB of LDS.  Parts are whole steps of a work-group.
+RowPlan row_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
+    constexpr int32_t kMost = 131072;
+    const int32_t step = kLoads * kLogThreads * (dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec);
+    const int64_t steps = ((int64_t)vocab + step - 1) / step;
+    int64_t parts = n >= 512 ? 1 : (512 + n - 1) / (n < 1 ? 1 : n);
+    if (parts > steps) parts = steps;
+    if (parts * kMost < vocab) parts = ((int64_t)vocab + kMost - 1) / kMost;
+    RowPlan r{};
+    r.part = (int32_t)((steps + parts - 1) / parts * step);
+    r.parts = (int32_t)(((int64_t)vocab + r.part - 1) / r.part);
+    if (r.parts == 1) return r;
+    const int64_t all = (int64_t)n * r.parts;
+    auto aligned16 = [](int64_t b) { return (b + 15) / 16 * 16; };
+    r.v = aligned16(all * (int64_t)sizeof(Stats));
+    r.j = r.v + aligned16(all * top * 4);
+    r.bytes = r.j + all * top * 4;
+    return r;
+}
+
 float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
 
 }  // namespace
@@ -444,7 +601,7 @@ extern "C" edb_status edb_logprobs_bytes(int32_t n, int32_t vocab, int32_t dtype
     if (top < 0 || top > EDB_LOGPROBS_MAX_TOP)
         return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs_bytes: top must be in [0, " +
                                              std::to_string(EDB_LOGPROBS_MAX_TOP) + "]");
-    *bytes = 0;
+    *bytes = row_plan(n, vocab, dtype, top).bytes;
     edb::clear_error();
     return EDB_OK;
 }
@@ -459,22 +616,46 @@ extern "C" edb_status edb_logprobs(const void* logits, int32_t dtype, int32_t n,
         return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs: top must be in [0, " + std::to_string(EDB_LOGPROBS_MAX_TOP) + "]");
     if (logprob && !ids) return fail(EDB_ERR_INVALID, "edb_logprobs: log probabilities need the given tokens");
     if (n && top && (!top_ids || !top_logprobs)) return fail(EDB_ERR_INVALID, "edb_logprobs: NULL list of alternatives");
-    (void)workspace;
-    (void)workspace_bytes;
     if (n == 0) {
         edb::clear_error();
         return EDB_OK;
     }
-    LogprobArgs a{logits, stride, n,      vocab,   ids,   log2e_over(temperature), (float)(1.0 / (double)temperature),
-                  top,    logprob, entropy, stats, top_ids, top_logprobs};
+    const RowPlan r = row_plan(n, vocab, dtype, top);
+    if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+        return fail(EDB_ERR_INVALID, "edb_logprobs: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
+                                         " bytes is needed");
+    if ((int64_t)n * r.parts > INT32_MAX) return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs: more than 2^31 parts of rows");
+    char* ws = static_cast<char*>(workspace);
+    const LogprobArgs a{logits,
+                        stride,
+                        n,
+                        vocab,
+                        ids,
+                        log2e_over(temperature),
+                        (float)(1.0 / (double)temperature),
+                        top,
+                        logprob,
+                        entropy,
+                        stats,
+                        top_ids,
+                        top_logprobs,
+                        r.part,
+                        r.parts,
+                        reinterpret_cast<Stats*>(ws + r.stats),
+                        reinterpret_cast<float*>(ws + r.v),
+                        reinterpret_cast<int32_t*>(ws + r.j)};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const dim3 grid(n), block(256);
+    const dim3 grid(n * r.parts);
     if (dtype == EDB_F32) {
-        if (top) logprobs_kernel<float, true><<<grid, block, 0, st>>>(a);
-        else logprobs_kernel<float, false><<<grid, block, 0, st>>>(a);
+        const size_t lds = ((size_t)(r.part < vocab ? r.part : vocab) / (4 * Elem<float>::kVec) + 1) * 4;
+        if (top) logprobs_kernel<float, true><<<grid, kLogThreads, lds, st>>>(a);
+        else logprobs_kernel<float, false><<<grid, kLogThreads, 0, st>>>(a);
+        if (r.parts > 1) logprobs_join<float><<<n, 64, 0, st>>>(a);
     } else {
-        if (top) logprobs_kernel<bf16, true><<<grid, block, 0, st>>>(a);
-        else logprobs_kernel<bf16, false><<<grid, block, 0, st>>>(a);
+        const size_t lds = ((size_t)(r.part < vocab ? r.part : vocab) / (4 * Elem<bf16>::kVec) + 1) * 4;
+        if (top) logprobs_kernel<bf16, true><<<grid, kLogThreads, lds, st>>>(a);
+        else logprobs_kernel<bf16, false><<<grid, kLogThreads, 0, st>>>(a);
+        if (r.parts > 1) logprobs_join<bf16><<<n, 64, 0, st>>>(a);
     }
     return launched(who);
 }

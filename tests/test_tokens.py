@@ -669,7 +669,8 @@ REFUSED = (
         (dict(n=5000, ws=4 * A + 8), INVALID)]]
     + [(_logprobs, k, e) for k, e in [(q, e) for q, e in ROWS_BAD if "os" not in q] + [
         (dict(top=-1), UNSUPPORTED), (dict(top=65), UNSUPPORTED), (dict(ids=None), INVALID), (dict(ti=None), INVALID),
-        (dict(tl=None), INVALID)]]
+        (dict(tl=None), INVALID), (dict(n=1, V=100000, s=100000, wb=0), INVALID), (dict(n=1, V=100000, s=100000, ws=None), INVALID),
+        (dict(n=1, V=100000, s=100000, ws=4 * A + 4), INVALID)]]
     + [(_lp_grad, k, e) for k, e in ROWS_BAD + [
         (dict(ids=None), INVALID), (dict(st=None), INVALID), (dict(h=None), INVALID), (dict(out=None), INVALID), (dict(os=9), INVALID),
         (dict(out=A + 4), INVALID), (dict(out=A, os=12), INVALID), (dict(out=4 * A + 2), INVALID)]]
@@ -694,6 +695,7 @@ def test_workspace_sizes():
     lib, nb = L.load(), C.c_int64(-1)
     assert lib.edb_logprobs_bytes(5, 1000, L.BF16, 3, C.byref(nb)) == L.EDB_OK and nb.value >= 0
     assert lib.edb_embed_grad_bytes(9000, 500, 64, C.byref(nb)) == L.EDB_OK and nb.value > 0
+    assert lib.edb_logprobs_bytes(1, 1 << 30, L.F32, 64, C.byref(nb)) == L.EDB_OK and nb.value > 0
     assert lib.edb_logprobs_bytes(5, 1000, L.BF16, 65, C.byref(nb)) == UNSUPPORTED
     assert lib.edb_logprobs_bytes(5, 1000, 9, 3, C.byref(nb)) == INVALID
     assert lib.edb_logprobs_bytes(5, 1000, L.F32, 3, None) == INVALID
