@@ -27,7 +27,6 @@ constexpr float kLn2 = 0.69314718055994531f;
 // of 0 would be inf * 0 (a logit of -inf, or a difference past the fp32 range).
 constexpr float kLow = -1.0e4f;
 constexpr float kInf = __builtin_huge_valf();
-constexpr int kNoIndex = 0x7fffffff;
 
 __device__ __forceinline__ float exp2_hw(float y) { return __builtin_amdgcn_exp2f(y); }
 
@@ -88,66 +87,125 @@ __device__ __forceinline__ float largest(const float* x) {
     return top;
 }
 
-__device__ __forceinline__ float lane_value(float v, int lane) {  // lane: the same in every lane
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+// ---- the best entries of a row
+//
+// An entry (value, index) is a 64-bit key that orders it: larger values first,
+// the lowest index first among equal ones (+0 and -0 are equal).  -inf and NaN
+// are no entries, key 0.
+typedef uint64_t Key;
+
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ Key key_of(float v, int j) {
+    return v > -kInf ? (Key)ordered(v) << 32 | (uint32_t)~j : 0;
+}
+__device__ __forceinline__ float key_value(Key k) {
+    const uint32_t u = (uint32_t)(k >> 32);
+    return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ int key_index(Key k) { return (int)~(uint32_t)k; }
 
-// The best entries seen by a wave, lane i holding the i-th best: larger
-// values first, the lowest index first among equal ones.  -inf and NaN are no
-// entries.
+// The value of lane (l ^ D), by data-parallel moves inside rows of 16 lanes.
+template <int D>
+__device__ __forceinline__ uint32_t from_lane_xor(uint32_t v) {
+    if constexpr (D == 4) return from_lane_xor<3>(from_lane_xor<7>(v));
+    else if constexpr (D == 1 || D == 2 || D == 3 || D == 7 || D == 8 || D == 15) {
+        // quad permutations 1,0,3,2 / 2,3,0,1 / 3,2,1,0, half-row and row mirrors, row rotation by 8
+        constexpr int kMove = D == 1 ? 0xb1 : D == 2 ? 0x4e : D == 3 ? 0x1b : D == 7 ? 0x141 : D == 15 ? 0x140 : 0x128;
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kMove, 0xf, 0xf, false);
+    } else {
+        return (uint32_t)__shfl_xor((int)v, D);
+    }
+}
+
+// Lanes l and l ^ D end with their larger key in the lower lane.
+template <int D>
+__device__ __forceinline__ Key order_with(Key k, int lane) {
+    constexpr int kHigh = D & 32 ? 32 : D & 16 ? 16 : D & 8 ? 8 : D & 4 ? 4 : D & 2 ? 2 : 1;
+    const Key o = (Key)from_lane_xor<D>((uint32_t)(k >> 32)) << 32 | from_lane_xor<D>((uint32_t)k);
+    return (o > k) == ((lane & kHigh) == 0) ? o : k;
+}
+
+// Sorts a wave's keys, the largest in lane 0 (bitonic, the first step of every
+// merge against the mirrored half, so that all steps order the same way).
+__device__ __forceinline__ Key merge_down(Key k, int lane) {  // of a bitonic sequence over the wave
+    k = order_with<32>(k, lane);
+    k = order_with<16>(k, lane);
+    k = order_with<8>(k, lane);
+    k = order_with<4>(k, lane);
+    k = order_with<2>(k, lane);
+    return order_with<1>(k, lane);
+}
+__device__ __forceinline__ Key sort_down(Key k, int lane) {
+    k = order_with<1>(k, lane);
+    k = order_with<3>(k, lane);
+    k = order_with<1>(k, lane);
+    k = order_with<7>(k, lane);
+    k = order_with<2>(k, lane);
+    k = order_with<1>(k, lane);
+    k = order_with<15>(k, lane);
+    k = order_with<4>(k, lane);
+    k = order_with<2>(k, lane);
+    k = order_with<1>(k, lane);
+    k = order_with<31>(k, lane);
+    k = order_with<8>(k, lane);
+    k = order_with<4>(k, lane);
+    k = order_with<2>(k, lane);
+    k = order_with<1>(k, lane);
+    k = order_with<63>(k, lane);
+    k = order_with<16>(k, lane);
+    k = order_with<8>(k, lane);
+    k = order_with<4>(k, lane);
+    k = order_with<2>(k, lane);
+    return order_with<1>(k, lane);
+}
+
+// The best entries among those offered to a wave, sorted, lane i holding the
+// i-th.  Offered entries wait in LDS until there are 64 or no more come.
 struct Best {
-    float v = -kInf;
-    int j = kNoIndex;
+    Key key = 0;
+    int waiting = 0;
+    uint32_t bound;  // order of a value that at least `top` entries reach
 
-    __device__ __forceinline__ static bool better(float v, int j, float w, int k) { return v > w || (v == w && j < k); }
-    // nv, nj: the same in every lane
-    __device__ __forceinline__ void insert(float nv, int nj, int lane) {
-        constexpr int kUp = 0x138;  // DPP: every lane takes the value of the one before it
-        const int at = __popcll(__ballot(better(v, j, nv, nj)));
-        const float pv = __builtin_bit_cast(
-            float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kUp, 0xf, 0xf, false));
-        const int pj = __builtin_amdgcn_update_dpp(0, j, kUp, 0xf, 0xf, false);
-        v = lane < at ? v : lane == at ? nv : pv;
-        j = lane < at ? j : lane == at ? nj : pj;
-    }
-    // takes one candidate per lane; `top`: entries that count
-    __device__ __forceinline__ void offer(float nv, int nj, int top, int lane) {
-        for (;;) {
-            const float wv = lane_value(v, top - 1);
-            const int wj = lane_value(j, top - 1);
-            const uint64_t who = __ballot(nv > -kInf && better(nv, nj, wv, wj));
-            if (!who) return;
-            const int src = __ffsll((unsigned long long)who) - 1;
-            insert(lane_value(nv, src), lane_value(nj, src), lane);
-            if (lane == src) nv = -kInf;
-        }
-    }
-    // The best `top` of n candidates, get(i) giving value and index.  The lanes'
-    // own largest values come first: the top-th of these is a bound that at
-    // least `top` candidates reach, and only few more do, so that there are
-    // about `top` insertions whatever the candidates' order.
-    template <class Get>
-    __device__ __forceinline__ static Best of(int n, int top, int lane, Get get) {
-        float own = -kInf;
-        int j;
-        for (int i = lane; i < n; i += 64) {
-            float w;
-            get(i, w, j);
-            own = fmaxf(own, w);
-        }
-        int above = 0;
+    // A bound from the orders of values of different entries, one a lane (0 for none): the
+    // top-th largest, its lower 16 bits left open.
+    __device__ __forceinline__ static uint32_t bound_of(uint32_t u, int top) {
+        uint32_t b = 0;
 #pragma unroll
-        for (int k = 0; k < 64; ++k) above += better(lane_value(own, k), k, own, lane);
-        const float bound = lane_value(own, __ffsll((unsigned long long)__ballot(above == top - 1)) - 1);
-        Best b;
-        for (int i = lane; i - lane < n; i += 64) {
-            float w = -kInf;
-            j = kNoIndex;
-            if (i < n) get(i, w, j);
-            b.offer(w >= bound ? w : -kInf, j, top, lane);
+        for (int bit = 31; bit >= 16; --bit) {
+            const uint32_t t = b | 1u << bit;
+            if (__popcll(__ballot(u >= t)) >= top) b = t;
         }
         return b;
+    }
+    __device__ __forceinline__ void take(Key* wait, int top, int lane) {
+        Key k = sort_down(lane < waiting ? wait[lane] : 0, lane);
+        if (key_at(0)) {  // the larger ones of the list and the mirrored newcomers: a bitonic sequence
+            const Key o = (Key)(uint32_t)__shfl_xor((int)(k >> 32), 63) << 32 | (uint32_t)__shfl_xor((int)k, 63);
+            k = merge_down(o > key ? o : key, lane);
+        }
+        key = k;
+        waiting = 0;
+        const uint32_t last = (uint32_t)(key_at(top - 1) >> 32);
+        bound = last > bound ? last : bound;
+    }
+    __device__ __forceinline__ Key key_at(int lane) const {  // lane: the same in every lane
+        return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)key, lane);
+    }
+    // one entry a lane, 0 for none
+    __device__ __forceinline__ void offer(Key k, Key* wait, int top, int lane) {
+        uint64_t who = __ballot(k && (uint32_t)(k >> 32) >= bound);
+        if (!who) return;
+        if (waiting + __popcll(who) > 64) {
+            take(wait, top, lane);
+            who = __ballot(k && (uint32_t)(k >> 32) >= bound);
+        }
+        if ((who >> lane) & 1) wait[waiting + __popcll(who & ((1ull << lane) - 1))] = k;
+        waiting += __popcll(who);
+        __builtin_amdgcn_wave_barrier();
     }
 };
 
@@ -163,8 +221,7 @@ struct LogprobArgs {
     float* top_logprobs;
     int32_t part, parts;  // a row is split into `parts` parts of `part` logits
     Stats* part_stats;    // [n][parts]
-    float* part_v;        // [n][parts][top]
-    int32_t* part_j;
+    Key* part_keys;       // [n][parts][top]
 };
 
 __device__ __forceinline__ void put_left_out(const LogprobArgs& a, int64_t row, int lane) {
@@ -180,14 +237,13 @@ __device__ __forceinline__ void put_left_out(const LogprobArgs& a, int64_t row, 
 }
 
 // The results of a row from its joined statistics and best entries (one wave).
-__device__ __forceinline__ void put_row(const LogprobArgs& a, int64_t row, const Stats& st, const Best& best,
-                                        float given, int lane) {
+__device__ __forceinline__ void put_row(const LogprobArgs& a, int64_t row, const Stats& st, Key best, float given,
+                                        int lane) {
     const bool empty = st.m == -kInf && st.s == 0.f;
     const float l = empty ? 0.f : logf(st.s), ref = empty ? 0.f : st.m;
     if (lane < a.top) {
-        const bool there = best.v > -kInf;
-        a.top_ids[row * a.top + lane] = there ? best.j : -1;
-        a.top_logprobs[row * a.top + lane] = there ? (best.v - ref) * a.inv_t - l : -kInf;
+        a.top_ids[row * a.top + lane] = best ? key_index(best) : -1;
+        a.top_logprobs[row * a.top + lane] = best ? (key_value(best) - ref) * a.inv_t - l : -kInf;
     }
     if (lane == 0) {
         if (a.logprob) a.logprob[row] = (given - ref) * a.inv_t - l;
@@ -202,9 +258,8 @@ __device__ __forceinline__ void put_row(const LogprobArgs& a, int64_t row, const
 
 // A quad is four neighbouring lanes: together they load 64 bytes of the row.
 __device__ __forceinline__ float quad_max(float v) {
-    constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e;  // DPP quad permutations 1,0,3,2 and 2,3,0,1
-    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kSwap1, 0xf, 0xf, false)));
-    return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kSwap2, 0xf, 0xf, false)));
+    v = fmaxf(v, __builtin_bit_cast(float, from_lane_xor<1>(__builtin_bit_cast(uint32_t, v))));
+    return fmaxf(v, __builtin_bit_cast(float, from_lane_xor<2>(__builtin_bit_cast(uint32_t, v))));
 }
 
 constexpr int kLogThreads = 256, kLogWaves = kLogThreads / 64;
@@ -220,6 +275,7 @@ __global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
     constexpr int N = Elem<T>::kVec, kStep = kLogThreads * N;
     extern __shared__ float group_max[];
     __shared__ float part_m[kLogWaves], part_s[kLogWaves], part_t[kLogWaves];
+    __shared__ Key wait[64];
     const int64_t row = blockIdx.x / a.parts;
     const int which = blockIdx.x - (int)row * a.parts;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -232,18 +288,18 @@ __global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
     }
     Stats st = Stats::none();
     for (int j0 = begin; j0 < end; j0 += kLoads * kStep) {
-        const int j = j0 + tid * N;
+        const int j = j0 + (wave * kLoads * 64 + lane) * N;  // a wave's loads are neighbours
         float v[kLoads][N];
         if (j0 + kLoads * kStep <= end) {
             u32x4 raw[kLoads];
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + u * kStep);
+            for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + u * 64 * N);
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) Elem<T>::unpack(raw[u], v[u]);
         } else {
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
-                const int k = j + u * kStep;
+                const int k = j + u * 64 * N;
                 if (k + N <= end) {
                     Elem<T>::unpack(Elem<T>::load(x + k), v[u]);
                 } else {
@@ -260,7 +316,7 @@ __global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
                 const float q = quad_max(top[u]);
-                if ((lane & 3) == 0 && j + u * kStep < end) group_max[(j + u * kStep - begin) / (4 * N)] = q;
+                if ((lane & 3) == 0 && j + u * 64 * N < end) group_max[(j + u * 64 * N - begin) / (4 * N)] = q;
             }
         }
     }
@@ -276,34 +332,35 @@ __global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
     Best best;
     if constexpr (TOP) {
         constexpr int kGroup = 4 * N, kAtOnce = 64 / kGroup;
-        const Best groups = Best::of((end - begin + kGroup - 1) / kGroup, a.top, lane, [&](int i, float& w, int& j) {
-            w = group_max[i];
-            j = i;
-        });
-        const int there = __popcll(__ballot(lane < a.top && groups.v > -kInf));
-        const float bound = lane_value(groups.v, a.top - 1);
+        const int n = (end - begin + kGroup - 1) / kGroup;
+        float own = -kInf;
+        for (int i = lane; i < n; i += 64) own = fmaxf(own, group_max[i]);
+        Best groups;
+        groups.bound = Best::bound_of(own > -kInf ? ordered(own) : 0, a.top);
+        for (int i = lane; i - lane < n; i += 64) groups.offer(i < n ? key_of(group_max[i], i) : 0, wait, a.top, lane);
+        groups.take(wait, a.top, lane);
+        const int there = __popcll(__ballot(lane < a.top && groups.key));
+        best.bound = groups.bound;
         for (int g0 = 0; g0 < there; g0 += 4 * kAtOnce) {
             float w[4];
             int j[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int g = g0 + u * kAtOnce + lane / kGroup;
-                j[u] = begin + __shfl(groups.j, g & 63) * kGroup + lane % kGroup;
+                j[u] = begin + key_index((Key)(uint32_t)__shfl((int)groups.key, g & 63)) * kGroup + lane % kGroup;
                 w[u] = g < there && j[u] < end ? Elem<T>::get(x + j[u]) : -kInf;
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) best.offer(w[u] >= bound ? w[u] : -kInf, j[u], a.top, lane);
+            for (int u = 0; u < 4; ++u) best.offer(key_of(w[u], j[u]), wait, a.top, lane);
         }
+        best.take(wait, a.top, lane);
     }
     if (a.parts == 1) {
-        put_row(a, row, st, best, a.ids ? Elem<T>::get(x + id) : 0.f, lane);
+        put_row(a, row, st, best.key, a.ids ? Elem<T>::get(x + id) : 0.f, lane);
     } else {
         const int64_t at = row * a.parts + which;
         if (lane == 0) a.part_stats[at] = st;
-        if (lane < a.top) {
-            a.part_v[at * a.top + lane] = best.v;
-            a.part_j[at * a.top + lane] = best.j;
-        }
+        if (lane < a.top) a.part_keys[at * a.top + lane] = best.key;
     }
 }
 
@@ -322,14 +379,19 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
     st = wave_join(st, a.c);
     Best best;
     if (a.top) {
-        const float* v = a.part_v + row * a.parts * a.top;
-        const int32_t* idx = a.part_j + row * a.parts * a.top;
-        best = Best::of(a.parts * a.top, a.top, lane, [&](int i, float& w, int& j) {
-            w = v[i];
-            j = idx[i];
-        });
+        __shared__ Key wait[64];
+        const Key* keys = a.part_keys + row * a.parts * a.top;
+        const int n = a.parts * a.top;
+        // bounds: every part's last entry, and the lanes' own largest ones
+        uint32_t own = 0, last = 0;
+        for (int i = lane; i < n; i += 64) own = max(own, (uint32_t)(keys[i] >> 32));
+        for (int i = lane; i < a.parts; i += 64) last = max(last, (uint32_t)(keys[(i + 1) * a.top - 1] >> 32));
+        for (int d = 1; d < 64; d <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, d));
+        best.bound = max(last, Best::bound_of(own, a.top));
+        for (int i = lane; i - lane < n; i += 64) best.offer(i < n ? keys[i] : 0, wait, a.top, lane);
+        best.take(wait, a.top, lane);
     }
-    put_row(a, row, st, best, a.ids ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.stride + id) : 0.f, lane);
+    put_row(a, row, st, best.key, a.ids ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.stride + id) : 0.f, lane);
 }
 
 struct GradArgs {
@@ -567,14 +629,14 @@ edb_status launched(const char* who) {
 // How a forward call splits its rows, and its scratch memory.
 struct RowPlan {
     int32_t part, parts;
-    int64_t stats, v, j, bytes;  // offsets
+    int64_t stats, keys, bytes;  // offsets
 };
 
 // A row is split where there are too few rows for the card, and where a part's
 // group maxima would pass 32 KB of LDS.  Parts are whole steps of a work-group.
 RowPlan row_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     constexpr int32_t kMost = 131072;
-    const int32_t step = kLoads * kLogThreads * (dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec);
+    const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec, step = kLoads * kLogThreads * vec;
     const int64_t steps = ((int64_t)vocab + step - 1) / step;
     int64_t parts = n >= 512 ? 1 : (512 + n - 1) / (n < 1 ? 1 : n);
     if (parts > steps) parts = steps;
@@ -584,11 +646,16 @@ RowPlan row_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     r.parts = (int32_t)(((int64_t)vocab + r.part - 1) / r.part);
     if (r.parts == 1) return r;
     const int64_t all = (int64_t)n * r.parts;
-    auto aligned16 = [](int64_t b) { return (b + 15) / 16 * 16; };
-    r.v = aligned16(all * (int64_t)sizeof(Stats));
-    r.j = r.v + aligned16(all * top * 4);
-    r.bytes = r.j + all * top * 4;
+    r.keys = (all * (int64_t)sizeof(Stats) + 15) / 16 * 16;
+    r.bytes = r.keys + all * top * (int64_t)sizeof(Key);
     return r;
+}
+
+// LDS for the group maxima of a part.
+template <class T>
+size_t group_bytes(const RowPlan& r, int32_t vocab) {
+    const size_t places = r.parts > 1 ? (size_t)r.part : (size_t)vocab;
+    return (places / (4 * Elem<T>::kVec) + 1) * 4;
 }
 
 float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
@@ -642,17 +709,16 @@ extern "C" edb_status edb_logprobs(const void* logits, int32_t dtype, int32_t n,
                         r.part,
                         r.parts,
                         reinterpret_cast<Stats*>(ws + r.stats),
-                        reinterpret_cast<float*>(ws + r.v),
-                        reinterpret_cast<int32_t*>(ws + r.j)};
+                        reinterpret_cast<Key*>(ws + r.keys)};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const dim3 grid(n * r.parts);
     if (dtype == EDB_F32) {
-        const size_t lds = ((size_t)(r.part < vocab ? r.part : vocab) / (4 * Elem<float>::kVec) + 1) * 4;
+        const size_t lds = group_bytes<float>(r, vocab);
         if (top) logprobs_kernel<float, true><<<grid, kLogThreads, lds, st>>>(a);
         else logprobs_kernel<float, false><<<grid, kLogThreads, 0, st>>>(a);
         if (r.parts > 1) logprobs_join<float><<<n, 64, 0, st>>>(a);
     } else {
-        const size_t lds = ((size_t)(r.part < vocab ? r.part : vocab) / (4 * Elem<bf16>::kVec) + 1) * 4;
+        const size_t lds = group_bytes<bf16>(r, vocab);
         if (top) logprobs_kernel<bf16, true><<<grid, kLogThreads, lds, st>>>(a);
         else logprobs_kernel<bf16, false><<<grid, kLogThreads, 0, st>>>(a);
         if (r.parts > 1) logprobs_join<bf16><<<n, 64, 0, st>>>(a);
