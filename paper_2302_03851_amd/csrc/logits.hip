@@ -30,54 +30,109 @@ constexpr float kInf = __builtin_huge_valf();
 
 __device__ __forceinline__ float exp2_hw(float y) { return __builtin_amdgcn_exp2f(y); }
 
-// Running softmax statistics relative to the maximum so far: s = sum 2^y and
-// t = sum y 2^y with y = (x - m) c.  A NaN or +inf logit makes s NaN.
+// The value of lane (l ^ D), by data-parallel moves inside rows of 16 lanes.
+template <int D>
+__device__ __forceinline__ uint32_t from_lane_xor(uint32_t v) {
+    if constexpr (D == 4) return from_lane_xor<3>(from_lane_xor<7>(v));
+    else if constexpr (D == 1 || D == 2 || D == 3 || D == 7 || D == 8 || D == 15) {
+        // quad permutations 1,0,3,2 / 2,3,0,1 / 3,2,1,0, half-row and row mirrors, row rotation by 8
+        constexpr int kMove = D == 1 ? 0xb1 : D == 2 ? 0x4e : D == 3 ? 0x1b : D == 7 ? 0x141 : D == 15 ? 0x140 : 0x128;
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kMove, 0xf, 0xf, false);
+    } else {
+        return (uint32_t)__shfl_xor((int)v, D);
+    }
+}
+
+template <int D>
+__device__ __forceinline__ float from_lane_xor(float v) {
+    return __builtin_bit_cast(float, from_lane_xor<D>(__builtin_bit_cast(uint32_t, v)));
+}
+// Over the wave, in every lane; sums in the same order in every run.
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, from_lane_xor<1>(v));
+    v = fmaxf(v, from_lane_xor<2>(v));
+    v = fmaxf(v, from_lane_xor<7>(v));
+    v = fmaxf(v, from_lane_xor<8>(v));
+    v = fmaxf(v, from_lane_xor<16>(v));
+    return fmaxf(v, from_lane_xor<32>(v));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v += from_lane_xor<1>(v);
+    v += from_lane_xor<2>(v);
+    v += from_lane_xor<7>(v);
+    v += from_lane_xor<8>(v);
+    v += from_lane_xor<16>(v);
+    return v + from_lane_xor<32>(v);
+}
+
+// Running softmax statistics: the largest logit m, and s = sum 2^y, t = sum y 2^y
+// with y = x c - r(m).  The reference r is m c rounded to fp32, so that y is one
+// fused multiply-add and its own rounding the only one; where m c comes near
+// the fp32 range (rows of the lowest values) r is m c itself and y = (x - m) c.
+// A NaN or +inf logit makes s NaN.
 struct Stats {
     float m, s, t;
 
     static __device__ __forceinline__ Stats none() { return {-kInf, 0.f, 0.f}; }
-    // the sums rescaled to the reference `ref` (the maximum, 0 while it is -inf)
-    __device__ __forceinline__ void rescale(float ref, float c) {
-        const float d = fmaxf((m - ref) * c, kLow), f = exp2_hw(d);
+    static __device__ __forceinline__ bool plain(float mc) { return fabsf(mc) < 1e30f; }
+    // the sums taken to the reference of `to`, a number at or above m
+    __device__ __forceinline__ void rescale(float to, float c) {
+        const float a = m * c, b = to * c, d = fmaxf(plain(a) && plain(b) ? a - b : (m - to) * c, kLow), f = exp2_hw(d);
         t = (t + s * d) * f;
         s = s * f;
+        m = to;
     }
-    // N values, with `top` their largest
+    // N values, with `top` their largest.  `masked` (the same in every lane) says
+    // that logits of -inf have come: until then y 2^y is taken as it is, and a NaN
+    // in t sends the values through again with y raised to kLow.
     template <int N>
-    __device__ __forceinline__ void add(const float* x, float top, float c) {
-        const float nm = fmaxf(m, top), ref = nm == -kInf ? 0.f : nm;
+    __device__ __forceinline__ void add(const float* x, float top, float c, bool& masked) {
+        const float to = fmaxf(m, top), ref = to == -kInf ? 0.f : to, r = ref * c;
         rescale(ref, c);
-        m = nm;
+        m = to;
+        const float s0 = s, t0 = t;
+        const bool all_plain = __ballot(!plain(r)) == 0;
+        if (all_plain && !masked) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float y = (x[i] - ref) * c, e = exp2_hw(y);
-            s += e;
-            t = __builtin_fmaf(fmaxf(y, kLow), e, t);
+            for (int i = 0; i < N; ++i) {
+                const float y = __builtin_fmaf(x[i], c, -r), e = exp2_hw(y);
+                s += e;
+                t = __builtin_fmaf(y, e, t);
+            }
+            if (__ballot(t != t) == 0) return;
+            masked = true;
+            s = s0;
+            t = t0;
+        }
+        if (all_plain) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) count(__builtin_fmaf(x[i], c, -r));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) count(plain(r) ? __builtin_fmaf(x[i], c, -r) : (x[i] - ref) * c);
         }
     }
-    __device__ __forceinline__ void join(const Stats& o, float c) {
-        const float nm = fmaxf(m, o.m), ref = nm == -kInf ? 0.f : nm;
-        Stats b = o;
-        rescale(ref, c);
-        b.rescale(ref, c);
-        m = nm;
-        s += b.s;
-        t += b.t;
+    __device__ __forceinline__ void count(float y) {
+        const float e = exp2_hw(y);
+        s += e;
+        t = __builtin_fmaf(fmaxf(y, kLow), e, t);
     }
+    // the lanes' statistics joined, in every lane
+    __device__ __forceinline__ void join_wave(float c) {
+        const float to = wave_max(m);
+        rescale(to == -kInf ? 0.f : to, c);
+        m = to;
+        s = wave_sum(s);
+        t = wave_sum(t);
+    }
+    __device__ __forceinline__ bool empty() const { return m == -kInf && s == 0.f; }
+    // ln sum exp((x - m) / T), 0 for a row that is masked out whole
+    __device__ __forceinline__ float log_sum(float c) const {
+        const float r = m * c;
+        return empty() ? 0.f : plain(r) ? __builtin_fmaf(-kLn2, __builtin_fmaf(m, c, -r), logf(s)) : logf(s);
+    }
+    __device__ __forceinline__ float entropy() const { return empty() ? 0.f : __builtin_fmaf(-kLn2, t / s, logf(s)); }
 };
-
-// Every lane of the wave gets the join over its 64 lanes (a butterfly: the
-// same order of additions in every run).
-__device__ __forceinline__ Stats wave_join(Stats a, float c) {
-    for (int d = 1; d < 64; d <<= 1) {
-        Stats o;
-        o.m = __shfl_xor(a.m, d);
-        o.s = __shfl_xor(a.s, d);
-        o.t = __shfl_xor(a.t, d);
-        a.join(o, c);
-    }
-    return a;
-}
 
 template <int N>
 __device__ __forceinline__ float largest(const float* x) {
@@ -106,19 +161,6 @@ __device__ __forceinline__ float key_value(Key k) {
     return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ int key_index(Key k) { return (int)~(uint32_t)k; }
-
-// The value of lane (l ^ D), by data-parallel moves inside rows of 16 lanes.
-template <int D>
-__device__ __forceinline__ uint32_t from_lane_xor(uint32_t v) {
-    if constexpr (D == 4) return from_lane_xor<3>(from_lane_xor<7>(v));
-    else if constexpr (D == 1 || D == 2 || D == 3 || D == 7 || D == 8 || D == 15) {
-        // quad permutations 1,0,3,2 / 2,3,0,1 / 3,2,1,0, half-row and row mirrors, row rotation by 8
-        constexpr int kMove = D == 1 ? 0xb1 : D == 2 ? 0x4e : D == 3 ? 0x1b : D == 7 ? 0x141 : D == 15 ? 0x140 : 0x128;
-        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kMove, 0xf, 0xf, false);
-    } else {
-        return (uint32_t)__shfl_xor((int)v, D);
-    }
-}
 
 // Lanes l and l ^ D end with their larger key in the lower lane.
 template <int D>
@@ -169,14 +211,17 @@ struct Best {
     int waiting = 0;
     uint32_t bound;  // order of a value that at least `top` entries reach
 
-    // A bound from the orders of values of different entries, one a lane (0 for none): the
-    // top-th largest, its lower 16 bits left open.
-    __device__ __forceinline__ static uint32_t bound_of(uint32_t u, int top) {
+    // A bound from the orders of values of different entries, four a lane (0 for
+    // none): the top-th largest, its lower 16 bits left open.
+    __device__ __forceinline__ static uint32_t bound_of(const uint32_t (&u)[4], int top) {
         uint32_t b = 0;
 #pragma unroll
         for (int bit = 31; bit >= 16; --bit) {
             const uint32_t t = b | 1u << bit;
-            if (__popcll(__ballot(u >= t)) >= top) b = t;
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(u[i] >= t));
+            if (n >= top) b = t;
         }
         return b;
     }
@@ -239,15 +284,14 @@ __device__ __forceinline__ void put_left_out(const LogprobArgs& a, int64_t row, 
 // The results of a row from its joined statistics and best entries (one wave).
 __device__ __forceinline__ void put_row(const LogprobArgs& a, int64_t row, const Stats& st, Key best, float given,
                                         int lane) {
-    const bool empty = st.m == -kInf && st.s == 0.f;
-    const float l = empty ? 0.f : logf(st.s), ref = empty ? 0.f : st.m;
+    const float l = st.log_sum(a.c), ref = st.empty() ? 0.f : st.m;
     if (lane < a.top) {
         a.top_ids[row * a.top + lane] = best ? key_index(best) : -1;
         a.top_logprobs[row * a.top + lane] = best ? (key_value(best) - ref) * a.inv_t - l : -kInf;
     }
     if (lane == 0) {
         if (a.logprob) a.logprob[row] = (given - ref) * a.inv_t - l;
-        if (a.entropy) a.entropy[row] = empty ? 0.f : l - kLn2 * (st.t / st.s);
+        if (a.entropy) a.entropy[row] = st.entropy();
         if (a.stats) {
             const bool none = st.s != st.s;
             a.stats[2 * row] = none ? st.s : st.m;
@@ -258,60 +302,49 @@ __device__ __forceinline__ void put_row(const LogprobArgs& a, int64_t row, const
 
 // A quad is four neighbouring lanes: together they load 64 bytes of the row.
 __device__ __forceinline__ float quad_max(float v) {
-    v = fmaxf(v, __builtin_bit_cast(float, from_lane_xor<1>(__builtin_bit_cast(uint32_t, v))));
-    return fmaxf(v, __builtin_bit_cast(float, from_lane_xor<2>(__builtin_bit_cast(uint32_t, v))));
+    v = fmaxf(v, from_lane_xor<1>(v));
+    return fmaxf(v, from_lane_xor<2>(v));
 }
 
-constexpr int kLogThreads = 256, kLogWaves = kLogThreads / 64;
-constexpr int kLoads = 4;  // 16-byte loads of a thread in flight
+constexpr int kLoads = 2;  // 16-byte loads of a thread in flight, beside as many at work
 
 // A work-group takes a part of a row (mostly all of it) in one pass, 16 bytes a
 // load.  For the alternatives each quad of lanes leaves the largest of its 64
 // bytes in LDS: the best `top` logits lie in the best `top` of these groups (a
 // group that does not belong to them has `top` groups with a better logit
 // before it), so at the end one wave looks for those groups and reads them again.
-template <class T, bool TOP>
-__global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
-    constexpr int N = Elem<T>::kVec, kStep = kLogThreads * N;
+// W waves: 4, and 1 for short rows, whose time goes into that last part.
+template <class T, bool TOP, int W>
+__global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
+    constexpr int N = Elem<T>::kVec, kStep = kLoads * W * 64 * N;
     extern __shared__ float group_max[];
-    __shared__ float part_m[kLogWaves], part_s[kLogWaves], part_t[kLogWaves];
+    __shared__ float part_m[W], part_s[W], part_t[W];
     __shared__ Key wait[64];
     const int64_t row = blockIdx.x / a.parts;
     const int which = blockIdx.x - (int)row * a.parts;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     const int V = a.vocab, begin = which * a.part, end = min(V, begin + a.part);
     const int id = a.ids ? a.ids[row] : 0;
+    int j = begin + (wave * kLoads * 64 + lane) * N;  // a wave's loads are neighbours
+    const int whole = (end - begin) / kStep;
+    u32x4 raw[kLoads];
+    if (whole > 0) {
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + u * 64 * N);
+    }
     if (id < 0 || id >= V) {
         if (a.parts == 1 && wave == 0) put_left_out(a, row, lane);
         return;
     }
+    const float given = a.ids ? Elem<T>::get(x + id) : 0.f;
     Stats st = Stats::none();
-    for (int j0 = begin; j0 < end; j0 += kLoads * kStep) {
-        const int j = j0 + (wave * kLoads * 64 + lane) * N;  // a wave's loads are neighbours
-        float v[kLoads][N];
-        if (j0 + kLoads * kStep <= end) {
-            u32x4 raw[kLoads];
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + u * 64 * N);
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) Elem<T>::unpack(raw[u], v[u]);
-        } else {
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const int k = j + u * 64 * N;
-                if (k + N <= end) {
-                    Elem<T>::unpack(Elem<T>::load(x + k), v[u]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) v[u][i] = k + i < end ? Elem<T>::get(x + k + i) : -kInf;
-                }
-            }
-        }
+    bool masked = false;
+    auto use = [&](const float(&v)[kLoads][N]) {
         float top[kLoads];
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) top[u] = largest<N>(v[u]);
-        st.add<kLoads * N>(&v[0][0], largest<kLoads>(top), a.c);
+        st.add<kLoads * N>(&v[0][0], largest<kLoads>(top), a.c, masked);
         if constexpr (TOP) {
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
@@ -319,24 +352,62 @@ __global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
                 if ((lane & 3) == 0 && j + u * 64 * N < end) group_max[(j + u * 64 * N - begin) / (4 * N)] = q;
             }
         }
+    };
+    for (int i = 0; i < whole; ++i) {
+        float v[kLoads][N];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) Elem<T>::unpack(raw[u], v[u]);
+        if (i + 1 < whole) {
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + kStep + u * 64 * N);
+        }
+        use(v);
+        j += kStep;
     }
-    st = wave_join(st, a.c);
-    if (lane == 0) {
-        part_m[wave] = st.m;
-        part_s[wave] = st.s;
-        part_t[wave] = st.t;
+    if (begin + whole * kStep < end) {
+        float v[kLoads][N];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int k = j + u * 64 * N;
+            if (k + N <= end) {
+                Elem<T>::unpack(Elem<T>::load(x + k), v[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[u][i] = k + i < end ? Elem<T>::get(x + k + i) : -kInf;
+            }
+        }
+        use(v);
     }
-    __syncthreads();
-    if (wave) return;
-    for (int w = 1; w < kLogWaves; ++w) st.join(Stats{part_m[w], part_s[w], part_t[w]}, a.c);
+    st.join_wave(a.c);
+    if constexpr (W > 1) {
+        if (lane == 0) {
+            part_m[wave] = st.m;
+            part_s[wave] = st.s;
+            part_t[wave] = st.t;
+        }
+        __syncthreads();
+        if (wave) return;
+        st = lane < W ? Stats{part_m[lane], part_s[lane], part_t[lane]} : Stats::none();
+        st.join_wave(a.c);
+    } else {
+        __builtin_amdgcn_wave_barrier();
+    }
     Best best;
     if constexpr (TOP) {
         constexpr int kGroup = 4 * N, kAtOnce = 64 / kGroup;
         const int n = (end - begin + kGroup - 1) / kGroup;
-        float own = -kInf;
-        for (int i = lane; i < n; i += 64) own = fmaxf(own, group_max[i]);
+        float own[4] = {-kInf, -kInf, -kInf, -kInf};
+        for (int i0 = 0; i0 < n; i0 += 256)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * 64 + lane;
+                if (i < n) own[u] = fmaxf(own[u], group_max[i]);
+            }
+        uint32_t order[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) order[u] = own[u] > -kInf ? ordered(own[u]) : 0;
         Best groups;
-        groups.bound = Best::bound_of(own > -kInf ? ordered(own) : 0, a.top);
+        groups.bound = Best::bound_of(order, a.top);
         for (int i = lane; i - lane < n; i += 64) groups.offer(i < n ? key_of(group_max[i], i) : 0, wait, a.top, lane);
         groups.take(wait, a.top, lane);
         const int there = __popcll(__ballot(lane < a.top && groups.key));
@@ -356,7 +427,7 @@ __global__ __launch_bounds__(kLogThreads) void logprobs_kernel(LogprobArgs a) {
         best.take(wait, a.top, lane);
     }
     if (a.parts == 1) {
-        put_row(a, row, st, best.key, a.ids ? Elem<T>::get(x + id) : 0.f, lane);
+        put_row(a, row, st, best.key, given, lane);
     } else {
         const int64_t at = row * a.parts + which;
         if (lane == 0) a.part_stats[at] = st;
@@ -374,24 +445,35 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
         put_left_out(a, row, lane);
         return;
     }
+    const float given = a.ids ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.stride + id) : 0.f;
     Stats st = Stats::none();
-    for (int i = lane; i < a.parts; i += 64) st.join(a.part_stats[row * a.parts + i], a.c);
-    st = wave_join(st, a.c);
+    for (int i0 = 0; i0 < a.parts; i0 += 64) {
+        // lane 0 carries the parts before these
+        Stats next = i0 + lane < a.parts ? a.part_stats[row * a.parts + i0 + lane] : Stats::none();
+        next.join_wave(a.c);
+        st = lane == 0 ? st : lane == 1 ? next : Stats::none();
+        st.join_wave(a.c);
+    }
     Best best;
     if (a.top) {
         __shared__ Key wait[64];
         const Key* keys = a.part_keys + row * a.parts * a.top;
         const int n = a.parts * a.top;
         // bounds: every part's last entry, and the lanes' own largest ones
-        uint32_t own = 0, last = 0;
-        for (int i = lane; i < n; i += 64) own = max(own, (uint32_t)(keys[i] >> 32));
+        uint32_t own[4] = {}, last = 0;
+        for (int i0 = 0; i0 < n; i0 += 256)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * 64 + lane;
+                if (i < n) own[u] = max(own[u], (uint32_t)(keys[i] >> 32));
+            }
         for (int i = lane; i < a.parts; i += 64) last = max(last, (uint32_t)(keys[(i + 1) * a.top - 1] >> 32));
         for (int d = 1; d < 64; d <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, d));
         best.bound = max(last, Best::bound_of(own, a.top));
         for (int i = lane; i - lane < n; i += 64) best.offer(i < n ? keys[i] : 0, wait, a.top, lane);
         best.take(wait, a.top, lane);
     }
-    put_row(a, row, st, best.key, a.ids ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.stride + id) : 0.f, lane);
+    put_row(a, row, st, best.key, given, lane);
 }
 
 struct GradArgs {
@@ -433,7 +515,7 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(GradArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float y = (v[i] - m) * a.c - l2;
+                const float y = __builtin_fmaf(v[i] - m, a.c, -l2);
                 v[i] = exp2_hw(y) * __builtin_fmaf(k1, fmaxf(y, kLow), k0) + (j + i == id ? g1 : 0.f);
             }
         }
@@ -462,15 +544,6 @@ struct DistillArgs {
     void* out;
     int64_t out_stride;
 };
-
-__device__ __forceinline__ float wave_max(float v) {
-    for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return v;
-}
 
 // One work-group a row.  The teacher's list (one entry a thread) becomes
 // masses q, equal ids as one; a first pass takes the student's statistics, a
@@ -521,6 +594,7 @@ __global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
     const float z = first ? Elem<T>::get(x + id) : 0.f;
 
     Stats st = Stats::none();
+    bool masked = false;
     if (!out)
         for (int j = tid * N; j < V; j += 256 * N) {
             float v[N];
@@ -530,15 +604,15 @@ __global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
             }
-            st.add<N>(v, largest<N>(v), a.c);
+            st.add<N>(v, largest<N>(v), a.c, masked);
         }
-    st = wave_join(st, a.c);
+    st.join_wave(a.c);
     if (lane == 0) part[wave] = st;
     __syncthreads();
-    st = part[0];
-    for (int k = 1; k < 4; ++k) st.join(part[k], a.c);
-    const bool empty = st.m == -kInf && st.s == 0.f;
-    const float l = empty ? 0.f : logf(st.s), m = empty ? 0.f : st.m, l2 = l * (1.f / kLn2);
+    st = lane < 4 ? part[lane] : Stats::none();
+    st.join_wave(a.c);
+    const bool empty = st.empty();
+    const float l = st.log_sum(a.c), m = empty ? 0.f : st.m, l2 = l * (1.f / kLn2);
 
     float each = 0.f;
     if (first && !(mass == 0.f)) each = mass * (logf(mass) - ((z - m) * a.inv_t - l));
@@ -565,7 +639,7 @@ __global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
                 for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
             }
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = exp2_hw((v[i] - m) * a.c - l2) * k;
+            for (int i = 0; i < N; ++i) v[i] = exp2_hw(__builtin_fmaf(v[i] - m, a.c, -l2)) * k;
         }
         if (whole) {
             Elem<T>::store(d + j, Elem<T>::pack(v));
@@ -576,7 +650,7 @@ __global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
         }
     }
     __syncthreads();
-    if (first && !zero) Elem<T>::put(d + id, (exp2_hw((z - m) * a.c - l2) - mass) * k);
+    if (first && !zero) Elem<T>::put(d + id, (exp2_hw(__builtin_fmaf(z - m, a.c, -l2)) - mass) * k);
 }
 
 constexpr int64_t kMaxElems = INT64_C(1) << 48;  // of a matrix, gaps included: offsets in bytes stay far inside 64 bits
@@ -626,6 +700,16 @@ edb_status launched(const char* who) {
     return EDB_OK;
 }
 
+constexpr int kRowWaves = 4;
+// One wave takes a row of up to 4 KB, and of up to 16 KB where there are enough
+// rows to fill the card with single waves (8192 rows of 4096 bf16: 23 us, by
+// four waves 28; 63 rows of 8192: 11 us, by four 8).
+bool brief_row(int32_t n, int64_t bytes) { return bytes <= 4096 || (bytes <= 16384 && n >= 2048); }
+// Rows of at least so many logits are split where there are fewer than kFill
+// rows (one row of 32003 bf16: 12.0 us, whole 13.9; of 131072: 12.6, whole 32;
+// 300 rows of 10007: 15.1, whole 12.8, for the join is a launch more).
+constexpr int32_t kSplit = 16384, kFill = 512;
+
 // How a forward call splits its rows, and its scratch memory.
 struct RowPlan {
     int32_t part, parts;
@@ -633,12 +717,13 @@ struct RowPlan {
 };
 
 // A row is split where there are too few rows for the card, and where a part's
-// group maxima would pass 32 KB of LDS.  Parts are whole steps of a work-group.
+// group maxima would pass 32 KB of LDS.  Parts are whole steps of a work-group,
+// two at least.
 RowPlan row_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     constexpr int32_t kMost = 131072;
-    const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec, step = kLoads * kLogThreads * vec;
+    const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec, step = 2 * kLoads * kRowWaves * 64 * vec;
     const int64_t steps = ((int64_t)vocab + step - 1) / step;
-    int64_t parts = n >= 512 ? 1 : (512 + n - 1) / (n < 1 ? 1 : n);
+    int64_t parts = n >= kFill || n < 1 || vocab < kSplit ? 1 : (kFill + n - 1) / n;
     if (parts > steps) parts = steps;
     if (parts * kMost < vocab) parts = ((int64_t)vocab + kMost - 1) / kMost;
     RowPlan r{};
@@ -656,6 +741,15 @@ template <class T>
 size_t group_bytes(const RowPlan& r, int32_t vocab) {
     const size_t places = r.parts > 1 ? (size_t)r.part : (size_t)vocab;
     return (places / (4 * Elem<T>::kVec) + 1) * 4;
+}
+
+template <class T>
+void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st) {
+    const bool brief = a.parts == 1 && brief_row(a.n, (int64_t)a.vocab * sizeof(T));
+    if (a.top && brief) logprobs_kernel<T, true, 1><<<grid, 64, lds, st>>>(a);
+    else if (a.top) logprobs_kernel<T, true, kRowWaves><<<grid, 64 * kRowWaves, lds, st>>>(a);
+    else if (brief) logprobs_kernel<T, false, 1><<<grid, 64, 0, st>>>(a);
+    else logprobs_kernel<T, false, kRowWaves><<<grid, 64 * kRowWaves, 0, st>>>(a);
 }
 
 float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
@@ -714,13 +808,11 @@ extern "C" edb_status edb_logprobs(const void* logits, int32_t dtype, int32_t n,
     const dim3 grid(n * r.parts);
     if (dtype == EDB_F32) {
         const size_t lds = group_bytes<float>(r, vocab);
-        if (top) logprobs_kernel<float, true><<<grid, kLogThreads, lds, st>>>(a);
-        else logprobs_kernel<float, false><<<grid, kLogThreads, 0, st>>>(a);
+        launch_logprobs<float>(a, grid, lds, st);
         if (r.parts > 1) logprobs_join<float><<<n, 64, 0, st>>>(a);
     } else {
         const size_t lds = group_bytes<bf16>(r, vocab);
-        if (top) logprobs_kernel<bf16, true><<<grid, kLogThreads, lds, st>>>(a);
-        else logprobs_kernel<bf16, false><<<grid, kLogThreads, 0, st>>>(a);
+        launch_logprobs<bf16>(a, grid, lds, st);
         if (r.parts > 1) logprobs_join<bf16><<<n, 64, 0, st>>>(a);
     }
     return launched(who);
