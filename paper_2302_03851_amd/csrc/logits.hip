@@ -545,104 +545,272 @@ struct DistillArgs {
     int64_t out_stride;
 };
 
-// One work-group a row.  The teacher's list (one entry a thread) becomes
-// masses q, equal ids as one; a first pass takes the student's statistics, a
-// second writes w T p_j, and the list's owners then write w T (p_j - q_j).
+// The teacher's list of a row as masses: one entry a thread (the first
+// kMaxListed threads), equal ids as one, at the first of them.
+struct Listed {
+    int id;      // -1: nothing to account for here
+    float mass;
+};
+
+struct ListedShared {
+    int ids[kMaxListed];
+    float q[kMaxListed];
+    float part[2][kMaxListed / 64];
+};
+
+// Called by all W waves of the work-group (W >= 4); `total` is 0 where nothing is listed.
+__device__ __forceinline__ Listed take_list(const DistillArgs& a, int id, float u, ListedShared& sh, float& total) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int kWaves = kMaxListed / 64;
+    const float um = wave_max(u);
+    if (lane == 0 && wave < kWaves) sh.part[0][wave] = um;
+    __syncthreads();
+    float tm = sh.part[0][0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) tm = fmaxf(tm, sh.part[0][i]);
+    const float e = id < 0 ? 0.f : exp2_hw((u - (tm == -kInf ? 0.f : tm)) * a.c);
+    const float es = wave_sum(e);
+    if (lane == 0 && wave < kWaves) sh.part[1][wave] = es;
+    if (tid < kMaxListed) sh.ids[tid] = id;
+    __syncthreads();
+    total = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) total += sh.part[1][i];
+    if (tid < kMaxListed) sh.q[tid] = e / total;
+    __syncthreads();
+    Listed l{total == 0.f ? -1 : id, 0.f};
+    if (l.id >= 0)
+        for (int k = 0; k < a.top; ++k)
+            if (sh.ids[k] == id) {
+                if (k < tid) l.id = -1;
+                l.mass += sh.q[k];
+            }
+    return l;
+}
+
+__device__ __forceinline__ void read_list(const DistillArgs& a, int64_t row, int& id, float& u) {
+    id = -1;
+    u = -kInf;
+    if ((int)threadIdx.x < a.top) {
+        id = a.top_ids[row * a.top + threadIdx.x];
+        const float v = a.top_logits[row * a.top + threadIdx.x];
+        if (id < 0 || id >= a.vocab) id = -1;
+        else u = v;
+    }
+}
+
+// The row's loss: the sum of the listed entries' terms, in the same order in every run.
+template <int W>
+__device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t row, const Listed& l, float lp, float* part) {
+    float each = l.id >= 0 && !(l.mass == 0.f) ? l.mass * (logf(l.mass) - lp) : 0.f;
+    each = wave_sum(each);
+    constexpr int kWaves = kMaxListed / 64 < W ? kMaxListed / 64 : W;
+    if ((threadIdx.x & 63) == 0 && (int)(threadIdx.x >> 6) < kWaves) part[threadIdx.x >> 6] = each;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float sum = 0.f;
+        for (int i = 0; i < kWaves; ++i) sum += part[i];
+        a.loss[row] = a.t * a.t * sum;
+    }
+}
+
 template <class T>
-__global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
+__device__ __forceinline__ void zero_row(T* d, int V, int threads) {
     constexpr int N = Elem<T>::kVec;
-    static_assert(kMaxListed == 256, "one listed entry a thread");
+    for (int j = threadIdx.x * N; j < V; j += threads * N) {
+        if (j + N <= V) Elem<T>::store(d + j, u32x4{0u, 0u, 0u, 0u});
+        else
+            for (int k = j; k < V; ++k) Elem<T>::put(d + k, 0.f);
+    }
+}
+
+// Rows of up to 16 W NV KB / 16: W waves hold a whole row in registers, NV
+// 16-byte vectors a thread, so that it is read once and the gradient written
+// once.  2^y with y = x c - r(m) (see Stats) is summed up in one pass over the
+// registers and w T p_j = 2^y (w T / S) written in another; the owners of the
+// listed entries then write w T (p_j - q_j).
+template <class T, int W, int NV>
+__global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
+    constexpr int N = Elem<T>::kVec, kThreads = 64 * W;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
     const int V = a.vocab;
-    __shared__ int ids[256];
-    __shared__ float q[256];
-    __shared__ Stats part[4];
-    __shared__ float red[4], red2[4];
+    __shared__ ListedShared sh;
+    __shared__ float part[3][W];
     const float w = a.weight ? a.weight[row] : 1.f;
-
-    int id = -1;
-    float u = -kInf;
-    if (tid < a.top) {
-        id = a.top_ids[row * a.top + tid];
-        if (id < 0 || id >= V) id = -1;
-        else u = a.top_logits[row * a.top + tid];
+    if (w == 0.f) {
+        if (tid == 0) a.loss[row] = 0.f;
+        if (d) zero_row(d, V, kThreads);
+        return;
     }
-    const float um = wave_max(u);
-    if (lane == 0) red[wave] = um;
+    int id;
+    float u;
+    read_list(a, row, id, u);
+    // vector i of this thread starts at (i kThreads + tid) N; whether a wave has any of it is the same in all its lanes
+    const int first = __builtin_amdgcn_readfirstlane(wave) * 64 * N;
+    u32x4 raw[NV];
+    float edge[N];  // a vector that the row ends in
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (first + i * kThreads * N >= V) break;
+        const int j = (i * kThreads + tid) * N;
+        if (j + N <= V) {
+            raw[i] = Elem<T>::load_nt(x + j);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) edge[k] = j + k < V ? Elem<T>::get(x + j + k) : -kInf;
+            raw[i] = Elem<T>::pack(edge);
+        }
+    }
+    float total;
+    const Listed l = take_list(a, id, u, sh, total);
+    const bool out = total == 0.f;
+    const float z = l.id >= 0 ? Elem<T>::get(x + l.id) : 0.f;
+
+    float m = -kInf;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (first + i * kThreads * N >= V) break;
+        float v[N];
+        Elem<T>::unpack(raw[i], v);
+        m = fmaxf(m, largest<N>(v));
+    }
+    m = wave_max(m);
+    if (lane == 0) part[0][wave] = m;
     __syncthreads();
-    const float tm = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float e = id < 0 ? 0.f : exp2_hw((u - (tm == -kInf ? 0.f : tm)) * a.c);
-    const float es = wave_sum(e);
-    if (lane == 0) red2[wave] = es;
+    m = wave_max(lane < W ? part[0][lane] : -kInf);
+    const float ref = m == -kInf ? 0.f : m, r = ref * a.c;
+    float s = 0.f;
+    if (Stats::plain(r)) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (first + i * kThreads * N >= V) break;
+            float v[N];
+            Elem<T>::unpack(raw[i], v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) s += exp2_hw(__builtin_fmaf(v[k], a.c, -r));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (first + i * kThreads * N >= V) break;
+            float v[N];
+            Elem<T>::unpack(raw[i], v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) s += exp2_hw((v[k] - ref) * a.c);
+        }
+    }
+    s = wave_sum(s);
+    if (lane == 0) part[1][wave] = s;
     __syncthreads();
-    const float total = (red2[0] + red2[1]) + (red2[2] + red2[3]);
-    const bool out = w == 0.f || total == 0.f;
-    ids[tid] = id;
-    q[tid] = e / total;
+    const Stats st{m, wave_sum(lane < W ? part[1][lane] : 0.f), 0.f};
+    put_loss<W>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
+    if (out && tid == 0) a.loss[row] = 0.f;
+    if (!d) return;
+    if (out || st.empty()) {
+        zero_row(d, V, kThreads);
+        return;
+    }
+    const float k = w * a.t, ks = k / st.s;
+    const bool plain = Stats::plain(r);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (first + i * kThreads * N >= V) break;
+        const int j = (i * kThreads + tid) * N;
+        float v[N];
+        Elem<T>::unpack(raw[i], v);
+        if (plain) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = exp2_hw(__builtin_fmaf(v[e], a.c, -r)) * ks;
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = exp2_hw((v[e] - ref) * a.c) * ks;
+        }
+        if (j + N <= V) {
+            Elem<T>::store_nt(d + j, Elem<T>::pack(v));
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (j + e < V) Elem<T>::put(d + j + e, v[e]);
+        }
+    }
     __syncthreads();
-    float mass = 0.f;
-    bool first = id >= 0 && !out;
-    if (first)
-        for (int k = 0; k < a.top; ++k)
-            if (ids[k] == id) {
-                if (k < tid) first = false;
-                mass += q[k];
-            }
-    const float z = first ? Elem<T>::get(x + id) : 0.f;
+    if (l.id >= 0) {
+        const float p = exp2_hw(plain ? __builtin_fmaf(z, a.c, -r) : (z - ref) * a.c) / st.s;
+        Elem<T>::put(d + l.id, (p - l.mass) * k);
+    }
+}
+
+// Longer rows, read twice: a pass for the student's statistics, one for the gradient.
+constexpr int kLongWaves = 16;
+template <class T>
+__global__ __launch_bounds__(64 * kLongWaves) void distill_long(DistillArgs a) {
+    constexpr int N = Elem<T>::kVec, kThreads = 64 * kLongWaves;
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+    T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
+    const int V = a.vocab;
+    __shared__ ListedShared sh;
+    __shared__ float part[4][kLongWaves];
+    const float w = a.weight ? a.weight[row] : 1.f;
+    if (w == 0.f) {
+        if (tid == 0) a.loss[row] = 0.f;
+        if (d) zero_row(d, V, kThreads);
+        return;
+    }
+    int id;
+    float u, total;
+    read_list(a, row, id, u);
+    const Listed l = take_list(a, id, u, sh, total);
+    const bool out = total == 0.f;
+    const float z = l.id >= 0 ? Elem<T>::get(x + l.id) : 0.f;
 
     Stats st = Stats::none();
     bool masked = false;
-    if (!out)
-        for (int j = tid * N; j < V; j += 256 * N) {
-            float v[N];
-            if (j + N <= V) {
-                Elem<T>::unpack(Elem<T>::load(x + j), v);
-            } else {
+    for (int j = tid * N; j < V; j += kThreads * N) {
+        float v[N];
+        if (j + N <= V) {
+            Elem<T>::unpack(Elem<T>::load(x + j), v);
+        } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
-            }
-            st.add<N>(v, largest<N>(v), a.c, masked);
+            for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
         }
+        st.add<N>(v, largest<N>(v), a.c, masked);
+    }
     st.join_wave(a.c);
-    if (lane == 0) part[wave] = st;
+    if (lane == 0) {
+        part[0][wave] = st.m;
+        part[1][wave] = st.s;
+    }
     __syncthreads();
-    st = lane < 4 ? part[lane] : Stats::none();
+    st = lane < kLongWaves ? Stats{part[0][lane], part[1][lane], 0.f} : Stats::none();
     st.join_wave(a.c);
-    const bool empty = st.empty();
-    const float l = st.log_sum(a.c), m = empty ? 0.f : st.m, l2 = l * (1.f / kLn2);
-
-    float each = 0.f;
-    if (first && !(mass == 0.f)) each = mass * (logf(mass) - ((z - m) * a.inv_t - l));
-    each = wave_sum(each);
-    __syncthreads();
-    if (lane == 0) red[wave] = each;
-    __syncthreads();
-    if (tid == 0) a.loss[row] = out ? 0.f : a.t * a.t * ((red[0] + red[1]) + (red[2] + red[3]));
+    const float ref = st.m == -kInf ? 0.f : st.m, r = ref * a.c;
+    put_loss<kLongWaves>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
+    if (out && tid == 0) a.loss[row] = 0.f;
     if (!d) return;
-
-    const float k = w * a.t;
-    const bool zero = out || empty;
-    for (int j = tid * N; j < V; j += 256 * N) {
+    if (out || st.empty()) {
+        zero_row(d, V, kThreads);
+        return;
+    }
+    const float k = w * a.t, ks = k / st.s;
+    const bool plain = Stats::plain(r);
+    for (int j = tid * N; j < V; j += kThreads * N) {
         float v[N];
         const bool whole = j + N <= V;
-        if (zero) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = 0.f;
-        } else {
-            if (whole) {
-                Elem<T>::unpack(Elem<T>::load(x + j), v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = exp2_hw(__builtin_fmaf(v[i] - m, a.c, -l2)) * k;
-        }
         if (whole) {
-            Elem<T>::store(d + j, Elem<T>::pack(v));
+            Elem<T>::unpack(Elem<T>::load(x + j), v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = exp2_hw(plain ? __builtin_fmaf(v[i], a.c, -r) : (v[i] - ref) * a.c) * ks;
+        if (whole) {
+            Elem<T>::store_nt(d + j, Elem<T>::pack(v));
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -650,7 +818,10 @@ __global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
         }
     }
     __syncthreads();
-    if (first && !zero) Elem<T>::put(d + id, (exp2_hw(__builtin_fmaf(z - m, a.c, -l2)) - mass) * k);
+    if (l.id >= 0) {
+        const float p = exp2_hw(plain ? __builtin_fmaf(z, a.c, -r) : (z - ref) * a.c) / st.s;
+        Elem<T>::put(d + l.id, (p - l.mass) * k);
+    }
 }
 
 constexpr int64_t kMaxElems = INT64_C(1) << 48;  // of a matrix, gaps included: offsets in bytes stay far inside 64 bits
@@ -750,6 +921,18 @@ void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st
     else if (a.top) logprobs_kernel<T, true, kRowWaves><<<grid, 64 * kRowWaves, lds, st>>>(a);
     else if (brief) logprobs_kernel<T, false, 1><<<grid, 64, 0, st>>>(a);
     else logprobs_kernel<T, false, kRowWaves><<<grid, 64 * kRowWaves, 0, st>>>(a);
+}
+
+template <class T>
+void launch_distill(const DistillArgs& a, hipStream_t st) {
+    const int64_t vectors = ((int64_t)a.vocab + Elem<T>::kVec - 1) / Elem<T>::kVec;
+    if (vectors <= 2 * 256) distill_kernel<T, 4, 2><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 4 * 256) distill_kernel<T, 4, 4><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 8 * 256) distill_kernel<T, 4, 8><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 16 * 256) distill_kernel<T, 4, 16><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 16 * 512) distill_kernel<T, 8, 16><<<a.n, 512, 0, st>>>(a);
+    else if (vectors <= 16 * 1024) distill_kernel<T, 16, 16><<<a.n, 1024, 0, st>>>(a);
+    else distill_long<T><<<a.n, 64 * kLongWaves, 0, st>>>(a);
 }
 
 float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
@@ -858,8 +1041,7 @@ extern "C" edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, 
     DistillArgs a{logits, stride,      n,      vocab, top_ids, top_logits, top, log2e_over(temperature),
                   (float)(1.0 / (double)temperature), temperature, weight, loss, dlogits, dlogits_stride};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const dim3 grid(n), block(256);
-    if (dtype == EDB_F32) distill_kernel<float><<<grid, block, 0, st>>>(a);
-    else distill_kernel<bf16><<<grid, block, 0, st>>>(a);
+    if (dtype == EDB_F32) launch_distill<float>(a, st);
+    else launch_distill<bf16>(a, st);
     return launched(who);
 }
