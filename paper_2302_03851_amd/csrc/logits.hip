@@ -65,6 +65,154 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v + from_lane_xor<32>(v);
 }
 
+// ---- rows of bf16 at odd addresses
+//
+// A row of an odd number of bf16 leaves the next one 2 bytes off a dword, where
+// 16-byte accesses are slow (8192 x 65533 bf16 read once: 227 us, at any dword
+// 192).  Such a row is read from the dword before, the vectors of a wave being
+// neighbours, and shifted by one element with the next lane's first dword; it
+// is written from the dword after.  Which elements a thread holds does not
+// depend on the address, so neither do the results.
+
+template <class T>
+__device__ __forceinline__ bool odd_row(const T* p) {
+    return sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(p) & 2);
+}
+
+__device__ __forceinline__ uint32_t from_next_lane(uint32_t v, uint32_t last) {  // `last` in lane 63
+    constexpr int kDown = 0x130;  // DPP: every lane takes the value of the one after it
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)last, (int)v, kDown, 0xf, 0xf, false);
+}
+
+// The elements 0..7 of every lane's vector from the elements -1..6; the low
+// half of `last` is element 7 of lane 63.
+__device__ __forceinline__ u32x4 shift_in(u32x4 v, uint32_t last) {
+    const uint32_t n = from_next_lane(v[0], last);
+    return u32x4{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16),
+                 __builtin_amdgcn_alignbit(v[3], v[2], 16), __builtin_amdgcn_alignbit(n, v[3], 16)};
+}
+
+// `count` (the same in every lane) neighbouring vectors of a wave, read one
+// element early; `last`: the element after the last of them that was read.
+template <class T, int M>
+__device__ __forceinline__ void shift_in_all(u32x4 (&raw)[M], int count, const T* last) {
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t end = last->bits;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            if (i < count) {
+                uint32_t next = end;
+                if (i + 1 < M && i + 1 < count) next = (uint32_t)__builtin_amdgcn_readlane((int)raw[i + 1 < M ? i + 1 : i][0], 0);
+                raw[i] = shift_in(raw[i], next);
+            }
+        }
+    }
+}
+
+// 16 bytes of a result that is not read again here: past the caches where a
+// wave writes whole lines, through them where two waves share some (8192 x
+// 65532 bf16 read and written: 466 us past the caches, 448 through them;
+// 8192 x 65536: 412 and 430).
+template <class T>
+__device__ __forceinline__ void store_piece(T* p, u32x4 v, bool straight) {
+    if (straight) {
+        Elem<T>::store_nt(p, v);
+    } else {
+        asm volatile("" ::: "memory");  // these two keep the compiler from making one plain store of both
+        Elem<T>::store(p, v);
+        asm volatile("" ::: "memory");
+    }
+}
+template <class T>
+__device__ __forceinline__ bool straight_row(const T* p) {
+    return (reinterpret_cast<uintptr_t>(p) & 127) == 0;
+}
+
+// Writes every lane's vector v to d + j (j = the lane's place), up to V; all
+// lanes of the wave call it, with neighbouring vectors.
+template <class T>
+__device__ __forceinline__ void store_vector(T* d, int j, int V, u32x4 v, bool odd, bool straight, int lane) {
+    constexpr int N = Elem<T>::kVec;
+    if (j >= V && !odd) return;
+    if constexpr (sizeof(T) == 2) {
+        if (odd) {
+            const uint32_t n = from_next_lane(v[0], 0);
+            const u32x4 o{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16),
+                          __builtin_amdgcn_alignbit(v[3], v[2], 16), __builtin_amdgcn_alignbit(n, v[3], 16)};
+            if (lane == 0 && j < V) d[j].bits = (uint16_t)v[0];
+            if (lane != 63 && j + N < V) {
+                Elem<T>::store(d + j + 1, o);
+            } else {
+#pragma unroll
+                for (int k = 1; k < N; ++k)
+                    if (j + k < V) d[j + k].bits = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
+            }
+            return;
+        }
+    }
+    if (j + N <= V) {
+        store_piece(d + j, v, straight);
+    } else {
+        float e[N];
+        Elem<T>::unpack(v, e);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (j + k < V) Elem<T>::put(d + j + k, e[k]);
+    }
+}
+
+// A lane's 16 bytes of a wave's vector at p, the same in every lane: a scalar
+// base and a 32-bit offset, so that a row's many vectors need no address registers.
+template <class T>
+__device__ __forceinline__ T* lane_place(T* p, int lane) {
+    return p + (uint32_t)(lane * (int)(16 / sizeof(T)));
+}
+
+template <class T>
+__device__ __forceinline__ void store_first(T* d, u32x4 v) {  // the vector's first element
+    float e[Elem<T>::kVec];
+    Elem<T>::unpack(v, e);
+    Elem<T>::put(d, e[0]);
+}
+
+template <class T>
+__device__ __forceinline__ uint32_t element_bits(const T* p) {
+    if constexpr (sizeof(T) == 2) return p->bits;
+    else return __builtin_bit_cast(uint32_t, *p);
+}
+
+// Writes the elements from 1 on of every lane's vector v at an odd address d (the first lane's), the last lane's too.
+template <class T>
+__device__ __forceinline__ void store_end(T* d, u32x4 v, int lane) {
+    if constexpr (sizeof(T) == 2) {
+        const u32x4 o = shift_in(v, 0);
+        T* p = lane_place(d, lane) + 1;
+        if (lane != 63) {
+            Elem<T>::store(p, o);
+        } else {
+            uint32_t* q = reinterpret_cast<uint32_t*>(p);  // an odd address and one element more: a dword's
+            q[0] = o[0];
+            q[1] = o[1];
+            q[2] = o[2];
+            p[6].bits = (uint16_t)(v[3] >> 16);
+        }
+    }
+}
+
+// The vector at place j of a row of V, from `early` (0 or 1) elements before it; -inf past its end.
+template <class T>
+__device__ __forceinline__ u32x4 load_vector(const T* x, int j, int V, int early) {
+    constexpr int N = Elem<T>::kVec;
+    if (j - early + N <= V) return Elem<T>::load_nt(x + j - early);
+    float e[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int at = j - early + k;
+        e[k] = at >= 0 && at < V ? Elem<T>::get(x + at) : -kInf;
+    }
+    return Elem<T>::pack(e);
+}
+
 // Running softmax statistics: the largest logit m, and s = sum 2^y, t = sum y 2^y
 // with y = x c - r(m).  The reference r is m c rounded to fp32, so that y is one
 // fused multiply-add and its own rounding the only one; where m c comes near
@@ -328,10 +476,12 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     const int id = a.ids ? a.ids[row] : 0;
     int j = begin + (wave * kLoads * 64 + lane) * N;  // a wave's loads are neighbours
     const int whole = (end - begin) / kStep;
+    const bool odd = odd_row(x);
+    const T* from = x - (odd ? 1 : 0);
     u32x4 raw[kLoads];
     if (whole > 0) {
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + u * 64 * N);
+        for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(from + j + u * 64 * N);
     }
     if (id < 0 || id >= V) {
         if (a.parts == 1 && wave == 0) put_left_out(a, row, lane);
@@ -355,11 +505,12 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     };
     for (int i = 0; i < whole; ++i) {
         float v[kLoads][N];
+        if (odd) shift_in_all(raw, kLoads, x + j + (kLoads * 64 - lane) * N - 1);
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) Elem<T>::unpack(raw[u], v[u]);
         if (i + 1 < whole) {
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(x + j + kStep + u * 64 * N);
+            for (int u = 0; u < kLoads; ++u) raw[u] = Elem<T>::load_nt(from + j + kStep + u * 64 * N);
         }
         use(v);
         j += kStep;
@@ -476,6 +627,16 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
     put_row(a, row, st, best.key, given, lane);
 }
 
+template <class T>
+__device__ __forceinline__ void zero_row(T* d, int V, int threads, int before = 0) {
+    constexpr int N = Elem<T>::kVec;
+    for (int j = (before + threadIdx.x) * N; j < V; j += threads * N) {
+        if (j + N <= V) Elem<T>::store(d + j, u32x4{0u, 0u, 0u, 0u});
+        else
+            for (int k = j; k < V; ++k) Elem<T>::put(d + k, 0.f);
+    }
+}
+
 struct GradArgs {
     const void* logits;
     int64_t stride;
@@ -487,45 +648,77 @@ struct GradArgs {
     int64_t out_stride;
 };
 
-// dx_j = (g_lp (1[j = id] - p_j) - g_H p_j (lp_j + H)) / T.
+// dx_j = (g_lp (1[j = id] - p_j) - g_H p_j (lp_j + H)) / T.  The waves of a row's
+// work-groups (several in y where there are few rows) take kGradLoads
+// neighbouring vectors of 1 KB in turn.
+constexpr int kGradWaves = 8, kGradLoads = 4;  // waves of a work-group at most
+
 template <class T>
-__global__ __launch_bounds__(256) void logprobs_grad_kernel(GradArgs a) {
-    constexpr int N = Elem<T>::kVec;
+__global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs a) {
+    constexpr int N = Elem<T>::kVec, kAll = 64 * N;
     const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     T* d = static_cast<T*>(a.out) + row * a.out_stride;
     const int V = a.vocab, id = a.ids[row];
     const float g1 = a.g_logprob ? a.g_logprob[row] * a.inv_t : 0.f, g2 = a.g_entropy ? a.g_entropy[row] * a.inv_t : 0.f;
     const float m = a.stats[2 * row], l2 = a.stats[2 * row + 1] * (1.f / kLn2);
-    const bool zero = id < 0 || id >= V || (g1 == 0.f && g2 == 0.f) || m == -kInf;
+    if (id < 0 || id >= V || (g1 == 0.f && g2 == 0.f) || m == -kInf) {
+        zero_row(d, V, gridDim.y * blockDim.x, blockIdx.y * blockDim.x);
+        return;
+    }
     // p (k0 + k1 log2 p), k0 = -(g_lp + g_H H) / T, k1 = -g_H ln 2 / T
     const float k0 = -(g1 + (a.g_entropy ? g2 * a.entropy[row] : 0.f)), k1 = -g2 * kLn2;
-    for (int j = threadIdx.x * N; j < V; j += 256 * N) {
+    const bool odd = odd_row(x), odd_out = odd_row(d), straight = straight_row(d);
+    auto slope = [&](u32x4 q, int j) {
         float v[N];
-        const bool whole = j + N <= V;
-        if (zero) {
+        Elem<T>::unpack(q, v);
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = 0.f;
-        } else {
-            if (whole) {
-                Elem<T>::unpack(Elem<T>::load(x + j), v);
+        for (int i = 0; i < N; ++i) {
+            const float y = __builtin_fmaf(v[i] - m, a.c, -l2);
+            v[i] = exp2_hw(y) * __builtin_fmaf(k1, fmaxf(y, kLow), k0);
+        }
+        const int at = id - j;
+        if (at >= 0 && at < N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += i == at ? g1 : 0.f;
+        }
+        return Elem<T>::pack(v);
+    };
+    const int all = V / kAll;
+    const T* from = x - (odd ? 1 : 0);
+    const int waves = blockDim.x >> 6, turn = blockIdx.y * waves + wave, turns = gridDim.y * waves;
+    for (int g = turn * kGradLoads; g < all; g += turns * kGradLoads) {
+        const int count = min(kGradLoads, all - g);
+        u32x4 raw[kGradLoads];
+#pragma unroll
+        for (int u = 0; u < kGradLoads; ++u) raw[u] = Elem<T>::load_nt(lane_place(from + min(g + u, all - 1) * kAll, lane));
+        if (odd) shift_in_all(raw, count, x + (g + count) * kAll - 1);
+        u32x4 held{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int u = 0; u < kGradLoads; ++u) {
+            if (u >= count) break;
+            const u32x4 o = slope(raw[u], (g + u) * kAll + lane * N);
+            T* at = d + (g + u) * kAll;
+            if (!odd_out) {
+                store_piece(lane_place(at, lane), o, straight);
             } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float y = __builtin_fmaf(v[i] - m, a.c, -l2);
-                v[i] = exp2_hw(y) * __builtin_fmaf(k1, fmaxf(y, kLow), k0) + (j + i == id ? g1 : 0.f);
+                if (u == 0) {
+                    if (lane == 0) store_first(at, o);
+                } else {
+                    Elem<T>::store(lane_place(at - kAll + 1, lane),
+                                   shift_in(held, (uint32_t)__builtin_amdgcn_readlane((int)o[0], 0)));
+                }
+                if (u + 1 == count) store_end(at, o, lane);
+                held = o;
             }
         }
-        if (whole) {
-            Elem<T>::store(d + j, Elem<T>::pack(v));
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (j + i < V) Elem<T>::put(d + j + i, v[i]);
-        }
+    }
+    if (V % kAll != 0 && all / kGradLoads % turns == turn) {
+        const int j = all * kAll + lane * N;
+        u32x4 q = load_vector(x, j, V, odd ? 1 : 0);
+        if (odd) q = shift_in(q, 0);
+        store_vector(d, j, V, slope(q, j), odd_out, straight, lane);
     }
 }
 
@@ -552,18 +745,26 @@ struct Listed {
     float mass;
 };
 
+constexpr int kTable = 2 * kMaxListed;
+
 struct ListedShared {
     int ids[kMaxListed];
     float q[kMaxListed];
     float part[2][kMaxListed / 64];
+    int table[kTable];
+    int twice;
 };
 
-// Called by all W waves of the work-group (W >= 4); `total` is 0 where nothing is listed.
+// Called by all waves of the work-group (four at least); `total` is 0 where
+// nothing is listed.  A table of the ids tells whether one comes twice; only
+// then does every entry look through the others.
 __device__ __forceinline__ Listed take_list(const DistillArgs& a, int id, float u, ListedShared& sh, float& total) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int kWaves = kMaxListed / 64;
     const float um = wave_max(u);
     if (lane == 0 && wave < kWaves) sh.part[0][wave] = um;
+    for (int i = tid; i < kTable; i += blockDim.x) sh.table[i] = -1;
+    if (tid == 0) sh.twice = 0;
     __syncthreads();
     float tm = sh.part[0][0];
 #pragma unroll
@@ -571,20 +772,33 @@ __device__ __forceinline__ Listed take_list(const DistillArgs& a, int id, float 
     const float e = id < 0 ? 0.f : exp2_hw((u - (tm == -kInf ? 0.f : tm)) * a.c);
     const float es = wave_sum(e);
     if (lane == 0 && wave < kWaves) sh.part[1][wave] = es;
-    if (tid < kMaxListed) sh.ids[tid] = id;
+    if (id >= 0) {
+        // at most half of the places are taken: the search ends at a free one
+        for (uint32_t at = (uint32_t)id * 2654435761u >> 16;; ++at) {
+            const int before = atomicCAS(&sh.table[at & (kTable - 1)], -1, id);
+            if (before == id) sh.twice = 1;
+            if (before == id || before == -1) break;
+        }
+    }
     __syncthreads();
     total = 0.f;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) total += sh.part[1][i];
-    if (tid < kMaxListed) sh.q[tid] = e / total;
+    Listed l{total == 0.f ? -1 : id, e / total};
+    if (!sh.twice) return l;
+    if (tid < kMaxListed) {
+        sh.ids[tid] = id;
+        sh.q[tid] = l.mass;
+    }
     __syncthreads();
-    Listed l{total == 0.f ? -1 : id, 0.f};
-    if (l.id >= 0)
+    if (l.id >= 0) {
+        l.mass = 0.f;
         for (int k = 0; k < a.top; ++k)
             if (sh.ids[k] == id) {
                 if (k < tid) l.id = -1;
                 l.mass += sh.q[k];
             }
+    }
     return l;
 }
 
@@ -614,132 +828,177 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t row, cons
     }
 }
 
-template <class T>
-__device__ __forceinline__ void zero_row(T* d, int V, int threads) {
-    constexpr int N = Elem<T>::kVec;
-    for (int j = threadIdx.x * N; j < V; j += threads * N) {
-        if (j + N <= V) Elem<T>::store(d + j, u32x4{0u, 0u, 0u, 0u});
-        else
-            for (int k = j; k < V; ++k) Elem<T>::put(d + k, 0.f);
-    }
-}
+// W waves hold a whole row in registers, up to NV 16-byte vectors a thread, so
+// that it is read once and the gradient written once.  2^y with y = x c - r(m)
+// (see Stats) is summed up in one pass over the registers, w T p_j = 2^y (w T / S)
+// written in another; the owners of the listed entries then write
+// w T (p_j - q_j).  Where a row fills a compute unit's registers (LOOP), a
+// work-group takes the rows blockIdx.x, + gridDim.x, ... and reads the next one
+// into each register as soon as the last one's vector has been used.
+constexpr int kBlock = 2;
 
-// Rows of up to 16 W NV KB / 16: W waves hold a whole row in registers, NV
-// 16-byte vectors a thread, so that it is read once and the gradient written
-// once.  2^y with y = x c - r(m) (see Stats) is summed up in one pass over the
-// registers and w T p_j = 2^y (w T / S) written in another; the owners of the
-// listed entries then write w T (p_j - q_j).
-template <class T, int W, int NV>
+template <class T, int W, int NV, bool LOOP>
 __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
-    constexpr int N = Elem<T>::kVec, kThreads = 64 * W;
-    const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
-    T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
+    constexpr int N = Elem<T>::kVec, kThreads = 64 * W, kAll = 64 * N;  // elements of a wave's vector
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int V = a.vocab;
     __shared__ ListedShared sh;
     __shared__ float part[3][W];
-    const float w = a.weight ? a.weight[row] : 1.f;
-    if (w == 0.f) {
-        if (tid == 0) a.loss[row] = 0.f;
-        if (d) zero_row(d, V, kThreads);
-        return;
-    }
+    // The row's vectors of a wave's 1 KB are dealt to the waves in turn, kBlock neighbouring ones at a time: the
+    // wave's i-th is the row's number(i)-th.  `whole` of them are whole (in raw); the row's last, partial one is
+    // in its wave's rest.  The row has a whole one at least, and the registers past a wave's own take the row's
+    // last one, unused: loads without a condition keep the array in registers.
+    const int all = V / kAll;
+    auto number = [&](int i) { return (i / kBlock * W + wave) * kBlock + i % kBlock; };
+    int whole = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) whole += number(i) < all;
+    const bool has_rest = V % kAll != 0 && all / kBlock % W == wave;
+    const int j_rest = all * kAll + lane * N;
+    auto place = [&](int i) { return min(number(i), all - 1) * kAll; };
+    u32x4 raw[NV], rest{0u, 0u, 0u, 0u};
+    // the first row from `row` on that has a weight; the others get no loss and zeros
+    float w = 0.f;
+    auto seek = [&](int64_t row) {
+        for (; row < a.n; row += gridDim.x) {
+            w = a.weight ? a.weight[row] : 1.f;
+            if (w != 0.f) break;
+            if (tid == 0) a.loss[row] = 0.f;
+            if (a.out) zero_row(static_cast<T*>(a.out) + row * a.out_stride, V, kThreads);
+            if (!LOOP) return (int64_t)a.n;
+        }
+        return row;
+    };
+    int64_t row = seek(blockIdx.x);
+    if (row >= a.n) return;
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     int id;
     float u;
     read_list(a, row, id, u);
-    // vector i of this thread starts at (i kThreads + tid) N; whether a wave has any of it is the same in all its lanes
-    const int first = __builtin_amdgcn_readfirstlane(wave) * 64 * N;
-    u32x4 raw[NV];
-    float edge[N];  // a vector that the row ends in
+    {
+        const T* from = x - (odd_row(x) ? 1 : 0);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (first + i * kThreads * N >= V) break;
-        const int j = (i * kThreads + tid) * N;
-        if (j + N <= V) {
-            raw[i] = Elem<T>::load_nt(x + j);
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) edge[k] = j + k < V ? Elem<T>::get(x + j + k) : -kInf;
-            raw[i] = Elem<T>::pack(edge);
-        }
+        for (int i = 0; i < NV; ++i) raw[i] = Elem<T>::load_nt(lane_place(from + place(i), lane));
+        if (has_rest) rest = load_vector(x, j_rest, V, odd_row(x) ? 1 : 0);
     }
-    float total;
-    const Listed l = take_list(a, id, u, sh, total);
-    const bool out = total == 0.f;
-    const float z = l.id >= 0 ? Elem<T>::get(x + l.id) : 0.f;
+    for (;;) {
+        T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
+        float total;
+        const Listed l = take_list(a, id, u, sh, total);
+        const bool out = total == 0.f;
+        const float z = l.id >= 0 ? Elem<T>::get(x + l.id) : 0.f;
+        if (odd_row(x)) {
+            uint32_t after[NV / kBlock];  // the last element of each block
+#pragma unroll
+            for (int i = 0; i < NV; i += kBlock) after[i / kBlock] = element_bits(x + place(i + kBlock - 1) + kAll - 1);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                uint32_t next = after[i / kBlock];
+                if (i % kBlock != kBlock - 1 && i + 1 < whole)
+                    next = (uint32_t)__builtin_amdgcn_readlane((int)raw[i + 1 < NV ? i + 1 : i][0], 0);
+                raw[i] = shift_in(raw[i], next);
+            }
+            if (has_rest) rest = shift_in(rest, 0xff80);  // the row ends before lane 63 does: -inf
+        }
 
-    float m = -kInf;
+        float m = -kInf;
+        auto top = [&](u32x4 q) {
+            float v[N];
+            Elem<T>::unpack(q, v);
+            m = fmaxf(m, largest<N>(v));
+        };
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (first + i * kThreads * N >= V) break;
-        float v[N];
-        Elem<T>::unpack(raw[i], v);
-        m = fmaxf(m, largest<N>(v));
-    }
-    m = wave_max(m);
-    if (lane == 0) part[0][wave] = m;
-    __syncthreads();
-    m = wave_max(lane < W ? part[0][lane] : -kInf);
-    const float ref = m == -kInf ? 0.f : m, r = ref * a.c;
-    float s = 0.f;
-    if (Stats::plain(r)) {
+        for (int i = 0; i < NV; ++i)
+            if (i < whole) top(raw[i]);
+        if (has_rest) top(rest);
+        m = wave_max(m);
+        if (lane == 0) part[0][wave] = m;
+        __syncthreads();
+        m = wave_max(lane < W ? part[0][lane] : -kInf);
+        // y = (x - low) c - r, low 0 but for rows near the end of the fp32 range
+        const float ref = m == -kInf ? 0.f : m;
+        const bool plain = Stats::plain(ref * a.c);
+        const float low = plain ? 0.f : ref, r = plain ? ref * a.c : 0.f;
+        float s = 0.f;
+        auto add = [&](u32x4 q) {
+            float v[N];
+            Elem<T>::unpack(q, v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) s += exp2_hw(__builtin_fmaf(v[k] - low, a.c, -r));
+        };
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < whole) add(raw[i]);
+        if constexpr (LOOP && sizeof(T) == 4)  // no exponentials are kept for the next pass: registers are short
+#pragma unroll
+            for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(raw[i]));
+        if (has_rest) add(rest);
+        s = wave_sum(s);
+        if (lane == 0) part[1][wave] = s;
+        __syncthreads();
+        const Stats st{m, wave_sum(lane < W ? part[1][lane] : 0.f), 0.f};
+        put_loss<W>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
+        if (out && tid == 0) a.loss[row] = 0.f;
+        if (!LOOP && !d) return;
+
+        const float k = w * a.t, ks = k / st.s;
+        const bool zero = out || st.empty();
+        int64_t next = a.n;
+        const T *x_next = x, *from = x;
+        if constexpr (LOOP) {
+            next = seek(row + gridDim.x);
+            if (next < a.n) {
+                read_list(a, next, id, u);
+                x_next = static_cast<const T*>(a.logits) + next * a.stride;
+            }
+            from = x_next - (odd_row(x_next) ? 1 : 0);
+        }
+        auto slope = [&](u32x4 q) {
+            float v[N];
+            Elem<T>::unpack(q, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = exp2_hw(__builtin_fmaf(v[e] - low, a.c, -r)) * ks;
+            const u32x4 o = Elem<T>::pack(v);
+            return zero ? u32x4{0u, 0u, 0u, 0u} : o;
+        };
+        const u32x4 o_rest = has_rest ? slope(rest) : u32x4{0u, 0u, 0u, 0u};
+        const bool odd_out = odd_row(d), straight = straight_row(d);
+        u32x4 held{0u, 0u, 0u, 0u};  // at an odd address: the vector before, whose last lane wants this one's first element
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (first + i * kThreads * N >= V) break;
-            float v[N];
-            Elem<T>::unpack(raw[i], v);
-#pragma unroll
-            for (int k = 0; k < N; ++k) s += exp2_hw(__builtin_fmaf(v[k], a.c, -r));
+            if (i < whole) {
+                const u32x4 o = slope(raw[i]);
+                T* at = d + place(i);
+                if (!d) {
+                    // the loss alone
+                } else if (!odd_out) {
+                    store_piece(lane_place(at, lane), o, straight);
+                } else {
+                    if (i % kBlock == 0) {
+                        if (lane == 0) store_first(at, o);
+                    } else {
+                        Elem<T>::store(lane_place(at - kAll + 1, lane),
+                                       shift_in(held, (uint32_t)__builtin_amdgcn_readlane((int)o[0], 0)));
+                    }
+                    if (i % kBlock == kBlock - 1 || i + 1 == whole) store_end(at, o, lane);
+                    held = o;
+                }
+            }
+            if constexpr (LOOP) raw[i] = Elem<T>::load_nt(lane_place(from + (next < a.n ? place(i) : 0), lane));
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (first + i * kThreads * N >= V) break;
-            float v[N];
-            Elem<T>::unpack(raw[i], v);
-#pragma unroll
-            for (int k = 0; k < N; ++k) s += exp2_hw((v[k] - ref) * a.c);
+        if (d) {
+            if (has_rest) store_vector(d, j_rest, V, o_rest, odd_out, straight, lane);
+            __syncthreads();
+            if (l.id >= 0 && !zero) {
+                const float p = exp2_hw(__builtin_fmaf(z - low, a.c, -r)) / st.s;
+                Elem<T>::put(d + l.id, (p - l.mass) * k);
+            }
         }
-    }
-    s = wave_sum(s);
-    if (lane == 0) part[1][wave] = s;
-    __syncthreads();
-    const Stats st{m, wave_sum(lane < W ? part[1][lane] : 0.f), 0.f};
-    put_loss<W>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
-    if (out && tid == 0) a.loss[row] = 0.f;
-    if (!d) return;
-    if (out || st.empty()) {
-        zero_row(d, V, kThreads);
-        return;
-    }
-    const float k = w * a.t, ks = k / st.s;
-    const bool plain = Stats::plain(r);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (first + i * kThreads * N >= V) break;
-        const int j = (i * kThreads + tid) * N;
-        float v[N];
-        Elem<T>::unpack(raw[i], v);
-        if (plain) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = exp2_hw(__builtin_fmaf(v[e], a.c, -r)) * ks;
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = exp2_hw((v[e] - ref) * a.c) * ks;
-        }
-        if (j + N <= V) {
-            Elem<T>::store_nt(d + j, Elem<T>::pack(v));
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (j + e < V) Elem<T>::put(d + j + e, v[e]);
-        }
-    }
-    __syncthreads();
-    if (l.id >= 0) {
-        const float p = exp2_hw(plain ? __builtin_fmaf(z, a.c, -r) : (z - ref) * a.c) / st.s;
-        Elem<T>::put(d + l.id, (p - l.mass) * k);
+        if (!LOOP || next >= a.n) return;
+        if (has_rest) rest = load_vector(x_next, j_rest, V, odd_row(x_next) ? 1 : 0);
+        row = next;
+        x = x_next;
+        __syncthreads();  // the shared arrays are used again
     }
 }
 
@@ -923,15 +1182,19 @@ void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st
     else logprobs_kernel<T, false, kRowWaves><<<grid, 64 * kRowWaves, 0, st>>>(a);
 }
 
+constexpr int32_t kGradFill = 1024;  // work-groups of the gradient of log probabilities where rows can be split
+constexpr int kUnits = 256;  // compute units of the card
+
 template <class T>
 void launch_distill(const DistillArgs& a, hipStream_t st) {
     const int64_t vectors = ((int64_t)a.vocab + Elem<T>::kVec - 1) / Elem<T>::kVec;
-    if (vectors <= 2 * 256) distill_kernel<T, 4, 2><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 4 * 256) distill_kernel<T, 4, 4><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 8 * 256) distill_kernel<T, 4, 8><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 16 * 256) distill_kernel<T, 4, 16><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 16 * 512) distill_kernel<T, 8, 16><<<a.n, 512, 0, st>>>(a);
-    else if (vectors <= 16 * 1024) distill_kernel<T, 16, 16><<<a.n, 1024, 0, st>>>(a);
+    if (a.vocab < 64 * Elem<T>::kVec) distill_long<T><<<a.n, 64 * kLongWaves, 0, st>>>(a);
+    else if (vectors <= 2 * 256) distill_kernel<T, 4, 2, false><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 4 * 256) distill_kernel<T, 4, 4, false><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 8 * 256) distill_kernel<T, 4, 8, false><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 16 * 256) distill_kernel<T, 4, 16, false><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 16 * 512) distill_kernel<T, 8, 16, false><<<a.n, 512, 0, st>>>(a);
+    else if (vectors <= 16 * 1024) distill_kernel<T, 16, 16, true><<<a.n < kUnits ? a.n : kUnits, 1024, 0, st>>>(a);
     else distill_long<T><<<a.n, 64 * kLongWaves, 0, st>>>(a);
 }
 
@@ -1017,9 +1280,14 @@ extern "C" edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32
     GradArgs a{logits, stride,  n,         vocab,     ids,     log2e_over(temperature), (float)(1.0 / (double)temperature),
                stats,  entropy, g_logprob, g_entropy, dlogits, dlogits_stride};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const dim3 grid(n), block(256);
-    if (dtype == EDB_F32) logprobs_grad_kernel<float><<<grid, block, 0, st>>>(a);
-    else logprobs_grad_kernel<bf16><<<grid, block, 0, st>>>(a);
+    // work-groups of as many waves as a row has vectors for, and enough of them for the card
+    const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec;
+    const int32_t turns = (vocab + 64 * vec * kGradLoads - 1) / (64 * vec * kGradLoads);
+    const int32_t waves = turns < kGradWaves ? turns : kGradWaves, most = (turns + waves - 1) / waves;
+    const int32_t wanted = n < kGradFill ? (kGradFill + n - 1) / n : 1;
+    const dim3 grid(n, wanted < most ? wanted : most);
+    if (dtype == EDB_F32) logprobs_grad_kernel<float><<<grid, 64 * waves, 0, st>>>(a);
+    else logprobs_grad_kernel<bf16><<<grid, 64 * waves, 0, st>>>(a);
     return launched(who);
 }
 
