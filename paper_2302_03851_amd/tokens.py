@@ -13,6 +13,7 @@ allocated.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -20,7 +21,6 @@ import torch
 from . import _lib as L
 
 _DTYPE = {torch.float32: L.F32, torch.bfloat16: L.BF16}
-_FLOATS = (torch.float32, torch.bfloat16)
 
 
 class LogProbs(NamedTuple):
@@ -38,16 +38,19 @@ class Distilled(NamedTuple):
 
 def _matrix(t, name, dev=None):
     """Rows, columns and row stride in elements of a matrix operand."""
-    if t.dim() != 2 or t.dtype not in _FLOATS:
+    if t.dim() != 2 or t.dtype not in _DTYPE:
         raise ValueError(f"{name}: a 2-D float32 or bfloat16 tensor is needed, not {t.dim()}-D {t.dtype}")
-    _on(t, name, dev)
+    if dev is None or t.device != dev:
+        _on(t, name, dev)
     n, m = t.shape
-    if m > 1 and t.stride(1) != 1:
+    s, one = t.stride()
+    if one != 1 and m > 1:
         raise ValueError(f"{name}: the rows must be contiguous")
-    s = t.stride(0)
-    if n > 1 and s < m:
+    if s >= m:
+        return n, m, s
+    if n > 1:
         raise ValueError(f"{name}: the rows overlap")
-    return n, m, s if s > m else m
+    return n, m, m
 
 
 def _on(t, name, dev):
@@ -58,37 +61,50 @@ def _on(t, name, dev):
 
 
 def _array(t, name, shape, dtype, dev):
-    """A dense operand of one type (no copies are made)."""
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+    """Address of a dense operand of one type (no copies are made)."""
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} is needed, not {t.dtype} {tuple(t.shape)}")
-    _on(t, name, dev)
+    if t.device != dev:
+        _on(t, name, dev)
     return t.data_ptr()
+
+
+# the current stream's handle; the public call builds a Stream object first (2.5 us a call, this 0.1)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+_entry = {}
 
 
 def _call(name, dev, *args):
     """Run one entry point on the current stream of `dev`."""
-    fn = getattr(L.load(), name)
-    if torch.cuda.current_device() == dev.index:
-        status = fn(*args, torch.cuda.current_stream().cuda_stream)
+    fn = _entry.get(name)
+    if fn is None:
+        fn = _entry[name] = getattr(L.load(), name)
+    index = dev.index
+    if torch.cuda.current_device() == index:
+        status = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, torch.cuda.current_stream().cuda_stream)
+            status = fn(*args, _raw_stream(index))
     if status:
         L.check(status, name)
 
 
-def _workspace(name, dev, *args):
-    """Scratch memory of the current stream: torch hands it to later work of that stream only."""
+@functools.lru_cache(maxsize=1024)
+def _bytes(name, *args):
     nb = C.c_int64()
     L.check(getattr(L.load(), name)(*args, C.byref(nb)), name)
-    if not nb.value:
-        return None, 0, None
+    return nb.value
+
+
+def _workspace(dev, nb):
+    """Scratch memory of the current stream: torch hands it to later work of that stream only."""
+    if not nb:
+        return None
     if torch.cuda.current_device() == dev.index:
-        ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
-    else:
-        with torch.cuda.device(dev):   # its stream, not the current device's
-            ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
-    return ws.data_ptr(), nb.value, ws
+        return torch.empty(nb, dtype=torch.uint8, device=dev)
+    with torch.cuda.device(dev):   # its stream, not the current device's
+        return torch.empty(nb, dtype=torch.uint8, device=dev)
 
 
 def embed(ids, table, scale: float = 1.0, dtype=None, out=None) -> torch.Tensor:
@@ -126,9 +142,10 @@ def embed_grad(ids, dout, vocab: int, scale: float = 1.0, dtype=None, out=None, 
     on, om, ostride = _matrix(out, "out", dev)
     if (on, om) != (vocab, dim):
         raise ValueError(f"out: {vocab} x {dim} is needed, not {on} x {om}")
-    wp, wb, ws = _workspace("edb_embed_grad_bytes", dev, n, vocab, dim)
+    nb = _bytes("edb_embed_grad_bytes", n, vocab, dim)
+    ws = _workspace(dev, nb)
     _call("edb_embed_grad", dev, ip, n, dout.data_ptr(), _DTYPE[dout.dtype], vocab, dim, stride, scale,
-          1 if accumulate else 0, out.data_ptr(), _DTYPE[out.dtype], ostride, wp, wb)
+          1 if accumulate else 0, out.data_ptr(), _DTYPE[out.dtype], ostride, ws.data_ptr() if nb else None, nb)
     return out
 
 
@@ -147,11 +164,12 @@ def logprobs(logits, ids=None, temperature: float = 1.0, top: int = 0, out: Opti
     if (out.logprob is None) != (ids is None):
         raise ValueError("out: made with ids and used without, or the other way round")
     lp = None if ids is None else _array(out.logprob, "out.logprob", (n,), f32, dev)
-    wp, wb, ws = _workspace("edb_logprobs_bytes", dev, n, vocab, dt, top)
+    nb = _bytes("edb_logprobs_bytes", n, vocab, dt, top)
+    ws = _workspace(dev, nb)
     _call("edb_logprobs", dev, logits.data_ptr(), dt, n, vocab, stride, ip, temperature, top, lp,
           _array(out.entropy, "out.entropy", (n,), f32, dev), _array(out.stats, "out.stats", (n, 2), f32, dev),
           _array(out.top_ids, "out.top_ids", (n, top), torch.int32, dev),
-          _array(out.top_logprobs, "out.top_logprobs", (n, top), f32, dev), wp, wb)
+          _array(out.top_logprobs, "out.top_logprobs", (n, top), f32, dev), ws.data_ptr() if nb else None, nb)
     return out
 
 
