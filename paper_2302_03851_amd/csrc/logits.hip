@@ -328,7 +328,15 @@ __device__ __forceinline__ Key merge_down(Key k, int lane) {  // of a bitonic se
     k = order_with<2>(k, lane);
     return order_with<1>(k, lane);
 }
-__device__ __forceinline__ Key sort_down(Key k, int lane) {
+template <int D>
+__device__ __forceinline__ uint32_t order_with(uint32_t k, int lane) {
+    constexpr int kHigh = D & 32 ? 32 : D & 16 ? 16 : D & 8 ? 8 : D & 4 ? 4 : D & 2 ? 2 : 1;
+    const uint32_t o = from_lane_xor<D>(k);
+    return (lane & kHigh) == 0 ? max(o, k) : min(o, k);
+}
+
+template <class K>
+__device__ __forceinline__ K sort_down(K k, int lane) {
     k = order_with<1>(k, lane);
     k = order_with<3>(k, lane);
     k = order_with<1>(k, lane);
@@ -360,8 +368,11 @@ struct Best {
     uint32_t bound;  // order of a value that at least `top` entries reach
 
     // A bound from the orders of values of different entries, four a lane (0 for
-    // none): the top-th largest, its lower 16 bits left open.
-    __device__ __forceinline__ static uint32_t bound_of(const uint32_t (&u)[4], int top) {
+    // none): for short lists the top-th largest of the lanes' own largest, else
+    // the top-th largest of all, its lower 16 bits left open.
+    __device__ __forceinline__ static uint32_t bound_of(const uint32_t (&u)[4], int top, int lane) {
+        if (top <= 32)
+            return (uint32_t)__builtin_amdgcn_readlane((int)sort_down(max(max(u[0], u[1]), max(u[2], u[3])), lane), top - 1);
         uint32_t b = 0;
 #pragma unroll
         for (int bit = 31; bit >= 16; --bit) {
@@ -373,6 +384,8 @@ struct Best {
         }
         return b;
     }
+    // the least value that reaches the bound
+    __device__ __forceinline__ float bound_value() const { return bound ? key_value((Key)bound << 32) : -kInf; }
     __device__ __forceinline__ void take(Key* wait, int top, int lane) {
         Key k = sort_down(lane < waiting ? wait[lane] : 0, lane);
         if (key_at(0)) {  // the larger ones of the list and the mirrored newcomers: a bitonic sequence
@@ -456,12 +469,12 @@ __device__ __forceinline__ float quad_max(float v) {
 
 constexpr int kLoads = 2;  // 16-byte loads of a thread in flight, beside as many at work
 
-// A work-group takes a part of a row (mostly all of it) in one pass, 16 bytes a
+// A work-group takes a row (a part of it past 131072 logits) in one pass, 16 bytes a
 // load.  For the alternatives each quad of lanes leaves the largest of its 64
 // bytes in LDS: the best `top` logits lie in the best `top` of these groups (a
 // group that does not belong to them has `top` groups with a better logit
 // before it), so at the end one wave looks for those groups and reads them again.
-// W waves: 4, and 1 for short rows, whose time goes into that last part.
+// (W: row_waves)
 template <class T, bool TOP, int W>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     constexpr int N = Elem<T>::kVec, kStep = kLoads * W * 64 * N;
@@ -558,10 +571,24 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) order[u] = own[u] > -kInf ? ordered(own[u]) : 0;
         Best groups;
-        groups.bound = Best::bound_of(order, a.top);
-        for (int i = lane; i - lane < n; i += 64) groups.offer(i < n ? key_of(group_max[i], i) : 0, wait, a.top, lane);
-        groups.take(wait, a.top, lane);
-        const int there = __popcll(__ballot(lane < a.top && groups.key));
+        groups.bound = Best::bound_of(order, a.top, lane);
+        for (int i0 = lane; i0 - lane < n; i0 += 256) {
+            float w[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) w[u] = i0 + u * 64 < n ? group_max[i0 + u * 64] : -kInf;
+            if (__ballot(largest<4>(w) >= groups.bound_value()) == 0) continue;  // mostly none of 256 groups
+#pragma unroll
+            for (int u = 0; u < 4; ++u) groups.offer(key_of(w[u], i0 + u * 64), wait, a.top, lane);
+        }
+        // up to 64 groups reach the bound: all of them are read again; more: the best ones
+        int there = groups.waiting;
+        int mine = lane < there ? key_index(wait[lane]) : 0;
+        if (groups.key_at(0)) {
+            groups.take(wait, a.top, lane);
+            there = __popcll(__ballot(lane < a.top && groups.key));
+            mine = key_index(groups.key);
+        }
+        __builtin_amdgcn_wave_barrier();
         best.bound = groups.bound;
         for (int g0 = 0; g0 < there; g0 += 4 * kAtOnce) {
             float w[4];
@@ -569,7 +596,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int g = g0 + u * kAtOnce + lane / kGroup;
-                j[u] = begin + key_index((Key)(uint32_t)__shfl((int)groups.key, g & 63)) * kGroup + lane % kGroup;
+                j[u] = begin + __shfl(mine, g & 63) * kGroup + lane % kGroup;
                 w[u] = g < there && j[u] < end ? Elem<T>::get(x + j[u]) : -kInf;
             }
 #pragma unroll
@@ -597,12 +624,10 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
         return;
     }
     const float given = a.ids ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.stride + id) : 0.f;
-    Stats st = Stats::none();
-    for (int i0 = 0; i0 < a.parts; i0 += 64) {
-        // lane 0 carries the parts before these
-        Stats next = i0 + lane < a.parts ? a.part_stats[row * a.parts + i0 + lane] : Stats::none();
-        next.join_wave(a.c);
-        st = lane == 0 ? st : lane == 1 ? next : Stats::none();
+    Stats st = lane < a.parts ? a.part_stats[row * a.parts + lane] : Stats::none();
+    st.join_wave(a.c);
+    for (int i0 = 64; i0 < a.parts; i0 += 63) {  // lane 63 carries the parts before these
+        if (lane != 63) st = i0 + lane < a.parts ? a.part_stats[row * a.parts + i0 + lane] : Stats::none();
         st.join_wave(a.c);
     }
     Best best;
@@ -620,7 +645,7 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
             }
         for (int i = lane; i < a.parts; i += 64) last = max(last, (uint32_t)(keys[(i + 1) * a.top - 1] >> 32));
         for (int d = 1; d < 64; d <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, d));
-        best.bound = max(last, Best::bound_of(own, a.top));
+        best.bound = max(last, Best::bound_of(own, a.top, lane));
         for (int i = lane; i - lane < n; i += 64) best.offer(i < n ? keys[i] : 0, wait, a.top, lane);
         best.take(wait, a.top, lane);
     }
@@ -1130,15 +1155,14 @@ edb_status launched(const char* who) {
     return EDB_OK;
 }
 
-constexpr int kRowWaves = 4;
-// One wave takes a row of up to 4 KB, and of up to 16 KB where there are enough
-// rows to fill the card with single waves (8192 rows of 4096 bf16: 23 us, by
-// four waves 28; 63 rows of 8192: 11 us, by four 8).
-bool brief_row(int32_t n, int64_t bytes) { return bytes <= 4096 || (bytes <= 16384 && n >= 2048); }
-// Rows of at least so many logits are split where there are fewer than kFill
-// rows (one row of 32003 bf16: 12.0 us, whole 13.9; of 131072: 12.6, whole 32;
-// 300 rows of 10007: 15.1, whole 12.8, for the join is a launch more).
-constexpr int32_t kSplit = 16384, kFill = 512;
+// Waves that take a row: one up to 4 KB, and up to 16 KB where there are enough
+// rows to fill the card with single waves; eight for long rows where there are
+// too few to fill it with four.
+constexpr int kFewRows = 512, kManyRows = 2048;
+int row_waves(int32_t n, int64_t bytes) {
+    if (bytes <= 4096 || (bytes <= 16384 && n >= kManyRows)) return 1;
+    return n < kFewRows && bytes >= 32768 ? 8 : 4;
+}
 
 // How a forward call splits its rows, and its scratch memory.
 struct RowPlan {
@@ -1146,18 +1170,19 @@ struct RowPlan {
     int64_t stats, keys, bytes;  // offsets
 };
 
-// A row is split where there are too few rows for the card, and where a part's
-// group maxima would pass 32 KB of LDS.  Parts are whole steps of a work-group,
-// two at least.
-RowPlan row_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
-    constexpr int32_t kMost = 131072;
-    const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec, step = 2 * kLoads * kRowWaves * 64 * vec;
-    const int64_t steps = ((int64_t)vocab + step - 1) / step;
-    int64_t parts = n >= kFill || n < 1 || vocab < kSplit ? 1 : (kFill + n - 1) / n;
-    if (parts > steps) parts = steps;
+// Rows from 2^16 logits on are split into parts, joined by a second launch, where
+// there are few of them; and any row whose group maxima would pass 32 KB of LDS.
+RowPlan row_plan(int32_t n, int32_t vocab, int32_t top) {
+    constexpr int32_t kSplit = 65536, kMost = 131072, kLeast = 8192, kFill = 512;
+    int64_t parts = 1;
+    if (n > 0 && n < kFill / 2 && vocab >= kSplit) {
+        parts = kFill / n;
+        if (parts > vocab / kLeast) parts = vocab / kLeast;
+    }
     if (parts * kMost < vocab) parts = ((int64_t)vocab + kMost - 1) / kMost;
     RowPlan r{};
-    r.part = (int32_t)((steps + parts - 1) / parts * step);
+    const int64_t part = ((int64_t)vocab + parts - 1) / parts;
+    r.part = (int32_t)(parts > 1 ? (part + kLeast - 1) / kLeast * kLeast : vocab);
     r.parts = (int32_t)(((int64_t)vocab + r.part - 1) / r.part);
     if (r.parts == 1) return r;
     const int64_t all = (int64_t)n * r.parts;
@@ -1173,13 +1198,18 @@ size_t group_bytes(const RowPlan& r, int32_t vocab) {
     return (places / (4 * Elem<T>::kVec) + 1) * 4;
 }
 
+template <class T, int W>
+void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st) {
+    if (a.top) logprobs_kernel<T, true, W><<<grid, 64 * W, lds, st>>>(a);
+    else logprobs_kernel<T, false, W><<<grid, 64 * W, 0, st>>>(a);
+}
+
 template <class T>
 void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st) {
-    const bool brief = a.parts == 1 && brief_row(a.n, (int64_t)a.vocab * sizeof(T));
-    if (a.top && brief) logprobs_kernel<T, true, 1><<<grid, 64, lds, st>>>(a);
-    else if (a.top) logprobs_kernel<T, true, kRowWaves><<<grid, 64 * kRowWaves, lds, st>>>(a);
-    else if (brief) logprobs_kernel<T, false, 1><<<grid, 64, 0, st>>>(a);
-    else logprobs_kernel<T, false, kRowWaves><<<grid, 64 * kRowWaves, 0, st>>>(a);
+    const int waves = a.parts > 1 ? 4 : row_waves(a.n, (int64_t)a.vocab * sizeof(T));
+    if (waves == 1) launch_logprobs<T, 1>(a, grid, lds, st);
+    else if (waves == 4) launch_logprobs<T, 4>(a, grid, lds, st);
+    else launch_logprobs<T, 8>(a, grid, lds, st);
 }
 
 constexpr int32_t kGradFill = 1024;  // work-groups of the gradient of log probabilities where rows can be split
@@ -1208,7 +1238,7 @@ extern "C" edb_status edb_logprobs_bytes(int32_t n, int32_t vocab, int32_t dtype
     if (top < 0 || top > EDB_LOGPROBS_MAX_TOP)
         return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs_bytes: top must be in [0, " +
                                              std::to_string(EDB_LOGPROBS_MAX_TOP) + "]");
-    *bytes = row_plan(n, vocab, dtype, top).bytes;
+    *bytes = row_plan(n, vocab, top).bytes;
     edb::clear_error();
     return EDB_OK;
 }
@@ -1227,7 +1257,7 @@ extern "C" edb_status edb_logprobs(const void* logits, int32_t dtype, int32_t n,
         edb::clear_error();
         return EDB_OK;
     }
-    const RowPlan r = row_plan(n, vocab, dtype, top);
+    const RowPlan r = row_plan(n, vocab, top);
     if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
         return fail(EDB_ERR_INVALID, "edb_logprobs: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
                                          " bytes is needed");
