@@ -1222,8 +1222,8 @@ void launch_distill(const DistillArgs& a, hipStream_t st) {
     else if (vectors <= 2 * 256) distill_kernel<T, 4, 2, false><<<a.n, 256, 0, st>>>(a);
     else if (vectors <= 4 * 256) distill_kernel<T, 4, 4, false><<<a.n, 256, 0, st>>>(a);
     else if (vectors <= 8 * 256) distill_kernel<T, 4, 8, false><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 16 * 256) distill_kernel<T, 4, 16, false><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 16 * 512) distill_kernel<T, 8, 16, false><<<a.n, 512, 0, st>>>(a);
+    else if (vectors <= 8 * 512) distill_kernel<T, 8, 8, false><<<a.n, 512, 0, st>>>(a);
+    else if (vectors <= 8 * 1024) distill_kernel<T, 16, 8, false><<<a.n, 1024, 0, st>>>(a);
     else if (vectors <= 16 * 1024) distill_kernel<T, 16, 16, true><<<a.n < kUnits ? a.n : kUnits, 1024, 0, st>>>(a);
     else distill_long<T><<<a.n, 64 * kLongWaves, 0, st>>>(a);
 }
