@@ -15,8 +15,8 @@ using namespace edb::rows;
 
 namespace {
 
-// K consecutive elements of a row as fp32: 8 or 4 where rows hold whole groups
-// of so many (at any alignment), else 1.
+// K consecutive elements of a row as fp32, at any alignment.  K is 8 or 4, or 1
+// for rows shorter than 4.
 // ONCE: read once only, not worth a place in the caches.
 template <class T, int K, bool ONCE = false>
 __device__ __forceinline__ void load_k(const T* p, float* v) {
@@ -42,6 +42,26 @@ __device__ __forceinline__ void store_k(T* p, const float* v) {
     }
 }
 
+// Where the piece of K elements that starts at `nominal` is taken from in a row
+// of dim >= K: the last one, if the row ends inside it, from the row's end
+// backwards, and the `skip` elements that it shares with the piece before it
+// are left to that one (so that no element has two writers).
+template <int K>
+struct Piece {
+    int col, skip;
+    __device__ __forceinline__ Piece(int nominal, int dim) : col(min(nominal, dim - K)), skip(nominal - col) {}
+};
+template <class T, int K>
+__device__ __forceinline__ void store_from(T* p, const float* v, int skip) {
+    if (K == 1 || skip <= 0) {
+        store_k<T, K>(p, v);
+    } else {
+#pragma unroll
+        for (int k = 1; k < K; ++k)
+            if (k >= skip) Elem<T>::put(p + k, v[k]);
+    }
+}
+
 struct EmbedArgs {
     const int32_t* ids;
     int32_t n, vocab, dim;
@@ -55,36 +75,40 @@ struct EmbedArgs {
 // One thread per K elements of a row.
 template <class T, class O, int K>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
-    const int pieces = a.dim / K;
+    const int pieces = (a.dim + K - 1) / K;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / pieces;
     if (row >= a.n) return;
-    const int col = (int)(at - row * pieces) * K, id = a.ids[row];
+    const Piece<K> piece((int)(at - row * pieces) * K, a.dim);
+    const int id = a.ids[row];
     float v[K];
     if (id < 0 || id >= a.vocab) {
 #pragma unroll
         for (int i = 0; i < K; ++i) v[i] = 0.f;
     } else {
-        load_k<T, K>(static_cast<const T*>(a.table) + id * a.table_stride + col, v);
+        load_k<T, K>(static_cast<const T*>(a.table) + id * a.table_stride + piece.col, v);
 #pragma unroll
         for (int i = 0; i < K; ++i) v[i] *= a.scale;
     }
-    store_k<O, K>(static_cast<O*>(a.out) + row * a.out_stride + col, v);
+    O* to = static_cast<O*>(a.out) + row * a.out_stride + piece.col;
+    if constexpr (K == Elem<O>::kVec) {
+        if (piece.skip == 0) return Elem<O>::store_nt(to, Elem<O>::pack(v));
+    }
+    store_from<O, K>(to, v, piece.skip);
 }
 
 // ---- the gradient: positions sorted by word, then sums over the runs of a word
 //
 // The sort is a stable radix sort of (word, position), so a word's rows are
 // added in ascending position and the result does not depend on timing.  Ids
-// that are no token get the word V and sort to the end.  Up to kBlockSort ids
-// are sorted by one work-group in LDS; more by passes over digits of up to
-// kMaxDigit bits, three launches each (counts per tile, their prefix sums, the
-// scatter).  The zero rows of the other words are written in the launch of the
-// sums, by further work-groups.
+// that are no token get the word V and sort to the end.  It takes a pass for
+// every digit of up to kMaxDigit bits, of counts per tile, their prefix sums and
+// the scatter.  The zero rows of the other words are written in the launch of
+// the sums, by further work-groups.
 
-constexpr int kBlockSort = 8192;   // ids of the one-work-group sort: keys, positions and counts fill 56 KB of LDS
 constexpr int kMaxDigit = 10;
-constexpr int kTile = 1024;        // ids a work-group of the large sort ranks: 4 waves of 4 rounds
+constexpr int kTile = 1024;        // ids a work-group of the sort ranks: 4 waves of 4 rounds
 constexpr int kRounds = 4;
+constexpr int kSumTiles = 64;      // tiles up to which the scatter adds up the counts itself
 
 __device__ __forceinline__ uint32_t word_of(int32_t id, uint32_t vocab) {
     return (uint32_t)id < vocab ? (uint32_t)id : vocab;
@@ -124,80 +148,6 @@ struct SortArgs {
     int32_t n, tiles, shift, bits;
     uint32_t vocab;
 };
-
-// One work-group, everything in LDS: passes of 8 bits.  Each of the 16 waves
-// ranks a contiguous eighth-kilo of ids, so the order (digit, wave, round,
-// lane) is the stable one.
-__global__ __launch_bounds__(1024) void sort_block(SortArgs a) {
-    constexpr int kWaves = 16, kBins = 256, kPer = kBlockSort / 1024;
-    __shared__ uint32_t keys[kBlockSort];
-    __shared__ uint16_t pos[kBlockSort];
-    __shared__ uint16_t count[kBins][kWaves];
-    __shared__ uint32_t wave_sum[kWaves];
-    const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
-    const int rounds = (a.n + 1023) / 1024, first = wave * rounds * 64;
-    uint32_t k[kPer], p[kPer], rank[kPer];
-#pragma unroll
-    for (int r = 0; r < kPer; ++r) {
-        const int i = first + r * 64 + lane;
-        p[r] = i;
-        k[r] = r < rounds && i < a.n ? word_of(a.ids[i], a.vocab) : a.vocab;
-    }
-    for (int shift = 0;; shift += 8) {
-        for (int i = tid; i < kBins * kWaves; i += 1024) (&count[0][0])[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kPer; ++r)
-            if (r < rounds) {
-                const bool valid = first + r * 64 + lane < a.n;
-                const uint32_t d = (k[r] >> shift) & 255;
-                const uint64_t m = same_digit(d, 8, __ballot(valid));
-                const int before = __popcll(m & ((1ull << lane) - 1));
-                if (valid) rank[r] = count[d][wave] + before;
-                // the last lane of a digit updates its count, after every lane has read it
-                __builtin_amdgcn_wave_barrier();
-                if (valid && (m >> lane) == 1) count[d][wave] = (uint16_t)(rank[r] + 1);
-                __builtin_amdgcn_wave_barrier();
-            }
-        __syncthreads();
-        // exclusive sums in the order (digit, wave): four counts a thread
-        uint32_t c[4], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            c[i] = (&count[0][0])[4 * tid + i];
-            sum += c[i];
-        }
-        const uint32_t upto = wave_scan_inclusive(sum);
-        if (lane == 63) wave_sum[wave] = upto;
-        __syncthreads();
-        uint32_t base = upto - sum;
-        for (int w = 0; w < wave; ++w) base += wave_sum[w];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            (&count[0][0])[4 * tid + i] = (uint16_t)base;
-            base += c[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kPer; ++r)
-            if (r < rounds && first + r * 64 + lane < a.n) {
-                const int to = count[(k[r] >> shift) & 255][wave] + (int)rank[r];
-                keys[to] = k[r];
-                pos[to] = (uint16_t)p[r];
-            }
-        __syncthreads();
-        if (shift + 8 >= a.bits) break;
-#pragma unroll
-        for (int r = 0; r < kPer; ++r) {
-            const int i = first + r * 64 + lane;
-            if (r < rounds && i < a.n) {
-                k[r] = keys[i];
-                p[r] = pos[i];
-            }
-        }
-    }
-    for (int i = tid; i < a.n; i += 1024) a.out[i] = Pair{keys[i], pos[i]};
-}
 
 __device__ __forceinline__ Pair sort_pair(const SortArgs& a, int64_t i) {
     return a.ids ? Pair{word_of(a.ids[i], a.vocab), (uint32_t)i} : a.in[i];
@@ -250,7 +200,11 @@ __global__ __launch_bounds__(256) void sort_scan(SortArgs a) {
     if (mine == 15) a.totals[bin] = base;
 }
 
-// Ranks a tile's ids and writes them to their places.
+// Ranks a tile's ids and writes them to their places.  SUM: the counts are
+// still those of single tiles, and every work-group adds them up for itself;
+// for few tiles that takes less than another launch (20000 ids of 17 bits: the
+// sort 20 us, with a launch for the sums 24).
+template <bool SUM>
 __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
     constexpr int kBins = 1 << kMaxDigit;
     __shared__ uint32_t at[4][kBins];  // per wave: counts, then the next place of a digit
@@ -259,11 +213,27 @@ __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
     // each thread owns four neighbouring bins
     constexpr int kOwn = kBins / 256;
     uint32_t total[kOwn], prior[kOwn], sum = 0;
+    if constexpr (SUM) {
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        const int b = tid * kOwn + i;
-        total[i] = b < bins ? a.totals[b] : 0;
-        prior[i] = b < bins ? a.counts[(int64_t)tile * bins + b] : 0;
+        for (int i = 0; i < kOwn; ++i) total[i] = prior[i] = 0;
+        if (tid * kOwn < bins) {
+#pragma unroll 8
+            for (int t = 0; t < a.tiles; ++t) {
+                const u32x4 c = *reinterpret_cast<const u32x4*>(a.counts + (int64_t)t * bins + tid * kOwn);
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    total[i] += c[i];
+                    prior[i] += t < tile ? c[i] : 0;
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int b = tid * kOwn + i;
+            total[i] = b < bins ? a.totals[b] : 0;
+            prior[i] = b < bins ? a.counts[(int64_t)tile * bins + b] : 0;
+        }
     }
     const int64_t first = (int64_t)tile * kTile + wave * (kTile / 4);
     Pair k[kRounds];
@@ -374,8 +344,8 @@ __device__ __forceinline__ void add_groups(float* sum, int lanes) {
 }
 
 template <class O, int K, class A>
-__device__ __forceinline__ void put_word(const A& a, uint32_t word, int col, const float* sum) {
-    O* d = static_cast<O*>(a.dtable) + word * a.dtable_stride + col;
+__device__ __forceinline__ void put_word(const A& a, uint32_t word, Piece<K> piece, const float* sum) {
+    O* d = static_cast<O*>(a.dtable) + word * a.dtable_stride + piece.col;
     float v[K];
     if (a.accumulate) {
         load_k<O, K>(d, v);
@@ -385,7 +355,7 @@ __device__ __forceinline__ void put_word(const A& a, uint32_t word, int col, con
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] = sum[k] * a.scale;
     }
-    store_k<O, K>(d, v);
+    store_from<O, K>(d, v, piece.skip);
 }
 
 // Eight neighbouring entries of the sorted lists.  WAVE: the same ones in every
@@ -431,12 +401,13 @@ __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
     if constexpr (WAVE) chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     else chunk = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) / a.lanes);
     const int lanes = WAVE ? 64 : a.lanes;
-    const int col = (blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * K;
+    const int nominal = (blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * K;
     const int64_t begin64 = (int64_t)chunk * a.chunk;
-    if (begin64 >= a.n || col >= a.dim) return;
+    if (begin64 >= a.n || nominal >= a.dim) return;
+    const Piece<K> piece(nominal, a.dim);
     const int begin = (int)begin64, end = (int)min((int64_t)a.n, begin64 + a.chunk);
-    const T* rows = static_cast<const T*>(a.dout) + col;
-    float* partial = a.partial + 2 * (int64_t)chunk * a.dim + col;
+    const T* rows = static_cast<const T*>(a.dout) + piece.col;
+    float* partial = a.partial + 2 * (int64_t)chunk * a.dim + piece.col;
     Eight<WAVE> at;
     at.load(a, begin);
     const uint32_t before = begin > 0 ? a.sorted[begin - 1].word : a.vocab, after = end < a.n ? a.sorted[end].word : a.vocab;
@@ -459,8 +430,8 @@ __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
         for (int u = 0; u < 8; ++u) {
             if (i + u >= end) break;
             if (now.key[u] != cur) {
-                if (from_before) store_k<float, K>(partial, sum);
-                else put_word<O, K>(a, cur, col, sum);
+                if (from_before) store_from<float, K>(partial, sum, piece.skip);
+                else put_word<O, K>(a, cur, piece, sum);
                 from_before = false;
                 cur = now.key[u];
                 if (cur >= a.vocab) return;
@@ -472,13 +443,14 @@ __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
         }
         at.settle();
     }
-    if (from_before) store_k<float, K>(partial, sum);
-    else if (after == cur) store_k<float, K>(partial + a.dim, sum);
-    else put_word<O, K>(a, cur, col, sum);
+    if (from_before) store_from<float, K>(partial, sum, piece.skip);
+    else if (after == cur) store_from<float, K>(partial + a.dim, sum, piece.skip);
+    else put_word<O, K>(a, cur, piece, sum);
 }
 
 constexpr int kJoinWaves = 16;
 constexpr int kJoinAlone = 32;  // partial rows that a wave adds up by itself
+constexpr int kJoinLanes = 16;  // lanes to a row of a long run
 
 // The sum of the partial rows i0 .. i1 of the run that begins in `chunk`: the
 // chunk's second row, then the first rows of the chunks after it.
@@ -502,7 +474,10 @@ __device__ __forceinline__ void add_partial(const SumArgs& a, int64_t chunk, int
 // A wave a chunk: where a run begins in the chunk and goes on after it, its
 // partial rows are added up, by the wave or, of a run over more than kJoinAlone
 // chunks (at most one begins in a work-group's), by all waves together, each
-// group of lanes a contiguous part.
+// group of lanes a contiguous part.  A long run's columns are split over the
+// work-groups along z, which a CU by itself would take too long for (262144 ids
+// x 512 fp32, half of them one word: 205 us, 239 without the split); those but
+// the first have nothing else to do.
 template <class O, int K>
 __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
     static_assert(kJoinAlone >= kJoinWaves, "one long run a work-group");
@@ -511,13 +486,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
     __shared__ uint32_t long_word;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
     const int64_t chunk = (int64_t)blockIdx.x * kJoinWaves + wave, begin = chunk * a.chunk, end = begin + a.chunk;
-    const int col = (blockIdx.y * a.lanes + (lane & (a.lanes - 1))) * K, groups = 64 / a.lanes;
     if (threadIdx.x == 0) long_rows = 0;
     int64_t rows = 0;
     uint32_t word = a.vocab;
-    if (end < a.n) {
+    const int64_t far = blockIdx.z ? begin + (int64_t)kJoinAlone * a.chunk : end;
+    if (far < a.n) {
         word = a.sorted[end - 1].word;
-        const uint32_t after = a.sorted[end].word, head = a.sorted[begin].word,
+        const uint32_t after = a.sorted[far].word, head = a.sorted[begin].word,
                        before = begin > 0 ? a.sorted[begin - 1].word : a.vocab;
         if (word < a.vocab && after == word && !(head == word && before == word)) {
             // the chunks after this one that begin with the word: the first 64 looked at one by one, then 64
@@ -541,28 +516,33 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
             long_rows = rows;
             long_word = word;
         }
-    } else if (rows) {
+    } else if (rows && blockIdx.z == 0) {
+        const int groups = 64 / a.lanes, nominal = (blockIdx.y * a.lanes + (lane & (a.lanes - 1))) * K;
+        const Piece<K> piece(nominal, a.dim);
         const int64_t per = (rows + groups - 1) / groups, i0 = min(rows, (lane / a.lanes) * per), i1 = min(rows, i0 + per);
         float sum[K] = {};
-        if (col < a.dim) add_partial<K>(a, chunk, i0, i1, col, sum);
+        if (nominal < a.dim) add_partial<K>(a, chunk, i0, i1, piece.col, sum);
         add_groups<K>(sum, a.lanes);
-        if (lane < a.lanes && col < a.dim) put_word<O, K>(a, word, col, sum);
+        if (lane < a.lanes && nominal < a.dim) put_word<O, K>(a, word, piece, sum);
     }
     __syncthreads();
     if (!long_rows) return;
+    const int lanes = a.lanes / gridDim.z, groups = 64 / lanes;
+    const int nominal = (blockIdx.y * a.lanes + blockIdx.z * lanes + (lane & (lanes - 1))) * K;
+    const Piece<K> piece(nominal, a.dim);
     const int64_t n = long_rows, all = kJoinWaves * groups, per = (n + all - 1) / all;
-    const int64_t i0 = min(n, (threadIdx.x / a.lanes) * per), i1 = min(n, i0 + per);
+    const int64_t i0 = min(n, (threadIdx.x / lanes) * per), i1 = min(n, i0 + per);
     float sum[K] = {};
-    if (col < a.dim) add_partial<K>(a, long_chunk, i0, i1, col, sum);
-    add_groups<K>(sum, a.lanes);
+    if (nominal < a.dim) add_partial<K>(a, long_chunk, i0, i1, piece.col, sum);
+    add_groups<K>(sum, lanes);
 #pragma unroll
     for (int k = 0; k < K; ++k) part[wave][lane][k] = sum[k];
     __syncthreads();
-    if ((int)threadIdx.x >= a.lanes || col >= a.dim) return;
+    if ((int)threadIdx.x >= lanes || nominal >= a.dim) return;
     for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
         for (int k = 0; k < K; ++k) sum[k] += part[w][lane][k];
-    put_word<O, K>(a, long_word, col, sum);
+    put_word<O, K>(a, long_word, piece, sum);
 }
 
 // ---- a few ids: one launch, without a sort
@@ -649,10 +629,11 @@ __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
     const int i0 = min(n, (tid / a.lanes) * per), i1 = min(n, i0 + per);
     const int used = (n * a.lanes + 64 * per - 1) / (64 * per);         // waves with rows
     for (int t = 0; t < a.tiles; ++t) {
-        const int col = (t * a.lanes + (tid & (a.lanes - 1))) * K;
+        const int nominal = (t * a.lanes + (tid & (a.lanes - 1))) * K;
+        const Piece<K> piece(nominal, a.dim);
         float sum[K] = {};
-        if (col < a.dim) {
-            const T* rows = static_cast<const T*>(a.dout) + col;
+        if (nominal < a.dim) {
+            const T* rows = static_cast<const T*>(a.dout) + piece.col;
             for (int i = i0; i < i1; i += 8) {
                 float v[8][K];
 #pragma unroll
@@ -676,7 +657,7 @@ __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
 #pragma unroll
                     for (int k = 0; k < K; ++k) sum[k] += part[w][lane][k];
         }
-        if (tid < a.lanes && col < a.dim) put_word<O, K>(a, word, col, sum);
+        if (tid < a.lanes && nominal < a.dim) put_word<O, K>(a, word, piece, sum);
     }
 }
 
@@ -714,14 +695,19 @@ edb_status launched(const char* who) {
     return EDB_OK;
 }
 
-// Elements a lane takes of a row of `dim`.
-int piece_of(int dim) { return dim % 8 == 0 ? 8 : dim % 4 == 0 ? 4 : 1; }
+// Elements that a lane of the gradient's kernels takes of a row.  Short rows by
+// four, since a row's lanes are a power of two and more of them are used
+// (262144 ids of 64 fp32: 50 us, by eight 63; 150: 75 and 85); from 256 on by
+// eight, which asks for more bytes at a time (300 bf16: 98 us, by four 115).
+int piece_of(int dim) { return dim >= 256 ? 8 : dim >= 4 ? 4 : 1; }
 
 template <class T, class O>
 void launch_embed(const EmbedArgs& a, hipStream_t st) {
-    const int k = piece_of(a.dim);
-    const dim3 grid((unsigned)(((int64_t)a.n * (a.dim / k) + 255) / 256));
-    if (k == 8) embed_kernel<T, O, 8><<<grid, 256, 0, st>>>(a);
+    // 16 bytes of the result a lane, so that a wave writes whole lines
+    constexpr int kWhole = Elem<O>::kVec;
+    const int k = a.dim >= kWhole ? kWhole : a.dim >= 4 ? 4 : 1;
+    const dim3 grid((unsigned)(((int64_t)a.n * ((a.dim + k - 1) / k) + 255) / 256));
+    if (k == kWhole) embed_kernel<T, O, kWhole><<<grid, 256, 0, st>>>(a);
     else if (k == 4) embed_kernel<T, O, 4><<<grid, 256, 0, st>>>(a);
     else embed_kernel<T, O, 1><<<grid, 256, 0, st>>>(a);
 }
@@ -736,7 +722,7 @@ struct GradPlan {
 GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
     GradPlan g{};
     g.piece = piece_of(dim);
-    const int pieces = dim / g.piece;
+    const int pieces = (dim + g.piece - 1) / g.piece;
     g.lanes = 1;
     while (g.lanes < 64 && g.lanes < pieces) g.lanes *= 2;
     g.tiles_y = (pieces + g.lanes - 1) / g.lanes;
@@ -753,19 +739,14 @@ GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
         return here;
     };
     const int64_t list = ((int64_t)n + 7) / 8 * 8 * (int64_t)sizeof(Pair);
-    if (n <= kBlockSort) {
-        g.passes = 0;
-        g.digit = bits;
-        g.sorted[0] = take(list);
-    } else {
-        g.passes = (bits + kMaxDigit - 1) / kMaxDigit;
-        g.digit = (bits + g.passes - 1) / g.passes;
-        g.sort_tiles = (int32_t)(((int64_t)n + kTile - 1) / kTile);
-        g.sorted[0] = take(list);
-        g.sorted[1] = take(list);
-        g.counts = take((int64_t)g.sort_tiles * 4 << g.digit);
-        g.totals = take(INT64_C(4) << g.digit);
-    }
+    g.passes = (bits + kMaxDigit - 1) / kMaxDigit;
+    g.digit = (bits + g.passes - 1) / g.passes;
+    if (g.digit < 2) g.digit = 2;            // the scatter reads the counts by fours
+    g.sort_tiles = (int32_t)(((int64_t)n + kTile - 1) / kTile);
+    g.sorted[0] = take(list);
+    g.sorted[1] = take(list);
+    g.counts = take((int64_t)g.sort_tiles * 4 << g.digit);
+    g.totals = take(INT64_C(4) << g.digit);
     g.partial = take((int64_t)g.chunks * 2 * dim * 4);
     g.bytes = n > kSmall ? at : 0;
     return g;
@@ -790,8 +771,10 @@ void launch_sums(const GradPlan& g, const SumArgs& a, hipStream_t st) {
     if (grid.x == 0) return;
     if (g.lanes == 64) sum_chunks<T, O, K, true><<<grid, 256, 0, st>>>(a);
     else sum_chunks<T, O, K, false><<<grid, 256, 0, st>>>(a);
-    if (g.chunks > 1)
-        join_chunks<O, K><<<dim3((g.chunks + kJoinWaves - 1) / kJoinWaves, g.tiles_y), 64 * kJoinWaves, 0, st>>>(a);
+    if (g.chunks > 1) {
+        const int parts = g.chunks > kJoinAlone && a.lanes > kJoinLanes ? a.lanes / kJoinLanes : 1;
+        join_chunks<O, K><<<dim3((g.chunks + kJoinWaves - 1) / kJoinWaves, g.tiles_y, parts), 64 * kJoinWaves, 0, st>>>(a);
+    }
 }
 
 template <class T, class O>
@@ -878,26 +861,23 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
     s.n = n;
     s.vocab = (uint32_t)vocab;
     int last = 0;
-    if (g.passes == 0) {
-        s.ids = ids;
-        s.out = sorted(0);
-        s.bits = g.digit;
-        sort_block<<<1, 1024, 0, st>>>(s);
-    } else {
-        s.tiles = g.sort_tiles;
-        s.counts = reinterpret_cast<uint32_t*>(ws + g.counts);
-        s.totals = reinterpret_cast<uint32_t*>(ws + g.totals);
-        s.bits = g.digit;
-        for (int p = 0; p < g.passes; ++p) {
-            s.ids = p ? nullptr : ids;
-            s.in = sorted((p + 1) & 1);
-            s.out = sorted(p & 1);
-            s.shift = p * g.digit;
-            last = p & 1;
-            sort_count<<<g.sort_tiles, 256, 0, st>>>(s);
-            sort_scan<<<((1 << g.digit) + kScanBins - 1) / kScanBins, 256, 0, st>>>(s);
-            sort_scatter<<<g.sort_tiles, 256, 0, st>>>(s);
+    s.tiles = g.sort_tiles;
+    s.counts = reinterpret_cast<uint32_t*>(ws + g.counts);
+    s.totals = reinterpret_cast<uint32_t*>(ws + g.totals);
+    s.bits = g.digit;
+    for (int p = 0; p < g.passes; ++p) {
+        s.ids = p ? nullptr : ids;
+        s.in = sorted((p + 1) & 1);
+        s.out = sorted(p & 1);
+        s.shift = p * g.digit;
+        last = p & 1;
+        sort_count<<<g.sort_tiles, 256, 0, st>>>(s);
+        if (g.sort_tiles <= kSumTiles) {
+            sort_scatter<true><<<g.sort_tiles, 256, 0, st>>>(s);
+            continue;
         }
+        sort_scan<<<((1 << g.digit) + kScanBins - 1) / kScanBins, 256, 0, st>>>(s);
+        sort_scatter<false><<<g.sort_tiles, 256, 0, st>>>(s);
     }
     const int sum_groups = (int)(((int64_t)g.chunks * g.lanes + 255) / 256);
     const SumArgs a{sorted(last), n, g.chunk, (uint32_t)vocab, dim, g.lanes, dout, dout_stride, scale,
