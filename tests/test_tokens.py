@@ -93,6 +93,27 @@ def test_embed(n, V, E, table, out, pad, shift):
 
 
 @gpu
+@pytest.mark.parametrize("table,out", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("E", [2, 3, 4, 5, 6, 9, 12, 15, 33, 301])
+def test_embed_widths(E, table, out):
+    """Every way that a row can end, there and in the gradient's few rows."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(E)
+    n, V = 130, 60
+    w = torch.randn((V, E), generator=g, device="cuda").to(table)
+    ids = _some_ids(n, V, g, False)
+    dst, mem = _view(torch.zeros((n, E), dtype=out, device="cuda"), 1, 1)
+    before = mem.clone()
+    tokens.embed(ids, w, -0.3, out=dst)
+    assert torch.equal(dst, (w[ids.long()].float() * -0.3).to(out))
+    dst.zero_()
+    assert torch.equal(mem.view(torch.uint8), before.view(torch.uint8))
+    dout = torch.randn((n, E), generator=g, device="cuda").to(table)
+    old = torch.randn((V, E), generator=g, device="cuda").to(out)
+    _grad_check(ids, dout, V, 2.0, out, tokens.embed_grad(ids, dout, V, 2.0, out=old.clone(), accumulate=True), old)
+
+
+@gpu
 def test_embed_empty_and_values():
     from paper_2302_03851_amd import tokens
     w = torch.tensor([[1.0, -INF], [float("nan"), 3.0]], device="cuda")
@@ -155,6 +176,25 @@ def test_embed_grad(n, V, E, src, dst, accumulate):
     k = _grad_check(ids, dout, V, -1.3, dst, runs[0], old if accumulate else None)
     if accumulate:
         assert torch.equal(runs[0][k == 0], old[k == 0])
+
+
+@gpu
+@pytest.mark.parametrize("src,dst", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n", [4096, 4097, 65536, 65537, 131073])
+@pytest.mark.parametrize("E", [3, 6, 255, 300])
+def test_embed_grad_sizes(n, E, src, dst):
+    """At the sizes where the sort and the columns' split change, a third of the ids one word."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(n + E)
+    V = 3001
+    ids = _some_ids(n, V, g, True)
+    ids[1::3] = 77
+    dout = torch.randn((n, E), generator=g, device="cuda").to(src)
+    old = torch.randn((V, E), generator=g, device="cuda").to(dst)
+    got = [tokens.embed_grad(ids, dout, V, 0.5, out=old.clone(), accumulate=True) for _ in range(2)]
+    assert torch.equal(got[0].view(torch.uint8), got[1].view(torch.uint8))
+    _grad_check(ids, dout, V, 0.5, dst, got[0], old)
+    _grad_check(ids, dout, V, 0.5, dst, tokens.embed_grad(ids, dout, V, 0.5, dtype=dst))
 
 
 @gpu
@@ -323,6 +363,36 @@ def test_logprobs_split_rows(n, V, dtype, top):
     from paper_2302_03851_amd import tokens
     x, _ = _view(_rows("plain", n, V, dtype, _gen(V)), 5, 3)
     _check_logprobs(x, None, 1.3, top, tokens.logprobs(x, None, 1.3, top))
+
+
+@gpu
+@pytest.mark.parametrize("n,V,dtype", [(2048, 2049, BF16), (2100, 8191, BF16), (2049, 1025, F32), (511, 16385, BF16),
+                                       (300, 20001, F32), (260, 140001, BF16), (255, 65537, BF16), (256, 65537, F32), (40, 65536, F32)])
+@pytest.mark.parametrize("kind,top", [("masked", 0), ("masked", 31), ("ties", 32), ("broken", 33), ("plain", 63)])
+def test_logprobs_shapes(n, V, dtype, kind, top):
+    """Every number of waves to a row, at every length of the list."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(n + top)
+    x = _rows(kind, n, V, dtype, g)
+    ids = _given(n, V, g)
+    _check_logprobs(x, ids, 1.1, top, tokens.logprobs(x, ids, 1.1, top))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["plain", "masked"])
+def test_logprobs_longest(dtype, kind):
+    """More parts of one row than a wave has lanes."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(11)
+    V = 10_000_003
+    x = _rows(kind, 2, V, dtype, g)[1 if kind == "plain" else 0:][:1]
+    ids = torch.tensor([V - 1], dtype=torch.int32, device="cuda")
+    r = tokens.logprobs(x, ids, 1.0, 64)
+    _check_logprobs(x, ids, 1.0, 64, r)
+    one = torch.ones(1, device="cuda")
+    ref, tol = _grad_reference(x, ids, 1.0, one, one)
+    _close(tokens.logprobs_grad(x, ids, r.stats, r.entropy, one, one), ref, tol + 1.01 * _half_ulp(ref, dtype) + 1e-38)
 
 
 @gpu
@@ -522,6 +592,56 @@ def test_distill(n, V, dtype, kind, teacher, K, T):
     assert torch.equal(x.view(torch.uint8), full.dlogits.view(torch.uint8))
 
 
+def _check_distill(x, ids, u, T, weight, got):
+    ww = torch.ones(x.shape[0], device="cuda") if weight is None else weight
+    loss, d, tol_loss, tol_d = _distill_reference(x, ids, u, T, ww)
+    _close(got.loss, loss, tol_loss)
+    _close(got.dlogits, d, tol_d + 1.01 * _half_ulp(d, x.dtype) + 1e-38)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vectors", [64, 512, 1024, 2048, 4096, 8192, 16384])
+@pytest.mark.parametrize("more", [-1, 0, 1])
+def test_distill_row_lengths(dtype, vectors, more):
+    """About the lengths (in vectors of 16 bytes) at which a row is held by more threads or in more registers."""
+    from paper_2302_03851_amd import tokens
+    n, V = 5, vectors * (4 if dtype == F32 else 8) + more
+    g = _gen(V)
+    x = _rows("masked", n, V, dtype, g)
+    ids, u = _teacher(n, V, 7, g, "equal")
+    ids[:, 0] = V - 1
+    got = tokens.distill(x, ids, u, 1.2)
+    _check_distill(x, ids, u, 1.2, None, got)
+    tokens.distill(x, ids, u, 1.2, out=tokens.Distilled(got.loss, x))
+    assert torch.equal(x.view(torch.uint8), got.dlogits.view(torch.uint8))
+
+
+@gpu
+@pytest.mark.parametrize("n,V,dtype", [(700, 66001, BF16), (600, 33003, F32), (257, 131072, BF16), (1100, 33000, F32)])
+@pytest.mark.parametrize("kind", ["masked", "broken"])
+def test_distill_many_long_rows(n, V, dtype, kind):
+    """More long rows than work-groups take at a time, rows without weight and without a teacher among them."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = _rows(kind, n, V, dtype, g)
+    ids, u = _teacher(n, V, 20, g, "short")
+    w = torch.randn(n, generator=g, device="cuda")
+    w[torch.rand(n, generator=g, device="cuda") < 0.4] = 0
+    w[200:520] = 0
+    w[-1] = 0
+    full = tokens.distill(x, ids, u, 0.9, w)
+    for i in range(0, n, 100):       # the reference a few rows at a time: it is in 64 bits
+        part = tokens.Distilled(full.loss[i:i + 100], full.dlogits[i:i + 100])
+        _check_distill(x[i:i + 100], ids[i:i + 100], u[i:i + 100], 0.9, w[i:i + 100], part)
+    alone = tokens.distill(x, ids, u, 0.9, w, grad=False)
+    assert torch.equal(alone.loss.view(torch.uint8), full.loss.view(torch.uint8))
+    xv, _ = _view(x, 3, 1)
+    got = tokens.distill(xv, ids, u, 0.9, w, out=tokens.Distilled(alone.loss, xv))
+    assert torch.equal(got.loss.view(torch.uint8), full.loss.view(torch.uint8))
+    assert torch.equal(xv.contiguous().view(torch.uint8), full.dlogits.view(torch.uint8))
+
+
 @gpu
 def test_distill_differences():
     """Central differences of the 64-bit loss (as for the log probabilities)."""
@@ -575,6 +695,23 @@ def _everything(seed):
     return go
 
 
+def _larger(seed):
+    """As _everything, for the paths of many ids and of many long rows."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(seed)
+    V, n = 66001, 300
+    ids = _some_ids(70000, V, g, True)
+    dy = torch.randn((70000, 36), generator=g, device="cuda").to(BF16)
+    x = _rows("masked", n, V, BF16, g)
+    q = _teacher(n, V, 12, g, "short")
+    w = torch.randn(n, generator=g, device="cuda")
+
+    def go():
+        return [tokens.embed_grad(ids, dy, V), *tokens.distill(x, *q, 1.4, w), *tokens.logprobs(x, None, 1.0, 40)[1:]]
+
+    return go
+
+
 def _same(a, b):
     return all(torch.equal(s.view(torch.uint8), t.view(torch.uint8)) for s, t in zip(a, b))
 
@@ -596,9 +733,10 @@ def test_tokens_streams():
 
 
 @gpu
-def test_tokens_captured():
+@pytest.mark.parametrize("calls", [_everything, _larger])
+def test_tokens_captured(calls):
     """All calls in one HIP graph, replayed between eager calls."""
-    go = _everything(7)
+    go = calls(7)
     ref = go()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
