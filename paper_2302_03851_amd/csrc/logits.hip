@@ -47,22 +47,43 @@ template <int D>
 __device__ __forceinline__ float from_lane_xor(float v) {
     return __builtin_bit_cast(float, from_lane_xor<D>(__builtin_bit_cast(uint32_t, v)));
 }
+// Both rows of 16 lanes, or halves of the wave, of which the lane is in one: an
+// exchange of rows between two copies, in a few cycles.  (A shuffle through LDS
+// takes over a hundred, but fewer instructions where one side is wanted only.)
+template <class T>
+struct Both {
+    T a, b;
+};
+template <class T>
+__device__ __forceinline__ Both<T> both_rows(T v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return {__builtin_bit_cast(T, (uint32_t)p[0]), __builtin_bit_cast(T, (uint32_t)p[1])};
+}
+template <class T>
+__device__ __forceinline__ Both<T> both_halves(T v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return {__builtin_bit_cast(T, (uint32_t)p[0]), __builtin_bit_cast(T, (uint32_t)p[1])};
+}
 // Over the wave, in every lane; sums in the same order in every run.
 __device__ __forceinline__ float wave_max(float v) {
     v = fmaxf(v, from_lane_xor<1>(v));
     v = fmaxf(v, from_lane_xor<2>(v));
     v = fmaxf(v, from_lane_xor<7>(v));
     v = fmaxf(v, from_lane_xor<8>(v));
-    v = fmaxf(v, from_lane_xor<16>(v));
-    return fmaxf(v, from_lane_xor<32>(v));
+    const auto rows = both_rows(v);
+    const auto halves = both_halves(fmaxf(rows.a, rows.b));
+    return fmaxf(halves.a, halves.b);
 }
 __device__ __forceinline__ float wave_sum(float v) {
     v += from_lane_xor<1>(v);
     v += from_lane_xor<2>(v);
     v += from_lane_xor<7>(v);
     v += from_lane_xor<8>(v);
-    v += from_lane_xor<16>(v);
-    return v + from_lane_xor<32>(v);
+    const auto rows = both_rows(v);
+    const auto halves = both_halves(rows.a + rows.b);
+    return halves.a + halves.b;
 }
 
 // ---- rows of bf16 at odd addresses
@@ -335,8 +356,9 @@ __device__ __forceinline__ uint32_t order_with(uint32_t k, int lane) {
     return (lane & kHigh) == 0 ? max(o, k) : min(o, k);
 }
 
+// `first`: the lanes (the same number everywhere) from which on all keys are 0.
 template <class K>
-__device__ __forceinline__ K sort_down(K k, int lane) {
+__device__ __forceinline__ K sort_down(K k, int lane, int first = 64) {
     k = order_with<1>(k, lane);
     k = order_with<3>(k, lane);
     k = order_with<1>(k, lane);
@@ -347,11 +369,13 @@ __device__ __forceinline__ K sort_down(K k, int lane) {
     k = order_with<4>(k, lane);
     k = order_with<2>(k, lane);
     k = order_with<1>(k, lane);
+    if (first <= 16) return k;
     k = order_with<31>(k, lane);
     k = order_with<8>(k, lane);
     k = order_with<4>(k, lane);
     k = order_with<2>(k, lane);
     k = order_with<1>(k, lane);
+    if (first <= 32) return k;
     k = order_with<63>(k, lane);
     k = order_with<16>(k, lane);
     k = order_with<8>(k, lane);
@@ -360,17 +384,28 @@ __device__ __forceinline__ K sort_down(K k, int lane) {
     return order_with<1>(k, lane);
 }
 
-// The best entries among those offered to a wave, sorted, lane i holding the
-// i-th.  Offered entries wait in LDS until there are 64 or no more come.
+// The best entries among those pushed by a wave, sorted, lane i holding the i-th.
+// Pushed entries wait in LDS until `sort` puts them into the list.  Sorting is
+// a few hundred instructions, so it stands where a loop comes by, not behind
+// every push.
+constexpr int kWait = 320;
+
 struct Best {
     Key key = 0;
     int waiting = 0;
     uint32_t bound;  // order of a value that at least `top` entries reach
 
     // A bound from the orders of values of different entries, four a lane (0 for
-    // none): for short lists the top-th largest of the lanes' own largest, else
+    // none): for short lists the top-th largest of the lanes' own largest (for very
+    // short ones of four lanes' each, which takes half the sorting), else
     // the top-th largest of all, its lower 16 bits left open.
     __device__ __forceinline__ static uint32_t bound_of(const uint32_t (&u)[4], int top, int lane) {
+        if (top <= 8) {  // of 16 values, each the largest of four lanes
+            const auto rows = both_rows(max(max(u[0], u[1]), max(u[2], u[3])));
+            const auto halves = both_halves(max(rows.a, rows.b));
+            const uint32_t all = max(halves.a, halves.b);
+            return (uint32_t)__builtin_amdgcn_readlane((int)sort_down(all, lane, 16), top - 1);
+        }
         if (top <= 32)
             return (uint32_t)__builtin_amdgcn_readlane((int)sort_down(max(max(u[0], u[1]), max(u[2], u[3])), lane), top - 1);
         uint32_t b = 0;
@@ -386,31 +421,31 @@ struct Best {
     }
     // the least value that reaches the bound
     __device__ __forceinline__ float bound_value() const { return bound ? key_value((Key)bound << 32) : -kInf; }
-    __device__ __forceinline__ void take(Key* wait, int top, int lane) {
-        Key k = sort_down(lane < waiting ? wait[lane] : 0, lane);
-        if (key_at(0)) {  // the larger ones of the list and the mirrored newcomers: a bitonic sequence
-            const Key o = (Key)(uint32_t)__shfl_xor((int)(k >> 32), 63) << 32 | (uint32_t)__shfl_xor((int)k, 63);
-            k = merge_down(o > key ? o : key, lane);
-        }
-        key = k;
-        waiting = 0;
-        const uint32_t last = (uint32_t)(key_at(top - 1) >> 32);
-        bound = last > bound ? last : bound;
-    }
     __device__ __forceinline__ Key key_at(int lane) const {  // lane: the same in every lane
         return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 |
                (uint32_t)__builtin_amdgcn_readlane((int)key, lane);
     }
-    // one entry a lane, 0 for none
-    __device__ __forceinline__ void offer(Key k, Key* wait, int top, int lane) {
-        uint64_t who = __ballot(k && (uint32_t)(k >> 32) >= bound);
+    // One entry a lane, 0 for none.  Past kWait entries they are only counted.
+    __device__ __forceinline__ void push(Key k, Key* wait, int lane) {
+        const uint64_t who = __ballot(k && (uint32_t)(k >> 32) >= bound);
         if (!who) return;
-        if (waiting + __popcll(who) > 64) {
-            take(wait, top, lane);
-            who = __ballot(k && (uint32_t)(k >> 32) >= bound);
-        }
-        if ((who >> lane) & 1) wait[waiting + __popcll(who & ((1ull << lane) - 1))] = k;
+        const int at = waiting + __popcll(who & ((1ull << lane) - 1));
+        if (((who >> lane) & 1) && at < kWait) wait[at] = k;
         waiting += __popcll(who);
+    }
+    __device__ __forceinline__ void sort(const Key* wait, int top, int lane) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int i = 0; i < waiting; i += 64) {
+            Key k = sort_down(i + lane < waiting ? wait[i + lane] : 0, lane, waiting - i);
+            if (key_at(0)) {  // the larger ones of the list and the mirrored newcomers: a bitonic sequence
+                const Key o = (Key)from_lane_xor<63>((uint32_t)(k >> 32)) << 32 | from_lane_xor<63>((uint32_t)k);
+                k = merge_down(o > key ? o : key, lane);
+            }
+            key = k;
+        }
+        waiting = 0;
+        bound = max(bound, (uint32_t)(key_at(top - 1) >> 32));
         __builtin_amdgcn_wave_barrier();
     }
 };
@@ -476,11 +511,11 @@ constexpr int kLoads = 2;  // 16-byte loads of a thread in flight, beside as man
 // before it), so at the end one wave looks for those groups and reads them again.
 // (W: row_waves)
 template <class T, bool TOP, int W>
-__global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
     constexpr int N = Elem<T>::kVec, kStep = kLoads * W * 64 * N;
     extern __shared__ float group_max[];
     __shared__ float part_m[W], part_s[W], part_t[W];
-    __shared__ Key wait[64];
+    __shared__ Key wait[TOP ? kWait : 1];
     const int64_t row = blockIdx.x / a.parts;
     const int which = blockIdx.x - (int)row * a.parts;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -558,7 +593,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     }
     Best best;
     if constexpr (TOP) {
-        constexpr int kGroup = 4 * N, kAtOnce = 64 / kGroup;
+        constexpr int kGroup = 4 * N;
         const int n = (end - begin + kGroup - 1) / kGroup;
         float own[4] = {-kInf, -kInf, -kInf, -kInf};
         for (int i0 = 0; i0 < n; i0 += 256)
@@ -576,33 +611,74 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
             float w[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) w[u] = i0 + u * 64 < n ? group_max[i0 + u * 64] : -kInf;
-            if (__ballot(largest<4>(w) >= groups.bound_value()) == 0) continue;  // mostly none of 256 groups
+            if (__ballot(largest<4>(w) >= groups.bound_value()) != 0) {  // mostly none of 256 groups
 #pragma unroll
-            for (int u = 0; u < 4; ++u) groups.offer(key_of(w[u], i0 + u * 64), wait, a.top, lane);
+                for (int u = 0; u < 4; ++u) groups.push(key_of(w[u], i0 + u * 64), wait, lane);
+            }
+            if (groups.waiting > 64 || (groups.key_at(0) && i0 - lane + 256 >= n)) groups.sort(wait, a.top, lane);
         }
         // up to 64 groups reach the bound: all of them are read again; more: the best ones
         int there = groups.waiting;
+        __builtin_amdgcn_wave_barrier();
         int mine = lane < there ? key_index(wait[lane]) : 0;
         if (groups.key_at(0)) {
-            groups.take(wait, a.top, lane);
             there = __popcll(__ballot(lane < a.top && groups.key));
             mine = key_index(groups.key);
         }
         __builtin_amdgcn_wave_barrier();
         best.bound = groups.bound;
-        for (int g0 = 0; g0 < there; g0 += 4 * kAtOnce) {
-            float w[4];
-            int j[4];
+        // 16 groups a load, all of them on their way before the first is looked at
+        constexpr uint32_t kNone = N == 4 ? 0xff800000u : 0xff80ff80u;  // -inf
+        u32x4 again[4];
+        int at[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int g = u * 16 + lane / 4;
+            at[u] = begin + __shfl(mine, g) * kGroup + lane % 4 * N;
+            again[u] = u32x4{kNone, kNone, kNone, kNone};
+            if (g < there && at[u] < end) {
+                if (at[u] + N <= end) {
+                    again[u] = Elem<T>::load(x + at[u]);
+                } else {
+                    float w[N];
+#pragma unroll
+                    for (int k = 0; k < N; ++k) w[k] = at[u] + k < end ? Elem<T>::get(x + at[u] + k) : -kInf;
+                    again[u] = Elem<T>::pack(w);
+                }
+            }
+        }
+        if (there > 32) {  // a closer bound from the loads' own largest values: fewer entries to sort
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int g = g0 + u * kAtOnce + lane / kGroup;
-                j[u] = begin + __shfl(mine, g & 63) * kGroup + lane % kGroup;
-                w[u] = g < there && j[u] < end ? Elem<T>::get(x + j[u]) : -kInf;
+                float w[N];
+                Elem<T>::unpack(again[u], w);
+                const float most = largest<N>(w);
+                order[u] = most > -kInf ? ordered(most) : 0;
+                asm volatile("" : "+v"(again[u]));  // unpacked anew below: the values would take too many registers
             }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) best.offer(key_of(w[u], j[u]), wait, a.top, lane);
+            best.bound = max(best.bound, Best::bound_of(order, a.top, lane));
         }
-        best.take(wait, a.top, lane);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (u * 16 < there) {
+                float w[N];
+                Elem<T>::unpack(again[u], w);
+#pragma unroll
+                for (int k = 0; k < N; ++k) best.push(key_of(w[k], at[u] + k), wait, lane);
+            }
+        const bool many = best.waiting > kWait;  // equal ones: 64 at a time
+        if (many) best.waiting = 0;
+        int i0 = 0;
+        do {
+            if (many) {
+                const int g = i0 + lane / kGroup, j = begin + __shfl(mine, g & 63) * kGroup + lane % kGroup;
+                best.push(key_of(g < there && j < end ? Elem<T>::get(x + j) : -kInf, j), wait, lane);
+                i0 += 64 / kGroup;
+            } else {
+                i0 = there;
+            }
+            if (i0 >= there || best.waiting > kWait - 64) best.sort(wait, a.top, lane);
+        } while (i0 < there);
     }
     if (a.parts == 1) {
         put_row(a, row, st, best.key, given, lane);
@@ -632,7 +708,7 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
     }
     Best best;
     if (a.top) {
-        __shared__ Key wait[64];
+        __shared__ Key wait[kWait];
         const Key* keys = a.part_keys + row * a.parts * a.top;
         const int n = a.parts * a.top;
         // bounds: every part's last entry, and the lanes' own largest ones
@@ -646,8 +722,15 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
         for (int i = lane; i < a.parts; i += 64) last = max(last, (uint32_t)(keys[(i + 1) * a.top - 1] >> 32));
         for (int d = 1; d < 64; d <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, d));
         best.bound = max(last, Best::bound_of(own, a.top, lane));
-        for (int i = lane; i - lane < n; i += 64) best.offer(i < n ? keys[i] : 0, wait, a.top, lane);
-        best.take(wait, a.top, lane);
+#pragma unroll 1
+        for (int i0 = lane; i0 - lane < n; i0 += 256) {
+            Key k[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) k[u] = i0 + u * 64 < n ? keys[i0 + u * 64] : 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) best.push(k[u], wait, lane);
+            if (best.waiting > 64 || i0 - lane + 256 >= n) best.sort(wait, a.top, lane);
+        }
     }
     put_row(a, row, st, best.key, given, lane);
 }
@@ -1173,9 +1256,9 @@ struct RowPlan {
 // Rows from 2^16 logits on are split into parts, joined by a second launch, where
 // there are few of them; and any row whose group maxima would pass 32 KB of LDS.
 RowPlan row_plan(int32_t n, int32_t vocab, int32_t top) {
-    constexpr int32_t kSplit = 65536, kMost = 131072, kLeast = 8192, kFill = 512;
+    constexpr int32_t kSplit = 32768, kMost = 131072, kLeast = 4096, kFill = 512;
     int64_t parts = 1;
-    if (n > 0 && n < kFill / 2 && vocab >= kSplit) {
+    if (n > 0 && vocab >= kSplit && n < (vocab < 2 * kSplit ? kFill / 4 : kFill / 2)) {
         parts = kFill / n;
         if (parts > vocab / kLeast) parts = vocab / kLeast;
     }
