@@ -732,12 +732,14 @@ edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32_t n, int32
  *   loss     float[n] (without the weight)
  *   dlogits  the logits' dtype, or NULL (the loss alone); it may be the logits
  *            themselves (same address and stride)
- * A row of weight 0 or without a listed token is not read: loss 0, zero
- * gradient.  A listed token that the student masks out (-inf) makes the loss
+ * A row of weight 0 or without a listed token is left out, whatever its
+ * logits: loss 0, zero gradient.  A listed token that the student masks out (-inf) makes the loss
  * +inf; a row that the student masks out whole has a zero gradient besides. */
+edb_status edb_distill_bytes(int32_t n, int32_t vocab, int32_t dtype, int32_t top, int64_t* bytes);
 edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
                        const int32_t* top_ids, const float* top_logits, int32_t top, float temperature,
-                       const float* weight, float* loss, void* dlogits, int64_t dlogits_stride, void* stream);
+                       const float* weight, float* loss, void* dlogits, int64_t dlogits_stride, void* workspace,
+                       int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

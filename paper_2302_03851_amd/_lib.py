@@ -50,7 +50,7 @@ EXPORTS = [
     "edb_forward_noalloc",
     "edb_split_phase_bytes", "edb_split_phase", "edb_probe_mfma", "edb_probe_copy",
     "edb_embed", "edb_embed_grad_bytes", "edb_embed_grad",
-    "edb_logprobs_bytes", "edb_logprobs", "edb_logprobs_grad", "edb_distill",
+    "edb_logprobs_bytes", "edb_logprobs", "edb_logprobs_grad", "edb_distill_bytes", "edb_distill",
 ]
 
 
@@ -172,8 +172,9 @@ def load():
                                      vp, vp, vp, vp, C.c_int64, vp]),
         "edb_logprobs_grad": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, C.c_float, vp, vp, vp,
                                           vp, vp, C.c_int64, vp]),
+        "edb_distill_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, P(C.c_int64)]),
         "edb_distill": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, vp, C.c_int32, C.c_float, vp,
-                                    vp, vp, C.c_int64, vp]),
+                                    vp, vp, C.c_int64, vp, C.c_int64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

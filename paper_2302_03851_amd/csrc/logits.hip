@@ -689,6 +689,17 @@ __global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
     }
 }
 
+// The statistics of a row's parts joined, in every lane of the wave.
+__device__ __forceinline__ Stats join_parts(const Stats* part, int parts, float c, int lane) {
+    Stats st = lane < parts ? part[lane] : Stats::none();
+    st.join_wave(c);
+    for (int i0 = 64; i0 < parts; i0 += 63) {  // lane 63 carries the parts before these
+        if (lane != 63) st = i0 + lane < parts ? part[i0 + lane] : Stats::none();
+        st.join_wave(c);
+    }
+    return st;
+}
+
 // Joins the parts of split rows: a wave a row.
 template <class T>
 __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
@@ -700,12 +711,7 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
         return;
     }
     const float given = a.ids ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.stride + id) : 0.f;
-    Stats st = lane < a.parts ? a.part_stats[row * a.parts + lane] : Stats::none();
-    st.join_wave(a.c);
-    for (int i0 = 64; i0 < a.parts; i0 += 63) {  // lane 63 carries the parts before these
-        if (lane != 63) st = i0 + lane < a.parts ? a.part_stats[row * a.parts + i0 + lane] : Stats::none();
-        st.join_wave(a.c);
-    }
+    const Stats st = join_parts(a.part_stats + row * a.parts, a.parts, a.c, lane);
     Best best;
     if (a.top) {
         __shared__ Key wait[kWait];
@@ -844,6 +850,9 @@ struct DistillArgs {
     float* loss;
     void* out;
     int64_t out_stride;
+    int32_t part, parts;  // a split row: `parts` parts of `part` logits
+    Stats* part_stats;    // [n][parts]
+    float* listed;        // [n][top]: the student's logits at the listed tokens
 };
 
 // The teacher's list of a row as masses: one entry a thread (the first
@@ -1111,17 +1120,53 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
 }
 
 // Longer rows, read twice: a pass for the student's statistics, one for the gradient.
-constexpr int kLongWaves = 16;
+// 2^y of a logit, y = x c - r(m) (see Stats).
+__device__ __forceinline__ float mass_of(float v, float c, float ref) {
+    const float r = ref * c;
+    return exp2_hw(Stats::plain(r) ? __builtin_fmaf(v, c, -r) : (v - ref) * c);
+}
+
 template <class T>
-__global__ __launch_bounds__(64 * kLongWaves) void distill_long(DistillArgs a) {
-    constexpr int N = Elem<T>::kVec, kThreads = 64 * kLongWaves;
+__device__ __forceinline__ void load_up_to(const T* x, int j, int end, float (&v)[Elem<T>::kVec]) {
+    constexpr int N = Elem<T>::kVec;
+    if (j + N <= end) {
+        Elem<T>::unpack(Elem<T>::load(x + j), v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = j + i < end ? Elem<T>::get(x + j + i) : -kInf;
+    }
+}
+
+// d_j = 2^y_j ks for begin <= j < end, by all threads of the work-group.
+template <class T>
+__device__ __forceinline__ void put_masses(const T* x, T* d, int begin, int end, int threads, float c, float ref, float ks) {
+    constexpr int N = Elem<T>::kVec;
+    for (int j = begin + (int)threadIdx.x * N; j < end; j += threads * N) {
+        float v[N];
+        load_up_to<T>(x, j, end, v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = mass_of(v[i], c, ref) * ks;
+        if (j + N <= end) {
+            Elem<T>::store_nt(d + j, Elem<T>::pack(v));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (j + i < end) Elem<T>::put(d + j + i, v[i]);
+        }
+    }
+}
+
+constexpr int kShortWaves = 4;
+template <class T>
+__global__ __launch_bounds__(64 * kShortWaves) void distill_short(DistillArgs a) {
+    constexpr int N = Elem<T>::kVec, kThreads = 64 * kShortWaves;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
     const int V = a.vocab;
     __shared__ ListedShared sh;
-    __shared__ float part[4][kLongWaves];
+    __shared__ float part[4][kShortWaves];
     const float w = a.weight ? a.weight[row] : 1.f;
     if (w == 0.f) {
         if (tid == 0) a.loss[row] = 0.f;
@@ -1139,12 +1184,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void distill_long(DistillArgs a) {
     bool masked = false;
     for (int j = tid * N; j < V; j += kThreads * N) {
         float v[N];
-        if (j + N <= V) {
-            Elem<T>::unpack(Elem<T>::load(x + j), v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
-        }
+        load_up_to<T>(x, j, V, v);
         st.add<N>(v, largest<N>(v), a.c, masked);
     }
     st.join_wave(a.c);
@@ -1153,10 +1193,10 @@ __global__ __launch_bounds__(64 * kLongWaves) void distill_long(DistillArgs a) {
         part[1][wave] = st.s;
     }
     __syncthreads();
-    st = lane < kLongWaves ? Stats{part[0][lane], part[1][lane], 0.f} : Stats::none();
+    st = lane < kShortWaves ? Stats{part[0][lane], part[1][lane], 0.f} : Stats::none();
     st.join_wave(a.c);
     const float ref = st.m == -kInf ? 0.f : st.m, r = ref * a.c;
-    put_loss<kLongWaves>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
+    put_loss<kShortWaves>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
     if (out && tid == 0) a.loss[row] = 0.f;
     if (!d) return;
     if (out || st.empty()) {
@@ -1164,31 +1204,97 @@ __global__ __launch_bounds__(64 * kLongWaves) void distill_long(DistillArgs a) {
         return;
     }
     const float k = w * a.t, ks = k / st.s;
-    const bool plain = Stats::plain(r);
-    for (int j = tid * N; j < V; j += kThreads * N) {
+    put_masses<T>(x, d, 0, V, kThreads, a.c, ref, ks);
+    __syncthreads();
+    if (l.id >= 0) Elem<T>::put(d + l.id, (mass_of(z, a.c, ref) / st.s - l.mass) * k);
+}
+
+// Rows that are split over work-groups (see distill_plan).  A first launch takes the statistics of every part,
+// and the logits of the listed tokens before a gradient in their place can
+// overwrite them; a second one joins them, every work-group for itself, and
+// writes the gradient of its part (the first part's the loss).
+constexpr int kPartWaves = 4, kPartLoads = 4;  // 16-byte loads of a thread in flight
+
+template <class T>
+__global__ __launch_bounds__(64 * kPartWaves) void distill_parts(DistillArgs a) {
+    constexpr int N = Elem<T>::kVec, kThreads = 64 * kPartWaves;
+    __shared__ float part[2][kPartWaves];
+    const int64_t row = blockIdx.x / a.parts;
+    const int which = blockIdx.x - (int)row * a.parts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (a.weight && a.weight[row] == 0.f) return;
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+    const int begin = which * a.part, end = min(a.vocab, begin + a.part);
+    if (which == 0 && tid < a.top) {
+        const int id = a.top_ids[row * a.top + tid];
+        a.listed[row * a.top + tid] = id >= 0 && id < a.vocab ? Elem<T>::get(x + id) : 0.f;
+    }
+    Stats st = Stats::none();
+    bool masked = false;
+    int j = begin + tid * N;
+    for (; j - tid * N + kPartLoads * kThreads * N <= end; j += kPartLoads * kThreads * N) {
+        u32x4 raw[kPartLoads];
+#pragma unroll
+        for (int u = 0; u < kPartLoads; ++u) raw[u] = Elem<T>::load(x + j + u * kThreads * N);
+        float v[kPartLoads * N];
+#pragma unroll
+        for (int u = 0; u < kPartLoads; ++u) Elem<T>::unpack(raw[u], v + u * N);
+        st.add<kPartLoads * N>(v, largest<kPartLoads * N>(v), a.c, masked);
+    }
+    for (; j < end; j += kThreads * N) {
         float v[N];
-        const bool whole = j + N <= V;
-        if (whole) {
-            Elem<T>::unpack(Elem<T>::load(x + j), v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = j + i < V ? Elem<T>::get(x + j + i) : -kInf;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = exp2_hw(plain ? __builtin_fmaf(v[i], a.c, -r) : (v[i] - ref) * a.c) * ks;
-        if (whole) {
-            Elem<T>::store_nt(d + j, Elem<T>::pack(v));
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (j + i < V) Elem<T>::put(d + j + i, v[i]);
-        }
+        load_up_to<T>(x, j, end, v);
+        st.add<N>(v, largest<N>(v), a.c, masked);
+    }
+    st.join_wave(a.c);
+    if (lane == 0) {
+        part[0][wave] = st.m;
+        part[1][wave] = st.s;
     }
     __syncthreads();
-    if (l.id >= 0) {
-        const float p = exp2_hw(plain ? __builtin_fmaf(z, a.c, -r) : (z - ref) * a.c) / st.s;
-        Elem<T>::put(d + l.id, (p - l.mass) * k);
+    if (wave) return;
+    st = lane < kPartWaves ? Stats{part[0][lane], part[1][lane], 0.f} : Stats::none();
+    st.join_wave(a.c);
+    if (lane == 0) a.part_stats[row * a.parts + which] = st;
+}
+
+template <class T>
+__global__ __launch_bounds__(64 * kPartWaves) void distill_parts_grad(DistillArgs a) {
+    constexpr int N = Elem<T>::kVec, kThreads = 64 * kPartWaves;
+    __shared__ ListedShared sh;
+    __shared__ float part[kPartWaves];
+    const int groups = a.out ? a.parts : 1;
+    const int64_t row = blockIdx.x / groups;
+    const int which = blockIdx.x - (int)row * groups, tid = threadIdx.x, lane = tid & 63;
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+    const int begin = which * a.part, end = min(a.vocab, begin + a.part);
+    T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    if (w == 0.f) {
+        if (which == 0 && tid == 0) a.loss[row] = 0.f;
+        if (d) zero_row(d + begin, end - begin, kThreads);
+        return;
     }
+    int id;
+    float u, total;
+    read_list(a, row, id, u);
+    const float z = tid < a.top ? a.listed[row * a.top + tid] : 0.f;
+    const Stats st = join_parts(a.part_stats + row * a.parts, a.parts, a.c, lane);
+    const Listed l = take_list(a, id, u, sh, total);
+    const bool out = total == 0.f;
+    const float ref = st.m == -kInf ? 0.f : st.m, r = ref * a.c;
+    if (which == 0) {
+        put_loss<kPartWaves>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part);
+        if (out && tid == 0) a.loss[row] = 0.f;
+    }
+    if (!d) return;
+    if (out || st.empty()) {
+        zero_row(d + begin, end - begin, kThreads);
+        return;
+    }
+    const float k = w * a.t, ks = k / st.s;
+    put_masses<T>(x, d, begin, end, kThreads, a.c, ref, ks);
+    __syncthreads();
+    if (l.id >= begin && l.id < end) Elem<T>::put(d + l.id, (mass_of(z, a.c, ref) / st.s - l.mass) * k);
 }
 
 constexpr int64_t kMaxElems = INT64_C(1) << 48;  // of a matrix, gaps included: offsets in bytes stay far inside 64 bits
@@ -1297,18 +1403,49 @@ void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st
 
 constexpr int32_t kGradFill = 1024;  // work-groups of the gradient of log probabilities where rows can be split
 constexpr int kUnits = 256;  // compute units of the card
+constexpr int64_t kHeld = 16 * 1024;  // vectors of the longest row that a work-group holds
+
+// How a distillation splits its rows, and its scratch memory.
+struct DistillPlan {
+    int32_t part, parts;  // parts == 0: rows are not split
+    int64_t stats, listed, bytes;
+};
+
+// Rows of which a work-group needs more than half of a compute unit are split
+// while the logits are few enough that the second read finds them in the caches
+// of the memory side (1 x 131072 bf16: 8 us, by one work-group 21; 400 rows: 54
+// and 61; 1500 rows: 231 and 183); and rows that no work-group holds.
+DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
+    constexpr int64_t kCached = INT64_C(128) << 20;
+    constexpr int32_t kFill = 4096;
+    const int32_t bytes = dtype == EDB_BF16 ? 2 : 4, vec = 16 / bytes, least = kPartLoads * 64 * kPartWaves * vec;
+    DistillPlan r{};
+    if (n == 0 || vocab <= ((int64_t)n * vocab * bytes <= kCached ? kHeld / 2 : kHeld) * vec) return r;
+    int64_t parts = n < kFill ? kFill / n : 1;
+    if (parts > vocab / least) parts = vocab / least;
+    if (parts < 1) parts = 1;
+    r.part = (int32_t)((((int64_t)vocab + parts - 1) / parts + least - 1) / least * least);
+    r.parts = (int32_t)(((int64_t)vocab + r.part - 1) / r.part);
+    r.listed = ((int64_t)n * r.parts * (int64_t)sizeof(Stats) + 15) / 16 * 16;
+    r.bytes = r.listed + (int64_t)n * top * 4;
+    return r;
+}
 
 template <class T>
 void launch_distill(const DistillArgs& a, hipStream_t st) {
+    if (a.parts) {
+        distill_parts<T><<<a.n * a.parts, 64 * kPartWaves, 0, st>>>(a);
+        distill_parts_grad<T><<<a.out ? a.n * a.parts : a.n, 64 * kPartWaves, 0, st>>>(a);
+        return;
+    }
     const int64_t vectors = ((int64_t)a.vocab + Elem<T>::kVec - 1) / Elem<T>::kVec;
-    if (a.vocab < 64 * Elem<T>::kVec) distill_long<T><<<a.n, 64 * kLongWaves, 0, st>>>(a);
+    if (a.vocab < 64 * Elem<T>::kVec) distill_short<T><<<a.n, 64 * kShortWaves, 0, st>>>(a);
     else if (vectors <= 2 * 256) distill_kernel<T, 4, 2, false><<<a.n, 256, 0, st>>>(a);
     else if (vectors <= 4 * 256) distill_kernel<T, 4, 4, false><<<a.n, 256, 0, st>>>(a);
     else if (vectors <= 8 * 256) distill_kernel<T, 4, 8, false><<<a.n, 256, 0, st>>>(a);
     else if (vectors <= 8 * 512) distill_kernel<T, 8, 8, false><<<a.n, 512, 0, st>>>(a);
     else if (vectors <= 8 * 1024) distill_kernel<T, 16, 8, false><<<a.n, 1024, 0, st>>>(a);
-    else if (vectors <= 16 * 1024) distill_kernel<T, 16, 16, true><<<a.n < kUnits ? a.n : kUnits, 1024, 0, st>>>(a);
-    else distill_long<T><<<a.n, 64 * kLongWaves, 0, st>>>(a);
+    else distill_kernel<T, 16, 16, true><<<a.n < kUnits ? a.n : kUnits, 1024, 0, st>>>(a);
 }
 
 float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
@@ -1404,10 +1541,21 @@ extern "C" edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32
     return launched(who);
 }
 
+extern "C" edb_status edb_distill_bytes(int32_t n, int32_t vocab, int32_t dtype, int32_t top, int64_t* bytes) {
+    if (!bytes) return fail(EDB_ERR_INVALID, "edb_distill_bytes: NULL argument");
+    if (edb_status st = check_rows("edb_distill_bytes", bytes, dtype, n, vocab, vocab, 1.f)) return st;
+    if (top < 1 || top > EDB_DISTILL_MAX_TOP)
+        return fail(EDB_ERR_UNSUPPORTED, "edb_distill_bytes: top must be in [1, " +
+                                             std::to_string(EDB_DISTILL_MAX_TOP) + "]");
+    *bytes = distill_plan(n, vocab, dtype, top).bytes;
+    edb::clear_error();
+    return EDB_OK;
+}
+
 extern "C" edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
                                   const int32_t* top_ids, const float* top_logits, int32_t top, float temperature,
                                   const float* weight, float* loss, void* dlogits, int64_t dlogits_stride,
-                                  void* stream) {
+                                  void* workspace, int64_t workspace_bytes, void* stream) {
     const char* who = "edb_distill";
     if (edb_status st = check_rows(who, logits, dtype, n, vocab, stride, temperature)) return st;
     if (top < 1 || top > EDB_DISTILL_MAX_TOP)
@@ -1419,8 +1567,30 @@ extern "C" edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, 
         edb::clear_error();
         return EDB_OK;
     }
-    DistillArgs a{logits, stride,      n,      vocab, top_ids, top_logits, top, log2e_over(temperature),
-                  (float)(1.0 / (double)temperature), temperature, weight, loss, dlogits, dlogits_stride};
+    const DistillPlan r = distill_plan(n, vocab, dtype, top);
+    if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+        return fail(EDB_ERR_INVALID, "edb_distill: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
+                                         " bytes is needed");
+    if ((int64_t)n * r.parts > INT32_MAX) return fail(EDB_ERR_UNSUPPORTED, "edb_distill: more than 2^31 parts of rows");
+    char* ws = static_cast<char*>(workspace);
+    const DistillArgs a{logits,
+                        stride,
+                        n,
+                        vocab,
+                        top_ids,
+                        top_logits,
+                        top,
+                        log2e_over(temperature),
+                        (float)(1.0 / (double)temperature),
+                        temperature,
+                        weight,
+                        loss,
+                        dlogits,
+                        dlogits_stride,
+                        r.part,
+                        r.parts,
+                        reinterpret_cast<Stats*>(ws + r.stats),
+                        reinterpret_cast<float*>(ws + r.listed)};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (dtype == EDB_F32) launch_distill<float>(a, st);
     else launch_distill<bf16>(a, st);

@@ -220,9 +220,11 @@ def distill(logits, top_ids, top_logits, temperature: float = 1.0, weight=None, 
         dp = d.data_ptr()
         if dp == logits.data_ptr():
             ostride = stride if on <= 1 else ostride
+    nb = _bytes("edb_distill_bytes", n, vocab, dt, top) if top else 0
+    ws = _workspace(dev, nb)
     _call("edb_distill", dev, logits.data_ptr(), dt, n, vocab, stride,
           _array(top_ids, "top_ids", (n, top), torch.int32, dev),
           _array(top_logits, "top_logits", (n, top), f32, dev), top, temperature,
           None if weight is None else _array(weight, "weight", (n,), f32, dev),
-          _array(out.loss, "out.loss", (n,), f32, dev), dp, ostride)
+          _array(out.loss, "out.loss", (n,), f32, dev), dp, ostride, ws.data_ptr() if nb else None, nb)
     return out

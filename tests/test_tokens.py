@@ -624,7 +624,8 @@ def test_distill_row_lengths(dtype, vectors, more):
 
 
 @gpu
-@pytest.mark.parametrize("n,V,dtype", [(700, 66001, BF16), (600, 33003, F32), (257, 131072, BF16), (1100, 33000, F32)])
+@pytest.mark.parametrize("n,V,dtype", [(700, 66001, BF16), (600, 33003, F32), (1100, 66001, BF16), (520, 131072, BF16),
+                                       (1020, 33003, F32), (1100, 33000, F32), (520, 65536, F32)])
 @pytest.mark.parametrize("kind", ["masked", "broken"])
 def test_distill_many_long_rows(n, V, dtype, kind):
     """More long rows than work-groups take at a time, rows without weight and without a teacher among them."""
@@ -646,6 +647,34 @@ def test_distill_many_long_rows(n, V, dtype, kind):
     got = tokens.distill(xv, ids, u, 0.9, w, out=tokens.Distilled(alone.loss, xv))
     assert torch.equal(got.loss.view(torch.uint8), full.loss.view(torch.uint8))
     assert torch.equal(xv.contiguous().view(torch.uint8), full.dlogits.view(torch.uint8))
+
+
+@gpu
+@pytest.mark.parametrize("n,V,dtype", [(1, 131072, BF16), (9, 65537, BF16), (70, 70001, BF16), (5, 32769, F32), (300, 40001, F32),
+                                       (1, 3_000_001, BF16), (3, 2_000_003, F32), (400, 150001, BF16)])
+@pytest.mark.parametrize("kind,teacher", [("masked", "short"), ("broken", "equal"), ("lowest", "distinct")])
+def test_distill_split_rows(n, V, dtype, kind, teacher):
+    """Rows that several work-groups take: the loss alone, strides, and in place, where listed tokens lie in other parts."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = _rows(kind, n, V, dtype, g)
+    ids, u = _teacher(n, V, 11, g, teacher)
+    ids[:, 1] = V - 1
+    w = torch.randn(n, generator=g, device="cuda")
+    w[1::6] = 0
+    full = tokens.distill(x, ids, u, 1.7, w)
+    for i in range(0, n, 100):
+        part = tokens.Distilled(full.loss[i:i + 100], full.dlogits[i:i + 100])
+        _check_distill(x[i:i + 100], ids[i:i + 100], u[i:i + 100], 1.7, w[i:i + 100], part)
+    alone = tokens.distill(x, ids, u, 1.7, w, grad=False)
+    assert torch.equal(alone.loss.view(torch.uint8), full.loss.view(torch.uint8))
+    xv, mem = _view(x, 3, 1)
+    before = mem.clone()
+    got = tokens.distill(xv, ids, u, 1.7, w, out=tokens.Distilled(alone.loss, xv))
+    assert torch.equal(got.loss.view(torch.uint8), full.loss.view(torch.uint8))
+    assert torch.equal(xv.contiguous().view(torch.uint8), full.dlogits.view(torch.uint8))
+    xv.copy_(x)
+    assert torch.equal(mem.view(torch.uint8), before.view(torch.uint8))
 
 
 @gpu
@@ -799,7 +828,8 @@ def _lp_grad(**k):
 
 
 def _distill(**k):
-    a = dict(x=A, d=L.F32, n=4, V=10, s=10, ti=2 * A, tl=3 * A, top=2, T=1.0, w=3 * A, loss=3 * A, out=4 * A, os=10)
+    a = dict(x=A, d=L.F32, n=4, V=10, s=10, ti=2 * A, tl=3 * A, top=2, T=1.0, w=3 * A, loss=3 * A, out=4 * A, os=10,
+             ws=5 * A, wb=1 << 40)
     a.update(k)
     return L.load().edb_distill(*a.values(), None)
 
@@ -831,7 +861,9 @@ REFUSED = (
         (dict(out=A + 4), INVALID), (dict(out=A, os=12), INVALID), (dict(out=4 * A + 2), INVALID)]]
     + [(_distill, k, e) for k, e in ROWS_BAD + [
         (dict(ti=None), INVALID), (dict(tl=None), INVALID), (dict(loss=None), INVALID), (dict(top=0), UNSUPPORTED),
-        (dict(top=257), UNSUPPORTED), (dict(os=9), INVALID), (dict(out=A + 4), INVALID), (dict(out=A, os=12), INVALID)]])
+        (dict(top=257), UNSUPPORTED), (dict(os=9), INVALID), (dict(out=A + 4), INVALID), (dict(out=A, os=12), INVALID),
+        (dict(n=1, V=200000, s=200000, os=200000, wb=0), INVALID), (dict(n=1, V=200000, s=200000, os=200000, ws=None), INVALID),
+        (dict(n=1, V=200000, s=200000, os=200000, ws=5 * A + 8), INVALID)]])
 
 
 @pytest.mark.parametrize("call,changed,status", REFUSED, ids=[f"{f.__name__[1:]}-{i}" for i, (f, _, _) in enumerate(REFUSED)])
@@ -854,6 +886,11 @@ def test_workspace_sizes():
     assert lib.edb_logprobs_bytes(5, 1000, L.BF16, 65, C.byref(nb)) == UNSUPPORTED
     assert lib.edb_logprobs_bytes(5, 1000, 9, 3, C.byref(nb)) == INVALID
     assert lib.edb_logprobs_bytes(5, 1000, L.F32, 3, None) == INVALID
+    assert lib.edb_distill_bytes(5, 1000, L.BF16, 3, C.byref(nb)) == L.EDB_OK and nb.value >= 0
+    assert lib.edb_distill_bytes(1, 1 << 30, L.F32, 256, C.byref(nb)) == L.EDB_OK and nb.value > 0
+    assert lib.edb_distill_bytes(5, 1000, L.BF16, 0, C.byref(nb)) == UNSUPPORTED
+    assert lib.edb_distill_bytes(5, 1000, 4, 3, C.byref(nb)) == INVALID
+    assert lib.edb_distill_bytes(5, 1000, L.F32, 3, None) == INVALID
     assert lib.edb_embed_grad_bytes(-1, 500, 64, C.byref(nb)) == INVALID
     assert lib.edb_embed_grad_bytes(1, 500, 64, None) == INVALID
 
