@@ -1423,16 +1423,19 @@ struct DistillPlan {
     int64_t stats, listed, bytes;
 };
 
-// Rows of which a work-group needs more than half of a compute unit are split
-// while the logits are few enough that the second read finds them in the caches
-// of the memory side (1 x 131072 bf16: 8 us, by one work-group 21; 400 rows: 54
-// and 61; 1500 rows: 231 and 183); and rows that no work-group holds.
+// Rows are split that no work-group holds.  So are those of which a work-group
+// needs more than half of a compute unit, while the logits are few enough that
+// the second read finds them in the caches of the memory side (1 x 131072 bf16:
+// 8 us, by one work-group 21; 400 rows: 54 and 61; 1500 rows: 231 and 183), and
+// from three eighths on where there are few rows (64 x 65536 bf16: 9 and 13 us;
+// 256 rows: 20 and 17).
 DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     constexpr int64_t kCached = INT64_C(128) << 20;
-    constexpr int32_t kFill = 4096;
+    constexpr int32_t kFill = 4096, kFew = 128;
     const int32_t bytes = dtype == EDB_BF16 ? 2 : 4, vec = 16 / bytes, least = kPartLoads * 64 * kPartWaves * vec;
+    const int64_t held = n <= kFew ? kHeld / 8 * 3 : (int64_t)n * vocab * bytes <= kCached ? kHeld / 2 : kHeld;
     DistillPlan r{};
-    if (n == 0 || vocab <= ((int64_t)n * vocab * bytes <= kCached ? kHeld / 2 : kHeld) * vec) return r;
+    if (n == 0 || vocab <= held * vec) return r;
     int64_t parts = n < kFill ? kFill / n : 1;
     if (parts > vocab / least) parts = vocab / least;
     if (parts < 1) parts = 1;
