@@ -858,6 +858,7 @@ struct DistillArgs {
     float* loss;
     void* out;
     int64_t out_stride;
+    bool cached;          // all logits fit the caches of the memory side
     int32_t part, parts;  // a split row: `parts` parts of `part` logits
     Stats* part_stats;    // [n][parts]
     float* listed;        // [n][top]: the student's logits at the listed tokens
@@ -957,18 +958,25 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t row, cons
 // that it is read once and the gradient written once.  2^y with y = x c - r(m)
 // (see Stats) is summed up in one pass over the registers, w T p_j = 2^y (w T / S)
 // written in another; the owners of the listed entries then write
-// w T (p_j - q_j).  Where a row fills a compute unit's registers (LOOP), a
-// work-group takes the rows blockIdx.x, + gridDim.x, ... and reads the next one
-// into each register as soon as the last one's vector has been used.
+// w T (p_j - q_j).  Memory bound: FIGURES
 constexpr int kBlock = 2;
 
-template <class T, int W, int NV, bool LOOP>
+template <class T, int W, int NV, bool CACHED>
 __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
     constexpr int N = Elem<T>::kVec, kThreads = 64 * W, kAll = 64 * N;  // elements of a wave's vector
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int V = a.vocab;
     __shared__ ListedShared sh;
     __shared__ float part[3][W];
+    const int64_t row = blockIdx.x;
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+    T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    if (w == 0.f) {
+        if (tid == 0) a.loss[row] = 0.f;
+        if (d) zero_row(d, V, kThreads);
+        return;
+    }
     // The row's vectors of a wave's 1 KB are dealt to the waves in turn, kBlock neighbouring ones at a time: the
     // wave's i-th is the row's number(i)-th.  `whole` of them are whole (in raw); the row's last, partial one is
     // in its wave's rest.  The row has a whole one at least, and the registers past a wave's own take the row's
@@ -978,152 +986,110 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
     int whole = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) whole += number(i) < all;
-    const bool has_rest = V % kAll != 0 && all / kBlock % W == wave;
+    const bool has_rest = V % kAll != 0 && all / kBlock % W == wave, odd = odd_row(x);
     const int j_rest = all * kAll + lane * N;
     auto place = [&](int i) { return min(number(i), all - 1) * kAll; };
     u32x4 raw[NV], rest{0u, 0u, 0u, 0u};
-    // the first row from `row` on that has a weight; the others get no loss and zeros
-    float w = 0.f;
-    auto seek = [&](int64_t row) {
-        for (; row < a.n; row += gridDim.x) {
-            w = a.weight ? a.weight[row] : 1.f;
-            if (w != 0.f) break;
-            if (tid == 0) a.loss[row] = 0.f;
-            if (a.out) zero_row(static_cast<T*>(a.out) + row * a.out_stride, V, kThreads);
-            if (!LOOP) return (int64_t)a.n;
-        }
-        return row;
-    };
-    int64_t row = seek(blockIdx.x);
-    if (row >= a.n) return;
-    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     int id;
-    float u;
+    float u, total;
     read_list(a, row, id, u);
-    {
-        const T* from = x - (odd_row(x) ? 1 : 0);
+    const T* from = x - (odd ? 1 : 0);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) raw[i] = Elem<T>::load_nt(lane_place(from + place(i), lane));
-        if (has_rest) rest = load_vector(x, j_rest, V, odd_row(x) ? 1 : 0);
+    for (int i = 0; i < NV; ++i) {
+        const T* at = lane_place(from + place(i), lane);
+        raw[i] = CACHED ? Elem<T>::load(at) : Elem<T>::load_nt(at);
     }
-    for (;;) {
-        T* d = a.out ? static_cast<T*>(a.out) + row * a.out_stride : nullptr;
-        float total;
-        const Listed l = take_list(a, id, u, sh, total);
-        const bool out = total == 0.f;
-        const float z = l.id >= 0 ? Elem<T>::get(x + l.id) : 0.f;
-        if (odd_row(x)) {
-            uint32_t after[NV / kBlock];  // the last element of each block
+    if (has_rest) rest = load_vector(x, j_rest, V, odd ? 1 : 0);
+    const Listed l = take_list(a, id, u, sh, total);
+    const bool out = total == 0.f;
+    const float z = l.id >= 0 ? Elem<T>::get(x + l.id) : 0.f;
+    if (odd) {
+        uint32_t after[NV / kBlock];  // the last element of each block
 #pragma unroll
-            for (int i = 0; i < NV; i += kBlock) after[i / kBlock] = element_bits(x + place(i + kBlock - 1) + kAll - 1);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                uint32_t next = after[i / kBlock];
-                if (i % kBlock != kBlock - 1 && i + 1 < whole)
-                    next = (uint32_t)__builtin_amdgcn_readlane((int)raw[i + 1 < NV ? i + 1 : i][0], 0);
-                raw[i] = shift_in(raw[i], next);
-            }
-            if (has_rest) rest = shift_in(rest, 0xff80);  // the row ends before lane 63 does: -inf
-        }
-
-        float m = -kInf;
-        auto top = [&](u32x4 q) {
-            float v[N];
-            Elem<T>::unpack(q, v);
-            m = fmaxf(m, largest<N>(v));
-        };
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i < whole) top(raw[i]);
-        if (has_rest) top(rest);
-        m = wave_max(m);
-        if (lane == 0) part[0][wave] = m;
-        __syncthreads();
-        m = wave_max(lane < W ? part[0][lane] : -kInf);
-        // y = (x - low) c - r, low 0 but for rows near the end of the fp32 range
-        const float ref = m == -kInf ? 0.f : m;
-        const bool plain = Stats::plain(ref * a.c);
-        const float low = plain ? 0.f : ref, r = plain ? ref * a.c : 0.f;
-        float s = 0.f;
-        auto add = [&](u32x4 q) {
-            float v[N];
-            Elem<T>::unpack(q, v);
-#pragma unroll
-            for (int k = 0; k < N; ++k) s += exp2_hw(__builtin_fmaf(v[k] - low, a.c, -r));
-        };
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i < whole) add(raw[i]);
-        if constexpr (LOOP && sizeof(T) == 4)  // no exponentials are kept for the next pass: registers are short
-#pragma unroll
-            for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(raw[i]));
-        if (has_rest) add(rest);
-        s = wave_sum(s);
-        if (lane == 0) part[1][wave] = s;
-        __syncthreads();
-        const Stats st{m, wave_sum(lane < W ? part[1][lane] : 0.f), 0.f};
-        put_loss<W>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
-        if (out && tid == 0) a.loss[row] = 0.f;
-        if (!LOOP && !d) return;
-
-        const float k = w * a.t, ks = k / st.s;
-        const bool zero = out || st.empty();
-        int64_t next = a.n;
-        const T *x_next = x, *from = x;
-        if constexpr (LOOP) {
-            next = seek(row + gridDim.x);
-            if (next < a.n) {
-                read_list(a, next, id, u);
-                x_next = static_cast<const T*>(a.logits) + next * a.stride;
-            }
-            from = x_next - (odd_row(x_next) ? 1 : 0);
-        }
-        auto slope = [&](u32x4 q) {
-            float v[N];
-            Elem<T>::unpack(q, v);
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = exp2_hw(__builtin_fmaf(v[e] - low, a.c, -r)) * ks;
-            const u32x4 o = Elem<T>::pack(v);
-            return zero ? u32x4{0u, 0u, 0u, 0u} : o;
-        };
-        const u32x4 o_rest = has_rest ? slope(rest) : u32x4{0u, 0u, 0u, 0u};
-        const bool odd_out = odd_row(d), straight = straight_row(d);
-        u32x4 held{0u, 0u, 0u, 0u};  // at an odd address: the vector before, whose last lane wants this one's first element
+        for (int i = 0; i < NV; i += kBlock) after[i / kBlock] = element_bits(x + place(i + kBlock - 1) + kAll - 1);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (i < whole) {
-                const u32x4 o = slope(raw[i]);
-                T* at = d + place(i);
-                if (!d) {
-                    // the loss alone
-                } else if (!odd_out) {
-                    store_piece(lane_place(at, lane), o, straight);
+            uint32_t next = after[i / kBlock];
+            if (i % kBlock != kBlock - 1 && i + 1 < whole)
+                next = (uint32_t)__builtin_amdgcn_readlane((int)raw[i + 1 < NV ? i + 1 : i][0], 0);
+            raw[i] = shift_in(raw[i], next);
+        }
+        if (has_rest) rest = shift_in(rest, 0xff80);  // the row ends before lane 63 does: -inf
+    }
+
+    float m = -kInf;
+    auto top = [&](u32x4 q) {
+        float v[N];
+        Elem<T>::unpack(q, v);
+        m = fmaxf(m, largest<N>(v));
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i < whole) top(raw[i]);
+    if (has_rest) top(rest);
+    m = wave_max(m);
+    if (lane == 0) part[0][wave] = m;
+    __syncthreads();
+    m = wave_max(lane < W ? part[0][lane] : -kInf);
+    // y = (x - low) c - r, low 0 but for rows near the end of the fp32 range
+    const float ref = m == -kInf ? 0.f : m;
+    const bool plain = Stats::plain(ref * a.c);
+    const float low = plain ? 0.f : ref, r = plain ? ref * a.c : 0.f;
+    float s = 0.f;
+    auto add = [&](u32x4 q) {
+        float v[N];
+        Elem<T>::unpack(q, v);
+#pragma unroll
+        for (int k = 0; k < N; ++k) s += exp2_hw(__builtin_fmaf(v[k] - low, a.c, -r));
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i < whole) add(raw[i]);
+    if (has_rest) add(rest);
+    s = wave_sum(s);
+    if (lane == 0) part[1][wave] = s;
+    __syncthreads();
+    const Stats st{m, wave_sum(lane < W ? part[1][lane] : 0.f), 0.f};
+    put_loss<W>(a, row, l, (z - ref) * a.inv_t - st.log_sum(a.c), part[2]);
+    if (out && tid == 0) a.loss[row] = 0.f;
+    if (!d) return;
+
+    const float k = w * a.t, ks = k / st.s;
+    const bool zero = out || st.empty();
+    auto slope = [&](u32x4 q) {
+        float v[N];
+        Elem<T>::unpack(q, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = exp2_hw(__builtin_fmaf(v[e] - low, a.c, -r)) * ks;
+        const u32x4 o = Elem<T>::pack(v);
+        return zero ? u32x4{0u, 0u, 0u, 0u} : o;
+    };
+    const bool odd_out = odd_row(d), straight = straight_row(d);
+    u32x4 held{0u, 0u, 0u, 0u};  // at an odd address: the vector before, whose last lane wants this one's first element
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i < whole) {
+            const u32x4 o = slope(raw[i]);
+            T* at = d + place(i);
+            if (!odd_out) {
+                store_piece(lane_place(at, lane), o, straight);
+            } else {
+                if (i % kBlock == 0) {
+                    if (lane == 0) store_first(at, o);
                 } else {
-                    if (i % kBlock == 0) {
-                        if (lane == 0) store_first(at, o);
-                    } else {
-                        Elem<T>::store(lane_place(at - kAll + 1, lane),
-                                       shift_in(held, (uint32_t)__builtin_amdgcn_readlane((int)o[0], 0)));
-                    }
-                    if (i % kBlock == kBlock - 1 || i + 1 == whole) store_end(at, o, lane);
-                    held = o;
+                    Elem<T>::store(lane_place(at - kAll + 1, lane),
+                                   shift_in(held, (uint32_t)__builtin_amdgcn_readlane((int)o[0], 0)));
                 }
-            }
-            if constexpr (LOOP) raw[i] = Elem<T>::load_nt(lane_place(from + (next < a.n ? place(i) : 0), lane));
-        }
-        if (d) {
-            if (has_rest) store_vector(d, j_rest, V, o_rest, odd_out, straight, lane);
-            __syncthreads();
-            if (l.id >= 0 && !zero) {
-                const float p = exp2_hw(__builtin_fmaf(z - low, a.c, -r)) / st.s;
-                Elem<T>::put(d + l.id, (p - l.mass) * k);
+                if (i % kBlock == kBlock - 1 || i + 1 == whole) store_end(at, o, lane);
+                held = o;
             }
         }
-        if (!LOOP || next >= a.n) return;
-        if (has_rest) rest = load_vector(x_next, j_rest, V, odd_row(x_next) ? 1 : 0);
-        row = next;
-        x = x_next;
-        __syncthreads();  // the shared arrays are used again
+    }
+    if (has_rest) store_vector(d, j_rest, V, slope(rest), odd_out, straight, lane);
+    __syncthreads();
+    if (l.id >= 0 && !zero) {
+        const float p = exp2_hw(__builtin_fmaf(z - low, a.c, -r)) / st.s;
+        Elem<T>::put(d + l.id, (p - l.mass) * k);
     }
 }
 
@@ -1414,11 +1380,11 @@ void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st
 }
 
 constexpr int32_t kGradFill = 1024;  // work-groups of the gradient of log probabilities where rows can be split
-constexpr int kUnits = 256;  // compute units of the card
 constexpr int64_t kHeld = 16 * 1024;  // vectors of the longest row that a work-group holds
 
 // How a distillation splits its rows, and its scratch memory.
 struct DistillPlan {
+    bool cached;
     int32_t part, parts;  // parts == 0: rows are not split
     int64_t stats, listed, bytes;
 };
@@ -1433,8 +1399,9 @@ DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     constexpr int64_t kCached = INT64_C(128) << 20;
     constexpr int32_t kFill = 4096, kFew = 128;
     const int32_t bytes = dtype == EDB_BF16 ? 2 : 4, vec = 16 / bytes, least = kPartLoads * 64 * kPartWaves * vec;
-    const int64_t held = n <= kFew ? kHeld / 8 * 3 : (int64_t)n * vocab * bytes <= kCached ? kHeld / 2 : kHeld;
     DistillPlan r{};
+    r.cached = (int64_t)n * vocab <= kCached / bytes;
+    const int64_t held = n <= kFew ? kHeld / 8 * 3 : r.cached ? kHeld / 2 : kHeld;
     if (n == 0 || vocab <= held * vec) return r;
     int64_t parts = n < kFill ? kFill / n : 1;
     if (parts > vocab / least) parts = vocab / least;
@@ -1446,6 +1413,17 @@ DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     return r;
 }
 
+template <class T, bool CACHED>
+void launch_held(const DistillArgs& a, hipStream_t st) {
+    const int64_t vectors = ((int64_t)a.vocab + Elem<T>::kVec - 1) / Elem<T>::kVec;
+    if (vectors <= 2 * 256) distill_kernel<T, 4, 2, CACHED><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 4 * 256) distill_kernel<T, 4, 4, CACHED><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 8 * 256) distill_kernel<T, 4, 8, CACHED><<<a.n, 256, 0, st>>>(a);
+    else if (vectors <= 8 * 512) distill_kernel<T, 8, 8, CACHED><<<a.n, 512, 0, st>>>(a);
+    else if (vectors <= 8 * 1024) distill_kernel<T, 16, 8, CACHED><<<a.n, 1024, 0, st>>>(a);
+    else distill_kernel<T, 16, 16, CACHED><<<a.n, 1024, 0, st>>>(a);
+}
+
 template <class T>
 void launch_distill(const DistillArgs& a, hipStream_t st) {
     if (a.parts) {
@@ -1453,14 +1431,9 @@ void launch_distill(const DistillArgs& a, hipStream_t st) {
         distill_parts_grad<T><<<a.out ? a.n * a.parts : a.n, 64 * kPartWaves, 0, st>>>(a);
         return;
     }
-    const int64_t vectors = ((int64_t)a.vocab + Elem<T>::kVec - 1) / Elem<T>::kVec;
     if (a.vocab < 64 * Elem<T>::kVec) distill_short<T><<<a.n, 64 * kShortWaves, 0, st>>>(a);
-    else if (vectors <= 2 * 256) distill_kernel<T, 4, 2, false><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 4 * 256) distill_kernel<T, 4, 4, false><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 8 * 256) distill_kernel<T, 4, 8, false><<<a.n, 256, 0, st>>>(a);
-    else if (vectors <= 8 * 512) distill_kernel<T, 8, 8, false><<<a.n, 512, 0, st>>>(a);
-    else if (vectors <= 8 * 1024) distill_kernel<T, 16, 8, false><<<a.n, 1024, 0, st>>>(a);
-    else distill_kernel<T, 16, 16, true><<<a.n < kUnits ? a.n : kUnits, 1024, 0, st>>>(a);
+    else if (a.cached) launch_held<T, true>(a, st);
+    else launch_held<T, false>(a, st);
 }
 
 float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
@@ -1602,6 +1575,7 @@ extern "C" edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, 
                         loss,
                         dlogits,
                         dlogits_stride,
+                        r.cached,
                         r.part,
                         r.parts,
                         reinterpret_cast<Stats*>(ws + r.stats),

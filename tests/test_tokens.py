@@ -625,7 +625,8 @@ def test_distill_row_lengths(dtype, vectors, more):
 
 @gpu
 @pytest.mark.parametrize("n,V,dtype", [(700, 66001, BF16), (600, 33003, F32), (1100, 66001, BF16), (520, 131072, BF16),
-                                       (1020, 33003, F32), (1100, 33000, F32), (520, 65536, F32)])
+                                       (1020, 33003, F32), (1100, 33000, F32), (520, 65536, F32), (200, 65536, BF16),
+                                       (300, 40001, BF16), (140, 32767, F32)])
 @pytest.mark.parametrize("kind", ["masked", "broken"])
 def test_distill_many_long_rows(n, V, dtype, kind):
     """More long rows than work-groups take at a time, rows without weight and without a teacher among them."""
