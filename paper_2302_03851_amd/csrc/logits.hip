@@ -775,7 +775,7 @@ struct GradArgs {
 // neighbouring vectors of 1 KB in turn.
 constexpr int kGradWaves = 8, kGradLoads = 4;  // waves of a work-group at most
 
-template <class T>
+template <class T, bool CACHED>
 __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs a) {
     constexpr int N = Elem<T>::kVec, kAll = 64 * N;
     const int64_t row = blockIdx.x;
@@ -814,7 +814,10 @@ __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs
         const int count = min(kGradLoads, all - g);
         u32x4 raw[kGradLoads];
 #pragma unroll
-        for (int u = 0; u < kGradLoads; ++u) raw[u] = Elem<T>::load_nt(lane_place(from + min(g + u, all - 1) * kAll, lane));
+        for (int u = 0; u < kGradLoads; ++u) {
+            const T* at = lane_place(from + min(g + u, all - 1) * kAll, lane);
+            raw[u] = CACHED ? Elem<T>::load(at) : Elem<T>::load_nt(at);
+        }
         if (odd) shift_in_all(raw, count, x + (g + count) * kAll - 1);
         u32x4 held{0u, 0u, 0u, 0u};
 #pragma unroll
@@ -1382,6 +1385,21 @@ void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st
 constexpr int32_t kGradFill = 1024;  // work-groups of the gradient of log probabilities where rows can be split
 constexpr int64_t kHeld = 16 * 1024;  // vectors of the longest row that a work-group holds
 
+// Whether the caches of the memory side can hold all logits, and may do so since
+// they were written.  A gradient then reads them by plain loads, else past the
+// caches (distillation of 1000 x 65536 bf16: 46 and 52 us, of 1500 x 131072 179
+// and 170; gradient of log probabilities of 1000 x 65536: 43 and 54 us, of 8192
+// x 65536 406 and 398).
+bool caches_hold(int32_t n, int32_t vocab, int32_t dtype) {
+    return (int64_t)n * vocab <= (INT64_C(128) << 20) / (dtype == EDB_BF16 ? 2 : 4);
+}
+
+template <class T>
+void launch_grad(const GradArgs& a, bool cached, dim3 grid, int threads, hipStream_t st) {
+    if (cached) logprobs_grad_kernel<T, true><<<grid, threads, 0, st>>>(a);
+    else logprobs_grad_kernel<T, false><<<grid, threads, 0, st>>>(a);
+}
+
 // How a distillation splits its rows, and its scratch memory.
 struct DistillPlan {
     bool cached;
@@ -1390,17 +1408,16 @@ struct DistillPlan {
 };
 
 // Rows are split that no work-group holds.  So are those of which a work-group
-// needs more than half of a compute unit, while the logits are few enough that
-// the second read finds them in the caches of the memory side (1 x 131072 bf16:
+// needs more than half of a compute unit, while the second read can find the
+// logits in the caches (1 x 131072 bf16:
 // 8 us, by one work-group 21; 400 rows: 54 and 61; 1500 rows: 231 and 183), and
 // from three eighths on where there are few rows (64 x 65536 bf16: 9 and 13 us;
 // 256 rows: 20 and 17).
 DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
-    constexpr int64_t kCached = INT64_C(128) << 20;
     constexpr int32_t kFill = 4096, kFew = 128;
     const int32_t bytes = dtype == EDB_BF16 ? 2 : 4, vec = 16 / bytes, least = kPartLoads * 64 * kPartWaves * vec;
     DistillPlan r{};
-    r.cached = (int64_t)n * vocab <= kCached / bytes;
+    r.cached = caches_hold(n, vocab, dtype);
     const int64_t held = n <= kFew ? kHeld / 8 * 3 : r.cached ? kHeld / 2 : kHeld;
     if (n == 0 || vocab <= held * vec) return r;
     int64_t parts = n < kFill ? kFill / n : 1;
@@ -1524,8 +1541,9 @@ extern "C" edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32
     const int32_t waves = turns < kGradWaves ? turns : kGradWaves, most = (turns + waves - 1) / waves;
     const int32_t wanted = n < kGradFill ? (kGradFill + n - 1) / n : 1;
     const dim3 grid(n, wanted < most ? wanted : most);
-    if (dtype == EDB_F32) logprobs_grad_kernel<float><<<grid, 64 * waves, 0, st>>>(a);
-    else logprobs_grad_kernel<bf16><<<grid, 64 * waves, 0, st>>>(a);
+    const bool cached = caches_hold(n, vocab, dtype);
+    if (dtype == EDB_F32) launch_grad<float>(a, cached, grid, 64 * waves, st);
+    else launch_grad<bf16>(a, cached, grid, 64 * waves, st);
     return launched(who);
 }
 
