@@ -102,8 +102,11 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
 // added in ascending position and the result does not depend on timing.  Ids
 // that are no token get the word V and sort to the end.  It takes a pass for
 // every digit of up to kMaxDigit bits, of counts per tile, their prefix sums and
-// the scatter.  The zero rows of the other words are written in the launch of
-// the sums, by further work-groups.
+// the scatter.  These launches leave the memory idle, so further work-groups of
+// theirs write the zero rows: of all words, because those that occur are not
+// known yet; the sums come over them later (rows of 512 bf16 into 65536 rows of
+// fp32, with the zeros of the other words beside the sums in brackets: 5000 ids
+// 42 us [51], 20000 51 [58], 262144 120 [119]).
 
 constexpr int kMaxDigit = 10;
 constexpr int kTile = 1024;        // ids a work-group of the sort ranks: 4 waves of 4 rounds
@@ -139,6 +142,40 @@ struct alignas(8) Pair {
     uint32_t word, pos;
 };
 
+// A launch's share of the zero rows: the work-groups from `from` on write them.
+struct Fill {
+    char* table;
+    int64_t row, stride;    // bytes
+    uint32_t first, rows;
+    int32_t from, per;      // per: rows of a work-group
+};
+
+constexpr int kFillBytes = 65536;  // a work-group's, about
+
+__device__ __forceinline__ void fill_rows(const Fill& f, int group) {
+    const uint32_t first = group * (uint32_t)f.per, rows = min((uint32_t)f.per, f.rows - first);
+    char* base = f.table + (int64_t)(f.first + first) * f.stride;
+    if (f.row == f.stride) {  // one piece of memory: 16 bytes a store where it is aligned, 2 before and after
+        char* end = base + rows * f.row;
+        char* body = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(base) + 15) & ~(uintptr_t)15);
+        char* stop = reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(end) & ~(uintptr_t)15);
+        for (char* p = body + threadIdx.x * 16; p < stop; p += 256 * 16)
+            __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<u32x4*>(p));
+        const int at = threadIdx.x * 2;
+        if (base + at < min(body, end)) *reinterpret_cast<uint16_t*>(base + at) = 0;
+        if (stop >= body && stop + at < end) *reinterpret_cast<uint16_t*>(stop + at) = 0;
+        return;
+    }
+    const uint32_t pieces = (uint32_t)((f.row + 15) / 16), items = rows * pieces;
+    for (uint32_t i = threadIdx.x; i < items; i += 256) {
+        const uint32_t r = i / pieces, c = (i - r * pieces) * 16;
+        char* d = base + r * f.stride + c;
+        if (c + 16 <= f.row) Elem<bf16>::store_nt(reinterpret_cast<bf16*>(d), u32x4{0u, 0u, 0u, 0u});
+        else
+            for (uint32_t k = 0; c + k < f.row; k += 2) *reinterpret_cast<uint16_t*>(d + k) = 0;
+    }
+}
+
 struct SortArgs {
     const int32_t* ids;  // pass 0 reads the ids
     const Pair* in;      // later passes read these
@@ -147,6 +184,7 @@ struct SortArgs {
     uint32_t* totals;    // [bin]
     int32_t n, tiles, shift, bits;
     uint32_t vocab;
+    Fill fill;
 };
 
 __device__ __forceinline__ Pair sort_pair(const SortArgs& a, int64_t i) {
@@ -156,6 +194,7 @@ __device__ __forceinline__ Pair sort_pair(const SortArgs& a, int64_t i) {
 // counts[tile][bin] of one digit.
 __global__ __launch_bounds__(256) void sort_count(SortArgs a) {
     __shared__ uint32_t count[1 << kMaxDigit];
+    if ((int)blockIdx.x >= a.fill.from) return fill_rows(a.fill, blockIdx.x - a.fill.from);
     const int bins = 1 << a.bits, tile = blockIdx.x;
     for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
     uint32_t k[kTile / 256];
@@ -178,6 +217,7 @@ constexpr int kScanBins = 16;
 __global__ __launch_bounds__(256) void sort_scan(SortArgs a) {
     const int bins = 1 << a.bits;
     __shared__ uint32_t part[16][kScanBins];
+    if ((int)blockIdx.x >= a.fill.from) return fill_rows(a.fill, blockIdx.x - a.fill.from);
     const int mine = threadIdx.x >> 4, bin = blockIdx.x * kScanBins + (threadIdx.x & 15);
     const int per = (a.tiles + 15) / 16, t0 = min(a.tiles, mine * per), t1 = min(a.tiles, t0 + per);
     uint32_t* c = a.counts + bin;
@@ -201,14 +241,15 @@ __global__ __launch_bounds__(256) void sort_scan(SortArgs a) {
 }
 
 // Ranks a tile's ids and writes them to their places.  SUM: the counts are
-// still those of single tiles, and every work-group adds them up for itself;
-// for few tiles that takes less than another launch (20000 ids of 17 bits: the
-// sort 20 us, with a launch for the sums 24).
+// still those of single tiles, and every work-group adds them up for itself,
+// which for few tiles takes less than another launch (the gradient of 9000 ids
+// x 300 into 65536 words: 44 us, with a launch for the sums 48; 60000 ids: 70 both).
 template <bool SUM>
 __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
     constexpr int kBins = 1 << kMaxDigit;
     __shared__ uint32_t at[4][kBins];  // per wave: counts, then the next place of a digit
     __shared__ uint32_t wave_sum[4];
+    if ((int)blockIdx.x >= a.fill.from) return fill_rows(a.fill, blockIdx.x - a.fill.from);
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, tile = blockIdx.x, bins = 1 << a.bits;
     // each thread owns four neighbouring bins
     constexpr int kOwn = kBins / 256;
@@ -293,8 +334,6 @@ struct SumArgs {
     void* dtable;
     int64_t dtable_stride;
     float* partial;      // [chunks][2][dim]
-    int32_t sum_groups;  // work-groups of the sums (per column tile); the others zero rows
-    int32_t fill_rows;   // rows that one of those looks at, at most kFillRows
 };
 
 constexpr int kFillRows = 256;
@@ -314,25 +353,6 @@ __device__ __forceinline__ void zero_rows(void* dtable, int64_t stride, int32_t 
         else
             for (int k = c; k < dim; ++k) Elem<O>::put(d + (k - c), 0.f);
     }
-}
-
-// Zeroes those of a group's fill_rows rows whose words do not occur.
-template <class O>
-__device__ __forceinline__ void fill_absent(const SumArgs& a, int group) {
-    __shared__ uint8_t there[kFillRows];
-    const uint32_t first = (uint32_t)group * a.fill_rows, rows = min((uint32_t)a.fill_rows, a.vocab - first);
-    if (threadIdx.x < rows) {
-        const uint32_t word = first + threadIdx.x;
-        int lo = 0, hi = a.n;  // the first place whose word is not below
-        while (lo < hi) {
-            const int mid = lo + (hi - lo) / 2;
-            if (a.sorted[mid].word < word) lo = mid + 1;
-            else hi = mid;
-        }
-        there[threadIdx.x] = lo < a.n && a.sorted[lo].word == word;
-    }
-    __syncthreads();
-    zero_rows<O>(a.dtable, a.dtable_stride, a.dim, first, rows, there, 256);
 }
 
 // The sums over the groups of `lanes` lanes of a wave, in every group.
@@ -393,10 +413,6 @@ struct Eight {
 // and a place without a row reads its chunk's first one, without a branch.
 template <class T, class O, int K, bool WAVE>
 __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
-    if ((int)blockIdx.x >= a.sum_groups) {
-        if (blockIdx.y == 0) fill_absent<O>(a, blockIdx.x - a.sum_groups);
-        return;
-    }
     int chunk;
     if constexpr (WAVE) chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     else chunk = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) / a.lanes);
@@ -476,7 +492,7 @@ __device__ __forceinline__ void add_partial(const SumArgs& a, int64_t chunk, int
 // chunks (at most one begins in a work-group's), by all waves together, each
 // group of lanes a contiguous part.  A long run's columns are split over the
 // work-groups along z, which a CU by itself would take too long for (262144 ids
-// x 512 fp32, half of them one word: 205 us, 239 without the split); those but
+// x 512 fp32, half of them one word: 210 us, 239 without the split); those but
 // the first have nothing else to do.
 template <class O, int K>
 __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
@@ -766,9 +782,7 @@ void launch_small(int piece, const SmallArgs& a, hipStream_t st) {
 
 template <class T, class O, int K>
 void launch_sums(const GradPlan& g, const SumArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)(a.sum_groups + (a.accumulate ? 0 : ((int64_t)a.vocab + a.fill_rows - 1) / a.fill_rows)),
-                    g.tiles_y);
-    if (grid.x == 0) return;
+    const dim3 grid((unsigned)(((int64_t)g.chunks * g.lanes + 255) / 256), g.tiles_y);
     if (g.lanes == 64) sum_chunks<T, O, K, true><<<grid, 256, 0, st>>>(a);
     else sum_chunks<T, O, K, false><<<grid, 256, 0, st>>>(a);
     if (g.chunks > 1) {
@@ -839,10 +853,10 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
         return fail(EDB_ERR_INVALID, "edb_embed_grad: a 16-byte aligned workspace of " + std::to_string(g.bytes) +
                                          " bytes is needed");
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    // a work-group zeroes 16 KB, 64 KB where it has to search the sorted list
-    const int64_t fit = (n <= kSmall ? 16384 : 65536) / (dim * elem_bytes(dtable_dtype));
-    const int fill_rows = (int)(fit < 1 ? 1 : fit > kFillRows ? kFillRows : fit);
+    const int64_t row_bytes = dim * elem_bytes(dtable_dtype);
     if (n <= kSmall) {
+        const int64_t fit = 16384 / row_bytes;  // rows that a work-group zeroes
+        const int fill_rows = (int)(fit < 1 ? 1 : fit > kFillRows ? kFillRows : fit);
         const int fill_groups = accumulate ? 0 : (int)(((int64_t)vocab + fill_rows - 1) / fill_rows);
         const SmallArgs a{ids,   n,          (uint32_t)vocab, dim,           g.lanes,   g.tiles_y,  dout, dout_stride,
                           scale, accumulate, dtable,          dtable_stride, fill_rows, fill_groups};
@@ -865,23 +879,36 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
     s.counts = reinterpret_cast<uint32_t*>(ws + g.counts);
     s.totals = reinterpret_cast<uint32_t*>(ws + g.totals);
     s.bits = g.digit;
+    const bool scan = g.sort_tiles > kSumTiles;
+    const int launches = g.passes * (scan ? 3 : 2);
+    int launch = 0;
+    // the work-groups of the next launch, its share of the zero rows behind `groups` of its own
+    auto next = [&](int groups) {
+        const int64_t first = (int64_t)vocab * launch / launches, end = (int64_t)vocab * (launch + 1) / launches;
+        const int64_t per = row_bytes < kFillBytes ? kFillBytes / row_bytes : 1;
+        ++launch;
+        s.fill = Fill{static_cast<char*>(dtable), row_bytes, dtable_stride * elem_bytes(dtable_dtype), (uint32_t)first,
+                      (uint32_t)(end - first), groups, (int32_t)per};
+        return (unsigned)(groups + (accumulate ? 0 : (end - first + per - 1) / per));
+    };
     for (int p = 0; p < g.passes; ++p) {
         s.ids = p ? nullptr : ids;
         s.in = sorted((p + 1) & 1);
         s.out = sorted(p & 1);
         s.shift = p * g.digit;
         last = p & 1;
-        sort_count<<<g.sort_tiles, 256, 0, st>>>(s);
-        if (g.sort_tiles <= kSumTiles) {
-            sort_scatter<true><<<g.sort_tiles, 256, 0, st>>>(s);
-            continue;
+        const unsigned count = next(g.sort_tiles);
+        sort_count<<<count, 256, 0, st>>>(s);
+        if (scan) {
+            const unsigned sums = next(((1 << g.digit) + kScanBins - 1) / kScanBins);
+            sort_scan<<<sums, 256, 0, st>>>(s);
         }
-        sort_scan<<<((1 << g.digit) + kScanBins - 1) / kScanBins, 256, 0, st>>>(s);
-        sort_scatter<false><<<g.sort_tiles, 256, 0, st>>>(s);
+        const unsigned scatter = next(g.sort_tiles);
+        if (scan) sort_scatter<false><<<scatter, 256, 0, st>>>(s);
+        else sort_scatter<true><<<scatter, 256, 0, st>>>(s);
     }
-    const int sum_groups = (int)(((int64_t)g.chunks * g.lanes + 255) / 256);
     const SumArgs a{sorted(last), n, g.chunk, (uint32_t)vocab, dim, g.lanes, dout, dout_stride, scale,
-                    accumulate, dtable, dtable_stride, reinterpret_cast<float*>(ws + g.partial), sum_groups, fill_rows};
+                    accumulate, dtable, dtable_stride, reinterpret_cast<float*>(ws + g.partial)};
     if (dout_dtype == EDB_F32) {
         if (dtable_dtype == EDB_F32) launch_sums<float, float>(g, a, st);
         else launch_sums<float, bf16>(g, a, st);
