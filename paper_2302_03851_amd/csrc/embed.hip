@@ -72,7 +72,10 @@ struct EmbedArgs {
     int64_t out_stride;
 };
 
-// One thread per K elements of a row.
+// One thread per K elements of a row: 16 bytes of the result, so that a wave
+// writes whole lines, past the caches.  Memory bound: 262144 x 512 bf16, 536 MB
+// written and read, 59 us (5.5 TB/s; through the caches 95); 28629 x 512 from
+// fp32 to bf16 10.5 us.  112 x 64: 2.5 us, a launch.
 template <class T, class O, int K>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
     const int pieces = (a.dim + K - 1) / K;
@@ -411,6 +414,8 @@ struct Eight {
 // All eight entries are there before the first row is asked for (loads return
 // in order: a wait for a later entry would wait for the rows before it too),
 // and a place without a row reads its chunk's first one, without a branch.
+// Memory bound: 262144 rows of 512 bf16 (268 MB) into those that occur of 131072
+// in fp32: 78 us.
 template <class T, class O, int K, bool WAVE>
 __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
     int chunk;
@@ -565,10 +570,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
 //
 // A work-group an id looks through all ids.  The one at a word's first place
 // adds up the word's rows (a contiguous part of them for each group of lanes),
-// the others end; the first work-groups zero the rows of the other words.
-// 1627 ids x 100 fp32 into 20011 words: 7.1 us, by sorting 19; 4000 x 512 into
-// 65536: 33 and 50, but 88 and 53 where one word has half of the ids.
+// of a frequent word the ones at its first up to eight places a part of the
+// columns each; the others end.  The first work-groups zero the rows of the
+// other words, which is what most of the time goes to where the table is large.
+// 1627 ids x 100 fp32 into 20011 words: 9 us, by sorting 24; 4000 x 512 into
+// 65536: 34 and 43, also where one word has half of the ids (90 without the parts).
 constexpr int kSmall = 4096;
+constexpr int kSmallOften = 64;   // rows from which on a word's columns are split
 constexpr int kSmallThreads = 256, kSmallWaves = kSmallThreads / 64;
 
 struct SmallArgs {
@@ -629,11 +637,27 @@ __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
         early[wave] = before;
     }
     __syncthreads();
-    int at = 0, n = 0;
+    int at = 0, n = 0, turn = 0;
     for (int w = 0; w < kSmallWaves; ++w) {
-        if (early[w]) return;
+        turn |= early[w];
         if (w < wave) at += count[w];
         n += count[w];
+    }
+    const int parts = n >= kSmallOften ? max(1, min(8, a.lanes / 4)) : 1, lanes = a.lanes / parts;
+    if (turn) {  // not the first: which place of the word's is it
+        if (parts == 1) return;
+        __syncthreads();
+        int places = 0;
+#pragma unroll
+        for (int r = 0; r < kLook; ++r) {
+            const int to_me = me - (first + r * 64);
+            places += __popcll(to_me >= 64 ? same[r] : to_me > 0 ? same[r] & ((1ull << to_me) - 1) : 0ull);
+        }
+        if (lane == 0) early[wave] = places;
+        __syncthreads();
+        turn = 0;
+        for (int w = 0; w < kSmallWaves; ++w) turn += early[w];
+        if (turn >= parts) return;
     }
 #pragma unroll
     for (int r = 0; r < kLook; ++r) {
@@ -641,11 +665,11 @@ __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
         at += __popcll(same[r]);
     }
     __syncthreads();
-    const int per = (n * a.lanes + kSmallThreads - 1) / kSmallThreads;  // rows a group of lanes
-    const int i0 = min(n, (tid / a.lanes) * per), i1 = min(n, i0 + per);
-    const int used = (n * a.lanes + 64 * per - 1) / (64 * per);         // waves with rows
+    const int per = (n * lanes + kSmallThreads - 1) / kSmallThreads;  // rows a group of lanes
+    const int i0 = min(n, (tid / lanes) * per), i1 = min(n, i0 + per);
+    const int used = (n * lanes + 64 * per - 1) / (64 * per);         // waves with rows
     for (int t = 0; t < a.tiles; ++t) {
-        const int nominal = (t * a.lanes + (tid & (a.lanes - 1))) * K;
+        const int nominal = (t * a.lanes + turn * lanes + (tid & (lanes - 1))) * K;
         const Piece<K> piece(nominal, a.dim);
         float sum[K] = {};
         if (nominal < a.dim) {
@@ -662,7 +686,7 @@ __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
                         for (int k = 0; k < K; ++k) sum[k] += v[u][k];
             }
         }
-        add_groups<K>(sum, a.lanes);
+        add_groups<K>(sum, lanes);
         if (used > 1) {
             if (t) __syncthreads();
 #pragma unroll
@@ -673,7 +697,7 @@ __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
 #pragma unroll
                     for (int k = 0; k < K; ++k) sum[k] += part[w][lane][k];
         }
-        if (tid < a.lanes && nominal < a.dim) put_word<O, K>(a, word, piece, sum);
+        if (tid < lanes && nominal < a.dim) put_word<O, K>(a, word, piece, sum);
     }
 }
 

@@ -89,11 +89,12 @@ __device__ __forceinline__ float wave_sum(float v) {
 // ---- rows of bf16 at odd addresses
 //
 // A row of an odd number of bf16 leaves the next one 2 bytes off a dword, where
-// 16-byte accesses are slow (8192 x 65533 bf16 read once: 227 us, at any dword
-// 192).  Such a row is read from the dword before, the vectors of a wave being
-// neighbours, and shifted by one element with the next lane's first dword; it
-// is written from the dword after.  Which elements a thread holds does not
-// depend on the address, so neither do the results.
+// 16-byte accesses are slow (log probabilities of 8192 x 65533: 227 us so, at
+// dwords, 65532, 189).  Such a row is read from the dword before, the vectors of
+// a wave being neighbours, and shifted by one element with the next lane's first
+// dword (206 us; distillation 505 and 439); it is written from the dword after.
+// Which elements a thread holds does not depend on the address, so neither do
+// the results.
 
 template <class T>
 __device__ __forceinline__ bool odd_row(const T* p) {
@@ -131,9 +132,9 @@ __device__ __forceinline__ void shift_in_all(u32x4 (&raw)[M], int count, const T
 }
 
 // 16 bytes of a result that is not read again here: past the caches where a
-// wave writes whole lines, through them where two waves share some (8192 x
-// 65532 bf16 read and written: 466 us past the caches, 448 through them;
-// 8192 x 65536: 412 and 430).
+// wave writes whole lines, through them where two waves share some (gradient of
+// log probabilities, 8192 x 65536 bf16: 397 us past the caches, 418 through
+// them; 8192 x 65532: 463 and 436).
 template <class T>
 __device__ __forceinline__ void store_piece(T* p, u32x4 v, bool straight) {
     if (straight) {
@@ -504,12 +505,18 @@ __device__ __forceinline__ float quad_max(float v) {
 
 constexpr int kLoads = 2;  // 16-byte loads of a thread in flight, beside as many at work
 
-// A work-group takes a row (a part of it past 131072 logits) in one pass, 16 bytes a
-// load.  For the alternatives each quad of lanes leaves the largest of its 64
-// bytes in LDS: the best `top` logits lie in the best `top` of these groups (a
-// group that does not belong to them has `top` groups with a better logit
-// before it), so at the end one wave looks for those groups and reads them again.
-// (W: row_waves)
+// A work-group takes a row (a part of it past 131072 logits) in one pass, 16
+// bytes a load: per logit a difference, an exponential and two sums against the
+// running maximum (see Stats).  For the alternatives each quad of lanes leaves
+// the largest of its 64 bytes in LDS: the best `top` logits lie in the best
+// `top` of these groups (a group that does not belong to them has `top` groups
+// with a better logit before it), so at the end one wave looks for those groups
+// and reads them again.  Memory bound where there are many logits: 8192 x 65536
+// bf16, 1.07 GB, 169 us without alternatives (6.4 TB/s), 180 with 5, 201 with
+// 63.  Few or short rows are bound by the chain of steps of the choice, about 3
+// us a row and wave: 23 x 3801 bf16 4 us, 7 with 5 alternatives.
+// (W: row_waves; at most 64 registers, for eight waves a SIMD: 4381 x 4108 fp32,
+// 5 alternatives, 24 us, at 86 registers 27)
 template <class T, bool TOP, int W>
 __global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
     constexpr int N = Elem<T>::kVec, kStep = kLoads * W * 64 * N;
@@ -708,7 +715,8 @@ __device__ __forceinline__ Stats join_parts(const Stats* part, int parts, float 
     return st;
 }
 
-// Joins the parts of split rows: a wave a row.
+// Joins the parts of split rows: a wave a row; bound by its chain of loads and
+// steps, 5 us for the 32 parts of 1 x 131072 with 8 alternatives.
 template <class T>
 __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
     const int64_t row = blockIdx.x;
@@ -770,9 +778,11 @@ struct GradArgs {
     int64_t out_stride;
 };
 
-// dx_j = (g_lp (1[j = id] - p_j) - g_H p_j (lp_j + H)) / T.  The waves of a row's
-// work-groups (several in y where there are few rows) take kGradLoads
-// neighbouring vectors of 1 KB in turn.
+// dx_j = (g_lp (1[j = id] - p_j) - g_H p_j (lp_j + H)) / T, in one pass that
+// takes p_j from the row's statistics.  The waves of a row's work-groups (several
+// in y where there are few rows: 2 x 131072 bf16 4 us, by one each 15) take
+// kGradLoads neighbouring vectors of 1 KB in turn.  Memory bound: 8192 x 65536
+// bf16, read and written, 2.15 GB, 394 us (5.4 TB/s; a copy reaches as much).
 constexpr int kGradWaves = 8, kGradLoads = 4;  // waves of a work-group at most
 
 template <class T, bool CACHED>
@@ -961,7 +971,10 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t row, cons
 // that it is read once and the gradient written once.  2^y with y = x c - r(m)
 // (see Stats) is summed up in one pass over the registers, w T p_j = 2^y (w T / S)
 // written in another; the owners of the listed entries then write
-// w T (p_j - q_j).  Memory bound: FIGURES
+// w T (p_j - q_j).  Memory bound with many rows: 8192 x 65536 bf16, 2.15 GB, 389
+// us (5.5 TB/s); 4096 x 131072 437 (4.9), where a row fills the registers of a
+// compute unit, so that no other one is read while it is summed up; the chain of
+// these steps with few: 128 x 8192 fp32 6 us.
 constexpr int kBlock = 2;
 
 template <class T, int W, int NV, bool CACHED>
@@ -1096,7 +1109,6 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
     }
 }
 
-// Longer rows, read twice: a pass for the student's statistics, one for the gradient.
 // 2^y of a logit, y = x c - r(m) (see Stats).
 __device__ __forceinline__ float mass_of(float v, float c, float ref) {
     const float r = ref * c;
@@ -1133,6 +1145,8 @@ __device__ __forceinline__ void put_masses(const T* x, T* d, int begin, int end,
     }
 }
 
+// Rows shorter than one vector of a wave, elements past the end taken one by one;
+// bound by the chain of steps (128 x 100 fp32: 5 us).
 constexpr int kShortWaves = 4;
 template <class T>
 __global__ __launch_bounds__(64 * kShortWaves) void distill_short(DistillArgs a) {
@@ -1189,7 +1203,10 @@ __global__ __launch_bounds__(64 * kShortWaves) void distill_short(DistillArgs a)
 // Rows that are split over work-groups (see distill_plan).  A first launch takes the statistics of every part,
 // and the logits of the listed tokens before a gradient in their place can
 // overwrite them; a second one joins them, every work-group for itself, and
-// writes the gradient of its part (the first part's the loss).
+// writes the gradient of its part (the first part's the loss).  Bound by the two
+// launches' chains of steps for few rows (1 x 131072 bf16: 8 us), by memory, with
+// the logits read twice, for long ones (1000 x 262144 bf16: 309 us, 5.1 TB/s of
+// the 1.57 GB).
 constexpr int kPartWaves = 4, kPartLoads = 4;  // 16-byte loads of a thread in flight
 
 template <class T>
@@ -1340,8 +1357,10 @@ struct RowPlan {
     int64_t stats, keys, bytes;  // offsets
 };
 
-// Rows from 2^16 logits on are split into parts, joined by a second launch, where
-// there are few of them; and any row whose group maxima would pass 32 KB of LDS.
+// Rows are split into parts, joined by a second launch, where too few of them
+// would fill the card: up to 255 from 65536 logits on, up to 127 from 32768 on
+// (24 x 40602 fp32, 31 alternatives: 15 us, unsplit 19; 250 x 33000: 22 and 20);
+// and so is any row whose group maxima would pass 32 KB of LDS.
 RowPlan row_plan(int32_t n, int32_t vocab, int32_t top) {
     constexpr int32_t kSplit = 32768, kMost = 131072, kLeast = 4096, kFill = 512;
     int64_t parts = 1;
@@ -1430,6 +1449,10 @@ DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     return r;
 }
 
+// As few registers as hold a row, so that several work-groups share a compute
+// unit (one reads while another is at its sums); more waves rather than more
+// vectors a thread from 32 KB on (8192 x 65536 bf16: 389 us with 16 waves of 8,
+// 411 with 8 of 16).
 template <class T, bool CACHED>
 void launch_held(const DistillArgs& a, hipStream_t st) {
     const int64_t vectors = ((int64_t)a.vocab + Elem<T>::kVec - 1) / Elem<T>::kVec;
