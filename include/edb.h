@@ -19,6 +19,9 @@
  *                     scatter into the planned slots, the whole batch
  *                     sequence replayed from one HIP graph
  *
+ * Beside them stand operators for models over words (edb_embed, edb_logprobs,
+ * edb_distill and their gradients, at the end of this file).
+ *
  * Conventions
  *   - Every call returns an edb_status.  On failure no output handle is
  *     created (*out is set to NULL) and edb_last_error() describes the error.
@@ -660,6 +663,7 @@ void edb_exec_free(edb_exec_t* e);
  *     matching *_bytes call gives; NULL where that is 0) is written before it
  *     is read and must not be shared by calls that can overlap;
  *   - results do not depend on timing: the same inputs give the same bits;
+ *   - rows of logits: vocab <= 2^30, n * ceil(vocab / 131072) <= 2^23;
  *   - n == 0 rows are allowed.
  * Errors: EDB_ERR_INVALID (NULL, sizes, strides, alignment, dtype, overlapping
  * input and output, a workspace that is too small), EDB_ERR_UNSUPPORTED (a
@@ -686,7 +690,7 @@ edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* dout, int32
 
 /* Log probabilities of given tokens under softmax(logits / temperature), with
  * the entropy and the best alternatives of every row, in one pass.
- *   logits   [n x vocab], vocab <= 2^30; a token is masked out by -inf
+ *   logits   [n x vocab]; a token is masked out by -inf
  *   ids      int32[n], or NULL: no given tokens (logprob must be NULL then)
  *   logprob  float[n] or NULL: ln p of the given token (-inf if masked out)
  *   entropy  float[n] or NULL: -sum p ln p

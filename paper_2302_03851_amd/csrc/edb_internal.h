@@ -1,6 +1,7 @@
 // Internal structures shared by the host-side parts of the library.
 #pragma once
 
+#include <new>
 #include <cstdint>
 #include <map>
 #include <string>
@@ -41,6 +42,18 @@ namespace edb {
 // Thread-local last-error message; returns the status for `return fail(...)`.
 edb_status fail(edb_status st, const std::string& msg);
 void clear_error();
+
+// The body of an entry point that allocates only for its messages: running out
+// of host memory there does not cross the C interface.
+template <class F>
+edb_status guarded(F&& body) {
+    try {
+        return body();
+    } catch (const std::bad_alloc&) {
+        clear_error();
+        return EDB_ERR_OOM;
+    }
+}
 
 // edb_build_graph with the acyclicity check optional: without it the graph
 // must go to a frontier policy's schedule, which reports a cycle itself (no

@@ -746,10 +746,18 @@ void launch_embed(const EmbedArgs& a, hipStream_t st) {
     // 16 bytes of the result a lane, so that a wave writes whole lines
     constexpr int kWhole = Elem<O>::kVec;
     const int k = a.dim >= kWhole ? kWhole : a.dim >= 4 ? 4 : 1;
-    const dim3 grid((unsigned)(((int64_t)a.n * ((a.dim + k - 1) / k) + 255) / 256));
-    if (k == kWhole) embed_kernel<T, O, kWhole><<<grid, 256, 0, st>>>(a);
-    else if (k == 4) embed_kernel<T, O, 4><<<grid, 256, 0, st>>>(a);
-    else embed_kernel<T, O, 1><<<grid, 256, 0, st>>>(a);
+    // a launch has less than 2^32 threads: more are taken in slices of rows
+    const int64_t pieces = (a.dim + k - 1) / k, most = (INT64_C(1) << 31) / pieces;
+    for (int64_t i = 0; i < a.n; i += most) {
+        EmbedArgs b = a;
+        b.ids = a.ids + i;
+        b.n = (int32_t)(a.n - i < most ? a.n - i : most);
+        b.out = static_cast<O*>(a.out) + i * a.out_stride;
+        const dim3 grid((unsigned)((b.n * pieces + 255) / 256));
+        if (k == kWhole) embed_kernel<T, O, kWhole><<<grid, 256, 0, st>>>(b);
+        else if (k == 4) embed_kernel<T, O, 4><<<grid, 256, 0, st>>>(b);
+        else embed_kernel<T, O, 1><<<grid, 256, 0, st>>>(b);
+    }
 }
 
 // How the gradient's work is laid out, and its scratch memory.
@@ -827,118 +835,124 @@ void launch_sums(const GradPlan& g, const SumArgs& a, hipStream_t st) {
 extern "C" edb_status edb_embed(const int32_t* ids, int32_t n, const void* table, int32_t table_dtype, int32_t vocab,
                                 int32_t dim, int64_t table_stride, float scale, void* out, int32_t out_dtype,
                                 int64_t out_stride, void* stream) {
-    const char* who = "edb_embed";
-    if (edb_status st = check_table(who, n, vocab, dim, out_dtype, table_dtype, out_stride, table_stride, scale)) return st;
-    if (n == 0) {
-        edb::clear_error();
-        return EDB_OK;
-    }
-    if (!ids || !table || !out) return fail(EDB_ERR_INVALID, "edb_embed: NULL argument");
-    if (!element_aligned(table, table_dtype) || !element_aligned(out, out_dtype))
-        return fail(EDB_ERR_INVALID, "edb_embed: the table and the result must be aligned to their elements");
-    if (overlap(table, ((vocab - 1) * table_stride + dim) * elem_bytes(table_dtype), out,
-                ((n - 1) * out_stride + dim) * elem_bytes(out_dtype)))
-        return fail(EDB_ERR_INVALID, "edb_embed: the result overlaps the table");
-    if ((int64_t)n * dim > (INT64_C(1) << 38)) return fail(EDB_ERR_UNSUPPORTED, "edb_embed: n * dim exceeds 2^38");
-    const EmbedArgs a{ids, n, vocab, dim, table, table_stride, scale, out, out_stride};
-    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (table_dtype == EDB_F32) {
-        if (out_dtype == EDB_F32) launch_embed<float, float>(a, st);
-        else launch_embed<float, bf16>(a, st);
-    } else {
-        if (out_dtype == EDB_F32) launch_embed<bf16, float>(a, st);
-        else launch_embed<bf16, bf16>(a, st);
-    }
-    return launched(who);
+    return edb::guarded([&]() -> edb_status {
+        const char* who = "edb_embed";
+        if (edb_status st = check_table(who, n, vocab, dim, out_dtype, table_dtype, out_stride, table_stride, scale)) return st;
+        if (n == 0) {
+            edb::clear_error();
+            return EDB_OK;
+        }
+        if (!ids || !table || !out) return fail(EDB_ERR_INVALID, "edb_embed: NULL argument");
+        if (!element_aligned(table, table_dtype) || !element_aligned(out, out_dtype))
+            return fail(EDB_ERR_INVALID, "edb_embed: the table and the result must be aligned to their elements");
+        if (overlap(table, ((vocab - 1) * table_stride + dim) * elem_bytes(table_dtype), out,
+                    ((n - 1) * out_stride + dim) * elem_bytes(out_dtype)))
+            return fail(EDB_ERR_INVALID, "edb_embed: the result overlaps the table");
+        if ((int64_t)n * dim > (INT64_C(1) << 38)) return fail(EDB_ERR_UNSUPPORTED, "edb_embed: n * dim exceeds 2^38");
+        const EmbedArgs a{ids, n, vocab, dim, table, table_stride, scale, out, out_stride};
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        if (table_dtype == EDB_F32) {
+            if (out_dtype == EDB_F32) launch_embed<float, float>(a, st);
+            else launch_embed<float, bf16>(a, st);
+        } else {
+            if (out_dtype == EDB_F32) launch_embed<bf16, float>(a, st);
+            else launch_embed<bf16, bf16>(a, st);
+        }
+        return launched(who);
+    });
 }
 
 extern "C" edb_status edb_embed_grad_bytes(int32_t n, int32_t vocab, int32_t dim, int64_t* bytes) {
-    if (!bytes) return fail(EDB_ERR_INVALID, "edb_embed_grad_bytes: NULL argument");
-    if (edb_status st = check_table("edb_embed_grad_bytes", n, vocab, dim, EDB_F32, EDB_F32, dim, dim, 1.f)) return st;
-    *bytes = grad_plan(n, vocab, dim).bytes;
-    edb::clear_error();
-    return EDB_OK;
+    return edb::guarded([&]() -> edb_status {
+        if (!bytes) return fail(EDB_ERR_INVALID, "edb_embed_grad_bytes: NULL argument");
+        if (edb_status st = check_table("edb_embed_grad_bytes", n, vocab, dim, EDB_F32, EDB_F32, dim, dim, 1.f)) return st;
+        *bytes = grad_plan(n, vocab, dim).bytes;
+        edb::clear_error();
+        return EDB_OK;
+    });
 }
 
 extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* dout, int32_t dout_dtype, int32_t vocab,
                                      int32_t dim, int64_t dout_stride, float scale, int32_t accumulate, void* dtable,
                                      int32_t dtable_dtype, int64_t dtable_stride, void* workspace,
                                      int64_t workspace_bytes, void* stream) {
-    const char* who = "edb_embed_grad";
-    if (edb_status st = check_table(who, n, vocab, dim, dout_dtype, dtable_dtype, dout_stride, dtable_stride, scale)) return st;
-    if (!dtable || (n && (!ids || !dout))) return fail(EDB_ERR_INVALID, "edb_embed_grad: NULL argument");
-    if (!element_aligned(dout, dout_dtype) || !element_aligned(dtable, dtable_dtype))
-        return fail(EDB_ERR_INVALID, "edb_embed_grad: both gradients must be aligned to their elements");
-    if (n && overlap(dout, ((n - 1) * dout_stride + dim) * elem_bytes(dout_dtype), dtable,
-                     ((vocab - 1) * dtable_stride + dim) * elem_bytes(dtable_dtype)))
-        return fail(EDB_ERR_INVALID, "edb_embed_grad: the table's gradient overlaps the rows' gradients");
-    const GradPlan g = grad_plan(n, vocab, dim);
-    if (workspace_bytes < g.bytes || (g.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
-        return fail(EDB_ERR_INVALID, "edb_embed_grad: a 16-byte aligned workspace of " + std::to_string(g.bytes) +
-                                         " bytes is needed");
-    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const int64_t row_bytes = dim * elem_bytes(dtable_dtype);
-    if (n <= kSmall) {
-        const int64_t fit = 16384 / row_bytes;  // rows that a work-group zeroes
-        const int fill_rows = (int)(fit < 1 ? 1 : fit > kFillRows ? kFillRows : fit);
-        const int fill_groups = accumulate ? 0 : (int)(((int64_t)vocab + fill_rows - 1) / fill_rows);
-        const SmallArgs a{ids,   n,          (uint32_t)vocab, dim,           g.lanes,   g.tiles_y,  dout, dout_stride,
-                          scale, accumulate, dtable,          dtable_stride, fill_rows, fill_groups};
+    return edb::guarded([&]() -> edb_status {
+        const char* who = "edb_embed_grad";
+        if (edb_status st = check_table(who, n, vocab, dim, dout_dtype, dtable_dtype, dout_stride, dtable_stride, scale)) return st;
+        if (!dtable || (n && (!ids || !dout))) return fail(EDB_ERR_INVALID, "edb_embed_grad: NULL argument");
+        if (!element_aligned(dout, dout_dtype) || !element_aligned(dtable, dtable_dtype))
+            return fail(EDB_ERR_INVALID, "edb_embed_grad: both gradients must be aligned to their elements");
+        if (n && overlap(dout, ((n - 1) * dout_stride + dim) * elem_bytes(dout_dtype), dtable,
+                         ((vocab - 1) * dtable_stride + dim) * elem_bytes(dtable_dtype)))
+            return fail(EDB_ERR_INVALID, "edb_embed_grad: the table's gradient overlaps the rows' gradients");
+        const GradPlan g = grad_plan(n, vocab, dim);
+        if (workspace_bytes < g.bytes || (g.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+            return fail(EDB_ERR_INVALID, "edb_embed_grad: a 16-byte aligned workspace of " + std::to_string(g.bytes) +
+                                             " bytes is needed");
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        const int64_t row_bytes = dim * elem_bytes(dtable_dtype);
+        if (n <= kSmall) {
+            const int64_t fit = 16384 / row_bytes;  // rows that a work-group zeroes
+            const int fill_rows = (int)(fit < 1 ? 1 : fit > kFillRows ? kFillRows : fit);
+            const int fill_groups = accumulate ? 0 : (int)(((int64_t)vocab + fill_rows - 1) / fill_rows);
+            const SmallArgs a{ids,   n,          (uint32_t)vocab, dim,           g.lanes,   g.tiles_y,  dout, dout_stride,
+                              scale, accumulate, dtable,          dtable_stride, fill_rows, fill_groups};
+            if (dout_dtype == EDB_F32) {
+                if (dtable_dtype == EDB_F32) launch_small<float, float>(g.piece, a, st);
+                else launch_small<float, bf16>(g.piece, a, st);
+            } else {
+                if (dtable_dtype == EDB_F32) launch_small<bf16, float>(g.piece, a, st);
+                else launch_small<bf16, bf16>(g.piece, a, st);
+            }
+            return launched(who);
+        }
+        char* ws = static_cast<char*>(workspace);
+        auto sorted = [&](int i) { return reinterpret_cast<Pair*>(ws + g.sorted[i]); };
+        SortArgs s{};
+        s.n = n;
+        s.vocab = (uint32_t)vocab;
+        int last = 0;
+        s.tiles = g.sort_tiles;
+        s.counts = reinterpret_cast<uint32_t*>(ws + g.counts);
+        s.totals = reinterpret_cast<uint32_t*>(ws + g.totals);
+        s.bits = g.digit;
+        const bool scan = g.sort_tiles > kSumTiles;
+        const int launches = g.passes * (scan ? 3 : 2);
+        int launch = 0;
+        // the work-groups of the next launch, its share of the zero rows behind `groups` of its own
+        auto next = [&](int groups) {
+            const int64_t first = (int64_t)vocab * launch / launches, end = (int64_t)vocab * (launch + 1) / launches;
+            const int64_t per = row_bytes < kFillBytes ? kFillBytes / row_bytes : 1;
+            ++launch;
+            s.fill = Fill{static_cast<char*>(dtable), row_bytes, dtable_stride * elem_bytes(dtable_dtype), (uint32_t)first,
+                          (uint32_t)(end - first), groups, (int32_t)per};
+            return (unsigned)(groups + (accumulate ? 0 : (end - first + per - 1) / per));
+        };
+        for (int p = 0; p < g.passes; ++p) {
+            s.ids = p ? nullptr : ids;
+            s.in = sorted((p + 1) & 1);
+            s.out = sorted(p & 1);
+            s.shift = p * g.digit;
+            last = p & 1;
+            const unsigned count = next(g.sort_tiles);
+            sort_count<<<count, 256, 0, st>>>(s);
+            if (scan) {
+                const unsigned sums = next(((1 << g.digit) + kScanBins - 1) / kScanBins);
+                sort_scan<<<sums, 256, 0, st>>>(s);
+            }
+            const unsigned scatter = next(g.sort_tiles);
+            if (scan) sort_scatter<false><<<scatter, 256, 0, st>>>(s);
+            else sort_scatter<true><<<scatter, 256, 0, st>>>(s);
+        }
+        const SumArgs a{sorted(last), n, g.chunk, (uint32_t)vocab, dim, g.lanes, dout, dout_stride, scale,
+                        accumulate, dtable, dtable_stride, reinterpret_cast<float*>(ws + g.partial)};
         if (dout_dtype == EDB_F32) {
-            if (dtable_dtype == EDB_F32) launch_small<float, float>(g.piece, a, st);
-            else launch_small<float, bf16>(g.piece, a, st);
+            if (dtable_dtype == EDB_F32) launch_sums<float, float>(g, a, st);
+            else launch_sums<float, bf16>(g, a, st);
         } else {
-            if (dtable_dtype == EDB_F32) launch_small<bf16, float>(g.piece, a, st);
-            else launch_small<bf16, bf16>(g.piece, a, st);
+            if (dtable_dtype == EDB_F32) launch_sums<bf16, float>(g, a, st);
+            else launch_sums<bf16, bf16>(g, a, st);
         }
         return launched(who);
-    }
-    char* ws = static_cast<char*>(workspace);
-    auto sorted = [&](int i) { return reinterpret_cast<Pair*>(ws + g.sorted[i]); };
-    SortArgs s{};
-    s.n = n;
-    s.vocab = (uint32_t)vocab;
-    int last = 0;
-    s.tiles = g.sort_tiles;
-    s.counts = reinterpret_cast<uint32_t*>(ws + g.counts);
-    s.totals = reinterpret_cast<uint32_t*>(ws + g.totals);
-    s.bits = g.digit;
-    const bool scan = g.sort_tiles > kSumTiles;
-    const int launches = g.passes * (scan ? 3 : 2);
-    int launch = 0;
-    // the work-groups of the next launch, its share of the zero rows behind `groups` of its own
-    auto next = [&](int groups) {
-        const int64_t first = (int64_t)vocab * launch / launches, end = (int64_t)vocab * (launch + 1) / launches;
-        const int64_t per = row_bytes < kFillBytes ? kFillBytes / row_bytes : 1;
-        ++launch;
-        s.fill = Fill{static_cast<char*>(dtable), row_bytes, dtable_stride * elem_bytes(dtable_dtype), (uint32_t)first,
-                      (uint32_t)(end - first), groups, (int32_t)per};
-        return (unsigned)(groups + (accumulate ? 0 : (end - first + per - 1) / per));
-    };
-    for (int p = 0; p < g.passes; ++p) {
-        s.ids = p ? nullptr : ids;
-        s.in = sorted((p + 1) & 1);
-        s.out = sorted(p & 1);
-        s.shift = p * g.digit;
-        last = p & 1;
-        const unsigned count = next(g.sort_tiles);
-        sort_count<<<count, 256, 0, st>>>(s);
-        if (scan) {
-            const unsigned sums = next(((1 << g.digit) + kScanBins - 1) / kScanBins);
-            sort_scan<<<sums, 256, 0, st>>>(s);
-        }
-        const unsigned scatter = next(g.sort_tiles);
-        if (scan) sort_scatter<false><<<scatter, 256, 0, st>>>(s);
-        else sort_scatter<true><<<scatter, 256, 0, st>>>(s);
-    }
-    const SumArgs a{sorted(last), n, g.chunk, (uint32_t)vocab, dim, g.lanes, dout, dout_stride, scale,
-                    accumulate, dtable, dtable_stride, reinterpret_cast<float*>(ws + g.partial)};
-    if (dout_dtype == EDB_F32) {
-        if (dtable_dtype == EDB_F32) launch_sums<float, float>(g, a, st);
-        else launch_sums<float, bf16>(g, a, st);
-    } else {
-        if (dtable_dtype == EDB_F32) launch_sums<bf16, float>(g, a, st);
-        else launch_sums<bf16, bf16>(g, a, st);
-    }
-    return launched(who);
+    });
 }

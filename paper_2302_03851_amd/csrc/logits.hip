@@ -1476,153 +1476,206 @@ void launch_distill(const DistillArgs& a, hipStream_t st) {
     else launch_held<T, false>(a, st);
 }
 
+// A launch has less than 2^32 threads: more rows than this are taken in equal slices, one after the other.
+constexpr int32_t kMostRows = 1 << 21;
+
+template <class F>
+edb_status in_slices(int32_t n, F&& call) {
+    const int32_t slices = (n + kMostRows - 1) / kMostRows, per = (int32_t)(((int64_t)n + slices - 1) / slices);
+    for (int64_t i = 0; i < n; i += per)
+        if (edb_status st = call(i, (int32_t)(n - i < per ? n - i : per))) return st;
+    return EDB_OK;
+}
+
+template <class P>
+P* rows_from(P* p, int64_t elems) {
+    return p ? p + elems : nullptr;
+}
+const void* rows_from(const void* p, int64_t row, int64_t stride, int32_t dtype) {
+    return static_cast<const char*>(p) + row * stride * (dtype == EDB_BF16 ? 2 : 4);
+}
+
 float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
 
 }  // namespace
 
 extern "C" edb_status edb_logprobs_bytes(int32_t n, int32_t vocab, int32_t dtype, int32_t top, int64_t* bytes) {
-    if (!bytes) return fail(EDB_ERR_INVALID, "edb_logprobs_bytes: NULL argument");
-    if (edb_status st = check_rows("edb_logprobs_bytes", bytes, dtype, n, vocab, vocab, 1.f)) return st;
-    if (top < 0 || top > EDB_LOGPROBS_MAX_TOP)
-        return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs_bytes: top must be in [0, " +
-                                             std::to_string(EDB_LOGPROBS_MAX_TOP) + "]");
-    *bytes = row_plan(n, vocab, top).bytes;
-    edb::clear_error();
-    return EDB_OK;
+    return edb::guarded([&]() -> edb_status {
+        if (!bytes) return fail(EDB_ERR_INVALID, "edb_logprobs_bytes: NULL argument");
+        if (edb_status st = check_rows("edb_logprobs_bytes", bytes, dtype, n, vocab, vocab, 1.f)) return st;
+        if (top < 0 || top > EDB_LOGPROBS_MAX_TOP)
+            return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs_bytes: top must be in [0, " +
+                                                 std::to_string(EDB_LOGPROBS_MAX_TOP) + "]");
+        *bytes = row_plan(n, vocab, top).bytes;
+        edb::clear_error();
+        return EDB_OK;
+    });
 }
 
 extern "C" edb_status edb_logprobs(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
                                    const int32_t* ids, float temperature, int32_t top, float* logprob, float* entropy,
                                    float* stats, int32_t* top_ids, float* top_logprobs, void* workspace,
                                    int64_t workspace_bytes, void* stream) {
-    const char* who = "edb_logprobs";
-    if (edb_status st = check_rows(who, logits, dtype, n, vocab, stride, temperature)) return st;
-    if (top < 0 || top > EDB_LOGPROBS_MAX_TOP)
-        return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs: top must be in [0, " + std::to_string(EDB_LOGPROBS_MAX_TOP) + "]");
-    if (logprob && !ids) return fail(EDB_ERR_INVALID, "edb_logprobs: log probabilities need the given tokens");
-    if (n && top && (!top_ids || !top_logprobs)) return fail(EDB_ERR_INVALID, "edb_logprobs: NULL list of alternatives");
-    if (n == 0) {
-        edb::clear_error();
-        return EDB_OK;
-    }
-    const RowPlan r = row_plan(n, vocab, top);
-    if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
-        return fail(EDB_ERR_INVALID, "edb_logprobs: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
-                                         " bytes is needed");
-    if ((int64_t)n * r.parts > INT32_MAX) return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs: more than 2^31 parts of rows");
-    char* ws = static_cast<char*>(workspace);
-    const LogprobArgs a{logits,
-                        stride,
-                        n,
-                        vocab,
-                        ids,
-                        log2e_over(temperature),
-                        (float)(1.0 / (double)temperature),
-                        top,
-                        logprob,
-                        entropy,
-                        stats,
-                        top_ids,
-                        top_logprobs,
-                        r.part,
-                        r.parts,
-                        reinterpret_cast<Stats*>(ws + r.stats),
-                        reinterpret_cast<Key*>(ws + r.keys)};
-    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const dim3 grid(n * r.parts);
-    if (dtype == EDB_F32) {
-        const size_t lds = group_bytes<float>(r, vocab);
-        launch_logprobs<float>(a, grid, lds, st);
-        if (r.parts > 1) logprobs_join<float><<<n, 64, 0, st>>>(a);
-    } else {
-        const size_t lds = group_bytes<bf16>(r, vocab);
-        launch_logprobs<bf16>(a, grid, lds, st);
-        if (r.parts > 1) logprobs_join<bf16><<<n, 64, 0, st>>>(a);
-    }
-    return launched(who);
+    return edb::guarded([&]() -> edb_status {
+        const char* who = "edb_logprobs";
+        if (edb_status st = check_rows(who, logits, dtype, n, vocab, stride, temperature)) return st;
+        if (top < 0 || top > EDB_LOGPROBS_MAX_TOP)
+            return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs: top must be in [0, " + std::to_string(EDB_LOGPROBS_MAX_TOP) + "]");
+        if (logprob && !ids) return fail(EDB_ERR_INVALID, "edb_logprobs: log probabilities need the given tokens");
+        if (n && top && (!top_ids || !top_logprobs)) return fail(EDB_ERR_INVALID, "edb_logprobs: NULL list of alternatives");
+        if (n == 0) {
+            edb::clear_error();
+            return EDB_OK;
+        }
+        const RowPlan r = row_plan(n, vocab, top);
+        if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+            return fail(EDB_ERR_INVALID, "edb_logprobs: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
+                                             " bytes is needed");
+        if (n > kMostRows)
+            return in_slices(n, [&](int64_t i, int32_t m) {
+                return edb_logprobs(rows_from(logits, i, stride, dtype), dtype, m, vocab, stride, rows_from(ids, i),
+                                    temperature, top, rows_from(logprob, i), rows_from(entropy, i),
+                                    rows_from(stats, 2 * i), rows_from(top_ids, i * top),
+                                    rows_from(top_logprobs, i * top), workspace, workspace_bytes, stream);
+            });
+        if ((int64_t)n * r.parts > kMostRows * INT64_C(4))
+            return fail(EDB_ERR_UNSUPPORTED, "edb_logprobs: more than 2^23 parts of rows");
+        char* ws = static_cast<char*>(workspace);
+        const LogprobArgs a{logits,
+                            stride,
+                            n,
+                            vocab,
+                            ids,
+                            log2e_over(temperature),
+                            (float)(1.0 / (double)temperature),
+                            top,
+                            logprob,
+                            entropy,
+                            stats,
+                            top_ids,
+                            top_logprobs,
+                            r.part,
+                            r.parts,
+                            reinterpret_cast<Stats*>(ws + r.stats),
+                            reinterpret_cast<Key*>(ws + r.keys)};
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        const dim3 grid(n * r.parts);
+        if (dtype == EDB_F32) {
+            const size_t lds = group_bytes<float>(r, vocab);
+            launch_logprobs<float>(a, grid, lds, st);
+            if (r.parts > 1) logprobs_join<float><<<n, 64, 0, st>>>(a);
+        } else {
+            const size_t lds = group_bytes<bf16>(r, vocab);
+            launch_logprobs<bf16>(a, grid, lds, st);
+            if (r.parts > 1) logprobs_join<bf16><<<n, 64, 0, st>>>(a);
+        }
+        return launched(who);
+    });
 }
 
 extern "C" edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
                                         const int32_t* ids, float temperature, const float* stats,
                                         const float* entropy, const float* g_logprob, const float* g_entropy,
                                         void* dlogits, int64_t dlogits_stride, void* stream) {
-    const char* who = "edb_logprobs_grad";
-    if (edb_status st = check_rows(who, logits, dtype, n, vocab, stride, temperature)) return st;
-    if (n && (!ids || !stats || !dlogits)) return fail(EDB_ERR_INVALID, "edb_logprobs_grad: NULL argument");
-    if (g_entropy && !entropy) return fail(EDB_ERR_INVALID, "edb_logprobs_grad: the entropies' gradient needs the entropies");
-    if (edb_status st = check_grad(who, logits, stride, dlogits, dlogits_stride, dtype, n, vocab)) return st;
-    if (n == 0) {
-        edb::clear_error();
-        return EDB_OK;
-    }
-    GradArgs a{logits, stride,  n,         vocab,     ids,     log2e_over(temperature), (float)(1.0 / (double)temperature),
-               stats,  entropy, g_logprob, g_entropy, dlogits, dlogits_stride};
-    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    // work-groups of as many waves as a row has vectors for, and enough of them for the card
-    const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec;
-    const int32_t turns = (vocab + 64 * vec * kGradLoads - 1) / (64 * vec * kGradLoads);
-    const int32_t waves = turns < kGradWaves ? turns : kGradWaves, most = (turns + waves - 1) / waves;
-    const int32_t wanted = n < kGradFill ? (kGradFill + n - 1) / n : 1;
-    const dim3 grid(n, wanted < most ? wanted : most);
-    const bool cached = caches_hold(n, vocab, dtype);
-    if (dtype == EDB_F32) launch_grad<float>(a, cached, grid, 64 * waves, st);
-    else launch_grad<bf16>(a, cached, grid, 64 * waves, st);
-    return launched(who);
+    return edb::guarded([&]() -> edb_status {
+        const char* who = "edb_logprobs_grad";
+        if (edb_status st = check_rows(who, logits, dtype, n, vocab, stride, temperature)) return st;
+        if (n && (!ids || !stats || !dlogits)) return fail(EDB_ERR_INVALID, "edb_logprobs_grad: NULL argument");
+        if (g_entropy && !entropy) return fail(EDB_ERR_INVALID, "edb_logprobs_grad: the entropies' gradient needs the entropies");
+        if (edb_status st = check_grad(who, logits, stride, dlogits, dlogits_stride, dtype, n, vocab)) return st;
+        if (n == 0) {
+            edb::clear_error();
+            return EDB_OK;
+        }
+        if (n > kMostRows)
+            return in_slices(n, [&](int64_t i, int32_t m) {
+                return edb_logprobs_grad(rows_from(logits, i, stride, dtype), dtype, m, vocab, stride, ids + i,
+                                         temperature, stats + 2 * i, rows_from(entropy, i), rows_from(g_logprob, i),
+                                         rows_from(g_entropy, i),
+                                         const_cast<void*>(rows_from(dlogits, i, dlogits_stride, dtype)),
+                                         dlogits_stride, stream);
+            });
+        GradArgs a{logits, stride,  n,         vocab,     ids,     log2e_over(temperature), (float)(1.0 / (double)temperature),
+                   stats,  entropy, g_logprob, g_entropy, dlogits, dlogits_stride};
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        // work-groups of as many waves as a row has vectors for, and enough of them for the card
+        const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec;
+        const int32_t turns = (vocab + 64 * vec * kGradLoads - 1) / (64 * vec * kGradLoads);
+        const int32_t waves = turns < kGradWaves ? turns : kGradWaves, most = (turns + waves - 1) / waves;
+        const int32_t wanted = n < kGradFill ? (kGradFill + n - 1) / n : 1;
+        const dim3 grid(n, wanted < most ? wanted : most);
+        const bool cached = caches_hold(n, vocab, dtype);
+        if (dtype == EDB_F32) launch_grad<float>(a, cached, grid, 64 * waves, st);
+        else launch_grad<bf16>(a, cached, grid, 64 * waves, st);
+        return launched(who);
+    });
 }
 
 extern "C" edb_status edb_distill_bytes(int32_t n, int32_t vocab, int32_t dtype, int32_t top, int64_t* bytes) {
-    if (!bytes) return fail(EDB_ERR_INVALID, "edb_distill_bytes: NULL argument");
-    if (edb_status st = check_rows("edb_distill_bytes", bytes, dtype, n, vocab, vocab, 1.f)) return st;
-    if (top < 1 || top > EDB_DISTILL_MAX_TOP)
-        return fail(EDB_ERR_UNSUPPORTED, "edb_distill_bytes: top must be in [1, " +
-                                             std::to_string(EDB_DISTILL_MAX_TOP) + "]");
-    *bytes = distill_plan(n, vocab, dtype, top).bytes;
-    edb::clear_error();
-    return EDB_OK;
+    return edb::guarded([&]() -> edb_status {
+        if (!bytes) return fail(EDB_ERR_INVALID, "edb_distill_bytes: NULL argument");
+        if (edb_status st = check_rows("edb_distill_bytes", bytes, dtype, n, vocab, vocab, 1.f)) return st;
+        if (top < 1 || top > EDB_DISTILL_MAX_TOP)
+            return fail(EDB_ERR_UNSUPPORTED, "edb_distill_bytes: top must be in [1, " +
+                                                 std::to_string(EDB_DISTILL_MAX_TOP) + "]");
+        *bytes = distill_plan(n, vocab, dtype, top).bytes;
+        edb::clear_error();
+        return EDB_OK;
+    });
 }
 
 extern "C" edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
                                   const int32_t* top_ids, const float* top_logits, int32_t top, float temperature,
                                   const float* weight, float* loss, void* dlogits, int64_t dlogits_stride,
                                   void* workspace, int64_t workspace_bytes, void* stream) {
-    const char* who = "edb_distill";
-    if (edb_status st = check_rows(who, logits, dtype, n, vocab, stride, temperature)) return st;
-    if (top < 1 || top > EDB_DISTILL_MAX_TOP)
-        return fail(EDB_ERR_UNSUPPORTED, "edb_distill: top must be in [1, " + std::to_string(EDB_DISTILL_MAX_TOP) + "]");
-    if (n && (!top_ids || !top_logits || !loss)) return fail(EDB_ERR_INVALID, "edb_distill: NULL argument");
-    if (dlogits)
-        if (edb_status st = check_grad(who, logits, stride, dlogits, dlogits_stride, dtype, n, vocab)) return st;
-    if (n == 0) {
-        edb::clear_error();
-        return EDB_OK;
-    }
-    const DistillPlan r = distill_plan(n, vocab, dtype, top);
-    if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
-        return fail(EDB_ERR_INVALID, "edb_distill: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
-                                         " bytes is needed");
-    if ((int64_t)n * r.parts > INT32_MAX) return fail(EDB_ERR_UNSUPPORTED, "edb_distill: more than 2^31 parts of rows");
-    char* ws = static_cast<char*>(workspace);
-    const DistillArgs a{logits,
-                        stride,
-                        n,
-                        vocab,
-                        top_ids,
-                        top_logits,
-                        top,
-                        log2e_over(temperature),
-                        (float)(1.0 / (double)temperature),
-                        temperature,
-                        weight,
-                        loss,
-                        dlogits,
-                        dlogits_stride,
-                        r.cached,
-                        r.part,
-                        r.parts,
-                        reinterpret_cast<Stats*>(ws + r.stats),
-                        reinterpret_cast<float*>(ws + r.listed)};
-    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (dtype == EDB_F32) launch_distill<float>(a, st);
-    else launch_distill<bf16>(a, st);
-    return launched(who);
+    return edb::guarded([&]() -> edb_status {
+        const char* who = "edb_distill";
+        if (edb_status st = check_rows(who, logits, dtype, n, vocab, stride, temperature)) return st;
+        if (top < 1 || top > EDB_DISTILL_MAX_TOP)
+            return fail(EDB_ERR_UNSUPPORTED, "edb_distill: top must be in [1, " + std::to_string(EDB_DISTILL_MAX_TOP) + "]");
+        if (n && (!top_ids || !top_logits || !loss)) return fail(EDB_ERR_INVALID, "edb_distill: NULL argument");
+        if (dlogits)
+            if (edb_status st = check_grad(who, logits, stride, dlogits, dlogits_stride, dtype, n, vocab)) return st;
+        if (n == 0) {
+            edb::clear_error();
+            return EDB_OK;
+        }
+        const DistillPlan r = distill_plan(n, vocab, dtype, top);
+        if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+            return fail(EDB_ERR_INVALID, "edb_distill: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
+                                             " bytes is needed");
+        if (n > kMostRows)
+            return in_slices(n, [&](int64_t i, int32_t m) {
+                return edb_distill(rows_from(logits, i, stride, dtype), dtype, m, vocab, stride, top_ids + i * top,
+                                   top_logits + i * top, top, temperature, rows_from(weight, i), loss + i,
+                                   dlogits ? const_cast<void*>(rows_from(dlogits, i, dlogits_stride, dtype)) : nullptr,
+                                   dlogits_stride, workspace, workspace_bytes, stream);
+            });
+        if ((int64_t)n * r.parts > kMostRows * INT64_C(4))
+            return fail(EDB_ERR_UNSUPPORTED, "edb_distill: more than 2^23 parts of rows");
+        char* ws = static_cast<char*>(workspace);
+        const DistillArgs a{logits,
+                            stride,
+                            n,
+                            vocab,
+                            top_ids,
+                            top_logits,
+                            top,
+                            log2e_over(temperature),
+                            (float)(1.0 / (double)temperature),
+                            temperature,
+                            weight,
+                            loss,
+                            dlogits,
+                            dlogits_stride,
+                            r.cached,
+                            r.part,
+                            r.parts,
+                            reinterpret_cast<Stats*>(ws + r.stats),
+                            reinterpret_cast<float*>(ws + r.listed)};
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        if (dtype == EDB_F32) launch_distill<float>(a, st);
+        else launch_distill<bf16>(a, st);
+        return launched(who);
+    });
 }

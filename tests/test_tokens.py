@@ -700,6 +700,30 @@ def test_distill_differences():
             assert abs(float((f(x.double() + step) - f(x.double() - step)) / 2e-4 - d[i, j])) <= 1e-5
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_millions_of_rows(dtype):
+    """More rows than one launch takes: the same bits as the rows by themselves."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(21)
+    n, V = (1 << 22) + 77, 5
+    x = torch.randn((n, V), generator=g, device="cuda").to(dtype)
+    ids = torch.randint(-1, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    q = torch.randint(-1, V, (n, 2), generator=g, device="cuda", dtype=torch.int32), torch.randn((n, 2), generator=g, device="cuda")
+    w = torch.randn(n, generator=g, device="cuda")
+
+    def rows(a, b):
+        part = x[a:b].contiguous()
+        r = tokens.logprobs(part, ids[a:b], 0.9, 2)
+        d = tokens.logprobs_grad(part, ids[a:b], r.stats, r.entropy, w[a:b], w[a:b], 0.9)
+        return [*r, d, *tokens.distill(part, q[0][a:b], q[1][a:b], 1.1, w[a:b])]
+
+    whole = rows(0, n)
+    for a, b in ((0, 1000), (1398000, 1399000), (2097000, 2098000), (2796000, 2797000), (n - 1000, n)):
+        for s, t in zip(whole, rows(a, b)):
+            assert torch.equal(s[a:b].contiguous().view(torch.uint8), t.view(torch.uint8))
+
+
 # ---- streams and graphs ------------------------------------------------------
 
 
