@@ -13,6 +13,7 @@
 
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "edb_internal.h"
 #include "row_access.h"
@@ -84,6 +85,22 @@ __device__ __forceinline__ float wave_sum(float v) {
     const auto rows = both_rows(v);
     const auto halves = both_halves(rows.a + rows.b);
     return halves.a + halves.b;
+}
+
+// Sums over the lanes up to this one: inside rows of 16, then from row to row.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    auto from = [](uint32_t v, auto move, auto rows) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(move)::value, decltype(rows)::value, 0xf, false);
+    };
+    using std::integral_constant;
+    constexpr integral_constant<int, 0xf> every;
+    v += from(v, integral_constant<int, 0x111>(), every);  // the lane 1, 2, 4, 8 before, 0 from outside the row
+    v += from(v, integral_constant<int, 0x112>(), every);
+    v += from(v, integral_constant<int, 0x114>(), every);
+    v += from(v, integral_constant<int, 0x118>(), every);
+    v += from(v, integral_constant<int, 0x142>(), integral_constant<int, 0xa>());  // each row's last lane to the next row
+    v += from(v, integral_constant<int, 0x143>(), integral_constant<int, 0xc>());  // lane 31 to the upper half
+    return v;
 }
 
 // ---- rows of bf16 at odd addresses
@@ -426,12 +443,11 @@ struct Best {
         return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 |
                (uint32_t)__builtin_amdgcn_readlane((int)key, lane);
     }
-    // One entry a lane, 0 for none.  Past kWait entries they are only counted.
+    // One entry a lane, 0 for none; at most kWait - 64 wait already.
     __device__ __forceinline__ void push(Key k, Key* wait, int lane) {
         const uint64_t who = __ballot(k && (uint32_t)(k >> 32) >= bound);
         if (!who) return;
-        const int at = waiting + __popcll(who & ((1ull << lane) - 1));
-        if (((who >> lane) & 1) && at < kWait) wait[at] = k;
+        if ((who >> lane) & 1) wait[waiting + __popcll(who & ((1ull << lane) - 1))] = k;
         waiting += __popcll(who);
     }
     __device__ __forceinline__ void sort(const Key* wait, int top, int lane) {
@@ -665,16 +681,34 @@ __global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
             }
             best.bound = max(best.bound, Best::bound_of(order, a.top, lane));
         }
+        // the entries that reach the bound, a bit each; their places in the list follow from the lanes' counts
+        const float least = fmaxf(best.bound_value(), -__FLT_MAX__);
+        uint32_t reach = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (u * 16 < there) {
                 float w[N];
                 Elem<T>::unpack(again[u], w);
 #pragma unroll
-                for (int k = 0; k < N; ++k) best.push(key_of(w[k], at[u] + k), wait, lane);
+                for (int k = 0; k < N; ++k) reach |= (w[k] >= least ? 1u : 0u) << (u * N + k);
+                asm volatile("" : "+v"(again[u]));
             }
-        const bool many = best.waiting > kWait;  // equal ones: 256 at a time
-        if (many) best.waiting = 0;
+        const uint32_t upto = wave_scan(__popc(reach));
+        const int all = __builtin_amdgcn_readlane((int)upto, 63);
+        const bool many = all > kWait;  // equal ones: 256 at a time
+        if (!many) {
+            int to = (int)(upto - __popc(reach));
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (u * 16 < there) {
+                    float w[N];
+                    Elem<T>::unpack(again[u], w);
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if ((reach >> (u * N + k)) & 1) wait[to++] = key_of(w[k], at[u] + k);
+                }
+            best.waiting = all;
+        }
         int i0 = 0;
         do {
             if (many) {
