@@ -443,6 +443,8 @@ struct Best {
         return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 |
                (uint32_t)__builtin_amdgcn_readlane((int)key, lane);
     }
+    // the least value that an entry can have and reach the bound
+    __device__ __forceinline__ float least() const { return fmaxf(bound_value(), -__FLT_MAX__); }
     // One entry a lane, 0 for none; at most kWait - 64 wait already.
     __device__ __forceinline__ void push(Key k, Key* wait, int lane) {
         const uint64_t who = __ballot(k && (uint32_t)(k >> 32) >= bound);
@@ -618,28 +620,65 @@ __global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
     if constexpr (TOP) {
         constexpr int kGroup = 4 * N;  // logits
         const int n = (end - begin + kGroup - 1) / kGroup;
-        float own[4] = {-kInf, -kInf, -kInf, -kInf};
-        for (int i0 = 0; i0 < n; i0 += 256)
+        // kLook x 256 groups at a time, more where rows are longer, all on their way before the first is looked at
+        constexpr int kLook = W == 1 ? 1 : W == 4 ? 2 : 4;
+        float w[kLook][4];
+        auto look = [&](int i0) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int i = i0 + u * 64 + lane;
-                if (i < n) own[u] = fmaxf(own[u], group_max[i]);
-            }
+            for (int c = 0; c < kLook; ++c)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = i0 + (c * 4 + u) * 64 + lane;
+                    w[c][u] = -kInf;
+                    if (i0 + c * 256 < n) w[c][u] = i < n ? group_max[min(i, n - 1)] : -kInf;
+                }
+        };
+        float own[4] = {-kInf, -kInf, -kInf, -kInf};
+        for (int i0 = 0; i0 < n; i0 += kLook * 256) {
+            look(i0);
+#pragma unroll
+            for (int c = 0; c < kLook; ++c)
+                if (i0 + c * 256 < n) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) own[u] = fmaxf(own[u], w[c][u]);
+                }
+        }
         uint32_t order[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) order[u] = own[u] > -kInf ? ordered(own[u]) : 0;
         Best groups;
         groups.bound = Best::bound_of(order, a.top, lane);
-        for (int i0 = lane; i0 - lane < n; i0 += 256) {
-            float w[4];
+        for (int i0 = 0; i0 < n; i0 += kLook * 256) {
+            if (n > kLook * 256) look(i0);
+            const float least = groups.least();
+            uint32_t reach = 0;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) w[u] = i0 + u * 64 < n ? group_max[i0 + u * 64] : -kInf;
-            if (__ballot(largest<4>(w) >= groups.bound_value()) != 0) {  // mostly none of 256 groups
+            for (int c = 0; c < kLook; ++c)
+                if (i0 + c * 256 < n) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) groups.push(key_of(w[u], i0 + u * 64), wait, lane);
+                    for (int u = 0; u < 4; ++u) reach |= (w[c][u] >= least ? 1u : 0u) << (c * 4 + u);
+                }
+            const uint32_t upto = wave_scan(__popc(reach));
+            const int all = __builtin_amdgcn_readlane((int)upto, 63);
+            if (all == 0) continue;
+            if (groups.waiting + all <= kWait) {
+                int to = groups.waiting + (int)(upto - __popc(reach));
+#pragma unroll
+                for (int c = 0; c < kLook; ++c)
+                    if (i0 + c * 256 < n) {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if ((reach >> (c * 4 + u)) & 1) wait[to++] = key_of(w[c][u], i0 + (c * 4 + u) * 64 + lane);
+                    }
+                groups.waiting += all;
+            } else {  // many equal ones: 64 at a time
+                for (int i = i0 + lane; i - lane < min(n, i0 + kLook * 256); i += 64) {
+                    groups.push(i < n ? key_of(group_max[i], i) : 0, wait, lane);
+                    if (groups.waiting > kWait - 64) groups.sort(wait, a.top, lane);
+                }
             }
-            if (groups.waiting > 64 || (groups.key_at(0) && i0 - lane + 256 >= n)) groups.sort(wait, a.top, lane);
         }
+        if (groups.waiting > 64 || groups.key_at(0)) groups.sort(wait, a.top, lane);
         // up to 64 groups reach the bound: all of them are read again; more: the best ones
         int there = groups.waiting;
         __builtin_amdgcn_wave_barrier();
@@ -682,7 +721,7 @@ __global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
             best.bound = max(best.bound, Best::bound_of(order, a.top, lane));
         }
         // the entries that reach the bound, a bit each; their places in the list follow from the lanes' counts
-        const float least = fmaxf(best.bound_value(), -__FLT_MAX__);
+        const float least = best.least();
         uint32_t reach = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -768,25 +807,39 @@ __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
         const Key* keys = a.part_keys + row * a.parts * a.top;
         const int n = a.parts * a.top;
         // bounds: every part's last entry, and the lanes' own largest ones
-        uint32_t own[4] = {}, last = 0;
-        for (int i0 = 0; i0 < n; i0 += 256)
+        Key k[4][4];
+        auto look = [&](int i0) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int i = i0 + u * 64 + lane;
-                if (i < n) own[u] = max(own[u], (uint32_t)(keys[i] >> 32));
-            }
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = i0 + (c * 4 + u) * 64 + lane;
+                    k[c][u] = 0;
+                    if (i0 + c * 256 < n) k[c][u] = i < n ? keys[i] : 0;
+                }
+        };
+        uint32_t own[4] = {}, last = 0;
+        for (int i0 = 0; i0 < n; i0 += 1024) {
+            look(i0);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) own[u] = max(own[u], (uint32_t)(k[c][u] >> 32));
+        }
         for (int i = lane; i < a.parts; i += 64) last = max(last, (uint32_t)(keys[(i + 1) * a.top - 1] >> 32));
         for (int d = 1; d < 64; d <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, d));
         best.bound = max(last, Best::bound_of(own, a.top, lane));
-#pragma unroll 1
-        for (int i0 = lane; i0 - lane < n; i0 += 256) {
-            Key k[4];
+        for (int i0 = 0; i0 < n; i0 += 1024) {
+            if (n > 1024) look(i0);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) k[u] = i0 + u * 64 < n ? keys[i0 + u * 64] : 0;
+            for (int c = 0; c < 4; ++c) {
+                if (i0 + c * 256 >= n) break;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) best.push(k[u], wait, lane);
-            if (best.waiting > 64 || i0 - lane + 256 >= n) best.sort(wait, a.top, lane);
+                for (int u = 0; u < 4; ++u) best.push(k[c][u], wait, lane);
+                if (best.waiting > 64) best.sort(wait, a.top, lane);
+            }
         }
+        best.sort(wait, a.top, lane);
     }
     put_row(a, row, st, best.key, given, lane);
 }
