@@ -573,7 +573,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
 // of a frequent word the ones at its first up to eight places a part of the
 // columns each; the others end.  The first work-groups zero the rows of the
 // other words, which is what most of the time goes to where the table is large.
-// 1627 ids x 100 fp32 into 20011 words: 9 us, by sorting 24; 4000 x 512 into
+// 1627 ids x 100 fp32 into 20011 words: 7 us, by sorting 24; 4000 x 512 into
 // 65536: 34 and 43, also where one word has half of the ids (90 without the parts).
 constexpr int kSmall = 4096;
 constexpr int kSmallOften = 64;   // rows from which on a word's columns are split
@@ -593,14 +593,14 @@ struct SmallArgs {
     int32_t fill_rows, fill_groups;  // rows that each of the first work-groups zeroes where their words do not occur
 };
 
-template <class T, class O, int K>
+// kLook: ids that a thread looks at.
+template <class T, class O, int K, int kLook>
 __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
     __shared__ uint8_t there[kFillRows];
-    __shared__ uint16_t list[kSmall];
+    __shared__ uint16_t list[kLook * kSmallThreads];
     __shared__ int count[kSmallWaves], early[kSmallWaves];
     __shared__ float part[kSmallWaves][64][K];
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
-    constexpr int kLook = kSmall / kSmallThreads;  // ids a thread looks at
     int32_t id[kLook];
     if ((int)blockIdx.x < a.fill_groups) {
         const uint32_t first = blockIdx.x * (uint32_t)a.fill_rows, rows = min((uint32_t)a.fill_rows, a.vocab - first);
@@ -802,7 +802,12 @@ GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
 
 template <class T, class O, int K>
 void launch_small(const SmallArgs& a, hipStream_t st) {
-    if (a.n + a.fill_groups) sum_small<T, O, K><<<(unsigned)(a.n + a.fill_groups), kSmallThreads, 0, st>>>(a);
+    const unsigned groups = a.n + a.fill_groups;
+    if (groups == 0) return;
+    // no more looks than the ids need (1627 ids x 100 into 20011 words: 7.4 us with 8, 9.1 with 16)
+    if (a.n <= 4 * kSmallThreads) sum_small<T, O, K, 4><<<groups, kSmallThreads, 0, st>>>(a);
+    else if (a.n <= 8 * kSmallThreads) sum_small<T, O, K, 8><<<groups, kSmallThreads, 0, st>>>(a);
+    else sum_small<T, O, K, kSmall / kSmallThreads><<<groups, kSmallThreads, 0, st>>>(a);
 }
 
 template <class T, class O>
