@@ -112,8 +112,8 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
 // 42 us [51], 20000 51 [58], 262144 120 [119]).
 
 constexpr int kMaxDigit = 10;
-constexpr int kTile = 1024;        // ids a work-group of the sort ranks: 4 waves of 4 rounds
-constexpr int kRounds = 4;
+constexpr int kRounds = 4, kFewRounds = 2;  // a work-group of the sort ranks the ids of 4 waves of so many rounds
+constexpr int kFewIds = 32768;     // ids up to which it takes fewer (20000: 2 us less, 33000: 2 us more)
 constexpr int kSumTiles = 64;      // tiles up to which the scatter adds up the counts itself
 
 __device__ __forceinline__ uint32_t word_of(int32_t id, uint32_t vocab) {
@@ -195,20 +195,22 @@ __device__ __forceinline__ Pair sort_pair(const SortArgs& a, int64_t i) {
 }
 
 // counts[tile][bin] of one digit.
+template <int ROUNDS>
 __global__ __launch_bounds__(256) void sort_count(SortArgs a) {
+    constexpr int kTile = 256 * ROUNDS;
     __shared__ uint32_t count[1 << kMaxDigit];
     if ((int)blockIdx.x >= a.fill.from) return fill_rows(a.fill, blockIdx.x - a.fill.from);
     const int bins = 1 << a.bits, tile = blockIdx.x;
     for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
-    uint32_t k[kTile / 256];
+    uint32_t k[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kTile / 256; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t i = (int64_t)tile * kTile + r * 256 + threadIdx.x;
         k[r] = i < a.n ? sort_pair(a, i).word : 0;
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kTile / 256; ++r)
+    for (int r = 0; r < ROUNDS; ++r)
         if ((int64_t)tile * kTile + r * 256 + threadIdx.x < a.n) atomicAdd(&count[(k[r] >> a.shift) & (bins - 1)], 1u);
     __syncthreads();
     for (int b = threadIdx.x; b < bins; b += 256) a.counts[(int64_t)tile * bins + b] = count[b];
@@ -247,8 +249,9 @@ __global__ __launch_bounds__(256) void sort_scan(SortArgs a) {
 // still those of single tiles, and every work-group adds them up for itself,
 // which for few tiles takes less than another launch (the gradient of 9000 ids
 // x 300 into 65536 words: 44 us, with a launch for the sums 48; 60000 ids: 70 both).
-template <bool SUM>
+template <bool SUM, int ROUNDS>
 __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
+    constexpr int kTile = 256 * ROUNDS;
     constexpr int kBins = 1 << kMaxDigit;
     __shared__ uint32_t at[4][kBins];  // per wave: counts, then the next place of a digit
     __shared__ uint32_t wave_sum[4];
@@ -280,10 +283,10 @@ __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
         }
     }
     const int64_t first = (int64_t)tile * kTile + wave * (kTile / 4);
-    Pair k[kRounds];
-    uint32_t rank[kRounds];
+    Pair k[ROUNDS];
+    uint32_t rank[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int64_t i = first + r * 64 + lane;
         k[r] = i < a.n ? sort_pair(a, i) : Pair{0, 0};
     }
@@ -294,7 +297,7 @@ __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
     if (lane == 63) wave_sum[wave] = upto;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const bool valid = first + r * 64 + lane < a.n;
         const uint32_t d = (k[r].word >> a.shift) & (bins - 1);
         const uint64_t m = same_digit(d, a.bits, __ballot(valid));
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(256) void sort_scatter(SortArgs a) {
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r)
+    for (int r = 0; r < ROUNDS; ++r)
         if (first + r * 64 + lane < a.n) a.out[at[wave][(k[r].word >> a.shift) & (bins - 1)] + rank[r]] = k[r];
 }
 
@@ -790,7 +793,8 @@ GradPlan grad_plan(int32_t n, int32_t vocab, int32_t dim) {
     g.passes = (bits + kMaxDigit - 1) / kMaxDigit;
     g.digit = (bits + g.passes - 1) / g.passes;
     if (g.digit < 2) g.digit = 2;            // the scatter reads the counts by fours
-    g.sort_tiles = (int32_t)(((int64_t)n + kTile - 1) / kTile);
+    const int tile = 256 * (n <= kFewIds ? kFewRounds : kRounds);
+    g.sort_tiles = (int32_t)(((int64_t)n + tile - 1) / tile);
     g.sorted[0] = take(list);
     g.sorted[1] = take(list);
     g.counts = take((int64_t)g.sort_tiles * 4 << g.digit);
@@ -940,14 +944,16 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
             s.shift = p * g.digit;
             last = p & 1;
             const unsigned count = next(g.sort_tiles);
-            sort_count<<<count, 256, 0, st>>>(s);
+            if (n <= kFewIds) sort_count<kFewRounds><<<count, 256, 0, st>>>(s);
+            else sort_count<kRounds><<<count, 256, 0, st>>>(s);
             if (scan) {
                 const unsigned sums = next(((1 << g.digit) + kScanBins - 1) / kScanBins);
                 sort_scan<<<sums, 256, 0, st>>>(s);
             }
             const unsigned scatter = next(g.sort_tiles);
-            if (scan) sort_scatter<false><<<scatter, 256, 0, st>>>(s);
-            else sort_scatter<true><<<scatter, 256, 0, st>>>(s);
+            if (scan) sort_scatter<false, kRounds><<<scatter, 256, 0, st>>>(s);
+            else if (n <= kFewIds) sort_scatter<true, kFewRounds><<<scatter, 256, 0, st>>>(s);
+            else sort_scatter<true, kRounds><<<scatter, 256, 0, st>>>(s);
         }
         const SumArgs a{sorted(last), n, g.chunk, (uint32_t)vocab, dim, g.lanes, dout, dout_stride, scale,
                         accumulate, dtable, dtable_stride, reinterpret_cast<float*>(ws + g.partial)};

@@ -186,7 +186,7 @@ def test_embed_grad(n, V, E, src, dst, accumulate):
 
 @gpu
 @pytest.mark.parametrize("src,dst", [(F32, F32), (BF16, BF16)])
-@pytest.mark.parametrize("n", [1024, 1025, 2048, 2049, 4096, 4097, 65536, 65537, 131073])
+@pytest.mark.parametrize("n", [1024, 1025, 2048, 2049, 4096, 4097, 32768, 32769, 65536, 65537, 131073])
 @pytest.mark.parametrize("E", [3, 6, 255, 300])
 def test_embed_grad_sizes(n, E, src, dst):
     """At the sizes where the sort and the columns' split change, a third of the ids one word."""
