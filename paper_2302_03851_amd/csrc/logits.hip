@@ -534,7 +534,7 @@ constexpr int kLoads = 2;  // 16-byte loads of a thread in flight, beside as man
 // 63.  Few or short rows are bound by the chain of steps of the choice, about 3
 // us a row and wave: 23 x 3801 bf16 4 us, 7 with 5 alternatives.
 // (W: row_waves; at most 64 registers, for eight waves a SIMD: 4381 x 4108 fp32,
-// 5 alternatives, 24 us, at 86 registers 27)
+// 5 alternatives, 21 us, without the limit 25)
 template <class T, bool TOP, int W>
 __global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
     constexpr int N = Elem<T>::kVec, kStep = kLoads * W * 64 * N;
@@ -789,7 +789,7 @@ __device__ __forceinline__ Stats join_parts(const Stats* part, int parts, float 
 }
 
 // Joins the parts of split rows: a wave a row; bound by its chain of loads and
-// steps, 5 us for the 32 parts of 1 x 131072 with 8 alternatives.
+// steps, 4 us for the 32 parts of 1 x 131072 with 8 alternatives.
 template <class T>
 __global__ __launch_bounds__(64) void logprobs_join(LogprobArgs a) {
     const int64_t row = blockIdx.x;
@@ -1058,8 +1058,8 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t row, cons
 // that it is read once and the gradient written once.  2^y with y = x c - r(m)
 // (see Stats) is summed up in one pass over the registers, w T p_j = 2^y (w T / S)
 // written in another; the owners of the listed entries then write
-// w T (p_j - q_j).  Memory bound with many rows: 8192 x 65536 bf16, 2.15 GB, 389
-// us (5.5 TB/s); 4096 x 131072 437 (4.9), where a row fills the registers of a
+// w T (p_j - q_j).  Memory bound with many rows: 8192 x 65536 bf16, 2.15 GB, 383
+// us (5.6 TB/s); 4096 x 131072 437 (4.9), where a row fills the registers of a
 // compute unit, so that no other one is read while it is summed up; the chain of
 // these steps with few: 128 x 8192 fp32 6 us.
 constexpr int kBlock = 2;
@@ -1446,7 +1446,7 @@ struct RowPlan {
 
 // Rows are split into parts, joined by a second launch, where too few of them
 // would fill the card: up to 255 from 65536 logits on, up to 127 from 32768 on
-// (24 x 40602 fp32, 31 alternatives: 15 us, unsplit 19; 250 x 33000: 22 and 20);
+// (24 x 40602 fp32, 31 alternatives: 14 us, unsplit 17; 250 x 33000: 20 and 18);
 // and so is any row whose group maxima would pass 32 KB of LDS.
 RowPlan row_plan(int32_t n, int32_t vocab, int32_t top) {
     constexpr int32_t kSplit = 32768, kMost = 131072, kLeast = 4096, kFill = 512;
@@ -1515,10 +1515,9 @@ struct DistillPlan {
 
 // Rows are split that no work-group holds.  So are those of which a work-group
 // needs more than half of a compute unit, while the second read can find the
-// logits in the caches (1 x 131072 bf16:
-// 8 us, by one work-group 21; 400 rows: 54 and 61; 1500 rows: 231 and 183), and
-// from three eighths on where there are few rows (64 x 65536 bf16: 9 and 13 us;
-// 256 rows: 20 and 17).
+// logits in the caches (400 x 66001 bf16: 32 us, by a work-group a row 35; 1500 x
+// 131072: 231 and 172), and from three eighths on where there are few rows (1 x
+// 131072: 8 and 19 us, 64 x 65536: 9 and 12; 256 rows: 20 and 16).
 DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
     constexpr int32_t kFill = 4096, kFew = 128;
     const int32_t bytes = dtype == EDB_BF16 ? 2 : 4, vec = 16 / bytes, least = kPartLoads * 64 * kPartWaves * vec;
@@ -1538,8 +1537,8 @@ DistillPlan distill_plan(int32_t n, int32_t vocab, int32_t dtype, int32_t top) {
 
 // As few registers as hold a row, so that several work-groups share a compute
 // unit (one reads while another is at its sums); more waves rather than more
-// vectors a thread from 32 KB on (8192 x 65536 bf16: 389 us with 16 waves of 8,
-// 411 with 8 of 16).
+// vectors a thread from 32 KB on (8192 x 65536 bf16: 383 us with 16 waves of 8,
+// 403 with 8 of 16).
 template <class T, bool CACHED>
 void launch_held(const DistillArgs& a, hipStream_t st) {
     const int64_t vectors = ((int64_t)a.vocab + Elem<T>::kVec - 1) / Elem<T>::kVec;
