@@ -737,7 +737,8 @@ edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32_t n, int32
  *   dlogits  the logits' dtype, or NULL (the loss alone); it may be the logits
  *            themselves (same address and stride)
  * A row of weight 0 or without a listed token is left out, whatever its
- * logits: loss 0, zero gradient.  A listed token that the student masks out (-inf) makes the loss
+ * logits: loss 0, zero gradient.  A listed token that the student masks out
+ * (-inf), or whose log probability is past the range of float, makes the loss
  * +inf; a row that the student masks out whole has a zero gradient besides. */
 edb_status edb_distill_bytes(int32_t n, int32_t vocab, int32_t dtype, int32_t top, int64_t* bytes);
 edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,

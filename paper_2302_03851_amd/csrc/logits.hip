@@ -867,12 +867,14 @@ struct GradArgs {
 
 // dx_j = (g_lp (1[j = id] - p_j) - g_H p_j (lp_j + H)) / T, in one pass that
 // takes p_j from the row's statistics.  The waves of a row's work-groups (several
-// in y where there are few rows: 2 x 131072 bf16 4 us, by one each 15) take
-// kGradLoads neighbouring vectors of 1 KB in turn.  Memory bound: 8192 x 65536
+// in y where there are few rows: 2 x 131072 bf16 4 us, by one each 15) take LOADS
+// neighbouring vectors of 1 KB in turn: eight, of which fewer begin or end in a
+// line that two waves write (8192 x 65533: 423 us, with four 432), or four where
+// rows are few (300 x 10007 fp32: 6.4 us, with eight 6.9).  Memory bound: 8192 x 65536
 // bf16, read and written, 2.15 GB, 394 us (5.4 TB/s; a copy reaches as much).
-constexpr int kGradWaves = 8, kGradLoads = 4;  // waves of a work-group at most
+constexpr int kGradWaves = 8;  // waves of a work-group at most
 
-template <class T, bool CACHED>
+template <class T, int LOADS, bool CACHED>
 __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs a) {
     constexpr int N = Elem<T>::kVec, kAll = 64 * N;
     const int64_t row = blockIdx.x;
@@ -907,18 +909,18 @@ __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs
     const int all = V / kAll;
     const T* from = x - (odd ? 1 : 0);
     const int waves = blockDim.x >> 6, turn = blockIdx.y * waves + wave, turns = gridDim.y * waves;
-    for (int g = turn * kGradLoads; g < all; g += turns * kGradLoads) {
-        const int count = min(kGradLoads, all - g);
-        u32x4 raw[kGradLoads];
+    for (int g = turn * LOADS; g < all; g += turns * LOADS) {
+        const int count = min(LOADS, all - g);
+        u32x4 raw[LOADS];
 #pragma unroll
-        for (int u = 0; u < kGradLoads; ++u) {
+        for (int u = 0; u < LOADS; ++u) {
             const T* at = lane_place(from + min(g + u, all - 1) * kAll, lane);
             raw[u] = CACHED ? Elem<T>::load(at) : Elem<T>::load_nt(at);
         }
         if (odd) shift_in_all(raw, count, x + (g + count) * kAll - 1);
         u32x4 held{0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int u = 0; u < kGradLoads; ++u) {
+        for (int u = 0; u < LOADS; ++u) {
             if (u >= count) break;
             const u32x4 o = slope(raw[u], (g + u) * kAll + lane * N);
             T* at = d + (g + u) * kAll;
@@ -936,7 +938,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs
             }
         }
     }
-    if (V % kAll != 0 && all / kGradLoads % turns == turn) {
+    if (V % kAll != 0 && all / LOADS % turns == turn) {
         const int j = all * kAll + lane * N;
         u32x4 q = load_vector(x, j, V, odd ? 1 : 0);
         if (odd) q = shift_in(q, 0);
@@ -1488,7 +1490,6 @@ void launch_logprobs(const LogprobArgs& a, dim3 grid, size_t lds, hipStream_t st
     else launch_logprobs<T, 8>(a, grid, lds, st);
 }
 
-constexpr int32_t kGradFill = 1024;  // work-groups of the gradient of log probabilities where rows can be split
 constexpr int64_t kHeld = 16 * 1024;  // vectors of the longest row that a work-group holds
 
 // Whether the caches of the memory side can hold all logits, and may do so since
@@ -1500,10 +1501,24 @@ bool caches_hold(int32_t n, int32_t vocab, int32_t dtype) {
     return (int64_t)n * vocab <= (INT64_C(128) << 20) / (dtype == EDB_BF16 ? 2 : 4);
 }
 
+constexpr int32_t kGradFill = 1024;  // work-groups of the gradient of log probabilities where rows can be split
+
+template <class T, int LOADS>
+void launch_grad(const GradArgs& a, bool cached, hipStream_t st) {
+    // work-groups of as many waves as a row has vectors for, and enough of them for the card
+    constexpr int32_t kTurn = 64 * Elem<T>::kVec * LOADS;
+    const int32_t turns = (a.vocab + kTurn - 1) / kTurn;
+    const int32_t waves = turns < kGradWaves ? turns : kGradWaves, most = (turns + waves - 1) / waves;
+    const int32_t wanted = a.n < kGradFill ? (kGradFill + a.n - 1) / a.n : 1;
+    const dim3 grid(a.n, wanted < most ? wanted : most);
+    if (cached) logprobs_grad_kernel<T, LOADS, true><<<grid, 64 * waves, 0, st>>>(a);
+    else logprobs_grad_kernel<T, LOADS, false><<<grid, 64 * waves, 0, st>>>(a);
+}
+
 template <class T>
-void launch_grad(const GradArgs& a, bool cached, dim3 grid, int threads, hipStream_t st) {
-    if (cached) logprobs_grad_kernel<T, true><<<grid, threads, 0, st>>>(a);
-    else logprobs_grad_kernel<T, false><<<grid, threads, 0, st>>>(a);
+void launch_grad(const GradArgs& a, bool cached, hipStream_t st) {
+    if (a.n < kGradFill / 2) launch_grad<T, 4>(a, cached, st);
+    else launch_grad<T, 8>(a, cached, st);
 }
 
 // How a distillation splits its rows, and its scratch memory.
@@ -1684,15 +1699,9 @@ extern "C" edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32
         GradArgs a{logits, stride,  n,         vocab,     ids,     log2e_over(temperature), (float)(1.0 / (double)temperature),
                    stats,  entropy, g_logprob, g_entropy, dlogits, dlogits_stride};
         hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-        // work-groups of as many waves as a row has vectors for, and enough of them for the card
-        const int32_t vec = dtype == EDB_BF16 ? Elem<bf16>::kVec : Elem<float>::kVec;
-        const int32_t turns = (vocab + 64 * vec * kGradLoads - 1) / (64 * vec * kGradLoads);
-        const int32_t waves = turns < kGradWaves ? turns : kGradWaves, most = (turns + waves - 1) / waves;
-        const int32_t wanted = n < kGradFill ? (kGradFill + n - 1) / n : 1;
-        const dim3 grid(n, wanted < most ? wanted : most);
         const bool cached = caches_hold(n, vocab, dtype);
-        if (dtype == EDB_F32) launch_grad<float>(a, cached, grid, 64 * waves, st);
-        else launch_grad<bf16>(a, cached, grid, 64 * waves, st);
+        if (dtype == EDB_F32) launch_grad<float>(a, cached, st);
+        else launch_grad<bf16>(a, cached, st);
         return launched(who);
     });
 }

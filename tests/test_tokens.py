@@ -452,7 +452,7 @@ def _grad_reference(x, ids, T, g1, g2):
 
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("n,V", SIZES + [(300, 10007), (2, 131071)])
+@pytest.mark.parametrize("n,V", SIZES + [(300, 10007), (600, 5003), (520, 8200), (2, 131071)])
 @pytest.mark.parametrize("kind,T", [("plain", 0.7), ("masked", 1.0), ("lowest", 1.0), ("broken", 1.0), ("ties", 2.0)])
 def test_logprobs_grad(n, V, dtype, kind, T):
     from paper_2302_03851_amd import tokens
