@@ -150,8 +150,8 @@ __device__ __forceinline__ void shift_in_all(u32x4 (&raw)[M], int count, const T
 
 // 16 bytes of a result that is not read again here: past the caches where a
 // wave writes whole lines, through them where two waves share some (gradient of
-// log probabilities, 8192 x 65536 bf16: 397 us past the caches, 418 through
-// them; 8192 x 65532: 463 and 436).
+// log probabilities with four vectors a turn, 8192 x 65536 bf16: 397 us past the
+// caches, 418 through them; 8192 x 65532: 463 and 436).
 template <class T>
 __device__ __forceinline__ void store_piece(T* p, u32x4 v, bool straight) {
     if (straight) {
@@ -869,9 +869,9 @@ struct GradArgs {
 // takes p_j from the row's statistics.  The waves of a row's work-groups (several
 // in y where there are few rows: 2 x 131072 bf16 4 us, by one each 15) take LOADS
 // neighbouring vectors of 1 KB in turn: eight, of which fewer begin or end in a
-// line that two waves write (8192 x 65533: 423 us, with four 432), or four where
-// rows are few (300 x 10007 fp32: 6.4 us, with eight 6.9).  Memory bound: 8192 x 65536
-// bf16, read and written, 2.15 GB, 394 us (5.4 TB/s; a copy reaches as much).
+// line that two waves write (8192 x 65533: 422 us, with four 432), or four where
+// rows are few (300 x 10007 fp32: 6.4 us, with eight 6.9).  Memory bound: 8192 x
+// 65536 bf16, read and written, 2.15 GB, 383 us (5.6 TB/s; a copy reaches 5.4).
 constexpr int kGradWaves = 8;  // waves of a work-group at most
 
 template <class T, int LOADS, bool CACHED>
