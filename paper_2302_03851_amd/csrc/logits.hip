@@ -672,6 +672,7 @@ __global__ __launch_bounds__(64 * W, 8) void logprobs_kernel(LogprobArgs a) {
                     }
                 groups.waiting += all;
             } else {  // many equal ones: 64 at a time
+                if (groups.waiting > kWait - 64) groups.sort(wait, a.top, lane);  // as many as push() expects
                 for (int i = i0 + lane; i - lane < min(n, i0 + kLook * 256); i += 64) {
                     groups.push(i < n ? key_of(group_max[i], i) : 0, wait, lane);
                     if (groups.waiting > kWait - 64) groups.sort(wait, a.top, lane);

@@ -385,6 +385,20 @@ def test_logprobs_shapes(n, V, dtype, kind, top):
 
 
 @gpu
+@pytest.mark.parametrize("n,V,dtype", [(520, 65536, BF16), (300, 65536, BF16), (520, 131072, BF16), (520, 40000, F32)])
+@pytest.mark.parametrize("share", [0.004, 0.006, 0.01, 0.025])
+@pytest.mark.parametrize("top", [5, 63])
+def test_logprobs_capped(n, V, dtype, share, top):
+    """A part of every row's logits at one cap: the first look through the groups fills the list of those that wait
+    nearly or just whole, and the next one has more."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V + top + int(1000 * share))
+    x = _rows("plain", n, V, dtype, g).clamp_(max=9.0)
+    x[torch.rand((n, V), generator=g, device="cuda") < share] = 9.0
+    _check_logprobs(x, None, 1.0, top, tokens.logprobs(x, None, 1.0, top))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("kind", ["plain", "masked"])
 def test_logprobs_longest(dtype, kind):
