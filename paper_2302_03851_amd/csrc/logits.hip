@@ -889,16 +889,18 @@ __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs
         zero_row(d, V, gridDim.y * blockDim.x, blockIdx.y * blockDim.x);
         return;
     }
-    // p (k0 + k1 log2 p), k0 = -(g_lp + g_H H) / T, k1 = -g_H ln 2 / T
-    const float k0 = -(g1 + (a.g_entropy ? g2 * a.entropy[row] : 0.f)), k1 = -g2 * kLn2;
+    // p (k0 + k1 log2 p / 2), k0 = -(g_lp + g_H H) / T, k1 = -2 g_H ln 2 / T.  p is the square of 2^(log2 p / 2), which
+    // is a normal number where p is not, and comes last: a result is 0 only where it is too small itself, not its p.
+    const float k0 = -(g1 + (a.g_entropy ? g2 * a.entropy[row] : 0.f)), k1 = -2.f * (g2 * kLn2);
+    const float half_c = 0.5f * a.c, half_l2 = 0.5f * l2;
     const bool odd = odd_row(x), odd_out = odd_row(d), straight = straight_row(d);
     auto slope = [&](u32x4 q, int j) {
         float v[N];
         Elem<T>::unpack(q, v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float y = __builtin_fmaf(v[i] - m, a.c, -l2);
-            v[i] = exp2_hw(y) * __builtin_fmaf(k1, fmaxf(y, kLow), k0);
+            const float y = __builtin_fmaf(v[i] - m, half_c, -half_l2), e = exp2_hw(y);
+            v[i] = e * (e * __builtin_fmaf(k1, fmaxf(y, kLow), k0));
         }
         const int at = id - j;
         if (at >= 0 && at < N) {

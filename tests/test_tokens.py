@@ -498,6 +498,24 @@ def test_logprobs_grad(n, V, dtype, kind, T):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [2001, 9001])
+def test_logprobs_grad_small(V, dtype):
+    """Probabilities on both sides of the least normal number, whose gradients the temperature lifts above it."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    n, T = 6, 0.1
+    x = (-8.6 - 0.8 * torch.rand((n, V), generator=g, device="cuda"))
+    x[:, V // 2] = 0.5 * torch.rand(n, generator=g, device="cuda")
+    x = x.to(dtype)
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    r = tokens.logprobs(x, ids, T)
+    g1, g2 = torch.randn(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    ref, tol = _grad_reference(x, ids, T, g1, g2)
+    _close(tokens.logprobs_grad(x, ids, r.stats, r.entropy, g1, g2, T), ref, tol + 1.01 * _half_ulp(ref, dtype) + 1e-38)
+
+
+@gpu
 def test_logprobs_grad_differences():
     """Central differences of the 64-bit definition, step 1e-4: their own error
     is below 1e-7, fp32's below 1e-5 of the gradients' scale."""
