@@ -254,17 +254,24 @@ __device__ __forceinline__ u32x4 load_vector(const T* x, int j, int V, int early
 
 // Running softmax statistics: the largest logit m, and s = sum 2^y, t = sum y 2^y
 // with y = x c - r(m).  The reference r is m c rounded to fp32, so that y is one
-// fused multiply-add and its own rounding the only one; where m c comes near
-// the fp32 range (rows of the lowest values) r is m c itself and y = (x - m) c.
-// A NaN or +inf logit makes s NaN.
+// fused multiply-add and its own rounding the only one.  At x = m it leaves the
+// rounding error of r there, which has to stay far below 1: from |m c| = 2^20 on
+// (where it reaches 2^-5; at 2^32 2^y would leave the fp32 range) r is m c itself
+// and y = (x - m) c, which is 0 there.  A NaN or +inf logit makes s NaN.
 struct Stats {
     float m, s, t;
 
     static __device__ __forceinline__ Stats none() { return {-kInf, 0.f, 0.f}; }
-    static __device__ __forceinline__ bool plain(float mc) { return fabsf(mc) < 1e30f; }
+    static __device__ __forceinline__ bool plain(float mc) { return fabsf(mc) < 1048576.f; }
+    // r(m) - r(to), each rounded or not
+    static __device__ __forceinline__ float between(float m, float to, float c) {
+        const float a = m * c, b = to * c;
+        if (plain(b)) return plain(a) ? a - b : __builtin_fmaf(m, c, -b);
+        return plain(a) ? __builtin_fmaf(-to, c, a) : (m - to) * c;
+    }
     // the sums taken to the reference of `to`, a number at or above m
     __device__ __forceinline__ void rescale(float to, float c) {
-        const float a = m * c, b = to * c, d = fmaxf(plain(a) && plain(b) ? a - b : (m - to) * c, kLow), f = exp2_hw(d);
+        const float d = fmaxf(between(m, to, c), kLow), f = exp2_hw(d);
         t = (t + s * d) * f;
         s = s * f;
         m = to;
@@ -1139,7 +1146,7 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
     if (lane == 0) part[0][wave] = m;
     __syncthreads();
     m = wave_max(lane < W ? part[0][lane] : -kInf);
-    // y = (x - low) c - r, low 0 but for rows near the end of the fp32 range
+    // y = (x - low) c - r, low 0 but for rows whose reference is not rounded (see Stats)
     const float ref = m == -kInf ? 0.f : m;
     const bool plain = Stats::plain(ref * a.c);
     const float low = plain ? 0.f : ref, r = plain ? ref * a.c : 0.f;

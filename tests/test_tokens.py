@@ -426,6 +426,45 @@ def test_logprobs_split_kinds(kind):
     _check_logprobs(x, ids, 1.0, 64, tokens.logprobs(x, ids, 1.0, 64))
 
 
+FAR = [(-1e9, 1.0), (-1e9, 0.1), (-1e10, 1.0), (-1e10, 2.0), (-1e15, 1.0), (-1e20, 0.1), (-1e30, 1.0), (-1e30, 2.0), (1e10, 1.0),
+       (1e10, 0.1), (-1e6, 1.0), (-6e5, 1.0), (8e5, 1.0), (0.0, 1e-6), (0.0, 1e-9), (0.0, 1e-30)]
+
+
+def _far(value, n, V, dtype, g):
+    """Ordinary logits with a finite number far away in their place: in whole rows, the first or the last part, here
+    and there, everywhere but at one place, at one place; 0: none."""
+    x = _rows("plain", n, V, F32, g)
+    if value:
+        x[0::6] = value
+        x[1::6, :V // 2] = value
+        x[2::6, V // 3:] = value
+        x[3::6][torch.rand(x[3::6].shape, generator=g, device="cuda") < 0.6] = value
+        one = x[4::6, V // 2].clone()
+        x[4::6] = value
+        x[4::6, V // 2] = one
+        x[5::6, 2 * V // 3] = value
+    return x.to(dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(6, 1), (12, 7), (30, 1000), (2052, 2049), (516, 16385), (66, 20001), (6, 70001), (6, 131072)])
+@pytest.mark.parametrize("value,T", FAR)
+def test_logprobs_far(n, V, dtype, value, T):
+    """Finite logits of every size have a distribution, at every temperature: forward and gradient."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = _far(value, n, V, dtype, g)
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    r = tokens.logprobs(x, ids, T, 9)
+    _check_logprobs(x, ids, T, 9, r)
+    g1, g2 = torch.randn(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    if T < 1e-20:
+        return                                         # the gradients pass fp32's range
+    ref, tol = _grad_reference(x, ids, T, g1, g2)
+    _close(tokens.logprobs_grad(x, ids, r.stats, r.entropy, g1, g2, T), ref, tol + 1.01 * _half_ulp(ref, dtype) + 1e-38)
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_logprobs_offsets_past_32_bits(dtype):
@@ -708,6 +747,20 @@ def test_distill_split_rows(n, V, dtype, kind, teacher):
     assert torch.equal(xv.contiguous().view(torch.uint8), full.dlogits.view(torch.uint8))
     xv.copy_(x)
     assert torch.equal(mem.view(torch.uint8), before.view(torch.uint8))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(6, 7), (12, 200), (30, 1000), (12, 5001), (12, 12001), (150, 33001), (140, 65000), (1020, 33003), (6, 131072)])
+@pytest.mark.parametrize("value,T", [(v, T) for v, T in FAR if T > 1e-20])
+def test_distill_far(n, V, dtype, value, T):
+    """As test_logprobs_far, in every layout of the rows."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = _far(value, n, V, dtype, g)
+    ids, u = _teacher(n, V, 9, g, "equal")
+    ids[:, 0] = V // 2
+    _check_distill(x, ids, u, T, None, tokens.distill(x, ids, u, T))
 
 
 @gpu
