@@ -7,8 +7,11 @@
 //   lp_j = (x_j - m) / T - l,  p_j = exp(lp_j),
 //   H    = -sum_j p_j lp_j = l - (sum_j e_j (x_j - m) / T) / S.
 // Both terms of H are >= 0, so nothing cancels.  Exponents are taken in base 2
-// (y = (x - m) c with c = log2(e) / T, e = 2^y); the difference comes first,
-// because x c can pass the largest fp32 number where x does not.  Sums are fp32.
+// (y = (x - m) c with c = log2(e) / T, e = 2^y) against a reference that is m c to
+// its rounding error (see Stats): l and H are corrected by it, which cancels
+// terms of its size, 2^-5 at most, and leaves fp32's rounding of those.  So l and H
+// are cut off at 0, below which they cannot lie; log probabilities then stay at
+// or below 0.  Sums are fp32.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -320,12 +323,15 @@ struct Stats {
         t = wave_sum(t);
     }
     __device__ __forceinline__ bool empty() const { return m == -kInf && s == 0.f; }
+    static __device__ __forceinline__ float not_below_0(float v) { return v < 0.f ? 0.f : v; }  // NaN stays
     // ln sum exp((x - m) / T), 0 for a row that is masked out whole
     __device__ __forceinline__ float log_sum(float c) const {
         const float r = m * c;
-        return empty() ? 0.f : plain(r) ? __builtin_fmaf(-kLn2, __builtin_fmaf(m, c, -r), logf(s)) : logf(s);
+        return empty() ? 0.f : not_below_0(plain(r) ? __builtin_fmaf(-kLn2, __builtin_fmaf(m, c, -r), logf(s)) : logf(s));
     }
-    __device__ __forceinline__ float entropy() const { return empty() ? 0.f : __builtin_fmaf(-kLn2, t / s, logf(s)); }
+    __device__ __forceinline__ float entropy() const {
+        return empty() ? 0.f : not_below_0(__builtin_fmaf(-kLn2, t / s, logf(s)));
+    }
 };
 
 template <int N>

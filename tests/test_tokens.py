@@ -426,6 +426,25 @@ def test_logprobs_split_kinds(kind):
     _check_logprobs(x, ids, 1.0, 64, tokens.logprobs(x, ids, 1.0, 64))
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(600, 1), (600, 30), (600, 5001), (600, 20001), (40, 70001)])
+@pytest.mark.parametrize("T", [1.0, 0.7, 0.01])
+def test_logprobs_peaked(n, V, dtype, T):
+    """Rows that one logit decides: entropies and ln sums do not fall below 0, nor log probabilities rise above it."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = _rows("plain", n, V, F32, g)
+    at = torch.randint(0, V, (n,), generator=g, device="cuda")
+    x[torch.arange(n, device="cuda"), at] = 20 + 40 * torch.rand(n, generator=g, device="cuda")
+    x = x.to(dtype)
+    ids = at.to(torch.int32)
+    r = tokens.logprobs(x, ids, T, 2)
+    _check_logprobs(x, ids, T, 2, r)
+    assert bool((r.entropy >= 0).all()) and bool((r.stats[:, 1] >= 0).all())
+    assert bool((r.logprob <= 0).all()) and bool((r.top_logprobs <= 0).all())
+
+
 FAR = [(-1e9, 1.0), (-1e9, 0.1), (-1e10, 1.0), (-1e10, 2.0), (-1e15, 1.0), (-1e20, 0.1), (-1e30, 1.0), (-1e30, 2.0), (1e10, 1.0),
        (1e10, 0.1), (-1e6, 1.0), (-6e5, 1.0), (8e5, 1.0), (0.0, 1e-6), (0.0, 1e-9), (0.0, 1e-30)]
 
