@@ -1402,6 +1402,8 @@ bool aligned(const void* p, int32_t dtype) {
     return (reinterpret_cast<uintptr_t>(p) & (dtype == EDB_BF16 ? 1u : 3u)) == 0;
 }
 
+float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
+
 // Arguments that every operator over rows of logits shares.
 edb_status check_rows(const char* who, const void* logits, int32_t dtype, int32_t n, int32_t vocab, int64_t stride,
                       float temperature) {
@@ -1411,8 +1413,8 @@ edb_status check_rows(const char* who, const void* logits, int32_t dtype, int32_
     if (vocab > (1 << 30)) return fail(EDB_ERR_UNSUPPORTED, w + ": vocab must not exceed 2^30");
     if (stride < vocab) return fail(EDB_ERR_INVALID, w + ": the row stride is below vocab");
     if (stride > kMaxElems / (n > 0 ? n : 1)) return fail(EDB_ERR_INVALID, w + ": the rows span more than 2^48 elements");
-    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-        return fail(EDB_ERR_INVALID, w + ": the temperature must be positive and finite");
+    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(log2e_over(temperature)))
+        return fail(EDB_ERR_INVALID, w + ": the temperature must be positive and finite, and log2(e) / temperature too");
     if (n && !logits) return fail(EDB_ERR_INVALID, w + ": NULL logits");
     if (!aligned(logits, dtype)) return fail(EDB_ERR_INVALID, w + ": logits must be aligned to their elements");
     return EDB_OK;
@@ -1611,8 +1613,6 @@ P* rows_from(P* p, int64_t elems) {
 const void* rows_from(const void* p, int64_t row, int64_t stride, int32_t dtype) {
     return static_cast<const char*>(p) + row * stride * (dtype == EDB_BF16 ? 2 : 4);
 }
-
-float log2e_over(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
 
 }  // namespace
 

@@ -1002,6 +1002,14 @@ def test_refusals(call, changed, status):
     assert L.load().edb_last_error()
 
 
+@pytest.mark.parametrize("call", [_logprobs, _lp_grad, _distill])
+def test_refused_temperatures(call):
+    """Where 1 / T is finite and the exponents' factor log2(e) / T is not."""
+    for n in (0, 4):
+        assert call(n=n, T=3e-39) == INVALID and call(n=n, T=4.2e-39) == INVALID
+    assert call(n=0, T=4.3e-39) == L.EDB_OK and call(n=0, T=3.4e38) == L.EDB_OK
+
+
 @pytest.mark.parametrize("call", [_embed, _logprobs, _lp_grad, _distill])
 def test_nothing_to_do(call):
     assert call(n=0) == L.EDB_OK
