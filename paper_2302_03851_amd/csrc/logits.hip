@@ -1068,7 +1068,7 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t row, cons
     if (threadIdx.x == 0) {
         float sum = 0.f;
         for (int i = 0; i < kWaves; ++i) sum += part[i];
-        a.loss[row] = a.t * a.t * sum;
+        a.loss[row] = a.t * (a.t * sum);  // T^2 can leave fp32's range where the loss does not
     }
 }
 

@@ -783,6 +783,19 @@ def test_distill_far(n, V, dtype, value, T):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(9, 1), (9, 200), (9, 9001), (9, 131072)])
+@pytest.mark.parametrize("T", [1e-25, 1e-15, 1e18, 1e25])
+def test_distill_temperatures(n, V, dtype, T):
+    """Temperatures whose square leaves fp32's range, where the loss stays in it (infinite where it does not)."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = _rows("plain", n, V, dtype, g)
+    ids, u = _teacher(n, V, 5, g, "equal")
+    _check_distill(x, ids, u, T, None, tokens.distill(x, ids, u, T))
+
+
+@gpu
 def test_distill_differences():
     """Central differences of the 64-bit loss (as for the log probabilities)."""
     from paper_2302_03851_amd import tokens
