@@ -36,13 +36,25 @@ class Distilled(NamedTuple):
     dlogits: Optional[torch.Tensor]        # like the logits, None for the loss alone
 
 
+_MOST = 2 ** 31 - 1     # of a size: the C calls take int32, and ctypes would cut off the rest
+
+
+def _size(v, name):
+    """A size that the C calls can take."""
+    if not 0 <= v <= _MOST:
+        raise ValueError(f"{name}: {v} is not a size from 0 to {_MOST}")
+    return v
+
+
 def _matrix(t, name, dev=None):
     """Rows, columns and row stride in elements of a matrix operand."""
     if t.dim() != 2 or t.dtype not in _DTYPE:
         raise ValueError(f"{name}: a 2-D float32 or bfloat16 tensor is needed, not {t.dim()}-D {t.dtype}")
+    n, m = t.shape
+    if n > _MOST or m > _MOST:
+        raise ValueError(f"{name}: {n} x {m} is more than {_MOST} rows or columns")
     if dev is None or t.device != dev:
         _on(t, name, dev)
-    n, m = t.shape
     s, one = t.stride()
     if one != 1 and m > 1:
         raise ValueError(f"{name}: the rows must be contiguous")
@@ -112,7 +124,7 @@ def embed(ids, table, scale: float = 1.0, dtype=None, out=None) -> torch.Tensor:
     (the table's by default); a zero row where an id is no token."""
     vocab, dim, stride = _matrix(table, "table")
     dev = table.device
-    n = ids.numel()
+    n = _size(ids.numel(), "ids")
     ip = _array(ids, "ids", (n,), torch.int32, dev)
     if out is None:
         out = torch.empty((n, dim), dtype=dtype or table.dtype, device=dev)
@@ -131,6 +143,7 @@ def embed_grad(ids, dout, vocab: int, scale: float = 1.0, dtype=None, out=None, 
     `dout` [n, dim], as `dtype` (float32 by default); with `accumulate` it is
     added to `out`."""
     n, dim, stride = _matrix(dout, "dout")
+    _size(vocab, "vocab")
     dev = dout.device
     ip = _array(ids, "ids", (n,), torch.int32, dev)
     if out is None:
@@ -153,6 +166,7 @@ def logprobs(logits, ids=None, temperature: float = 1.0, top: int = 0, out: Opti
     """Log probabilities of the tokens `ids` [n] under softmax(logits /
     temperature), the rows' entropies and the `top` best alternatives."""
     n, vocab, stride = _matrix(logits, "logits")
+    _size(top, "top")
     dev, dt = logits.device, _DTYPE[logits.dtype]
     ip = None if ids is None else _array(ids, "ids", (n,), torch.int32, dev)
     f32 = torch.float32
@@ -205,7 +219,7 @@ def distill(logits, top_ids, top_logits, temperature: float = 1.0, weight=None, 
     f32 = torch.float32
     if top_ids.dim() != 2:
         raise ValueError("top_ids: a 2-D tensor is needed")
-    top = top_ids.shape[1]
+    top = _size(top_ids.shape[1], "top_ids")
     if out is None:
         out = Distilled(torch.empty(n, dtype=f32, device=dev),
                         torch.empty((n, vocab), dtype=logits.dtype, device=dev) if grad else None)

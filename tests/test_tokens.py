@@ -1062,6 +1062,33 @@ def test_python_checks():
             tokens.distill(bad, ids.view(1, 3), torch.zeros((1, 3)))
 
 
+def test_python_sizes():
+    """Sizes past 31 bits, which the C calls would see cut off (meta tensors: nothing is allocated)."""
+    from paper_2302_03851_amd import tokens
+    ids = torch.empty(1, dtype=torch.int32, device="meta")
+    for shape in ((1, 2 ** 32 + 5), (2 ** 32 + 1, 5), (2 ** 31, 1)):
+        big = torch.empty(shape, dtype=BF16, device="meta")
+        one = torch.empty(1, device="meta")
+        for f in (lambda: tokens.embed(ids, big), lambda: tokens.embed_grad(ids, big, 5), lambda: tokens.logprobs(big),
+                  lambda: tokens.logprobs_grad(big, ids, one), lambda: tokens.distill(big, ids.view(1, 1), one.view(1, 1))):
+            with pytest.raises(ValueError, match="2147483647"):
+                f()
+
+
+@gpu
+def test_python_sizes_gpu():
+    """The sizes that are arguments of their own, before anything is allocated by them."""
+    from paper_2302_03851_amd import tokens
+    w = torch.zeros((4, 8), device="cuda")
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    far = torch.zeros(1, dtype=torch.int32, device="cuda").expand(2 ** 32 + 2)
+    for f in (lambda: tokens.embed_grad(ids, w, 2 ** 32 + 3), lambda: tokens.embed_grad(ids, w, -1),
+              lambda: tokens.logprobs(w, ids, top=2 ** 32 + 2), lambda: tokens.logprobs(w, ids, top=-1),
+              lambda: tokens.embed(far, w), lambda: tokens.distill(w, far[None].expand(4, -1), w)):
+        with pytest.raises(ValueError, match="2147483647"):
+            f()
+
+
 @gpu
 def test_python_checks_gpu():
     from paper_2302_03851_amd import tokens
