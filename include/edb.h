@@ -663,9 +663,9 @@ void edb_exec_free(edb_exec_t* e);
  *     matching *_bytes call gives; NULL where that is 0) is written before it
  *     is read and must not be shared by calls that can overlap;
  *   - results do not depend on timing: the same inputs give the same bits;
- *   - rows of logits: vocab <= 2^30, n * ceil(vocab / 131072) <= 2^23; the
- *     temperature is positive and finite, and so is log2(e) / temperature in
- *     fp32 (from 4.3e-39 on);
+ *   - rows of logits: vocab <= 2^30, min(n, 2^21) * ceil(vocab / 131072) <= 2^23;
+ *     the temperature is positive and finite, and so is log2(e) / temperature
+ *     in fp32 (from 4.3e-39 on);
  *   - n == 0 rows are allowed.
  * Errors: EDB_ERR_INVALID (NULL, sizes, strides, alignment, dtype, overlapping
  * input and output, a workspace that is too small), EDB_ERR_UNSUPPORTED (a

@@ -1600,7 +1600,7 @@ constexpr int32_t kMostRows = 1 << 21;
 
 template <class F>
 edb_status in_slices(int32_t n, F&& call) {
-    const int32_t slices = (n + kMostRows - 1) / kMostRows, per = (int32_t)(((int64_t)n + slices - 1) / slices);
+    const int64_t slices = ((int64_t)n + kMostRows - 1) / kMostRows, per = (n + slices - 1) / slices;
     for (int64_t i = 0; i < n; i += per)
         if (edb_status st = call(i, (int32_t)(n - i < per ? n - i : per))) return st;
     return EDB_OK;

@@ -841,6 +841,48 @@ def test_millions_of_rows(dtype):
             assert torch.equal(s[a:b].contiguous().view(torch.uint8), t.view(torch.uint8))
 
 
+def _room(gigabytes):
+    """Skips where the card has less memory left."""
+    import gc
+    gc.collect()
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gigabytes * 10 ** 9:
+        pytest.skip(f"needs {gigabytes} GB of free device memory")
+
+
+@gpu
+def test_most_rows():
+    """As many rows as 32 bits count, of one logit each, the same 1024 again and again: log probabilities, and the
+    gradient in the logits' place, have the bits of those 1024 by themselves."""
+    from paper_2302_03851_amd import tokens
+    _room(80)
+    n = 2 ** 31 - 1
+    few = torch.arange(0x3f00, 0x4300, dtype=torch.int16, device="cuda").view(BF16).view(-1, 1)
+    g1 = torch.arange(1024, device="cuda", dtype=F32) % 3
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ref = tokens.logprobs(few, ids[:1024])
+    ref_d = tokens.logprobs_grad(few, ids[:1024], ref.stats, g_logprob=g1)
+
+    def again(t):
+        return t.repeat(n // 1024 + 1, *[1] * (t.dim() - 1))[:n]
+
+    def check(got, one):
+        assert torch.equal(got[:n // 1024 * 1024].view(-1, *one.shape).amax(0), one)
+        assert torch.equal(got[:n // 1024 * 1024].view(-1, *one.shape).amin(0), one)
+        assert torch.equal(got[n // 1024 * 1024:], one[:n % 1024])
+
+    x = again(few).contiguous()
+    r = tokens.logprobs(x, ids)
+    check(r.logprob, ref.logprob)
+    check(r.entropy, ref.entropy)
+    check(r.stats, ref.stats)
+    g1 = again(g1).contiguous()
+    tokens.logprobs_grad(x, ids, r.stats, g_logprob=g1, out=x)
+    check(x, ref_d)
+    del x, ids, r, g1
+    torch.cuda.empty_cache()
+
+
 # ---- streams and graphs ------------------------------------------------------
 
 
