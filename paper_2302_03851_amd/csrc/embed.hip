@@ -441,18 +441,18 @@ __global__ __launch_bounds__(256) void sum_chunks(SumArgs a) {
     bool from_before = before == cur;
     const uint32_t some = at.pos[0];
     float sum[K] = {};
-    for (int i = begin; i < end; i += 8) {
+    for (int left = end - begin; left > 0; left -= 8) {  // counted down: a position and 8 can pass 2^31
         float v[8][K];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const uint32_t p = i + u < end ? at.pos[u] : some;
+            const uint32_t p = u < left ? at.pos[u] : some;
             load_k<T, K, true>(rows + p * a.dout_stride, v[u]);
         }
         const Eight<WAVE> now = at;
-        if (i + 8 < end) at.load(a, i + 8);
+        if (left > 8) at.load(a, end - left + 8);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            if (i + u >= end) break;
+            if (u >= left) break;
             if (now.key[u] != cur) {
                 if (from_before) store_from<float, K>(partial, sum, piece.skip);
                 else put_word<O, K>(a, cur, piece, sum);

@@ -883,6 +883,22 @@ def test_most_rows():
     torch.cuda.empty_cache()
 
 
+@gpu
+def test_embed_grad_most_rows():
+    """As many ids as 32 bits count.  Every product is 1; sums of them are exact up to 2^24, and less than 64 additions
+    come after that in any tree of threads, chunks and parts: 64 U of the sum."""
+    from paper_2302_03851_amd import tokens
+    _room(100)
+    n = 2 ** 31 - 1
+    ids = torch.arange(n, dtype=torch.int32, device="cuda").remainder_(3)
+    dout = torch.ones((n, 1), dtype=BF16, device="cuda")
+    got = tokens.embed_grad(ids, dout, 4)[:, 0].double()
+    ref = torch.tensor([(n + 2) // 3, (n + 1) // 3, n // 3, 0], dtype=torch.float64, device="cuda")
+    assert float(((got - ref).abs() - 64 * U * ref).max()) <= 0
+    del ids, dout
+    torch.cuda.empty_cache()
+
+
 # ---- streams and graphs ------------------------------------------------------
 
 
