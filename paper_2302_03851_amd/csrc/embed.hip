@@ -581,6 +581,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(SumArgs a) {
 constexpr int kSmall = 4096;
 constexpr int kSmallOften = 64;   // rows from which on a word's columns are split
 constexpr int kSmallThreads = 256, kSmallWaves = kSmallThreads / 64;
+constexpr int kMostFill = 1 << 22;  // work-groups that zero rows: a launch has less than 2^32 threads
 
 struct SmallArgs {
     const int32_t* ids;
@@ -593,7 +594,8 @@ struct SmallArgs {
     int32_t accumulate;
     void* dtable;
     int64_t dtable_stride;
-    int32_t fill_rows, fill_groups;  // rows that each of the first work-groups zeroes where their words do not occur
+    // the first work-groups zero the rows of words that do not occur, so many at a time each
+    int32_t fill_rows, fill_groups;
 };
 
 // kLook: ids that a thread looks at.
@@ -606,17 +608,22 @@ __global__ __launch_bounds__(kSmallThreads) void sum_small(SmallArgs a) {
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
     int32_t id[kLook];
     if ((int)blockIdx.x < a.fill_groups) {
-        const uint32_t first = blockIdx.x * (uint32_t)a.fill_rows, rows = min((uint32_t)a.fill_rows, a.vocab - first);
 #pragma unroll
         for (int r = 0; r < kLook; ++r) id[r] = r * kSmallThreads + tid < a.n ? a.ids[r * kSmallThreads + tid] : -1;
-        if (tid < kFillRows) there[tid] = 0;
-        __syncthreads();
+        uint32_t first = blockIdx.x * (uint32_t)a.fill_rows;
+        while (true) {  // once, but for the largest tables
+            const uint32_t rows = min((uint32_t)a.fill_rows, a.vocab - first);
+            if (tid < kFillRows) there[tid] = 0;
+            __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kLook; ++r)
-            if (id[r] >= 0 && (uint32_t)id[r] - first < rows) there[(uint32_t)id[r] - first] = 1;
-        __syncthreads();
-        zero_rows<O>(a.dtable, a.dtable_stride, a.dim, first, rows, there, kSmallThreads);
-        return;
+            for (int r = 0; r < kLook; ++r)
+                if (id[r] >= 0 && (uint32_t)id[r] - first < rows) there[(uint32_t)id[r] - first] = 1;
+            __syncthreads();
+            zero_rows<O>(a.dtable, a.dtable_stride, a.dim, first, rows, there, kSmallThreads);
+            first += (uint32_t)a.fill_groups * (uint32_t)a.fill_rows;
+            if (first >= a.vocab) return;
+            __syncthreads();
+        }
     }
     const int me = blockIdx.x - a.fill_groups, span = (a.n + kSmallThreads - 1) / kSmallThreads * 64, first = wave * span;
     const uint32_t word = word_of(a.ids[me], a.vocab);
@@ -903,7 +910,8 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
         if (n <= kSmall) {
             const int64_t fit = 16384 / row_bytes;  // rows that a work-group zeroes
             const int fill_rows = (int)(fit < 1 ? 1 : fit > kFillRows ? kFillRows : fit);
-            const int fill_groups = accumulate ? 0 : (int)(((int64_t)vocab + fill_rows - 1) / fill_rows);
+            const int64_t fills = ((int64_t)vocab + fill_rows - 1) / fill_rows;
+            const int fill_groups = accumulate ? 0 : (int)(fills < kMostFill ? fills : kMostFill);
             const SmallArgs a{ids,   n,          (uint32_t)vocab, dim,           g.lanes,   g.tiles_y,  dout, dout_stride,
                               scale, accumulate, dtable,          dtable_stride, fill_rows, fill_groups};
             if (dout_dtype == EDB_F32) {

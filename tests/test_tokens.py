@@ -899,6 +899,29 @@ def test_embed_grad_most_rows():
     torch.cuda.empty_cache()
 
 
+@gpu
+@pytest.mark.parametrize("V,E,dtype", [(2 ** 24 + 3, 2050, F32), (2 ** 23 + 5, 4097, BF16)])
+def test_embed_grad_largest_table(V, E, dtype):
+    """Few ids into a table of more blocks of rows than work-groups that zero them (137 and 69 GB)."""
+    from paper_2302_03851_amd import tokens
+    _room(145)
+    out = torch.empty((V, E), dtype=dtype, device="cuda")
+    step = 2 ** 18
+    for a in range(0, V, step):
+        out[a:a + step].fill_(float("nan"))
+    ids = torch.tensor([V - 1, 0, 2 ** 22, 2 ** 22 + 1, -1, V - 1, 2 ** 23 + 1], dtype=torch.int32, device="cuda")
+    dout = torch.randint(-8, 8, (7, E), device="cuda", generator=_gen(1)).to(dtype)
+    tokens.embed_grad(ids, dout, V, out=out)
+    ref = {V - 1: dout[0] + dout[5], 0: dout[1], 2 ** 22: dout[2], 2 ** 22 + 1: dout[3], 2 ** 23 + 1: dout[6]}
+    for v, row in ref.items():
+        assert torch.equal(out[v], row)
+        out[v] = 0
+    for a in range(0, V, step):
+        assert not out[a:a + step].any()
+    del out
+    torch.cuda.empty_cache()
+
+
 # ---- streams and graphs ------------------------------------------------------
 
 
