@@ -204,6 +204,24 @@ def test_embed_grad_sizes(n, E, src, dst):
 
 
 @gpu
+@pytest.mark.parametrize("n,src,dst", [(300, F32, BF16), (4096, BF16, F32), (5000, F32, F32), (70000, BF16, BF16)])
+@pytest.mark.parametrize("E", [511, 512, 513, 1032, 2049])
+def test_embed_grad_wide(n, E, src, dst):
+    """Rows of more columns than a wave takes at a time, a third of the ids one word."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(n + E)
+    V = 3001
+    ids = _some_ids(n, V, g, True)
+    ids[1::3] = 77
+    dout = torch.randn((n, E), generator=g, device="cuda").to(src)
+    old = torch.randn((V, E), generator=g, device="cuda").to(dst)
+    got = [tokens.embed_grad(ids, dout, V, 0.5, out=old.clone(), accumulate=True) for _ in range(2)]
+    assert torch.equal(got[0].view(torch.uint8), got[1].view(torch.uint8))
+    _grad_check(ids, dout, V, 0.5, dst, got[0], old)
+    _grad_check(ids, dout, V, 0.5, dst, tokens.embed_grad(ids, dout, V, 0.5, dtype=dst))
+
+
+@gpu
 @pytest.mark.parametrize("n", [1, 64, 3000, 5000, 70000])
 @pytest.mark.parametrize("kind", ["same", "two", "none", "ordered", "falling"])
 def test_embed_grad_runs(n, kind):
