@@ -667,8 +667,9 @@ void edb_exec_free(edb_exec_t* e);
  *     the temperature is positive and finite, and so is log2(e) / temperature
  *     in fp32 (from 4.3e-39 on);
  *   - n == 0 rows are allowed.
- * Errors: EDB_ERR_INVALID (NULL, sizes, strides, alignment, dtype, overlapping
- * input and output, a workspace that is too small), EDB_ERR_UNSUPPORTED (a
+ * Errors: EDB_ERR_INVALID (NULL, sizes, strides, alignment, dtype, a result or
+ * the workspace that overlaps another argument where that is not stated to be
+ * allowed, a workspace that is too small), EDB_ERR_UNSUPPORTED (a
  * size beyond the stated limits), EDB_ERR_HIP. */
 
 /* out[i][:] = scale * table[ids[i]][:], a zero row where there is no token.

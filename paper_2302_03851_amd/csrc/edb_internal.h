@@ -3,6 +3,7 @@
 
 #include <new>
 #include <cstdint>
+#include <initializer_list>
 #include <map>
 #include <string>
 #include <tuple>
@@ -53,6 +54,42 @@ edb_status guarded(F&& body) {
         clear_error();
         return EDB_ERR_OOM;
     }
+}
+
+// Device memory of an argument: `rows` rows of `row` bytes, `stride` bytes apart; NULL for none.
+struct Region {
+    const void* p;
+    int64_t rows, row, stride;
+
+    static Region array(const void* p, int64_t bytes) { return {bytes > 0 ? p : nullptr, 1, bytes, bytes}; }
+};
+
+// Whether an array (one row) has memory in common with `b`.
+inline bool overlap(const Region& array, const Region& b) {
+    if (!array.p || !b.p) return false;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(array.p), a1 = a0 + (uintptr_t)array.row,
+                    b0 = reinterpret_cast<uintptr_t>(b.p);
+    // the first row of b that ends behind the array's beginning
+    const int64_t r = a0 < b0 + (uintptr_t)b.row ? 0 : (int64_t)((a0 - b0 - (uintptr_t)b.row) / (uintptr_t)b.stride) + 1;
+    return r < b.rows && b0 + (uintptr_t)(r * b.stride) < a1;
+}
+
+// Arrays that a call writes (or uses as scratch memory) have to be apart from each other and from `others`.
+inline edb_status apart(const char* who, std::initializer_list<Region> arrays, std::initializer_list<Region> others) {
+    for (const Region* a = arrays.begin(); a != arrays.end(); ++a) {
+        bool bad = false;
+        for (const Region* b = a + 1; b != arrays.end(); ++b) bad = bad || overlap(*a, *b);
+        for (const Region& b : others) bad = bad || overlap(*a, b);
+        if (bad) return fail(EDB_ERR_INVALID, std::string(who) + ": a result or the workspace overlaps another argument");
+    }
+    return EDB_OK;
+}
+
+// Whether all are aligned to 4 bytes.
+inline bool word_aligned(std::initializer_list<const void*> all) {
+    uintptr_t bits = 0;
+    for (const void* p : all) bits |= reinterpret_cast<uintptr_t>(p);
+    return (bits & 3u) == 0;
 }
 
 // edb_build_graph with the acyclicity check optional: without it the graph

@@ -11,6 +11,7 @@
 #include "row_access.h"
 
 using edb::fail;
+using edb::Region;
 using namespace edb::rows;
 
 namespace {
@@ -861,6 +862,10 @@ extern "C" edb_status edb_embed(const int32_t* ids, int32_t n, const void* table
         if (!ids || !table || !out) return fail(EDB_ERR_INVALID, "edb_embed: NULL argument");
         if (!element_aligned(table, table_dtype) || !element_aligned(out, out_dtype))
             return fail(EDB_ERR_INVALID, "edb_embed: the table and the result must be aligned to their elements");
+        if (!edb::word_aligned({ids})) return fail(EDB_ERR_INVALID, "edb_embed: the ids must be aligned to 4 bytes");
+        const int64_t out_bytes = elem_bytes(out_dtype);
+        if (edb::overlap(Region::array(ids, n * INT64_C(4)), {out, n, dim * out_bytes, out_stride * out_bytes}))
+            return fail(EDB_ERR_INVALID, "edb_embed: the result overlaps the ids");
         if (overlap(table, ((vocab - 1) * table_stride + dim) * elem_bytes(table_dtype), out,
                     ((n - 1) * out_stride + dim) * elem_bytes(out_dtype)))
             return fail(EDB_ERR_INVALID, "edb_embed: the result overlaps the table");
@@ -901,12 +906,18 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
         if (n && overlap(dout, ((n - 1) * dout_stride + dim) * elem_bytes(dout_dtype), dtable,
                          ((vocab - 1) * dtable_stride + dim) * elem_bytes(dtable_dtype)))
             return fail(EDB_ERR_INVALID, "edb_embed_grad: the table's gradient overlaps the rows' gradients");
+        if (!edb::word_aligned({ids})) return fail(EDB_ERR_INVALID, "edb_embed_grad: the ids must be aligned to 4 bytes");
         const GradPlan g = grad_plan(n, vocab, dim);
         if (workspace_bytes < g.bytes || (g.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
             return fail(EDB_ERR_INVALID, "edb_embed_grad: a 16-byte aligned workspace of " + std::to_string(g.bytes) +
                                              " bytes is needed");
-        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
         const int64_t row_bytes = dim * elem_bytes(dtable_dtype);
+        const Region id_array = Region::array(ids, n * INT64_C(4)),
+                     rows{dtable, vocab, row_bytes, dtable_stride * elem_bytes(dtable_dtype)},
+                     drows{n ? dout : nullptr, n, dim * elem_bytes(dout_dtype), dout_stride * elem_bytes(dout_dtype)};
+        if (edb_status st = edb::apart(who, {Region::array(workspace, g.bytes)}, {id_array, rows, drows})) return st;
+        if (edb::overlap(id_array, rows)) return fail(EDB_ERR_INVALID, "edb_embed_grad: the table's gradient overlaps the ids");
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
         if (n <= kSmall) {
             const int64_t fit = 16384 / row_bytes;  // rows that a work-group zeroes
             const int fill_rows = (int)(fit < 1 ? 1 : fit > kFillRows ? kFillRows : fit);

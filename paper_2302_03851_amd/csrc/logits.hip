@@ -22,6 +22,7 @@
 #include "row_access.h"
 
 using edb::fail;
+using edb::Region;
 using namespace edb::rows;
 
 namespace {
@@ -1420,6 +1421,18 @@ edb_status check_rows(const char* who, const void* logits, int32_t dtype, int32_
     return EDB_OK;
 }
 
+Region matrix(const void* p, int32_t dtype, int32_t n, int32_t vocab, int64_t stride) {
+    const int64_t bytes = dtype == EDB_BF16 ? 2 : 4;
+    return {p, n, vocab * bytes, stride * bytes};
+}
+
+// An array of `each` 32-bit words a row.
+Region words(const void* p, int32_t n, int64_t each = 1) { return Region::array(p, n * each * 4); }
+
+edb_status misaligned(const char* who) {
+    return fail(EDB_ERR_INVALID, std::string(who) + ": ids and fp32 arrays must be aligned to 4 bytes");
+}
+
 // The gradient's rows: apart from the logits, or exactly in their place.
 edb_status check_grad(const char* who, const void* logits, int64_t stride, const void* out, int64_t out_stride,
                       int32_t dtype, int32_t n, int32_t vocab) {
@@ -1648,6 +1661,12 @@ extern "C" edb_status edb_logprobs(const void* logits, int32_t dtype, int32_t n,
         if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
             return fail(EDB_ERR_INVALID, "edb_logprobs: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
                                              " bytes is needed");
+        if (!edb::word_aligned({ids, logprob, entropy, stats, top_ids, top_logprobs})) return misaligned(who);
+        if (edb_status st = edb::apart(who,
+                                       {words(logprob, n), words(entropy, n), words(stats, n, 2), words(top_ids, n, top),
+                                        words(top_logprobs, n, top), Region::array(workspace, r.bytes)},
+                                       {matrix(logits, dtype, n, vocab, stride), words(ids, n)}))
+            return st;
         if (n > kMostRows)
             return in_slices(n, [&](int64_t i, int32_t m) {
                 return edb_logprobs(rows_from(logits, i, stride, dtype), dtype, m, vocab, stride, rows_from(ids, i),
@@ -1704,6 +1723,10 @@ extern "C" edb_status edb_logprobs_grad(const void* logits, int32_t dtype, int32
             edb::clear_error();
             return EDB_OK;
         }
+        if (!edb::word_aligned({ids, stats, entropy, g_logprob, g_entropy})) return misaligned(who);
+        const Region slopes = matrix(dlogits, dtype, n, vocab, dlogits_stride);
+        for (const Region& r : {words(ids, n), words(stats, n, 2), words(entropy, n), words(g_logprob, n), words(g_entropy, n)})
+            if (edb::overlap(r, slopes)) return fail(EDB_ERR_INVALID, "edb_logprobs_grad: the gradient overlaps another argument");
         if (n > kMostRows)
             return in_slices(n, [&](int64_t i, int32_t m) {
                 return edb_logprobs_grad(rows_from(logits, i, stride, dtype), dtype, m, vocab, stride, ids + i,
@@ -1755,6 +1778,14 @@ extern "C" edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, 
         if (workspace_bytes < r.bytes || (r.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
             return fail(EDB_ERR_INVALID, "edb_distill: a 16-byte aligned workspace of " + std::to_string(r.bytes) +
                                              " bytes is needed");
+        if (!edb::word_aligned({top_ids, top_logits, weight, loss})) return misaligned(who);
+        const Region ids = words(top_ids, n, top), listed = words(top_logits, n, top), weights = words(weight, n),
+                     slopes = matrix(dlogits, dtype, n, vocab, dlogits_stride);
+        if (edb_status st = edb::apart(who, {words(loss, n), Region::array(workspace, r.bytes)},
+                                       {ids, listed, weights, matrix(logits, dtype, n, vocab, stride), slopes}))
+            return st;
+        for (const Region& in : {ids, listed, weights})
+            if (edb::overlap(in, slopes)) return fail(EDB_ERR_INVALID, "edb_distill: the gradient overlaps another argument");
         if (n > kMostRows)
             return in_slices(n, [&](int64_t i, int32_t m) {
                 return edb_distill(rows_from(logits, i, stride, dtype), dtype, m, vocab, stride, top_ids + i * top,

@@ -1114,6 +1114,53 @@ def test_refusals(call, changed, status):
     assert L.load().edb_last_error()
 
 
+# arguments apart from each other; n = 4, V = 10, rows 40 bytes and 1 MB apart in `far`
+LP_APART = dict(lp=3 * A, h=3 * A + 64, st=3 * A + 128, ti=3 * A + 192, tl=3 * A + 256)
+DI_APART = dict(loss=6 * A)
+OVERLAPS = (
+    [(_embed, k) for k in [dict(out=A + 8), dict(out=A - 32 * 4 + 4), dict(out=A - 256 - 28, os=64), dict(ids=2), dict(ids=A + 1)]]
+    + [(_embed_grad, k) for k in [dict(out=A - 316), dict(out=A + 12), dict(ids=A + 2), dict(n=5000, ids=4 * A + 160),
+                                  dict(n=5000, out=4 * A - 64), dict(n=5000, dout=4 * A + 16, out=64 * A),
+                                  dict(n=5000, dout=4 * A - 159996, out=64 * A)]]
+    + [(_logprobs, dict(LP_APART, **k)) for k in [
+        dict(lp=A), dict(h=A + 156), dict(st=A - 28), dict(ti=A + 40), dict(tl=A + 128), dict(lp=2 * A + 12), dict(h=2 * A - 12),
+        dict(h=3 * A + 12), dict(st=3 * A + 76), dict(tl=3 * A + 220), dict(s=A // 4, lp=2 * A + 36, ids=9 * A),
+        dict(s=A // 4, lp=4 * A - 12, ids=9 * A), dict(lp=3 * A + 1), dict(h=3 * A + 66), dict(st=3 * A + 131), dict(ti=3 * A + 193),
+        dict(tl=3 * A + 258), dict(ids=2 * A + 2), dict(n=1, V=100000, s=100000, ids=9 * A, ws=3 * A),
+        dict(n=1, V=100000, s=100000, ids=9 * A, ws=A + 399984), dict(n=1, V=100000, s=100000, ids=4 * A + 64)]]
+    + [(_lp_grad, k) for k in [dict(out=2 * A - 156), dict(out=3 * A + 28), dict(out=2 * A + 12), dict(ids=2 * A + 1), dict(st=3 * A + 2),
+                               dict(h=3 * A + 1), dict(g1=3 * A + 3), dict(g2=3 * A + 2), dict(g1=4 * A + 144),
+                               dict(g2=4 * A + 36, os=20), dict(h=4 * A - 12), dict(st=4 * A - 28)]]
+    + [(_distill, dict(DI_APART, **k)) for k in [
+        dict(loss=3 * A), dict(loss=A + 156), dict(loss=2 * A + 28), dict(loss=4 * A + 120), dict(w=4 * A + 8), dict(ti=4 * A - 28),
+        dict(tl=4 * A + 156), dict(loss=6 * A + 2), dict(w=3 * A + 1), dict(ti=2 * A + 2), dict(tl=3 * A + 2),
+        dict(n=1, V=200000, s=200000, os=200000, ws=6 * A), dict(n=1, V=200000, s=200000, os=200000, ws=2 * A),
+        dict(n=1, V=200000, s=200000, os=200000, ws=4 * A + 799984)]])
+
+
+@pytest.mark.parametrize("call,changed", OVERLAPS, ids=[f"{f.__name__[1:]}-{i}" for i, (f, _) in enumerate(OVERLAPS)])
+def test_refused_overlaps(call, changed):
+    """Results and workspaces in another argument's memory, by one word at either end, and arrays off their words."""
+    assert call(**changed) == INVALID
+
+
+@gpu
+def test_arrays_between_rows():
+    """Results may lie between the rows of a matrix, right up to them."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(8)
+    n, V = 3, 10
+    mem = torch.zeros(200, device="cuda")
+    x = mem.as_strided((n, V), (60, 1), 8)
+    x.copy_(torch.randn((n, V), generator=g, device="cuda"))
+    ids = torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda")
+    ref = tokens.logprobs(x.contiguous(), ids, top=2)
+    out = tokens.LogProbs(mem[5:8], mem[18:21], mem[21:27].view(3, 2), mem[62:68].view(torch.int32).view(3, 2), mem[138:144].view(3, 2))
+    got = tokens.logprobs(x, ids, top=2, out=out)
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("call", [_logprobs, _lp_grad, _distill])
 def test_refused_temperatures(call):
     """Where 1 / T is finite and the exponents' factor log2(e) / T is not."""
