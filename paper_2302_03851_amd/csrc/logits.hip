@@ -33,7 +33,10 @@ constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLow = -1.0e4f;
 constexpr float kInf = __builtin_huge_valf();
 
-__device__ __forceinline__ float exp2_hw(float y) { return __builtin_amdgcn_exp2f(y); }
+__device__ __forceinline__ float exp2_hw(float y) { return __builtin_amdgcn_exp2f(y); }  // 0 below 2^-126
+
+// 2^y k from e = 2^(y/2), which is a normal number where 2^y is not: 0 only where the product itself is too small.
+__device__ __forceinline__ float squared_times(float e, float k) { return e * (e * k); }
 
 // The value of lane (l ^ D), by data-parallel moves inside rows of 16 lanes.
 template <int D>
@@ -903,8 +906,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs
         zero_row(d, V, gridDim.y * blockDim.x, blockIdx.y * blockDim.x);
         return;
     }
-    // p (k0 + k1 log2 p / 2), k0 = -(g_lp + g_H H) / T, k1 = -2 g_H ln 2 / T.  p is the square of 2^(log2 p / 2), which
-    // is a normal number where p is not, and comes last: a result is 0 only where it is too small itself, not its p.
+    // p (k0 + k1 log2 p / 2), k0 = -(g_lp + g_H H) / T, k1 = -2 g_H ln 2 / T
     const float k0 = -(g1 + (a.g_entropy ? g2 * a.entropy[row] : 0.f)), k1 = -2.f * (g2 * kLn2);
     const float half_c = 0.5f * a.c, half_l2 = 0.5f * l2;
     const bool odd = odd_row(x), odd_out = odd_row(d), straight = straight_row(d);
@@ -914,7 +916,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void logprobs_grad_kernel(GradArgs
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float y = __builtin_fmaf(v[i] - m, half_c, -half_l2), e = exp2_hw(y);
-            v[i] = e * (e * __builtin_fmaf(k1, fmaxf(y, kLow), k0));
+            v[i] = squared_times(e, __builtin_fmaf(k1, fmaxf(y, kLow), k0));
         }
         const int at = id - j;
         if (at >= 0 && at < N) {
@@ -1176,13 +1178,17 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
     if (out && tid == 0) a.loss[row] = 0.f;
     if (!d) return;
 
-    const float k = w * a.t, ks = k / st.s;
+    // A factor w T / S of 1 or more takes its power of two into the exponent, so that a result is 0 only where it is too
+    // small itself, not its 2^y.  (A square as in the other gradients costs 3% here: 4096 x 131072, 475 us for 460.)
+    const float k = w * a.t;
+    const int lift = max(0, __builtin_amdgcn_frexp_expf(k / st.s));
+    const float ks = __builtin_amdgcn_ldexpf(k / st.s, -lift), base = lift ? ref : low, shift = lift ? -(float)lift : r;
     const bool zero = out || st.empty();
     auto slope = [&](u32x4 q) {
         float v[N];
         Elem<T>::unpack(q, v);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = exp2_hw(__builtin_fmaf(v[e] - low, a.c, -r)) * ks;
+        for (int e = 0; e < N; ++e) v[e] = exp2_hw(__builtin_fmaf(v[e] - base, a.c, -shift)) * ks;
         const u32x4 o = Elem<T>::pack(v);
         return zero ? u32x4{0u, 0u, 0u, 0u} : o;
     };
@@ -1210,15 +1216,14 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs a) {
     if (has_rest) store_vector(d, j_rest, V, slope(rest), odd_out, straight, lane);
     __syncthreads();
     if (l.id >= 0 && !zero) {
-        const float p = exp2_hw(__builtin_fmaf(z - low, a.c, -r)) / st.s;
-        Elem<T>::put(d + l.id, (p - l.mass) * k);
+        Elem<T>::put(d + l.id, exp2_hw(__builtin_fmaf(z - base, a.c, -shift)) * ks - l.mass * k);
     }
 }
 
-// 2^y of a logit, y = x c - r(m) (see Stats).
-__device__ __forceinline__ float mass_of(float v, float c, float ref) {
-    const float r = ref * c;
-    return exp2_hw(Stats::plain(r) ? __builtin_fmaf(v, c, -r) : (v - ref) * c);
+// 2^y ks of a logit, y = x c - r(m) (see Stats).
+__device__ __forceinline__ float mass_of(float v, float c, float ref, float ks) {
+    const float r = ref * c, half_c = 0.5f * c;
+    return squared_times(exp2_hw(Stats::plain(r) ? __builtin_fmaf(v, half_c, -0.5f * r) : (v - ref) * half_c), ks);
 }
 
 template <class T>
@@ -1240,7 +1245,7 @@ __device__ __forceinline__ void put_masses(const T* x, T* d, int begin, int end,
         float v[N];
         load_up_to<T>(x, j, end, v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = mass_of(v[i], c, ref) * ks;
+        for (int i = 0; i < N; ++i) v[i] = mass_of(v[i], c, ref, ks);
         if (j + N <= end) {
             Elem<T>::store_nt(d + j, Elem<T>::pack(v));
         } else {
@@ -1303,7 +1308,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void distill_short(DistillArgs a)
     const float k = w * a.t, ks = k / st.s;
     put_masses<T>(x, d, 0, V, kThreads, a.c, ref, ks);
     __syncthreads();
-    if (l.id >= 0) Elem<T>::put(d + l.id, (mass_of(z, a.c, ref) / st.s - l.mass) * k);
+    if (l.id >= 0) Elem<T>::put(d + l.id, mass_of(z, a.c, ref, ks) - l.mass * k);
 }
 
 // Rows that are split over work-groups (see distill_plan).  A first launch takes the statistics of every part,
@@ -1394,7 +1399,7 @@ __global__ __launch_bounds__(64 * kPartWaves) void distill_parts_grad(DistillArg
     const float k = w * a.t, ks = k / st.s;
     put_masses<T>(x, d, begin, end, kThreads, a.c, ref, ks);
     __syncthreads();
-    if (l.id >= begin && l.id < end) Elem<T>::put(d + l.id, (mass_of(z, a.c, ref) / st.s - l.mass) * k);
+    if (l.id >= begin && l.id < end) Elem<T>::put(d + l.id, mass_of(z, a.c, ref, ks) - l.mass * k);
 }
 
 constexpr int64_t kMaxElems = INT64_C(1) << 48;  // of a matrix, gaps included: offsets in bytes stay far inside 64 bits

@@ -814,6 +814,25 @@ def test_distill_temperatures(n, V, dtype, T):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(6, 200), (6, 9001), (6, 131072)])
+def test_distill_small(n, V, dtype):
+    """Probabilities on both sides of the least normal number, whose gradients the weight lifts above it; listed tokens
+    without mass among them."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(V)
+    x = -86 - 8 * torch.rand((n, V), generator=g, device="cuda")
+    x[:, V // 2] = 0.5 * torch.rand(n, generator=g, device="cuda")
+    x = x.to(dtype)
+    ids, u = _teacher(n, V, 5, g, "distinct")
+    u[:, 3:] = -INF
+    w = torch.rand(n, generator=g, device="cuda") * 65536
+    _check_distill(x, ids, u, 1.5, w, tokens.distill(x, ids, u, 1.5, w))
+    x = (x.float() * 1.5).to(dtype)
+    _check_distill(x, ids, u, 1.5, w, tokens.distill(x, ids, u, 1.5, w))
+
+
+@gpu
 def test_distill_differences():
     """Central differences of the 64-bit loss (as for the log probabilities)."""
     from paper_2302_03851_amd import tokens
