@@ -656,7 +656,7 @@ void edb_exec_free(edb_exec_t* e);
  *     elements; dtype is EDB_F32 or EDB_BF16 and every sum is fp32 (a bf16
  *     result is rounded to nearest even once);
  *   - a token id outside [0, vocab) stands for no token (-1 by convention):
- *     nothing is read for it;
+ *     what stands in its row of gradients or logits has no effect;
  *   - the work is enqueued on `stream` on the current device; no call waits,
  *     allocates or keeps anything, so all may be captured into a HIP graph.  A
  *     workspace (device, 16-byte aligned, of at least the bytes that the
@@ -696,13 +696,13 @@ edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* dout, int32
  *   logits   [n x vocab]; a token is masked out by -inf
  *   ids      int32[n], or NULL: no given tokens (logprob must be NULL then)
  *   logprob  float[n] or NULL: ln p of the given token (-inf if masked out)
- *   entropy  float[n] or NULL: -sum p ln p
+ *   entropy  float[n] or NULL: -sum p ln p, not below 0 (nor is ln p above it)
  *   stats    float[n][2] or NULL: the largest logit m and
  *            ln sum exp((x - m) / temperature), for edb_logprobs_grad
  *   top_ids, top_logprobs  int32 and float [n][top], 0 <= top <=
  *            EDB_LOGPROBS_MAX_TOP: the largest logits, the lowest id first
  *            among equal ones; without masked ones, -1 and -inf past the end
- * A row whose id (where ids are given) is no token is not read: 0 everywhere,
+ * A row whose id (where ids are given) is no token is left out: 0 everywhere,
  * no alternatives.  A row that is masked out whole has log probability -inf,
  * entropy 0, stats (-inf, 0) and no alternatives.  A row with a NaN or +inf has
  * no distribution: NaN, stats (NaN, NaN); its alternatives are listed by value,

@@ -1,7 +1,7 @@
 // Embedding lookup with scaling, and the table's gradient.
 //
 //   y_i  = s W[id_i]                              (a zero row where id_i is outside [0, V))
-//   dW_v = s sum over i with id_i = v of dy_i     (in fp32, the i in ascending order)
+//   dW_v = s sum over i with id_i = v of dy_i     (in fp32, in an order that the places of v fix)
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -74,9 +74,11 @@ struct EmbedArgs {
 };
 
 // One thread per K elements of a row: 16 bytes of the result, so that a wave
-// writes whole lines, past the caches.  Memory bound: 262144 x 512 bf16, 536 MB
-// written and read, 59 us (5.5 TB/s; through the caches 95); 28629 x 512 from
-// fp32 to bf16 10.5 us.  112 x 64: 2.5 us, a launch.
+// writes whole lines, past the caches.  Memory bound: 262144 x 512 bf16, 268 MB
+// written and 59 MB of rows that occur read, 61 us (5.4 TB/s; through the caches
+// 99); 28629 x 512 from fp32 to bf16 11.5 us.  112 x 64: 2.5 us, a launch.  A
+// result that the caches could hold costs the next kernel what this one saves:
+// 4000 x 512 and a product with it 13.7 us, written through the caches 11.9.
 template <class T, class O, int K>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
     const int pieces = (a.dim + K - 1) / K;
@@ -102,8 +104,10 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
 
 // ---- the gradient: positions sorted by word, then sums over the runs of a word
 //
-// The sort is a stable radix sort of (word, position), so a word's rows are
-// added in ascending position and the result does not depend on timing.  Ids
+// The sort is a stable radix sort of (word, position), so a word's rows come in
+// ascending position.  They are added in that order inside a chunk, and the parts
+// of a run over several chunks by groups of lanes, then waves: an order that the
+// places fix, so that the result does not depend on timing.  Ids
 // that are no token get the word V and sort to the end.  It takes a pass for
 // every digit of up to kMaxDigit bits, of counts per tile, their prefix sums and
 // the scatter.  These launches leave the memory idle, so further work-groups of

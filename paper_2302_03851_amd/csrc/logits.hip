@@ -158,7 +158,9 @@ __device__ __forceinline__ void shift_in_all(u32x4 (&raw)[M], int count, const T
 // 16 bytes of a result that is not read again here: past the caches where a
 // wave writes whole lines, through them where two waves share some (gradient of
 // log probabilities with four vectors a turn, 8192 x 65536 bf16: 397 us past the
-// caches, 418 through them; 8192 x 65532: 463 and 436).
+// caches, 418 through them; 8192 x 65532: 463 and 436).  Where the caches could hold
+// the result, the next kernel pays for it: gradient of 1000 x 65536 and a product
+// with it 260 us, written through the caches 247; distillation 263 and 253.
 template <class T>
 __device__ __forceinline__ void store_piece(T* p, u32x4 v, bool straight) {
     if (straight) {
@@ -547,7 +549,7 @@ constexpr int kLoads = 2;  // 16-byte loads of a thread in flight, beside as man
 // `top` of these groups (a group that does not belong to them has `top` groups
 // with a better logit before it), so at the end one wave looks for those groups
 // and reads them again.  Memory bound where there are many logits: 8192 x 65536
-// bf16, 1.07 GB, 169 us without alternatives (6.4 TB/s), 180 with 5, 201 with
+// bf16, 1.07 GB, 171 us without alternatives (6.3 TB/s), 178 with 5, 204 with
 // 63.  Few or short rows are bound by the chain of steps of the choice, about 3
 // us a row and wave: 23 x 3801 bf16 4 us, 7 with 5 alternatives.
 // (W: row_waves; at most 64 registers, for eight waves a SIMD: 4381 x 4108 fp32,
@@ -889,7 +891,7 @@ struct GradArgs {
 // neighbouring vectors of 1 KB in turn: eight, of which fewer begin or end in a
 // line that two waves write (8192 x 65533: 422 us, with four 432), or four where
 // rows are few (300 x 10007 fp32: 6.4 us, with eight 6.9).  Memory bound: 8192 x
-// 65536 bf16, read and written, 2.15 GB, 383 us (5.6 TB/s; a copy reaches 5.4).
+// 65536 bf16, read and written, 2.15 GB, 385 us (5.6 TB/s; a copy reaches 5.4).
 constexpr int kGradWaves = 8;  // waves of a work-group at most
 
 template <class T, int LOADS, bool CACHED>
@@ -1080,7 +1082,7 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t row, cons
 // (see Stats) is summed up in one pass over the registers, w T p_j = 2^y (w T / S)
 // written in another; the owners of the listed entries then write
 // w T (p_j - q_j).  Memory bound with many rows: 8192 x 65536 bf16, 2.15 GB, 383
-// us (5.6 TB/s); 4096 x 131072 437 (4.9), where a row fills the registers of a
+// us (5.6 TB/s); 4096 x 131072 453 (4.7), where a row fills the registers of a
 // compute unit, so that no other one is read while it is summed up; the chain of
 // these steps with few: 128 x 8192 fp32 6 us.
 constexpr int kBlock = 2;
