@@ -669,7 +669,8 @@ void edb_exec_free(edb_exec_t* e);
  *   - n == 0 rows are allowed.
  * Errors: EDB_ERR_INVALID (NULL, sizes, strides, alignment, dtype, a result or
  * the workspace that overlaps another argument where that is not stated to be
- * allowed, a workspace that is too small), EDB_ERR_UNSUPPORTED (a
+ * allowed; matrices of one row stride may share a buffer as separate columns, of
+ * different ones they may not; a workspace that is too small), EDB_ERR_UNSUPPORTED (a
  * size beyond the stated limits), EDB_ERR_HIP. */
 
 /* out[i][:] = scale * table[ids[i]][:], a zero row where there is no token.

@@ -64,14 +64,22 @@ struct Region {
     static Region array(const void* p, int64_t bytes) { return {bytes > 0 ? p : nullptr, 1, bytes, bytes}; }
 };
 
-// Whether an array (one row) has memory in common with `b`.
-inline bool overlap(const Region& array, const Region& b) {
-    if (!array.p || !b.p) return false;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(array.p), a1 = a0 + (uintptr_t)array.row,
-                    b0 = reinterpret_cast<uintptr_t>(b.p);
-    // the first row of b that ends behind the array's beginning
-    const int64_t r = a0 < b0 + (uintptr_t)b.row ? 0 : (int64_t)((a0 - b0 - (uintptr_t)b.row) / (uintptr_t)b.stride) + 1;
-    return r < b.rows && b0 + (uintptr_t)(r * b.stride) < a1;
+// Whether two have memory in common.  (Matrices of different row strides: whether
+// they lie between each other's ends, which is as much as is looked at.)
+inline bool overlap(const Region& a, const Region& b) {
+    if (!a.p || !b.p) return false;
+    const int64_t a0 = (int64_t)reinterpret_cast<uintptr_t>(a.p), b0 = (int64_t)reinterpret_cast<uintptr_t>(b.p),
+                  a1 = a0 + (a.rows - 1) * a.stride + a.row, b1 = b0 + (b.rows - 1) * b.stride + b.row;
+    if (a0 >= b1 || b0 >= a1) return false;
+    if (a.rows > 1 && b.rows > 1) {
+        if (a.stride != b.stride) return true;
+        const int64_t apart = (b0 - a0) % a.stride, column = apart < 0 ? apart + a.stride : apart;  // of b in a's rows
+        return column < a.row || column + b.row > a.stride;
+    }
+    if (a.rows > 1) return overlap(b, a);
+    // the first row of b that ends behind the one of a begins
+    const int64_t r = a0 < b0 + b.row ? 0 : (a0 - b0 - b.row) / b.stride + 1;
+    return r < b.rows && b0 + r * b.stride < a1;
 }
 
 // Arrays that a call writes (or uses as scratch memory) have to be apart from each other and from `others`.

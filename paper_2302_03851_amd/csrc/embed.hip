@@ -738,9 +738,8 @@ bool element_aligned(const void* p, int32_t dtype) {
     return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(elem_bytes(dtype) - 1)) == 0;
 }
 
-bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+Region matrix(const void* p, int32_t dtype, int32_t rows, int32_t dim, int64_t stride) {
+    return {rows ? p : nullptr, rows, dim * elem_bytes(dtype), stride * elem_bytes(dtype)};
 }
 
 edb_status launched(const char* who) {
@@ -867,11 +866,10 @@ extern "C" edb_status edb_embed(const int32_t* ids, int32_t n, const void* table
         if (!element_aligned(table, table_dtype) || !element_aligned(out, out_dtype))
             return fail(EDB_ERR_INVALID, "edb_embed: the table and the result must be aligned to their elements");
         if (!edb::word_aligned({ids})) return fail(EDB_ERR_INVALID, "edb_embed: the ids must be aligned to 4 bytes");
-        const int64_t out_bytes = elem_bytes(out_dtype);
-        if (edb::overlap(Region::array(ids, n * INT64_C(4)), {out, n, dim * out_bytes, out_stride * out_bytes}))
+        const Region result = matrix(out, out_dtype, n, dim, out_stride);
+        if (edb::overlap(Region::array(ids, n * INT64_C(4)), result))
             return fail(EDB_ERR_INVALID, "edb_embed: the result overlaps the ids");
-        if (overlap(table, ((vocab - 1) * table_stride + dim) * elem_bytes(table_dtype), out,
-                    ((n - 1) * out_stride + dim) * elem_bytes(out_dtype)))
+        if (edb::overlap(matrix(table, table_dtype, vocab, dim, table_stride), result))
             return fail(EDB_ERR_INVALID, "edb_embed: the result overlaps the table");
         if ((int64_t)n * dim > (INT64_C(1) << 38)) return fail(EDB_ERR_UNSUPPORTED, "edb_embed: n * dim exceeds 2^38");
         const EmbedArgs a{ids, n, vocab, dim, table, table_stride, scale, out, out_stride};
@@ -907,21 +905,19 @@ extern "C" edb_status edb_embed_grad(const int32_t* ids, int32_t n, const void* 
         if (!dtable || (n && (!ids || !dout))) return fail(EDB_ERR_INVALID, "edb_embed_grad: NULL argument");
         if (!element_aligned(dout, dout_dtype) || !element_aligned(dtable, dtable_dtype))
             return fail(EDB_ERR_INVALID, "edb_embed_grad: both gradients must be aligned to their elements");
-        if (n && overlap(dout, ((n - 1) * dout_stride + dim) * elem_bytes(dout_dtype), dtable,
-                         ((vocab - 1) * dtable_stride + dim) * elem_bytes(dtable_dtype)))
+        const Region id_array = Region::array(ids, n * INT64_C(4)), rows = matrix(dtable, dtable_dtype, vocab, dim, dtable_stride),
+                     drows = matrix(dout, dout_dtype, n, dim, dout_stride);
+        if (edb::overlap(drows, rows))
             return fail(EDB_ERR_INVALID, "edb_embed_grad: the table's gradient overlaps the rows' gradients");
         if (!edb::word_aligned({ids})) return fail(EDB_ERR_INVALID, "edb_embed_grad: the ids must be aligned to 4 bytes");
         const GradPlan g = grad_plan(n, vocab, dim);
         if (workspace_bytes < g.bytes || (g.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
             return fail(EDB_ERR_INVALID, "edb_embed_grad: a 16-byte aligned workspace of " + std::to_string(g.bytes) +
                                              " bytes is needed");
-        const int64_t row_bytes = dim * elem_bytes(dtable_dtype);
-        const Region id_array = Region::array(ids, n * INT64_C(4)),
-                     rows{dtable, vocab, row_bytes, dtable_stride * elem_bytes(dtable_dtype)},
-                     drows{n ? dout : nullptr, n, dim * elem_bytes(dout_dtype), dout_stride * elem_bytes(dout_dtype)};
         if (edb_status st = edb::apart(who, {Region::array(workspace, g.bytes)}, {id_array, rows, drows})) return st;
         if (edb::overlap(id_array, rows)) return fail(EDB_ERR_INVALID, "edb_embed_grad: the table's gradient overlaps the ids");
         hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        const int64_t row_bytes = rows.row;
         if (n <= kSmall) {
             const int64_t fit = 16384 / row_bytes;  // rows that a work-group zeroes
             const int fill_rows = (int)(fit < 1 ? 1 : fit > kFillRows ? kFillRows : fit);

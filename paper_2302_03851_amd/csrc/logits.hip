@@ -1449,11 +1449,7 @@ edb_status check_grad(const char* who, const void* logits, int64_t stride, const
         return fail(EDB_ERR_INVALID, w + ": the gradient's rows span more than 2^48 elements");
     if (!aligned(out, dtype)) return fail(EDB_ERR_INVALID, w + ": the gradient must be aligned to its elements");
     if (n == 0 || (out == logits && out_stride == stride)) return EDB_OK;
-    const int64_t es = dtype == EDB_BF16 ? 2 : 4;
-    const uintptr_t x0 = reinterpret_cast<uintptr_t>(logits), d0 = reinterpret_cast<uintptr_t>(out);
-    const uintptr_t x1 = x0 + (uintptr_t)(((n - 1) * stride + vocab) * es),
-                    d1 = d0 + (uintptr_t)(((n - 1) * out_stride + vocab) * es);
-    if (x0 < d1 && d0 < x1)
+    if (edb::overlap(matrix(logits, dtype, n, vocab, stride), matrix(out, dtype, n, vocab, out_stride)))
         return fail(EDB_ERR_INVALID, w + ": the gradient overlaps the logits without being in their place");
     return EDB_OK;
 }

@@ -1163,6 +1163,50 @@ def test_refused_overlaps(call, changed):
     assert call(**changed) == INVALID
 
 
+BESIDE = [(_embed, dict(table=A, ts=30, os=30, out=A + k, ids=9 * A)) for k in (28, -28, 92, 4 * 30 * 3 + 28)] + \
+         [(_embed_grad, dict(dout=A, ds=30, os=30, out=A + k, ids=9 * A)) for k in (28, -28, 92)] + \
+         [(_lp_grad, dict(s=30, os=30, out=A + k)) for k in (36, -36, 84)] + \
+         [(_distill, dict(DI_APART, s=30, os=30, out=A + k)) for k in (36, -36, 84)]
+
+
+@pytest.mark.parametrize("call,changed", BESIDE, ids=[f"{f.__name__[1:]}-{i}" for i, (f, _) in enumerate(BESIDE)])
+def test_refused_columns(call, changed):
+    """Columns of one buffer that share one with the others."""
+    assert call(**changed) == INVALID
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("E,gap", [(10, 0), (513, 1), (64, 0), (4099, 0)])
+def test_columns_beside(E, gap, dtype):
+    """Inputs and results as columns of one buffer, right beside each other, give the bits of separate ones."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(E)
+    n, V = 70, 70
+    buf = torch.full((n, 3 * (E + gap)), float("nan"), dtype=dtype, device="cuda")
+    left, mid, right = (buf[:, i * (E + gap):i * (E + gap) + E] for i in range(3))
+    one = torch.randn((n, E), generator=g, device="cuda").to(dtype)
+    ids = _some_ids(n, min(V, E), g, True)
+    u = _teacher(n, E, 5, g, "equal")
+    w = torch.rand(n, generator=g, device="cuda")
+    r = tokens.logprobs(one, ids)
+    loss = torch.empty(n, device="cuda")
+    for x, y in ((mid, right), (mid, left), (left, right), (right, left)):
+        for f, ref in ((lambda: tokens.embed(ids, x, 0.7, out=y), tokens.embed(ids, one, 0.7)),
+                       (lambda: tokens.embed_grad(ids, x, V, 0.7, out=y), tokens.embed_grad(ids, one, V, 0.7, dtype=dtype)),
+                       (lambda: tokens.logprobs_grad(x, ids, r.stats, r.entropy, w, w, out=y),
+                        tokens.logprobs_grad(one, ids, r.stats, r.entropy, w, w)),
+                       (lambda: tokens.distill(x, *u, 1.3, w, out=tokens.Distilled(loss, y)).dlogits,
+                        tokens.distill(one, *u, 1.3, w).dlogits)):
+            buf.fill_(float("nan"))
+            x.copy_(one)
+            f()
+            assert torch.equal(y, ref) and torch.equal(x, one)
+            x.fill_(float("nan"))
+            y.fill_(float("nan"))
+            assert bool(torch.isnan(buf).all())
+
+
 @gpu
 def test_arrays_between_rows():
     """Results may lie between the rows of a matrix, right up to them."""
