@@ -186,12 +186,12 @@ def _own(s, case):
         r = s["out"] = head.linear_grad(s["x"], s["w"], s["dout"], case["act"], s["pre"], out=s.get("out"))
         return {"dx": r.dx, "dweight": r.dweight, "dbias": r.dbias}
     if op == "preference":
-        r = s["out"] = tokens.preference(s["logprob"], s["reference"], s["first"], case["kind"], BETA,
-                                         smoothing=SMOOTHING if case["kind"] == "logistic" else 0.0, mean=case["mean"],
-                                         ids=s["ids"], weight=s["weight"], out=s.get("out"))
+        r = s["out"] = tokens.preference_loss(s["logprob"], s["reference"], s["first"], case["kind"], BETA,
+                                              smoothing=SMOOTHING if case["kind"] == "logistic" else 0.0,
+                                              mean=case["mean"], ids=s["ids"], weight=s["weight"], out=s.get("out"))
         return {"loss": r.loss, "reward": r.reward, "g_logprob": r.g_logprob}
-    r = s["out"] = tokens.policy(s["logprob"], s["old"], s["first"], s["advantage"], (LOW, HIGH), s["reference"], KL,
-                                 mean=case["mean"], ids=s["ids"], weight=s["weight"], out=s.get("out"))
+    r = s["out"] = tokens.policy_loss(s["logprob"], s["old"], s["first"], s["advantage"], (LOW, HIGH), s["reference"], KL,
+                                      mean=case["mean"], ids=s["ids"], weight=s["weight"], out=s.get("out"))
     return {"loss": r.loss, "kl": r.kl, "clipped": r.clipped, "g_logprob": r.g_logprob}
 
 
