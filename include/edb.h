@@ -750,6 +750,119 @@ edb_status edb_distill(const void* logits, int32_t dtype, int32_t n, int32_t voc
                        const float* weight, float* loss, void* dlogits, int64_t dlogits_stride, void* workspace,
                        int64_t workspace_bytes, void* stream);
 
+/* ---- the head on the states, and losses over log probabilities ---- */
+/* What stands between the cells' states and the vocabulary logits (layer norm,
+ * linear layers, with their gradients), and what an answer's log probabilities
+ * are trained by.  The manner is that of the token operators above: device
+ * arrays, row strides in elements, EDB_F32 or EDB_BF16, sums in fp32 or wider,
+ * one rounding of a bf16 result, nothing kept, no wait, the same bits in every
+ * run, the same errors. */
+
+/* out[i][:] = (x[i][:] - mean_i) rstd_i weight[:] + bias[:], with the mean and
+ * rstd_i = 1 / sqrt(variance + eps) of x[i][:] (the variance over dim).
+ *   x, out    [n x dim], each of its own dtype; dim <= 2^20
+ *   weight, bias  [dim] of weight_dtype, each or NULL (1, 0)
+ *   eps       finite, not negative
+ *   stats     float[n][2] or NULL: mean and rstd, for edb_layer_norm_grad
+ * A row with an infinity or NaN gives NaN, in its stats too. */
+edb_status edb_layer_norm(const void* x, int32_t x_dtype, int32_t n, int32_t dim, int64_t x_stride, const void* weight,
+                          const void* bias, int32_t weight_dtype, double eps, void* out, int32_t out_dtype,
+                          int64_t out_stride, float* stats, void* stream);
+
+/* The gradients of edb_layer_norm for the result's gradient dout [n x dim], from
+ * the x and weight of that call and the stats that it left; with
+ * h = (x - mean) rstd, g = dout weight,
+ *   dx[i][:]   = rstd_i (g - average of g - h average of g h)   of x's dtype
+ *   dweight[:] = sum_i dout[i][:] h[i][:],  dbias[:] = sum_i dout[i][:]   float[dim]
+ * dx, dweight and dbias are each NULL where not wanted. */
+edb_status edb_layer_norm_grad_bytes(int32_t n, int32_t dim, int32_t x_dtype, int64_t* bytes);
+edb_status edb_layer_norm_grad(const void* x, int32_t x_dtype, int32_t n, int32_t dim, int64_t x_stride,
+                               const float* stats, const void* dout, int32_t dout_dtype, int64_t dout_stride,
+                               const void* weight, int32_t weight_dtype, void* dx, int64_t dx_stride, float* dweight,
+                               float* dbias, void* workspace, int64_t workspace_bytes, void* stream);
+
+enum { EDB_ACT_NONE = 0, EDB_ACT_RELU = 1, EDB_ACT_GELU = 2, EDB_ACT_SILU = 3, EDB_ACT_TANH = 4 };
+
+/* v = x weight + bias,  out = act(v) + residual.
+ *   x [n x k] and weight [k x m] of one dtype; turned != 0: the weight is stored
+ *             as [m x k] (weight_stride is then that of its m rows)
+ *   bias      [m] of bias_dtype, or NULL
+ *   residual  [n x m] of residual_dtype, or NULL; it may be out itself (same
+ *             address, dtype and stride)
+ *   out       [n x m] of out_dtype
+ *   pre       [n x m] of dtype, or NULL: v, for edb_linear_grad
+ * gelu is v Phi(v) with the normal distribution's Phi.  fp32 products are
+ * formed from three bf16 pieces of either factor, to 2^-24 of the terms.
+ * k, m <= 2^24; no matrix of more than 2^23 tiles of 128 x 128.  A row of x with an
+ * infinity or NaN affects its own row of results only. */
+edb_status edb_linear_bytes(int32_t n, int32_t k, int32_t m, int32_t dtype, int64_t* bytes);
+edb_status edb_linear(const void* x, const void* weight, int32_t dtype, int32_t n, int32_t k, int32_t m,
+                      int64_t x_stride, int64_t weight_stride, int32_t turned, const void* bias, int32_t bias_dtype,
+                      int32_t act, const void* residual, int32_t residual_dtype, int64_t residual_stride, void* out,
+                      int32_t out_dtype, int64_t out_stride, void* pre, int64_t pre_stride, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+#define EDB_LINEAR_DX 1
+#define EDB_LINEAR_DWEIGHT 2
+#define EDB_LINEAR_DBIAS 4
+
+/* The gradients of edb_linear for the result's gradient dout [n x m]; with
+ * g = dout act'(pre) (dout itself without an activation; pre may be NULL then),
+ *   dx = g weight^T,  dweight = x^T g   of dtype, dweight stored as the weight is
+ *   dbias = sum_i g[i][:]               float[m]
+ * (the residual's gradient is dout).  dx, dweight and dbias are each NULL where
+ * not wanted; x is read for dweight only, weight for dx only.  For bf16 operands
+ * dx and dweight are formed from g rounded to bf16.  results: the sum of the
+ * EDB_LINEAR_D* that are wanted. */
+edb_status edb_linear_grad_bytes(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t dout_dtype, int32_t act,
+                                 int32_t results, int64_t* bytes);
+edb_status edb_linear_grad(const void* x, const void* weight, int32_t dtype, int32_t n, int32_t k, int32_t m,
+                           int64_t x_stride, int64_t weight_stride, int32_t turned, const void* dout, int32_t dout_dtype,
+                           int64_t dout_stride, int32_t act, const void* pre, int64_t pre_stride, void* dx,
+                           int64_t dx_stride, void* dweight, int64_t dweight_stride, float* dbias, void* workspace,
+                           int64_t workspace_bytes, void* stream);
+
+/* Losses over the log probabilities of sequences' tokens (edb_logprobs gives
+ * them; the gradients go to edb_logprobs_grad).  Sequence s is the tokens
+ * first[s] .. first[s + 1] - 1 of n; first is int32, does not fall and stays in
+ * [0, n] (anything else gives no access outside the arrays, but no defined
+ * result).  ids is int32[n] or NULL: a token with a negative id does not count,
+ * whatever its log probabilities, and nor does a token of no sequence; their
+ * gradients are 0.  mean != 0: a sequence's sum is divided by the number of its
+ * tokens that count.  weight is float or NULL (1), one a pair or sequence; one
+ * of weight 0 is left out: loss and statistics 0, no gradient.  g_logprob is the
+ * gradient of the losses' sum weighted by weight.  Everything is computed in
+ * 64 bits and rounded once; infinite log probabilities give the limits where
+ * there are any, else NaN.  Up to 2^24 pairs or sequences. */
+
+enum { EDB_PREFERENCE_LOGISTIC = 0, EDB_PREFERENCE_HINGE = 1, EDB_PREFERENCE_SQUARED = 2 };
+
+/* Preference of sequence 2 p over sequence 2 p + 1, for each of `pairs` pairs:
+ * with the log ratios R_s = sum or mean of logprob - reference over the tokens
+ * (reference NULL: 0) and D = R_2p - R_2p+1,
+ *   logistic: (1 - smoothing) ln(1 + exp(-beta D)) + smoothing ln(1 + exp(beta D))
+ *   hinge:    max(0, 1 - beta D)
+ *   squared:  (D - 1 / (2 beta))^2
+ * loss is float[pairs], reward float[pairs][2]: beta R of either. */
+edb_status edb_preference_loss_bytes(int32_t n, int32_t pairs, int64_t* bytes);
+edb_status edb_preference_loss(const float* logprob, const float* reference, const int32_t* ids, int32_t n,
+                          const int32_t* first, int32_t pairs, int32_t kind, double beta, double smoothing, int32_t mean,
+                          const float* weight, float* loss, float* reward, float* g_logprob, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+
+/* The clipped policy loss of `sequences` sequences: with r = exp(logprob -
+ * old_logprob), q = reference - logprob and the advantage A of the sequence
+ * (float[sequences]), or with per_token != 0 of the token (float[n]),
+ *   loss[s] = sum or mean of -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(q) - 1 - q)
+ *   divergence[s] = sum or mean of exp(q) - 1 - q (0 without a reference)
+ *   clipped[s] = the number of tokens whose min is the clipped one
+ * 0 <= low <= 1, 0 <= high, 0 <= kl; kl > 0 needs a reference. */
+edb_status edb_policy_loss_bytes(int32_t n, int32_t sequences, int64_t* bytes);
+edb_status edb_policy_loss(const float* logprob, const float* old_logprob, const float* reference, const int32_t* ids, int32_t n,
+                      const int32_t* first, int32_t sequences, const float* advantage, int32_t per_token, double low,
+                      double high, double kl, int32_t mean, const float* weight, float* loss, float* divergence,
+                      int32_t* clipped, float* g_logprob, void* workspace, int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,6 +36,9 @@ SPLIT_VARIANTS = (18, 19, 20)            # split tile (fp32 through bf16 pieces)
 TEAM_VARIANT = 101                        # team launch (the tail of the schedule in one launch)
 NOALLOC_SCRATCH_BYTES = 32 << 20   # EDB_NOALLOC_SCRATCH_BYTES
 LOGPROBS_MAX_TOP, DISTILL_MAX_TOP = 64, 256
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, ACT_TANH = 0, 1, 2, 3, 4
+LINEAR_DX, LINEAR_DWEIGHT, LINEAR_DBIAS = 1, 2, 4
+PREFERENCE_LOGISTIC, PREFERENCE_HINGE, PREFERENCE_SQUARED = 0, 1, 2
 
 # every symbol include/edb.h declares
 EXPORTS = [
@@ -51,6 +54,9 @@ EXPORTS = [
     "edb_split_phase_bytes", "edb_split_phase", "edb_probe_mfma", "edb_probe_copy",
     "edb_embed", "edb_embed_grad_bytes", "edb_embed_grad",
     "edb_logprobs_bytes", "edb_logprobs", "edb_logprobs_grad", "edb_distill_bytes", "edb_distill",
+    "edb_layer_norm", "edb_layer_norm_grad_bytes", "edb_layer_norm_grad",
+    "edb_linear_bytes", "edb_linear", "edb_linear_grad_bytes", "edb_linear_grad",
+    "edb_preference_loss_bytes", "edb_preference_loss", "edb_policy_loss_bytes", "edb_policy_loss",
 ]
 
 
@@ -175,6 +181,26 @@ def load():
         "edb_distill_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, P(C.c_int64)]),
         "edb_distill": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, vp, C.c_int32, C.c_float, vp,
                                     vp, vp, C.c_int64, vp, C.c_int64, vp]),
+        "edb_layer_norm": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, vp, C.c_int32, C.c_double,
+                                       vp, C.c_int32, C.c_int64, vp, vp]),
+        "edb_layer_norm_grad_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, P(C.c_int64)]),
+        "edb_layer_norm_grad": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, vp, C.c_int32, C.c_int64,
+                                            vp, C.c_int32, vp, C.c_int64, vp, vp, vp, C.c_int64, vp]),
+        "edb_linear_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, P(C.c_int64)]),
+        "edb_linear": (C.c_int32, [vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_int32,
+                                   vp, C.c_int32, C.c_int32, vp, C.c_int32, C.c_int64, vp, C.c_int32, C.c_int64, vp,
+                                   C.c_int64, vp, C.c_int64, vp]),
+        "edb_linear_grad_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                              P(C.c_int64)]),
+        "edb_linear_grad": (C.c_int32, [vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+                                        C.c_int32, vp, C.c_int32, C.c_int64, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp,
+                                        C.c_int64, vp, vp, C.c_int64, vp]),
+        "edb_preference_loss_bytes": (C.c_int32, [C.c_int32, C.c_int32, P(C.c_int64)]),
+        "edb_preference_loss": (C.c_int32, [vp, vp, vp, C.c_int32, vp, C.c_int32, C.c_int32, C.c_double, C.c_double, C.c_int32,
+                                       vp, vp, vp, vp, vp, C.c_int64, vp]),
+        "edb_policy_loss_bytes": (C.c_int32, [C.c_int32, C.c_int32, P(C.c_int64)]),
+        "edb_policy_loss": (C.c_int32, [vp, vp, vp, vp, C.c_int32, vp, C.c_int32, vp, C.c_int32, C.c_double, C.c_double,
+                                   C.c_double, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_int64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

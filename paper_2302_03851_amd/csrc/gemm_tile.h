@@ -1,0 +1,454 @@
+// Matrix product C = A B on the matrix cores, fp32 or bf16 operands in any
+// layout, stride and alignment, fp32 sums.
+//
+// A work-group owns a TM x TN tile of C.  Every thread loads pieces of 8
+// elements of both operands into registers a step ahead, and writes them to
+// LDS as bf16:
+//   * bf16 as it is, 64 k a step;
+//   * fp32 as three bf16 values that add up to it to the last bit (8 + 8 + 8
+//     significant bits), 32 k a step.  Of the nine products the six largest are
+//     formed, which leaves out less than 2^-24 of a term; they take 6/16 of the
+//     time of the fp32 matrix instructions.
+// v_mfma_f32_16x16x32_bf16 wants 8 consecutive k of one row (or column) a lane.
+// An operand whose k are contiguous in memory (K_LINES) is kept line by line and
+// read 16 bytes at a time; one whose rows (columns) are (MN_LINES) is kept as it
+// is, k by k, and turned by ds_read_b64_tr_b16, which hands a lane 4 k of its
+// column.  Both are permuted within LDS so that no read meets its own banks.
+//
+// The products are formed as B^T A^T, so that a lane holds 4 neighbouring
+// columns of a row of C; each wave passes its accumulators through LDS once
+// more to finish (bias, activation, residual) and write whole pieces of rows.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "row_access.h"
+
+namespace edb {
+namespace gemm {
+
+using namespace edb::rows;
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+
+enum Layout { K_LINES, MN_LINES };
+
+template <class T>
+struct Kind;
+template <>
+struct Kind<bf16> {
+    static constexpr int kPlanes = 1, kDepth = 64, kStages = 2;
+};
+template <>
+struct Kind<float> {
+    static constexpr int kPlanes = 3, kDepth = 32, kStages = 1;
+};
+
+// ---- activations ------------------------------------------------------------
+
+__device__ __forceinline__ float activate(int act, float v) {
+    switch (act) {
+        case EDB_ACT_RELU: return v > 0.f ? v : v != v ? v : 0.f;
+        case EDB_ACT_GELU: return 0.5f * v * erfcf(-0.70710678118654752f * v);
+        case EDB_ACT_SILU: return v / (1.f + expf(-v));
+        case EDB_ACT_TANH: return tanhf(v);
+        default: return v;
+    }
+}
+
+__device__ __forceinline__ float slope(int act, float v) {
+    switch (act) {
+        case EDB_ACT_RELU: return v > 0.f ? 1.f : v != v ? v : 0.f;
+        case EDB_ACT_GELU: return 0.5f * erfcf(-0.70710678118654752f * v) + v * expf(-0.5f * v * v) * 0.39894228040143268f;
+        case EDB_ACT_SILU: {
+            const float p = 1.f / (1.f + expf(-v));
+            return p * (1.f + v * (1.f - p));
+        }
+        case EDB_ACT_TANH: {   // 1 / cosh^2: keeps its digits where tanh is next to 1
+            const float s = 2.f / (expf(v) + expf(-v));
+            return s * s;
+        }
+        default: return 1.f;
+    }
+}
+
+// ---- what becomes of a sum ---------------------------------------------------
+
+struct Finish {
+    const void* bias;        // or NULL
+    const void* residual;    // or NULL
+    int64_t residual_stride;
+    void* out;
+    int64_t out_stride;
+    void* pre;               // the sums with the bias, before the activation; or NULL
+    int64_t pre_stride;
+    int32_t act;
+    bool bias_bf16, residual_bf16, out_bf16, pre_bf16;
+};
+
+__device__ __forceinline__ void load8(const void* p, bool half, int64_t at, float (&v)[8]) {
+    if (half) load_k<bf16, 8>(static_cast<const bf16*>(p) + at, v);
+    else load_k<float, 8>(static_cast<const float*>(p) + at, v);
+}
+__device__ __forceinline__ void store8(void* p, bool half, int64_t at, const float (&v)[8]) {
+    if (half) store_k<bf16, 8>(static_cast<bf16*>(p) + at, v);
+    else store_k<float, 8>(static_cast<float*>(p) + at, v);
+}
+__device__ __forceinline__ float load1(const void* p, bool half, int64_t at) {
+    return half ? Elem<bf16>::get(static_cast<const bf16*>(p) + at) : static_cast<const float*>(p)[at];
+}
+__device__ __forceinline__ void store1(void* p, bool half, int64_t at, float v) {
+    if (half) Elem<bf16>::put(static_cast<bf16*>(p) + at, v);
+    else static_cast<float*>(p)[at] = v;
+}
+
+// 8 columns of a row of sums, of which the row has `left`.
+__device__ __forceinline__ void finish8(const Finish& f, int64_t row, int col, int left, float (&v)[8]) {
+    if (left >= 8) {
+        float t[8];
+        if (f.bias) {
+            load8(f.bias, f.bias_bf16, col, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+        if (f.pre) store8(f.pre, f.pre_bf16, row * f.pre_stride + col, v);
+        if (f.act != EDB_ACT_NONE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(f.act, v[i]);
+        }
+        if (f.residual) {
+            load8(f.residual, f.residual_bf16, row * f.residual_stride + col, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+        store8(f.out, f.out_bf16, row * f.out_stride + col, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= left) break;
+        float y = v[i];
+        if (f.bias) y += load1(f.bias, f.bias_bf16, col + i);
+        if (f.pre) store1(f.pre, f.pre_bf16, row * f.pre_stride + col + i, y);
+        y = activate(f.act, y);
+        if (f.residual) y += load1(f.residual, f.residual_bf16, row * f.residual_stride + col + i);
+        store1(f.out, f.out_bf16, row * f.out_stride + col + i, y);
+    }
+}
+
+// ---- operands ------------------------------------------------------------------
+
+// The three pieces of 8 fp32 values, each rounded to nearest.  A value whose
+// first piece would round to infinity takes the largest finite one; an infinity
+// goes into the last piece, beside a first piece of its sign: its products are
+// then with the other operand's first piece, which is zero for zeros only.  A
+// NaN is one in its pieces.
+__device__ __forceinline__ void split8(const u32x4 (&raw)[2], u32x4 (&o)[3]) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_bit_cast(float, (uint32_t)raw[i >> 2][i & 3]);
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+    constexpr float kLargest = 0x1.FEp127f;   // of the bf16 values
+    const bool far = most > kLargest;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+        if (__builtin_expect(far, 0)) {
+            v2f p[3];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float v = j ? b : a;
+                const bool inf = fabsf(v) == INFINITY;
+                const float hi = inf ? copysignf(1.f, v) : fabsf(v) > kLargest ? copysignf(kLargest, v) : (float)static_cast<__bf16>(v);
+                const float mid = inf ? 0.f : (float)static_cast<__bf16>(v - hi);
+                p[0][j] = hi;
+                p[1][j] = mid;
+                p[2][j] = inf ? v : v - hi - mid;
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) o[k][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p[k], v2bf));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), v2bf));
+                o[k][i] = u;
+                a -= __builtin_bit_cast(float, u << 16);
+                b -= __builtin_bit_cast(float, u & 0xFFFF0000u);
+            }
+        }
+    }
+}
+
+// A tile's operand: R rows (columns) by kDepth k a step, by NT threads.
+template <class T, Layout L, int R, int NT>
+struct Operand {
+    static constexpr int BK = Kind<T>::kDepth, P = Kind<T>::kPlanes;
+    static constexpr int NP = (L == K_LINES ? BK : R) / 8;       // pieces of a line
+    static constexpr int PIECES = R * BK / 8, PER = (PIECES + NT - 1) / NT;
+    static constexpr int PLANE = R * BK * 2;                     // bytes of one plane
+    static constexpr int WORDS = sizeof(T) / 2;                  // 16-byte words of a piece in memory
+
+    const T* p[PER];
+    u32x4 raw[PER][WORDS];
+    int64_t step;
+
+    static __device__ __forceinline__ int index(int j) { return min((int)threadIdx.x + j * NT, PIECES - 1); }
+
+    // mn0: the tile's first row (column) of mn; k0: the first k.
+    __device__ __forceinline__ void start(const T* base, int64_t stride, int mn0, int mn, int k0) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int line = index(j) / NP, q = index(j) % NP * 8;
+            // rows past the end: the last one again, whose results nobody writes
+            p[j] = L == K_LINES ? base + (int64_t)min(mn0 + line, mn - 1) * stride + k0 + q
+                                : base + (int64_t)(k0 + line) * stride + mn0 + q;
+        }
+        step = L == K_LINES ? BK : BK * stride;
+    }
+    __device__ __forceinline__ void load() {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) raw[j][i] = Elem<T>::load(p[j] + i * Elem<T>::kVec);
+            p[j] += step;
+        }
+    }
+    // The same where the step leaves the k before kend or the tile the matrix: zeros from there on.
+    __device__ __forceinline__ void load_edge(int mn0, int mn, int k0, int kend) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int line = index(j) / NP, q = index(j) % NP * 8;
+            const int left = L == K_LINES ? kend - (k0 + q) : k0 + line < kend ? mn - (mn0 + q) : 0;
+            if (left >= 8) {
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) raw[j][i] = Elem<T>::load(p[j] + i * Elem<T>::kVec);
+            } else {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = i < left ? Elem<T>::get(p[j] + i) : 0.f;
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) raw[j][i] = Elem<T>::pack(v + i * Elem<T>::kVec);
+            }
+            p[j] += step;
+        }
+    }
+    // Byte offset of a piece in a plane.
+    static __device__ __forceinline__ int place(int line, int q) {
+        if constexpr (L == K_LINES) return line * BK * 2 + 16 * (q ^ ((line / (128 / BK)) & (NP - 1)));
+        else return line * R * 2 + 32 * ((q >> 1) ^ turn(line)) + 16 * (q & 1);
+    }
+    // Where the 32-byte blocks of line k go: the 8 lines that two groups of 16
+    // lanes read at once (k = 8 g + 0..3) are kept in different banks.
+    static __device__ __forceinline__ int turn(int k) {
+        constexpr int NB = R / 16;
+        if constexpr (NB >= 8) return (k & 3) | (k >> 1 & 4);
+        else if constexpr (NB == 4) return (k >> 1 & 1) | (k >> 2 & 2);
+        else if constexpr (NB == 2) return k >> 3 & 1;
+        else return 0;
+    }
+    __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int at = place(index(j) / NP, index(j) % NP);
+            if constexpr (P == 1) {
+                *reinterpret_cast<u32x4*>(lds + at) = raw[j][0];
+            } else {
+                u32x4 o[3];
+                split8(raw[j], o);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<u32x4*>(lds + k * PLANE + at) = o[k];
+            }
+        }
+    }
+    // The 16 rows (columns) from r0, k = 32 kk + 8 (lane / 16) + 0..7.
+    static __device__ __forceinline__ v8bf fragment(const char* plane, int r0, int kk, int lane) {
+        if constexpr (L == K_LINES) {
+            return __builtin_bit_cast(v8bf, *reinterpret_cast<const u32x4*>(plane + place(r0 + (lane & 15), kk * 4 + (lane >> 4))));
+        } else {
+            v4s h[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int k = kk * 32 + (lane >> 4) * 8 + i * 4 + ((lane & 15) >> 2);
+                const char* at = plane + k * R * 2 + 32 * ((r0 >> 4) ^ turn(k)) + (lane & 3) * 8;
+                h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at);
+            }
+            return __builtin_bit_cast(v8bf, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+struct Args {
+    const void *a, *b;
+    int64_t a_stride, b_stride;
+    int32_t m, n, k;            // C is m x n
+    int32_t splits, k_per;      // k of a split (a multiple of the step's depth)
+    float* partial;             // splits > 1: [split][m][n rounded up to 8]
+    Finish finish;
+};
+
+template <class T, Layout AL, Layout BL, int TM, int TN, int WM, int WN>
+struct Shape {
+    static constexpr int NT = 64 * WM * WN;
+    typedef Operand<T, AL, TM, NT> A;
+    typedef Operand<T, BL, TN, NT> B;
+    static constexpr int STAGE = Kind<T>::kPlanes * (A::PLANE + B::PLANE);
+    static constexpr int ROWS = TM / WM, COLS = TN / WN;         // of a wave
+    static constexpr int PITCH = COLS + 4;                       // floats of a row on its way out
+    static constexpr int OUT = WM * WN * 16 * PITCH * 4;
+    static constexpr int LDS = Kind<T>::kStages * STAGE > OUT ? Kind<T>::kStages * STAGE : OUT;
+};
+
+template <class T, Layout AL, Layout BL, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
+    using S = Shape<T, AL, BL, TM, TN, WM, WN>;
+    using A = typename S::A;
+    using B = typename S::B;
+    constexpr int P = Kind<T>::kPlanes, BK = Kind<T>::kDepth, STAGES = Kind<T>::kStages;
+    constexpr int FM = S::ROWS / 16, FN = S::COLS / 16;
+    __shared__ __align__(16) char lds[S::LDS];
+
+    // Work-groups go round the 8 XCDs in turn; each XCD takes a run of tiles, by
+    // bands of 8 tile rows, so that what runs on it at once shares operands in its L2.
+    const int mt = (g.m + TM - 1) / TM, nt = (g.n + TN - 1) / TN, tiles = mt * nt, all = tiles * g.splits;
+    const int per = (all + 7) / 8, id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+    if (id >= all) return;
+    constexpr int kBand = 8;
+    const int split = id / tiles, t = id % tiles, band = t / (kBand * nt), rest = t % (kBand * nt);
+    const int high = min(kBand, mt - band * kBand);
+    const int m0 = (band * kBand + rest % high) * TM, n0 = rest / high * TN;
+
+    const int kbeg = split * g.k_per, kend = min(kbeg + g.k_per, g.k);
+    const int steps = (kend - kbeg + BK - 1) / BK;
+    const bool inside = (AL == K_LINES || m0 + TM <= g.m) && (BL == K_LINES || n0 + TN <= g.n);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN * S::ROWS, wn = wave % WN * S::COLS;
+
+    A a;
+    B b;
+    a.start(static_cast<const T*>(g.a), g.a_stride, m0, g.m, kbeg);
+    b.start(static_cast<const T*>(g.b), g.b_stride, n0, g.n, kbeg);
+    auto load = [&](int s) {
+        const int k0 = kbeg + s * BK;
+        if (inside && k0 + BK <= kend) {
+            a.load();
+            b.load();
+        } else {
+            a.load_edge(m0, g.m, k0, kend);
+            b.load_edge(n0, g.n, k0, kend);
+        }
+    };
+    auto store = [&](char* stage) {
+        a.store(stage);
+        b.store(stage + P * A::PLANE);
+    };
+
+    v4f acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    auto compute = [&](const char* stage) {
+        const char* as = stage;
+        const char* bs = stage + P * A::PLANE;
+#pragma unroll
+        for (int kk = 0; kk < BK / 32; ++kk) {
+            v8bf bf[P][FN];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) bf[p][j] = B::fragment(bs + p * B::PLANE, wn + j * 16, kk, lane);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                v8bf af[P];
+#pragma unroll
+                for (int p = 0; p < P; ++p) af[p] = A::fragment(as + p * A::PLANE, wm + i * 16, kk, lane);
+                // smallest products first
+#pragma unroll
+                for (int o = P - 1; o >= 0; --o)
+#pragma unroll
+                    for (int p = 0; p <= o; ++p)
+#pragma unroll
+                        for (int j = 0; j < FN; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[o - p][j], af[p], acc[i][j], 0, 0, 0);
+            }
+        }
+    };
+
+    if (steps > 0) load(0);
+    if constexpr (STAGES == 2) {
+        if (steps > 0) store(lds);
+        __syncthreads();
+        for (int s = 0; s < steps; ++s) {
+            if (s + 1 < steps) load(s + 1);
+            compute(lds + (s & 1) * S::STAGE);
+            if (s + 1 < steps) store(lds + (~s & 1) * S::STAGE);
+            __syncthreads();
+        }
+    } else {
+        for (int s = 0; s < steps; ++s) {
+            store(lds);
+            __syncthreads();
+            if (s + 1 < steps) load(s + 1);
+            compute(lds);
+            __syncthreads();
+        }
+    }
+
+    // out: 16 rows of the wave at a time through its own part of the LDS
+    float* buf = reinterpret_cast<float*>(lds) + wave * 16 * S::PITCH;
+    constexpr int ACROSS = S::COLS / 8, DOWN = 64 / ACROSS;
+    const int np = (g.n + 7) / 8 * 8;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            *reinterpret_cast<v4f*>(buf + (lane & 15) * S::PITCH + j * 16 + (lane >> 4) * 4) = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 16; r += DOWN) {
+            const int lr = r + lane / ACROSS, lc = lane % ACROSS * 8;
+            const int row = m0 + wm + i * 16 + lr, col = n0 + wn + lc;
+            if (DOWN > 16 && lr >= 16) continue;
+            float v[8];
+            const v4f* q = reinterpret_cast<const v4f*>(buf + lr * S::PITCH + lc);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = q[e >> 2][e & 3];
+            if (row < g.m && col < g.n) {
+                if (g.splits > 1) {
+                    float* to = g.partial + ((int64_t)split * g.m + row) * np + col;
+                    *reinterpret_cast<v4f*>(to) = v4f{v[0], v[1], v[2], v[3]};
+                    *reinterpret_cast<v4f*>(to + 4) = v4f{v[4], v[5], v[6], v[7]};
+                } else {
+                    finish8(g.finish, row, col, g.n - col, v);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// The splits' sums, finished: a thread takes 8 columns of a row.
+__global__ __launch_bounds__(256) inline void join_kernel(Args g) {
+    const int pieces = (g.n + 7) / 8;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / pieces;
+    if (row >= g.m) return;
+    const int col = (int)(at - row * pieces) * 8;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < g.splits; ++s) {
+        const v4f* q = reinterpret_cast<const v4f*>(g.partial + (((int64_t)s * g.m + row) * pieces) * 8 + col);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += q[e >> 2][e & 3];
+    }
+    finish8(g.finish, row, col, g.n - col, v);
+}
+
+}  // namespace gemm
+}  // namespace edb

@@ -1,0 +1,671 @@
+// Losses over the log probabilities of sequences' tokens, with the gradients
+// of the log probabilities.
+//
+// A sequence s is the tokens first[s] .. first[s + 1] - 1; T_s of them count
+// (those with an id, where ids are given), and c_s is 1, or 1 / T_s where the
+// loss goes by means.
+//
+// Preference of the sequence 2p over 2p + 1, with
+//   R_s = c_s sum_t (lp_t - ref_t),  D = R_2p - R_2p+1,  f one of
+//   (1 - e) ln(1 + exp(-b D)) + e ln(1 + exp(b D)),  max(0, 1 - b D),  (D - 1 / (2 b))^2:
+//   loss_p = f(D),  g_t = +-weight_p f'(D) c_s
+//
+// Policy, with r_t = exp(lp_t - old_t), q_t = ref_t - lp_t:
+//   loss_s = c_s sum_t -min(r A, clip(r, 1 - low, 1 + high) A) + k (exp q - 1 - q)
+//   g_t    = weight_s c_s (-A r [not clipped] - k (exp q - 1))
+//
+// All of it is computed in 64 bits and rounded once: log ratios of long
+// sequences are differences of large sums, exp q - 1 - q is what is left of
+// terms up to 10^7 times as large, and a ratio next to the clip's border has to
+// fall on its side of it.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <string>
+
+#include "edb_internal.h"
+
+using edb::fail;
+using edb::Region;
+
+namespace {
+
+struct alignas(8) Sums {
+    double a, b;              // preference: log ratios; policy: surrogate, divergence
+    int32_t live, clipped;
+};
+
+__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) {
+    return {x.a + y.a, x.b + y.b, x.live + y.live, x.clipped + y.clipped};
+}
+
+template <int LANES>
+__device__ __forceinline__ Sums lanes_sum(Sums s) {
+#pragma unroll
+    for (int d = LANES / 2; d; d >>= 1)
+        s = s + Sums{__shfl_xor(s.a, d), __shfl_xor(s.b, d), __shfl_xor(s.live, d), __shfl_xor(s.clipped, d)};
+    return s;
+}
+
+struct Loss {
+    const float *logprob, *other;   // other: the reference (or NULL), the old log probabilities
+    const float* reference;         // policy: or NULL
+    const int32_t* ids;             // or NULL
+    int32_t n;
+    const int32_t* first;
+    int32_t items;                  // pairs, sequences
+    const float* advantage;         // policy
+    int32_t per_token, mean, kind;
+    double beta, smoothing;         // preference
+    double low, high, coef;         // policy: the clip's borders (ratios), the divergence's factor
+    const float* weight;            // or NULL
+    float *loss, *second;           // second: rewards, divergences
+    int32_t* clipped;
+    float* grad;
+    // long calls only
+    Sums *parts, *whole;            // [chunk][2], [sequence]
+    double* slopes;                 // preference: [sequence]
+};
+
+struct Range {
+    int32_t from, to;
+};
+// Tokens of a sequence; offsets that fall or leave [0, n] give no tokens outside of it.
+__device__ __forceinline__ Range range_of(const Loss& l, int s) {
+    const int from = min(max(l.first[s], 0), l.n);
+    return {from, min(max(l.first[s + 1], from), l.n)};
+}
+__device__ __forceinline__ bool is_live(const Loss& l, int64_t t) { return !l.ids || l.ids[t] >= 0; }
+
+__device__ __forceinline__ double log_ratio(const Loss& l, int64_t t) {
+    return (double)l.logprob[t] - (l.other ? (double)l.other[t] : 0.0);
+}
+
+// f(D) and f'(D)
+__device__ __forceinline__ void preference(const Loss& l, double diff, double& loss, double& slope) {
+    const double y = l.beta * diff;
+    if (l.kind == EDB_PREFERENCE_LOGISTIC) {
+        const double near = log1p(exp(-fabs(y))), won = (y < 0.0 ? -y : 0.0) + near, lost = (y > 0.0 ? y : 0.0) + near;
+        const double p = y > 0.0 ? exp(-y) / (1.0 + exp(-y)) : 1.0 / (1.0 + exp(y));   // of the other being preferred
+        loss = l.smoothing != 0.0 ? (1.0 - l.smoothing) * won + l.smoothing * lost : won;
+        slope = l.beta * (l.smoothing - p);
+    } else if (l.kind == EDB_PREFERENCE_HINGE) {
+        loss = y < 1.0 ? 1.0 - y : y != y ? y : 0.0;
+        slope = y < 1.0 ? -l.beta : y != y ? y : 0.0;
+    } else {
+        const double off = diff - 0.5 / l.beta;
+        loss = off * off;
+        slope = 2.0 * off;
+    }
+}
+
+struct Token {
+    double gain, kl, slope;
+    bool clipped;
+};
+__device__ __forceinline__ Token policy(const Loss& l, float logprob, float old, float reference, double a) {
+    const double lp = logprob, r = exp(lp - (double)old);
+    const bool beyond = a > 0.0 ? r > l.high : a < 0.0 && r < l.low;
+    const double moved = a == 0.0 && r == r ? 0.0 : a * r;
+    Token t{beyond ? a * (a > 0.0 ? l.high : l.low) : moved, 0.0, beyond ? 0.0 : -moved, beyond};
+    if (l.reference) {
+        const double q = (double)reference - lp, grown = expm1(q);
+        t.kl = q == HUGE_VAL ? q : grown - q;
+        if (l.coef != 0.0) t.slope -= l.coef * grown;
+    }
+    return t;
+}
+__device__ __forceinline__ double policy_loss(const Loss& l, double gain, double kl) {
+    return l.coef != 0.0 ? l.coef * kl - gain : -gain;
+}
+
+// ---- few tokens: one launch, a group of threads for every pair or sequence ----
+
+template <int THREADS>
+__device__ __forceinline__ Sums group_sum(Sums s, Sums* held) {
+    s = lanes_sum<64>(s);
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) held[threadIdx.x >> 6] = s;
+        __syncthreads();
+        s = held[0];
+        for (int w = 1; w < THREADS / 64; ++w) s = s + held[w];
+    }
+    return s;
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void preference_kernel(Loss l) {
+    constexpr int kBlock = THREADS > 256 ? THREADS : 256;
+    __shared__ Sums held[kBlock / 64];
+    const int tid = threadIdx.x % THREADS, item = blockIdx.x * (kBlock / THREADS) + threadIdx.x / THREADS;
+    if (item >= l.items) return;
+    const double weight = l.weight ? (double)l.weight[item] : 1.0;
+    Range range[2];
+    double mean[2], ratio[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        range[i] = range_of(l, 2 * item + i);
+        Sums s{0.0, 0.0, 0, 0};
+        if (weight != 0.0)
+            for (int64_t t = range[i].from + tid; t < range[i].to; t += THREADS)
+                if (is_live(l, t)) {
+                    s.a += log_ratio(l, t);
+                    ++s.live;
+                }
+        s = group_sum<THREADS>(s, held);
+        mean[i] = l.mean && s.live ? 1.0 / s.live : 1.0;
+        ratio[i] = s.a * mean[i];
+    }
+    double loss = 0.0, slope = 0.0;
+    if (weight != 0.0) preference(l, ratio[0] - ratio[1], loss, slope);
+    if (tid == 0) {
+        l.loss[item] = (float)loss;
+        l.second[2 * item] = (float)(l.beta * ratio[0]);
+        l.second[2 * item + 1] = (float)(l.beta * ratio[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float g = weight != 0.0 ? (float)((i ? -slope : slope) * weight * mean[i]) : 0.f;
+        for (int64_t t = range[i].from + tid; t < range[i].to; t += THREADS) l.grad[t] = is_live(l, t) ? g : 0.f;
+    }
+    // tokens before the first sequence and behind the last
+    if (item == 0)
+        for (int64_t t = tid; t < range[0].from; t += THREADS) l.grad[t] = 0.f;
+    if (item == l.items - 1)
+        for (int64_t t = range[1].to + tid; t < l.n; t += THREADS) l.grad[t] = 0.f;
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void policy_kernel(Loss l) {
+    constexpr int kBlock = THREADS > 256 ? THREADS : 256;
+    __shared__ Sums held[kBlock / 64];
+    const int tid = threadIdx.x % THREADS, item = blockIdx.x * (kBlock / THREADS) + threadIdx.x / THREADS;
+    if (item >= l.items) return;
+    const Range range = range_of(l, item);
+    const double weight = l.weight ? (double)l.weight[item] : 1.0;
+    Sums s{0.0, 0.0, 0, 0};
+    double mean = 1.0;
+    if (weight == 0.0) {
+        for (int64_t t = range.from + tid; t < range.to; t += THREADS) l.grad[t] = 0.f;
+    } else {
+        if (l.mean) {
+            int live = range.to - range.from;
+            if (l.ids) {
+                for (int64_t t = range.from + tid; t < range.to; t += THREADS) s.live += l.ids[t] >= 0;
+                live = group_sum<THREADS>(s, held).live;
+                s.live = 0;
+            }
+            if (live) mean = 1.0 / live;
+        }
+        for (int64_t t = range.from + tid; t < range.to; t += THREADS) {
+            float g = 0.f;
+            if (is_live(l, t)) {
+                const Token k = policy(l, l.logprob[t], l.other[t], l.reference ? l.reference[t] : 0.f,
+                                       l.advantage[l.per_token ? t : item]);
+                s.a += k.gain;
+                s.b += k.kl;
+                s.clipped += k.clipped;
+                g = (float)(k.slope * weight * mean);
+            }
+            l.grad[t] = g;
+        }
+        s = group_sum<THREADS>(s, held);
+    }
+    if (tid == 0) {
+        l.loss[item] = (float)(policy_loss(l, s.a, s.b) * mean);
+        l.second[item] = (float)(s.b * mean);
+        l.clipped[item] = s.clipped;
+    }
+    if (item == 0)
+        for (int64_t t = tid; t < range.from; t += THREADS) l.grad[t] = 0.f;
+    if (item == l.items - 1)
+        for (int64_t t = range.to + tid; t < l.n; t += THREADS) l.grad[t] = 0.f;
+}
+
+// ---- many tokens: chunks of them, whatever sequences they belong to ----
+//
+// A chunk adds up each of its sequences' tokens.  What lies inside the chunk is
+// whole; the sequence that comes in from the chunk before leaves its share in
+// parts[chunk][0], the one that begins here and goes on in parts[chunk][1].
+
+constexpr int kChunk = 2048, kThreads = 256, kEach = kChunk / kThreads;
+
+struct Chunk {
+    int32_t from, to;       // tokens
+    int32_t s0, s1;         // sequences that may have tokens here: s0 <= s < s1
+};
+
+// The number of offsets first[0 .. count) that are at most t, found by the
+// whole work-group, 256 steps at a time.
+__device__ __forceinline__ int upto(const int32_t* first, int count, int t, int* held) {
+    int lo = 0, hi = count;
+    while (hi > lo) {
+        const int step = (hi - lo + kThreads - 1) / kThreads;
+        const int64_t at = lo + (int64_t)threadIdx.x * step;
+        const bool below = at < hi && first[at] <= t;
+        __syncthreads();
+        if (threadIdx.x == 0) *held = 0;
+        __syncthreads();
+        const int c = __popcll(__ballot(below));
+        if ((threadIdx.x & 63) == 0 && c) atomicAdd(held, c);
+        __syncthreads();
+        const int k = *held;
+        if (k == 0) return lo;
+        const int base = lo + (k - 1) * step;
+        hi = min(hi, (int)min((int64_t)base + step, (int64_t)count));
+        lo = base + 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ Chunk chunk_of(const Loss& l, int sequences, int* held) {
+    Chunk c;
+    c.from = blockIdx.x * kChunk;
+    c.to = (int)min((int64_t)c.from + kChunk, (int64_t)l.n);
+    c.s0 = max(upto(l.first, sequences, c.from, held) - 1, 0);
+    c.s1 = upto(l.first, sequences, c.to - 1, held);
+    return c;
+}
+
+// Calls body(s, tokens of s, from, to, lane) with a group of LANES lanes for every
+// sequence of the chunk; from and to count from the chunk's first token.
+template <int LANES, class F>
+__device__ __forceinline__ void by_sequence(const Loss& l, const Chunk& c, F&& body) {
+    for (int s = c.s0 + (int)threadIdx.x / LANES; s < c.s1; s += kThreads / LANES) {
+        const Range r = range_of(l, s);
+        body(s, r, max(r.from, c.from) - c.from, min(r.to, c.to) - c.from, (int)threadIdx.x % LANES);
+    }
+}
+
+// The sequence of each token of the chunk (-1: none), into LDS.
+__device__ __forceinline__ void find_sequences(const Loss& l, const Chunk& c, int32_t* of) {
+    for (int i = threadIdx.x; i < kChunk; i += kThreads) of[i] = -1;
+    __syncthreads();
+    auto fill = [&](auto lanes) {
+        constexpr int kLanes = decltype(lanes)::value;
+        by_sequence<kLanes>(l, c, [&](int s, Range, int from, int to, int lane) {
+            for (int t = from + lane; t < to; t += kLanes) of[t] = s;
+        });
+    };
+    const int count = c.s1 - c.s0;
+    if (count <= 8) fill(std::integral_constant<int, 64>());
+    else if (count <= 128) fill(std::integral_constant<int, 16>());
+    else fill(std::integral_constant<int, 2>());
+    __syncthreads();
+}
+
+// Adds up what the chunk's tokens left in LDS and hands every sequence's sum on.
+template <class Read>
+__device__ __forceinline__ void sum_sequences(const Loss& l, const Chunk& c, Read&& read) {
+    auto add = [&](auto lanes) {
+        constexpr int kLanes = decltype(lanes)::value;
+        by_sequence<kLanes>(l, c, [&](int s, Range r, int from, int to, int lane) {
+            Sums sum{0.0, 0.0, 0, 0};
+            for (int t = from + lane; t < to; t += kLanes) sum = sum + read(t);
+            sum = lanes_sum<kLanes>(sum);
+            if (lane || from >= to) return;
+            if (r.from < c.from) l.parts[2 * blockIdx.x] = sum;
+            else if (r.to > c.to) l.parts[2 * blockIdx.x + 1] = sum;
+            else l.whole[s] = sum;
+        });
+    };
+    const int count = c.s1 - c.s0;
+    if (count <= 8) add(std::integral_constant<int, 64>());
+    else if (count <= 128) add(std::integral_constant<int, 16>());
+    else add(std::integral_constant<int, 2>());
+}
+
+// A sequence's sums over its chunks, by a wave.
+__device__ __forceinline__ Sums sequence_sum(const Loss& l, int s) {
+    const Range r = range_of(l, s);
+    Sums sum{0.0, 0.0, 0, 0};
+    if (r.from >= r.to) return sum;
+    const int c0 = r.from / kChunk, c1 = (r.to - 1) / kChunk;
+    if (c0 == c1) return l.whole[s];
+    for (int c = c0 + (int)(threadIdx.x & 63); c <= c1; c += 64) {
+        // the first chunk's share began there, unless the sequence begins right at its start and fills it
+        const bool begins = c == c0;
+        sum = sum + l.parts[2 * c + (begins ? 1 : 0)];
+    }
+    return lanes_sum<64>(sum);
+}
+
+template <class T>
+__device__ __forceinline__ void load_tokens(const T* p, int64_t at, int64_t end, T none, T (&v)[kEach]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = p && at + i * kThreads < end ? p[at + i * kThreads] : none;
+}
+
+// Preference 1 of 3: the sequences' sums.
+__global__ __launch_bounds__(kThreads) void preference_sums(Loss l) {
+    __shared__ int found;
+    __shared__ double ratio[kChunk];
+    __shared__ uint8_t live[kChunk];
+    const Chunk c = chunk_of(l, 2 * l.items, &found);
+    const int64_t at = c.from + threadIdx.x;
+    float lp[kEach], ref[kEach];
+    int32_t id[kEach];
+    load_tokens(l.logprob, at, c.to, 0.f, lp);
+    load_tokens(l.other, at, c.to, 0.f, ref);
+    load_tokens(l.ids, at, c.to, 0, id);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        ratio[i * kThreads + threadIdx.x] = id[i] >= 0 ? (double)lp[i] - (double)ref[i] : 0.0;
+        live[i * kThreads + threadIdx.x] = id[i] >= 0;
+    }
+    __syncthreads();
+    sum_sequences(l, c, [&](int i) { return Sums{ratio[i], 0.0, live[i], 0}; });
+}
+
+// 2 of 3: the pairs' losses, a wave each.
+__global__ __launch_bounds__(kThreads) void preference_pairs(Loss l) {
+    const int item = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    if (item >= l.items) return;
+    const double weight = l.weight ? (double)l.weight[item] : 1.0;
+    double mean[2], ratio[2], loss = 0.0, slope = 0.0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        Sums s = sequence_sum(l, 2 * item + i);
+        if (weight == 0.0) s = {0.0, 0.0, 0, 0};
+        mean[i] = l.mean && s.live ? 1.0 / s.live : 1.0;
+        ratio[i] = s.a * mean[i];
+    }
+    if (weight != 0.0) preference(l, ratio[0] - ratio[1], loss, slope);
+    if (threadIdx.x & 63) return;
+    l.loss[item] = (float)loss;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        l.second[2 * item + i] = (float)(l.beta * ratio[i]);
+        l.slopes[2 * item + i] = weight != 0.0 ? (i ? -slope : slope) * weight * mean[i] : 0.0;
+    }
+}
+
+// 3 of 3: the tokens' gradients.
+__global__ __launch_bounds__(kThreads) void preference_grad(Loss l) {
+    __shared__ int found;
+    __shared__ int32_t of[kChunk];
+    const Chunk c = chunk_of(l, 2 * l.items, &found);
+    const int64_t at = c.from + threadIdx.x;
+    int32_t id[kEach];
+    load_tokens(l.ids, at, c.to, 0, id);
+    find_sequences(l, c, of);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int s = of[i * kThreads + threadIdx.x];
+        if (at + i * kThreads < c.to) l.grad[at + i * kThreads] = s >= 0 && id[i] >= 0 ? (float)l.slopes[s] : 0.f;
+    }
+}
+
+// Policy 1 of 3, for means over the tokens with an id: how many there are.
+__global__ __launch_bounds__(kThreads) void policy_counts(Loss l) {
+    __shared__ int found;
+    __shared__ uint8_t live[kChunk];
+    const Chunk c = chunk_of(l, l.items, &found);
+    const int64_t at = c.from + threadIdx.x;
+    int32_t id[kEach];
+    load_tokens(l.ids, at, c.to, 0, id);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) live[i * kThreads + threadIdx.x] = id[i] >= 0;
+    __syncthreads();
+    sum_sequences(l, c, [&](int i) { return Sums{0.0, 0.0, live[i], 0}; });
+}
+
+// The sequences' weight over their tokens, a wave each.
+__global__ __launch_bounds__(kThreads) void policy_scales(Loss l) {
+    const int s = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    if (s >= l.items) return;
+    const Range r = range_of(l, s);
+    const int live = l.ids ? sequence_sum(l, s).live : r.to - r.from;
+    const double weight = l.weight ? (double)l.weight[s] : 1.0;
+    if ((threadIdx.x & 63) == 0) l.slopes[s] = l.mean && live ? weight / live : weight;
+}
+
+// 2 of 3: the tokens' terms and gradients, and the sequences' sums.
+__global__ __launch_bounds__(kThreads) void policy_terms(Loss l) {
+    __shared__ int found;
+    __shared__ int32_t of[kChunk];
+    __shared__ double gain[kChunk], kl[kChunk];
+    __shared__ uint8_t flags[kChunk];
+    const Chunk c = chunk_of(l, l.items, &found);
+    const int64_t at = c.from + threadIdx.x;
+    float lp[kEach], old[kEach], ref[kEach];
+    int32_t id[kEach];
+    load_tokens(l.logprob, at, c.to, 0.f, lp);
+    load_tokens(l.other, at, c.to, 0.f, old);
+    load_tokens(l.reference, at, c.to, 0.f, ref);
+    load_tokens(l.ids, at, c.to, 0, id);
+    find_sequences(l, c, of);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int j = i * kThreads + threadIdx.x, s = of[j];
+        const int64_t t = at + i * kThreads;
+        Token k{0.0, 0.0, 0.0, false};
+        double scale = 0.0;
+        bool live = false;
+        if (t < c.to && s >= 0 && id[i] >= 0) {
+            scale = l.slopes[s];
+            live = scale != 0.0;
+            if (live) k = policy(l, lp[i], old[i], ref[i], l.advantage[l.per_token ? t : s]);
+        }
+        gain[j] = k.gain;
+        kl[j] = k.kl;
+        flags[j] = (live ? 1 : 0) | (k.clipped ? 2 : 0);
+        if (t < c.to) l.grad[t] = live ? (float)(k.slope * scale) : 0.f;
+    }
+    __syncthreads();
+    sum_sequences(l, c, [&](int i) { return Sums{gain[i], kl[i], flags[i] & 1, flags[i] >> 1}; });
+}
+
+// 3 of 3: the sequences' losses, a wave each.
+__global__ __launch_bounds__(kThreads) void policy_losses(Loss l) {
+    const int s = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    if (s >= l.items) return;
+    const Sums sum = sequence_sum(l, s);
+    if (threadIdx.x & 63) return;
+    const double mean = l.mean && sum.live ? 1.0 / sum.live : 1.0;
+    l.loss[s] = (float)(policy_loss(l, sum.a, sum.b) * mean);
+    l.second[s] = (float)(sum.b * mean);
+    l.clipped[s] = sum.clipped;
+}
+
+constexpr int32_t kFew = 32768;
+constexpr int32_t kMostItems = 1 << 24;
+
+struct Plan {
+    int32_t chunks;          // 0: one launch
+    int64_t whole, slopes, bytes;
+};
+Plan plan_of(int32_t n, int32_t sequences) {
+    Plan p{};
+    if (n <= kFew) return p;
+    p.chunks = (int32_t)(((int64_t)n + kChunk - 1) / kChunk);
+    p.whole = (int64_t)p.chunks * 2 * sizeof(Sums);
+    p.slopes = p.whole + (int64_t)sequences * sizeof(Sums);
+    p.bytes = p.slopes + (int64_t)sequences * 8;
+    return p;
+}
+
+Region words(const void* p, int64_t n) { return Region::array(p, n * 4); }
+
+edb_status launched(const char* who) {
+    const hipError_t he = hipGetLastError();
+    if (he != hipSuccess) return fail(EDB_ERR_HIP, std::string(who) + ": " + hipGetErrorString(he));
+    edb::clear_error();
+    return EDB_OK;
+}
+
+edb_status check_items(const char* who, int32_t n, int32_t items, const char* name) {
+    const std::string w(who);
+    if (n < 0 || items < 0) return fail(EDB_ERR_INVALID, w + ": n >= 0 and " + name + " >= 0 are needed");
+    if (items > kMostItems) return fail(EDB_ERR_UNSUPPORTED, w + ": " + name + " must not exceed 2^24");
+    return EDB_OK;
+}
+
+bool in_range(double v, double lo, double hi) { return v >= lo && v <= hi && std::isfinite(v); }
+
+__global__ __launch_bounds__(256) void no_sequences(float* grad, int32_t n) {
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t < n) grad[t] = 0.f;
+}
+
+unsigned groups(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
+
+}  // namespace
+
+extern "C" edb_status edb_preference_loss_bytes(int32_t n, int32_t pairs, int64_t* bytes) {
+    return edb::guarded([&]() -> edb_status {
+        if (!bytes) return fail(EDB_ERR_INVALID, "edb_preference_loss_bytes: NULL argument");
+        if (edb_status st = check_items("edb_preference_loss_bytes", n, pairs, "pairs")) return st;
+        *bytes = plan_of(n, 2 * pairs).bytes;
+        edb::clear_error();
+        return EDB_OK;
+    });
+}
+
+extern "C" edb_status edb_preference_loss(const float* logprob, const float* reference, const int32_t* ids, int32_t n,
+                                     const int32_t* first, int32_t pairs, int32_t kind, double beta, double smoothing,
+                                     int32_t mean, const float* weight, float* loss, float* reward, float* g_logprob,
+                                     void* workspace, int64_t workspace_bytes, void* stream) {
+    return edb::guarded([&]() -> edb_status {
+        const char* who = "edb_preference_loss";
+        if (edb_status st = check_items(who, n, pairs, "pairs")) return st;
+        if (kind < EDB_PREFERENCE_LOGISTIC || kind > EDB_PREFERENCE_SQUARED)
+            return fail(EDB_ERR_INVALID, "edb_preference_loss: unknown kind of loss");
+        if (!(beta > 0.0) || !std::isfinite(beta)) return fail(EDB_ERR_INVALID, "edb_preference_loss: beta must be positive and finite");
+        if (!in_range(smoothing, 0.0, 1.0) || (smoothing != 0.0 && kind != EDB_PREFERENCE_LOGISTIC))
+            return fail(EDB_ERR_INVALID, "edb_preference_loss: smoothing must be in [0, 1], and 0 but for the logistic loss");
+        if ((n && (!logprob || !g_logprob)) || (pairs && (!first || !loss || !reward)))
+            return fail(EDB_ERR_INVALID, "edb_preference_loss: NULL argument");
+        const Plan p = plan_of(n, 2 * pairs);
+        if (workspace_bytes < p.bytes || (p.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+            return fail(EDB_ERR_INVALID, "edb_preference_loss: a 16-byte aligned workspace of " + std::to_string(p.bytes) +
+                                             " bytes is needed");
+        if (!edb::word_aligned({logprob, reference, ids, first, weight, loss, reward, g_logprob}))
+            return fail(EDB_ERR_INVALID, "edb_preference_loss: all arrays must be aligned to 4 bytes");
+        if (edb_status st = edb::apart(who,
+                                       {words(loss, pairs), words(reward, 2 * (int64_t)pairs), words(g_logprob, n),
+                                        Region::array(workspace, p.bytes)},
+                                       {words(logprob, n), words(reference, n), words(ids, n),
+                                        words(first, pairs ? 2 * (int64_t)pairs + 1 : 0), words(weight, pairs)}))
+            return st;
+        if (n == 0 && pairs == 0) {
+            edb::clear_error();
+            return EDB_OK;
+        }
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        Loss l{};
+        l.logprob = logprob;
+        l.other = reference;
+        l.ids = ids;
+        l.n = n;
+        l.first = first;
+        l.items = pairs;
+        l.kind = kind;
+        l.beta = beta;
+        l.smoothing = smoothing;
+        l.mean = mean != 0;
+        l.weight = weight;
+        l.loss = loss;
+        l.second = reward;
+        l.grad = g_logprob;
+        if (pairs == 0) {
+            if (n) no_sequences<<<groups(n, 256), 256, 0, st>>>(g_logprob, n);
+        } else if (p.chunks == 0) {
+            if (n / pairs < 512) preference_kernel<64><<<groups(pairs, 4), 256, 0, st>>>(l);
+            else if (n / pairs < 4096) preference_kernel<256><<<pairs, 256, 0, st>>>(l);
+            else preference_kernel<1024><<<pairs, 1024, 0, st>>>(l);
+        } else {
+            char* ws = static_cast<char*>(workspace);
+            l.parts = reinterpret_cast<Sums*>(ws);
+            l.whole = reinterpret_cast<Sums*>(ws + p.whole);
+            l.slopes = reinterpret_cast<double*>(ws + p.slopes);
+            preference_sums<<<p.chunks, kThreads, 0, st>>>(l);
+            preference_pairs<<<groups(pairs, kThreads / 64), kThreads, 0, st>>>(l);
+            preference_grad<<<p.chunks, kThreads, 0, st>>>(l);
+        }
+        return launched(who);
+    });
+}
+
+extern "C" edb_status edb_policy_loss_bytes(int32_t n, int32_t sequences, int64_t* bytes) {
+    return edb::guarded([&]() -> edb_status {
+        if (!bytes) return fail(EDB_ERR_INVALID, "edb_policy_loss_bytes: NULL argument");
+        if (edb_status st = check_items("edb_policy_loss_bytes", n, sequences, "sequences")) return st;
+        *bytes = plan_of(n, sequences).bytes;
+        edb::clear_error();
+        return EDB_OK;
+    });
+}
+
+extern "C" edb_status edb_policy_loss(const float* logprob, const float* old_logprob, const float* reference, const int32_t* ids,
+                                 int32_t n, const int32_t* first, int32_t sequences, const float* advantage,
+                                 int32_t per_token, double low, double high, double kl, int32_t mean, const float* weight,
+                                 float* loss, float* divergence, int32_t* clipped, float* g_logprob, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+    return edb::guarded([&]() -> edb_status {
+        const char* who = "edb_policy_loss";
+        if (edb_status st = check_items(who, n, sequences, "sequences")) return st;
+        if (!in_range(low, 0.0, 1.0) || !(high >= 0.0) || !std::isfinite(high))
+            return fail(EDB_ERR_INVALID, "edb_policy_loss: low must be in [0, 1], high finite and not negative");
+        if (!(kl >= 0.0) || !std::isfinite(kl)) return fail(EDB_ERR_INVALID, "edb_policy_loss: kl must be finite and not negative");
+        if (kl != 0.0 && !reference) return fail(EDB_ERR_INVALID, "edb_policy_loss: the divergence needs a reference");
+        if ((n && (!logprob || !old_logprob || !g_logprob)) || (sequences && (!first || !loss || !divergence || !clipped)) ||
+            ((per_token ? n : sequences) && !advantage))
+            return fail(EDB_ERR_INVALID, "edb_policy_loss: NULL argument");
+        const Plan p = plan_of(n, sequences);
+        if (workspace_bytes < p.bytes || (p.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+            return fail(EDB_ERR_INVALID, "edb_policy_loss: a 16-byte aligned workspace of " + std::to_string(p.bytes) +
+                                             " bytes is needed");
+        if (!edb::word_aligned({logprob, old_logprob, reference, ids, first, advantage, weight, loss, divergence, clipped, g_logprob}))
+            return fail(EDB_ERR_INVALID, "edb_policy_loss: all arrays must be aligned to 4 bytes");
+        if (edb_status st = edb::apart(who,
+                                       {words(loss, sequences), words(divergence, sequences), words(clipped, sequences),
+                                        words(g_logprob, n), Region::array(workspace, p.bytes)},
+                                       {words(logprob, n), words(old_logprob, n), words(reference, n), words(ids, n),
+                                        words(first, sequences ? (int64_t)sequences + 1 : 0),
+                                        words(advantage, per_token ? n : sequences), words(weight, sequences)}))
+            return st;
+        if (n == 0 && sequences == 0) {
+            edb::clear_error();
+            return EDB_OK;
+        }
+        hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+        Loss l{};
+        l.logprob = logprob;
+        l.other = old_logprob;
+        l.reference = reference;
+        l.ids = ids;
+        l.n = n;
+        l.first = first;
+        l.items = sequences;
+        l.advantage = advantage;
+        l.per_token = per_token != 0;
+        l.low = 1.0 - low;
+        l.high = 1.0 + high;
+        l.coef = kl;
+        l.mean = mean != 0;
+        l.weight = weight;
+        l.loss = loss;
+        l.second = divergence;
+        l.clipped = clipped;
+        l.grad = g_logprob;
+        if (sequences == 0) {
+            if (n) no_sequences<<<groups(n, 256), 256, 0, st>>>(g_logprob, n);
+        } else if (p.chunks == 0) {
+            if (n / sequences < 512) policy_kernel<64><<<groups(sequences, 4), 256, 0, st>>>(l);
+            else if (n / sequences < 4096) policy_kernel<256><<<sequences, 256, 0, st>>>(l);
+            else policy_kernel<1024><<<sequences, 1024, 0, st>>>(l);
+        } else {
+            char* ws = static_cast<char*>(workspace);
+            l.parts = reinterpret_cast<Sums*>(ws);
+            l.whole = reinterpret_cast<Sums*>(ws + p.whole);
+            l.slopes = reinterpret_cast<double*>(ws + p.slopes);
+            if (l.mean && ids) policy_counts<<<p.chunks, kThreads, 0, st>>>(l);
+            policy_scales<<<groups(sequences, kThreads / 64), kThreads, 0, st>>>(l);
+            policy_terms<<<p.chunks, kThreads, 0, st>>>(l);
+            policy_losses<<<groups(sequences, kThreads / 64), kThreads, 0, st>>>(l);
+        }
+        return launched(who);
+    });
+}

@@ -1,5 +1,5 @@
-// Typed access to the rows of the token operators (embedding, log
-// probabilities, distillation): elements are fp32 or bf16 in memory and fp32 in
+// Typed access to the rows of the operators around the cells (embedding, layer
+// norm, linear layers, log probabilities, distillation): elements are fp32 or bf16 in memory and fp32 in
 // registers, 16 bytes at a time.  A row of an odd length leaves the next one
 // on an element boundary only, so vector accesses state the element's
 // alignment; the hardware takes 16-byte accesses at any address.
@@ -109,6 +109,53 @@ struct Elem<bf16> {
         return v;
     }
 };
+
+// K consecutive elements of a row as fp32, at any alignment.  K is 8 or 4, or 1
+// for rows shorter than 4.
+// ONCE: read once only, not worth a place in the caches.
+template <class T, int K, bool ONCE = false>
+__device__ __forceinline__ void load_k(const T* p, float* v) {
+    if constexpr (K == 1) {
+        v[0] = Elem<T>::get(p);
+    } else if constexpr (K < Elem<T>::kVec) {
+        Elem<T>::unpack_half(ONCE ? Elem<T>::load_half_nt(p) : Elem<T>::load_half(p), v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < K; i += Elem<T>::kVec)
+            Elem<T>::unpack(ONCE ? Elem<T>::load_nt(p + i) : Elem<T>::load(p + i), v + i);
+    }
+}
+template <class T, int K>
+__device__ __forceinline__ void store_k(T* p, const float* v) {
+    if constexpr (K == 1) {
+        Elem<T>::put(p, v[0]);
+    } else if constexpr (K < Elem<T>::kVec) {
+        Elem<T>::store_half(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < K; i += Elem<T>::kVec) Elem<T>::store(p + i, Elem<T>::pack(v + i));
+    }
+}
+
+// Where the piece of K elements that starts at `nominal` is taken from in a row
+// of dim >= K: the last one, if the row ends inside it, from the row's end
+// backwards, and the `skip` elements that it shares with the piece before it
+// are left to that one (so that no element has two writers).
+template <int K>
+struct Piece {
+    int col, skip;
+    __device__ __forceinline__ Piece(int nominal, int dim) : col(min(nominal, dim - K)), skip(nominal - col) {}
+};
+template <class T, int K>
+__device__ __forceinline__ void store_from(T* p, const float* v, int skip) {
+    if (K == 1 || skip <= 0) {
+        store_k<T, K>(p, v);
+    } else {
+#pragma unroll
+        for (int k = 1; k < K; ++k)
+            if (k >= skip) Elem<T>::put(p + k, v[k]);
+    }
+}
 
 }  // namespace rows
 }  // namespace edb

@@ -1,7 +1,7 @@
 """Token operators on torch tensors: embedding lookup and its gradient, log
 probabilities of given tokens with entropy and alternatives and their
-gradient, and distillation from a teacher's best logits (include/edb.h holds
-the definitions).  PyTorch provides device memory and the stream only: every
+gradient, distillation from a teacher's best logits, and the preference and
+policy losses over log probabilities (include/edb.h holds the definitions).  PyTorch provides device memory and the stream only: every
 call checks its tensors, enqueues libedb's kernels on the current stream of
 the tensors' device and returns without waiting.
 
@@ -36,6 +36,20 @@ class Distilled(NamedTuple):
     dlogits: Optional[torch.Tensor]        # like the logits, None for the loss alone
 
 
+class Preference(NamedTuple):
+    loss: torch.Tensor                     # float32 [pairs]
+    reward: torch.Tensor                   # float32 [pairs, 2]
+    g_logprob: torch.Tensor                # float32 [n], for logprobs_grad
+
+
+class Policy(NamedTuple):
+    loss: torch.Tensor                     # float32 [sequences]
+    kl: torch.Tensor                       # float32 [sequences]
+    clipped: torch.Tensor                  # int32 [sequences]
+    g_logprob: torch.Tensor                # float32 [n], for logprobs_grad
+
+
+_KIND = {"logistic": L.PREFERENCE_LOGISTIC, "hinge": L.PREFERENCE_HINGE, "squared": L.PREFERENCE_SQUARED}
 _MOST = 2 ** 31 - 1     # of a size: the C calls take int32, and ctypes would cut off the rest
 
 
@@ -241,4 +255,73 @@ def distill(logits, top_ids, top_logits, temperature: float = 1.0, weight=None, 
           _array(top_logits, "top_logits", (n, top), f32, dev), top, temperature,
           None if weight is None else _array(weight, "weight", (n,), f32, dev),
           _array(out.loss, "out.loss", (n,), f32, dev), dp, ostride, ws.data_ptr() if nb else None, nb)
+    return out
+
+
+def _optional(t, name, shape, dtype, dev):
+    return None if t is None else _array(t, name, shape, dtype, dev)
+
+
+def _sequences(logprob, first):
+    """Numbers of tokens and of sequences, and the device, of a loss over log probabilities."""
+    _on(logprob, "logprob", None)
+    if first.dim() != 1 or first.numel() < 1:
+        raise ValueError("first: a 1-D tensor of the sequences' first tokens and the last one's end is needed")
+    return _size(logprob.numel(), "logprob"), _size(first.numel() - 1, "first"), logprob.device
+
+
+def preference_loss(logprob, reference, first, kind: str = "logistic", beta: float = 0.1, smoothing: float = 0.0,
+                    mean: bool = False, ids=None, weight=None, out: Optional[Preference] = None) -> Preference:
+    """Loss of every pair of sequences 2 p (preferred) and 2 p + 1 from the
+    tokens' log probabilities [n] and a reference's ([n] or None); sequence s
+    is the tokens first[s] to first[s + 1] - 1.  `kind` is "logistic", "hinge"
+    or "squared"; with `mean` log ratios are divided by the tokens' number;
+    tokens with a negative id in `ids` [n] do not count.  `g_logprob` is the
+    gradient of the losses' sum weighted by `weight` [pairs]."""
+    n, sequences, dev = _sequences(logprob, first)
+    if kind not in _KIND:
+        raise ValueError(f"kind: one of {', '.join(_KIND)} is needed, not {kind}")
+    if sequences % 2:
+        raise ValueError(f"first: {sequences} sequences are no pairs")
+    pairs, f32, i32 = sequences // 2, torch.float32, torch.int32
+    if out is None:
+        out = Preference(torch.empty(pairs, dtype=f32, device=dev), torch.empty((pairs, 2), dtype=f32, device=dev),
+                         torch.empty(n, dtype=f32, device=dev))
+    nb = _bytes("edb_preference_loss_bytes", n, pairs)
+    ws = _workspace(dev, nb)
+    _call("edb_preference_loss", dev, _array(logprob, "logprob", (n,), f32, dev),
+          _optional(reference, "reference", (n,), f32, dev), _optional(ids, "ids", (n,), i32, dev), n,
+          _array(first, "first", (sequences + 1,), i32, dev), pairs, _KIND[kind], beta, smoothing, 1 if mean else 0,
+          _optional(weight, "weight", (pairs,), f32, dev), _array(out.loss, "out.loss", (pairs,), f32, dev),
+          _array(out.reward, "out.reward", (pairs, 2), f32, dev), _array(out.g_logprob, "out.g_logprob", (n,), f32, dev),
+          ws.data_ptr() if nb else None, nb)
+    return out
+
+
+def policy_loss(logprob, old_logprob, first, advantage, clip=(0.2, 0.2), reference=None, kl: float = 0.0,
+                per_token: bool = False, mean: bool = True, ids=None, weight=None, out: Optional[Policy] = None) -> Policy:
+    """Clipped policy loss of every sequence (the tokens first[s] to
+    first[s + 1] - 1) from the tokens' log probabilities now and when they were
+    drawn ([n] each), with the advantages [sequences], or [n] with `per_token`:
+    ratios are clipped to 1 - clip[0] and 1 + clip[1], and `kl` times the
+    divergence from `reference` [n] is added.  With `mean` a sequence's sum is
+    divided by its tokens' number; tokens with a negative id in `ids` [n] do
+    not count.  `g_logprob` is the gradient of the losses' sum weighted by
+    `weight` [sequences]."""
+    n, sequences, dev = _sequences(logprob, first)
+    low, high = clip
+    f32, i32 = torch.float32, torch.int32
+    if out is None:
+        out = Policy(*(torch.empty(sequences, dtype=t, device=dev) for t in (f32, f32, i32)),
+                     torch.empty(n, dtype=f32, device=dev))
+    nb = _bytes("edb_policy_loss_bytes", n, sequences)
+    ws = _workspace(dev, nb)
+    _call("edb_policy_loss", dev, _array(logprob, "logprob", (n,), f32, dev),
+          _array(old_logprob, "old_logprob", (n,), f32, dev), _optional(reference, "reference", (n,), f32, dev),
+          _optional(ids, "ids", (n,), i32, dev), n, _array(first, "first", (sequences + 1,), i32, dev), sequences,
+          _array(advantage, "advantage", (n if per_token else sequences,), f32, dev), 1 if per_token else 0, low, high, kl,
+          1 if mean else 0, _optional(weight, "weight", (sequences,), f32, dev),
+          _array(out.loss, "out.loss", (sequences,), f32, dev), _array(out.kl, "out.kl", (sequences,), f32, dev),
+          _array(out.clipped, "out.clipped", (sequences,), i32, dev),
+          _array(out.g_logprob, "out.g_logprob", (n,), f32, dev), ws.data_ptr() if nb else None, nb)
     return out
