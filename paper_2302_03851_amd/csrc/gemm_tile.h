@@ -16,8 +16,8 @@
 // column.  Both are permuted within LDS so that no read meets its own banks.
 //
 // The products are formed as B^T A^T, so that a lane holds 4 neighbouring
-// columns of a row of C; each wave passes its accumulators through LDS once
-// more to finish (bias, activation, residual) and write whole pieces of rows.
+// columns of a row of C; the tile passes through LDS once more, to be finished
+// (bias, activation, residual) and written by whole pieces of rows.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -51,32 +51,119 @@ struct Kind<float> {
 };
 
 // ---- activations ------------------------------------------------------------
+//
+// On the hardware's exponential and reciprocal (1 unit in the last place each);
+// with the library's erfc, exp and tanh a layer of 28629 x 512 x 1536 took twice
+// as long.  Infinities give the limits, NaN stays NaN.
 
-__device__ __forceinline__ float activate(int act, float v) {
-    switch (act) {
-        case EDB_ACT_RELU: return v > 0.f ? v : v != v ? v : 0.f;
-        case EDB_ACT_GELU: return 0.5f * v * erfcf(-0.70710678118654752f * v);
-        case EDB_ACT_SILU: return v / (1.f + expf(-v));
-        case EDB_ACT_TANH: return tanhf(v);
-        default: return v;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 2^x for x <= 0 as e times scale, so that what is multiplied with it before
+// `scale` keeps its digits where 2^x itself is below the normal numbers.
+struct Power {
+    float e, scale;
+    __device__ __forceinline__ explicit Power(float x) {
+        const bool far = x < -100.f;
+        e = __builtin_amdgcn_exp2f(far ? x + 64.f : x);
+        scale = far ? 0x1p-64f : 1.f;
     }
+};
+
+// erfc(z) exp(z^2) / 2 of z = a / sqrt(2) >= 0, as t Q(t) with t = 1 / (1 + z / 2)
+// and Q fitted for the least largest relative error up to z = 10.6 (4.4e-8; in
+// fp32 3.2e-7).
+__device__ __forceinline__ float tail(float a) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.35355339059327376f, 1.f));
+    float q = -0.029606621712446213f;
+    q = fmaf(q, t, 0.14263999462127686f);
+    q = fmaf(q, t, -0.2443310022354126f);
+    q = fmaf(q, t, 0.13987129926681519f);
+    q = fmaf(q, t, -0.013890879228711128f);
+    q = fmaf(q, t, 0.1015884131193161f);
+    q = fmaf(q, t, 0.12148986756801605f);
+    q = fmaf(q, t, 0.14119619131088257f);
+    q = fmaf(q, t, 0.14104272425174713f);
+    return q * t;
 }
 
-__device__ __forceinline__ float slope(int act, float v) {
-    switch (act) {
-        case EDB_ACT_RELU: return v > 0.f ? 1.f : v != v ? v : 0.f;
-        case EDB_ACT_GELU: return 0.5f * erfcf(-0.70710678118654752f * v) + v * expf(-0.5f * v * v) * 0.39894228040143268f;
-        case EDB_ACT_SILU: {
-            const float p = 1.f / (1.f + expf(-v));
-            return p * (1.f + v * (1.f - p));
-        }
-        case EDB_ACT_TANH: {   // 1 / cosh^2: keeps its digits where tanh is next to 1
-            const float s = 2.f / (expf(v) + expf(-v));
-            return s * s;
-        }
-        default: return 1.f;
+__device__ __forceinline__ float relu(float v) { return v < 0.f ? 0.f : v; }
+
+// v Phi(v) = max(v, 0) - |v| Phi(-|v|)
+__device__ __forceinline__ float gelu(float v) {
+    const float a = fminf(fabsf(v), 20.f);
+    return relu(v) - a * (__builtin_amdgcn_exp2f(-0.5f * kLog2e * (a * a)) * tail(a));
+}
+__device__ __forceinline__ float gelu_slope(float v) {
+    const float a = fminf(fabsf(v), 20.f);
+    const Power p(-0.5f * kLog2e * (a * a));
+    // Phi(-a) and a phi(a)
+    const float beyond = p.e * tail(a), bent = p.e * a * 0.39894228040143268f;
+    return v != v ? v : v < 0.f ? (beyond - bent) * p.scale : 1.f - (beyond - bent) * p.scale;
+}
+
+__device__ __forceinline__ float silu(float v) {
+    const float a = fminf(fabsf(v), 200.f);
+    const Power p(-kLog2e * a);
+    const float r = __builtin_amdgcn_rcpf(1.f + p.e * p.scale);
+    return v < 0.f ? -(a * r * p.e) * p.scale : v * r;
+}
+__device__ __forceinline__ float silu_slope(float v) {
+    const float a = fminf(fabsf(v), 200.f);
+    const Power p(-kLog2e * a);
+    const float r = __builtin_amdgcn_rcpf(1.f + p.e * p.scale);
+    // s (1 + v (1 - s)) with s = r or e r, 1 - s the other one
+    return v != v ? v : v < 0.f ? p.e * r * (1.f - a * r) * p.scale : r * fmaf(a * r * p.e, p.scale, 1.f);
+}
+
+// By (1 - e) / (1 + e), e = exp(-2 |v|), and next to 0 by v + v^3 P(v^2), P
+// fitted for the least largest relative error (1.5e-7 of P).
+__device__ __forceinline__ float tanh_of(float v) {
+    const float a = fabsf(v), s = v * v;
+    float p = -0.006045394577085972f;
+    p = fmaf(p, s, 0.020961513742804527f);
+    p = fmaf(p, s, -0.05384330824017525f);
+    p = fmaf(p, s, 0.1333271861076355f);
+    p = fmaf(p, s, -0.333333283662796f);
+    const float e = __builtin_amdgcn_exp2f(-2.f * kLog2e * a);
+    const float far = (1.f - e) * __builtin_amdgcn_rcpf(1.f + e);
+    return a < 0.63f ? fmaf(v * s, p, v) : copysignf(far, v);
+}
+// 1 / cosh^2: keeps its digits where tanh is next to 1
+__device__ __forceinline__ float tanh_slope(float v) {
+    const Power p(-2.f * kLog2e * fabsf(v));
+    const float r = __builtin_amdgcn_rcpf(1.f + p.e * p.scale);
+    return 4.f * p.e * r * r * p.scale;
+}
+
+__device__ __forceinline__ void activate8(int act, float (&v)[8]) {
+#define EDB_EACH(f)               \
+    _Pragma("unroll") for (int i = 0; i < 8; ++i) v[i] = f(v[i])
+    if (act == EDB_ACT_RELU) {
+        EDB_EACH(relu);
+    } else if (act == EDB_ACT_GELU) {
+        EDB_EACH(gelu);
+    } else if (act == EDB_ACT_SILU) {
+        EDB_EACH(silu);
+    } else if (act == EDB_ACT_TANH) {
+        EDB_EACH(tanh_of);
     }
 }
+// x times the derivative at v
+__device__ __forceinline__ void slope8(int act, const float (&v)[8], float (&x)[8]) {
+#define EDB_TIMES(f)              \
+    _Pragma("unroll") for (int i = 0; i < 8; ++i) x[i] *= f
+    if (act == EDB_ACT_RELU) {
+        EDB_TIMES((v[i] > 0.f ? 1.f : v[i] != v[i] ? v[i] : 0.f));
+    } else if (act == EDB_ACT_GELU) {
+        EDB_TIMES(gelu_slope(v[i]));
+    } else if (act == EDB_ACT_SILU) {
+        EDB_TIMES(silu_slope(v[i]));
+    } else if (act == EDB_ACT_TANH) {
+        EDB_TIMES(tanh_slope(v[i]));
+    }
+}
+#undef EDB_EACH
+#undef EDB_TIMES
 
 // ---- what becomes of a sum ---------------------------------------------------
 
@@ -108,38 +195,64 @@ __device__ __forceinline__ void store1(void* p, bool half, int64_t at, float v) 
     else static_cast<float*>(p)[at] = v;
 }
 
-// 8 columns of a row of sums, of which the row has `left`.
-__device__ __forceinline__ void finish8(const Finish& f, int64_t row, int col, int left, float (&v)[8]) {
-    if (left >= 8) {
+// 8 elements as they lie in memory.
+struct Raw8 {
+    u32x4 w[2];
+    __device__ __forceinline__ void load(const void* p, bool half, int64_t at) {
+        if (half) {
+            w[0] = Elem<bf16>::load(static_cast<const bf16*>(p) + at);
+        } else {
+            w[0] = Elem<float>::load(static_cast<const float*>(p) + at);
+            w[1] = Elem<float>::load(static_cast<const float*>(p) + at + 4);
+        }
+    }
+    __device__ __forceinline__ void add_to(bool half, float (&v)[8]) const {
         float t[8];
-        if (f.bias) {
-            load8(f.bias, f.bias_bf16, col, t);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        if (half) {
+            Elem<bf16>::unpack(w[0], t);
+        } else {
+            Elem<float>::unpack(w[0], t);
+            Elem<float>::unpack(w[1], t + 4);
         }
-        if (f.pre) store8(f.pre, f.pre_bf16, row * f.pre_stride + col, v);
-        if (f.act != EDB_ACT_NONE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(f.act, v[i]);
-        }
-        if (f.residual) {
-            load8(f.residual, f.residual_bf16, row * f.residual_stride + col, t);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += t[i];
-        }
-        store8(f.out, f.out_bf16, row * f.out_stride + col, v);
-        return;
+        for (int i = 0; i < 8; ++i) v[i] += t[i];
     }
+};
+
+// Of the 8 columns from col, `left` are the matrix's.
+__device__ __forceinline__ void load_bias(const Finish& f, int col, int left, float (&b)[8]) {
+    if (!f.bias) return;
+    if (left >= 8) {
+        load8(f.bias, f.bias_bf16, col, b);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i >= left) break;
-        float y = v[i];
-        if (f.bias) y += load1(f.bias, f.bias_bf16, col + i);
-        if (f.pre) store1(f.pre, f.pre_bf16, row * f.pre_stride + col + i, y);
-        y = activate(f.act, y);
-        if (f.residual) y += load1(f.residual, f.residual_bf16, row * f.residual_stride + col + i);
-        store1(f.out, f.out_bf16, row * f.out_stride + col + i, y);
+        for (int i = 0; i < 7; ++i)
+            if (i < left) b[i] = load1(f.bias, f.bias_bf16, col + i);
     }
+}
+
+// 8 columns of a row of sums with the bias; more: the residual's.
+__device__ __forceinline__ void finish8(const Finish& f, int64_t row, int col, float (&v)[8], const Raw8& more) {
+    if (f.pre) store8(f.pre, f.pre_bf16, row * f.pre_stride + col, v);
+    activate8(f.act, v);
+    if (f.residual) more.add_to(f.residual_bf16, v);
+    store8(f.out, f.out_bf16, row * f.out_stride + col, v);
+}
+
+// The last `left` < 8 columns.
+__device__ __forceinline__ void finish_edge(const Finish& f, int64_t row, int col, int left, float (&v)[8]) {
+    if (f.pre) {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) store1(f.pre, f.pre_bf16, row * f.pre_stride + col + i, v[i]);
+    }
+    activate8(f.act, v);
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) {
+            if (f.residual) v[i] += load1(f.residual, f.residual_bf16, row * f.residual_stride + col + i);
+            store1(f.out, f.out_bf16, row * f.out_stride + col + i, v[i]);
+        }
 }
 
 // ---- operands ------------------------------------------------------------------
@@ -301,9 +414,18 @@ struct Shape {
     typedef Operand<T, BL, TN, NT> B;
     static constexpr int STAGE = Kind<T>::kPlanes * (A::PLANE + B::PLANE);
     static constexpr int ROWS = TM / WM, COLS = TN / WN;         // of a wave
-    static constexpr int PITCH = COLS + 4;                       // floats of a row on its way out
-    static constexpr int OUT = WM * WN * 16 * PITCH * 4;
-    static constexpr int LDS = Kind<T>::kStages * STAGE > OUT ? Kind<T>::kStages * STAGE : OUT;
+    static constexpr int BLOCKS = ROWS / 16;
+    static constexpr int PITCH = TN + 4;                         // floats of a row on its way out
+    static constexpr int IN = Kind<T>::kStages * STAGE;
+    // blocks of 16 rows of each wave that go out at once
+    static constexpr int out_bytes(int blocks) { return WM * blocks * 16 * PITCH * 4; }
+    static constexpr int most() {
+        int b = BLOCKS;
+        while (b > 1 && out_bytes(b) > (IN > 68 * 1024 ? IN : 68 * 1024)) b /= 2;
+        return b;
+    }
+    static constexpr int OUT = most();
+    static constexpr int LDS = IN > out_bytes(OUT) ? IN : out_bytes(OUT);
 };
 
 template <class T, Layout AL, Layout BL, int TM, int TN, int WM, int WN>
@@ -402,36 +524,57 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
         }
     }
 
-    // out: 16 rows of the wave at a time through its own part of the LDS
-    float* buf = reinterpret_cast<float*>(lds) + wave * 16 * S::PITCH;
-    constexpr int ACROSS = S::COLS / 8, DOWN = 64 / ACROSS;
-    const int np = (g.n + 7) / 8 * 8;
+    // out: OUT blocks of 16 rows of every wave at a time through the LDS, then
+    // by whole pieces of rows
+    float* buf = reinterpret_cast<float*>(lds);
+    constexpr int OUT = S::OUT, ROWS = WM * OUT * 16, ACROSS = TN / 8, DOWN = S::NT / ACROSS;
+    constexpr int AT = ROWS / DOWN < 4 ? ROWS / DOWN : 4;
+    static_assert(S::NT % ACROSS == 0 && ROWS % (AT * DOWN) == 0, "every thread keeps its columns");
+    const int np = (g.n + 7) / 8 * 8, col = n0 + threadIdx.x % ACROSS * 8;
+    const bool whole = col + 8 <= g.n;
+    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (g.splits == 1) load_bias(g.finish, col, g.n - col, bias);
+#pragma unroll 1
+    for (int part = 0; part < FM / OUT; ++part) {
+        if (part) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
+        for (int i = 0; i < FM; ++i) {
+            if (i / OUT != part) continue;
+            float* to = buf + ((wave / WN * OUT + i % OUT) * 16 + (lane & 15)) * S::PITCH + wn + (lane >> 4) * 4;
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-            *reinterpret_cast<v4f*>(buf + (lane & 15) * S::PITCH + j * 16 + (lane >> 4) * 4) = acc[i][j];
-        __builtin_amdgcn_wave_barrier();
+            for (int j = 0; j < FN; ++j) *reinterpret_cast<v4f*>(to + j * 16) = acc[i][j];
+        }
+        __syncthreads();
+        if (col >= g.n) continue;
+        // this thread's rows: every DOWN-th of the part, AT of them at once
+#pragma unroll 1
+        for (int r0 = threadIdx.x / ACROSS; r0 < ROWS; r0 += AT * DOWN) {
+            int64_t row[AT];
+            Raw8 more[AT];
 #pragma unroll
-        for (int r = 0; r < 16; r += DOWN) {
-            const int lr = r + lane / ACROSS, lc = lane % ACROSS * 8;
-            const int row = m0 + wm + i * 16 + lr, col = n0 + wn + lc;
-            if (DOWN > 16 && lr >= 16) continue;
-            float v[8];
-            const v4f* q = reinterpret_cast<const v4f*>(buf + lr * S::PITCH + lc);
+            for (int i = 0; i < AT; ++i) {
+                const int r = r0 + i * DOWN;
+                row[i] = m0 + r / (OUT * 16) * S::ROWS + part * OUT * 16 + r % (OUT * 16);
+                if (whole && g.finish.residual && row[i] < g.m)
+                    more[i].load(g.finish.residual, g.finish.residual_bf16, row[i] * g.finish.residual_stride + col);
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = q[e >> 2][e & 3];
-            if (row < g.m && col < g.n) {
+            for (int i = 0; i < AT; ++i) {
+                if (row[i] >= g.m) continue;
+                const v4f* q = reinterpret_cast<const v4f*>(buf + (r0 + i * DOWN) * S::PITCH + threadIdx.x % ACROSS * 8);
                 if (g.splits > 1) {
-                    float* to = g.partial + ((int64_t)split * g.m + row) * np + col;
-                    *reinterpret_cast<v4f*>(to) = v4f{v[0], v[1], v[2], v[3]};
-                    *reinterpret_cast<v4f*>(to + 4) = v4f{v[4], v[5], v[6], v[7]};
-                } else {
-                    finish8(g.finish, row, col, g.n - col, v);
+                    v4f* to = reinterpret_cast<v4f*>(g.partial + ((int64_t)split * g.m + row[i]) * np + col);
+                    to[0] = q[0];
+                    to[1] = q[1];
+                    continue;
                 }
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = q[e >> 2][e & 3] + bias[e];
+                if (whole) finish8(g.finish, row[i], col, v, more[i]);
+                else finish_edge(g.finish, row[i], col, g.n - col, v);
             }
         }
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -447,7 +590,17 @@ __global__ __launch_bounds__(256) inline void join_kernel(Args g) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += q[e >> 2][e & 3];
     }
-    finish8(g.finish, row, col, g.n - col, v);
+    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    load_bias(g.finish, col, g.n - col, bias);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += bias[e];
+    if (col + 8 <= g.n) {
+        Raw8 more;
+        if (g.finish.residual) more.load(g.finish.residual, g.finish.residual_bf16, row * g.finish.residual_stride + col);
+        finish8(g.finish, row, col, v, more);
+    } else {
+        finish_edge(g.finish, row, col, g.n - col, v);
+    }
 }
 
 }  // namespace gemm

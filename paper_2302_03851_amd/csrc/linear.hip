@@ -58,11 +58,9 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
                     y[i] = i < left && a.act != EDB_ACT_NONE ? Elem<T>::get(v + i) : 0.f;
                 }
             }
+            edb::gemm::slope8(a.act, y, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (a.act != EDB_ACT_NONE && i < left) x[i] *= edb::gemm::slope(a.act, y[i]);
-                sum[i] += x[i];
-            }
+            for (int i = 0; i < 8; ++i) sum[i] += x[i];
             if (a.g) store_k<T, 8>(static_cast<T*>(a.g) + row * gm + col, x);
         }
     if (!a.part) return;
