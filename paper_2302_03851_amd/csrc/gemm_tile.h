@@ -16,8 +16,8 @@
 // column.  Both are permuted within LDS so that no read meets its own banks.
 //
 // The products are formed as B^T A^T, so that a lane holds 4 neighbouring
-// columns of a row of C; the tile passes through LDS once more, to be finished
-// (bias, activation, residual) and written by whole pieces of rows.
+// columns of a row of C; each wave passes its sums through LDS once more, to be
+// finished (bias, activation, residual) and written by whole pieces of rows.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -135,9 +135,10 @@ __device__ __forceinline__ float tanh_slope(float v) {
     return 4.f * p.e * r * r * p.scale;
 }
 
-__device__ __forceinline__ void activate8(int act, float (&v)[8]) {
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N]) {
 #define EDB_EACH(f)               \
-    _Pragma("unroll") for (int i = 0; i < 8; ++i) v[i] = f(v[i])
+    _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = f(v[i])
     if (act == EDB_ACT_RELU) {
         EDB_EACH(relu);
     } else if (act == EDB_ACT_GELU) {
@@ -234,21 +235,22 @@ __device__ __forceinline__ void load_bias(const Finish& f, int col, int left, fl
 // 8 columns of a row of sums with the bias; more: the residual's.
 __device__ __forceinline__ void finish8(const Finish& f, int64_t row, int col, float (&v)[8], const Raw8& more) {
     if (f.pre) store8(f.pre, f.pre_bf16, row * f.pre_stride + col, v);
-    activate8(f.act, v);
+    activate(f.act, v);
     if (f.residual) more.add_to(f.residual_bf16, v);
     store8(f.out, f.out_bf16, row * f.out_stride + col, v);
 }
 
-// The last `left` < 8 columns.
-__device__ __forceinline__ void finish_edge(const Finish& f, int64_t row, int col, int left, float (&v)[8]) {
+// Up to 8 columns one by one.
+template <int N>
+__device__ __forceinline__ void finish_edge(const Finish& f, int64_t row, int col, int left, float (&v)[N]) {
     if (f.pre) {
 #pragma unroll
-        for (int i = 0; i < 7; ++i)
+        for (int i = 0; i < N; ++i)
             if (i < left) store1(f.pre, f.pre_bf16, row * f.pre_stride + col + i, v[i]);
     }
-    activate8(f.act, v);
+    activate(f.act, v);
 #pragma unroll
-    for (int i = 0; i < 7; ++i)
+    for (int i = 0; i < N; ++i)
         if (i < left) {
             if (f.residual) v[i] += load1(f.residual, f.residual_bf16, row * f.residual_stride + col + i);
             store1(f.out, f.out_bf16, row * f.out_stride + col + i, v[i]);
@@ -353,6 +355,30 @@ struct Operand {
             p[j] += step;
         }
     }
+    // Adds the pieces up (MN_LINES: all of a thread's are of the same 8 columns).
+    __device__ __forceinline__ void add_to(float (&sum)[8]) const {
+        static_assert(L == MN_LINES && NT % NP == 0, "a thread keeps its columns");
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) Elem<T>::unpack(raw[j][i], v + i * Elem<T>::kVec);
+            if (PIECES % NT && (int)threadIdx.x + j * NT >= PIECES) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        }
+    }
+    // The columns' sums over the threads, through LDS of NT x 32 bytes; the caller's barriers are around it.
+    static __device__ __forceinline__ void sums_out(const float (&sum)[8], float* lds, float* out, int mn0, int mn) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds[i * NT + threadIdx.x] = sum[i];
+        __syncthreads();
+        const int c = threadIdx.x;
+        if (c >= R || mn0 + c >= mn) return;
+        float s = 0.f;
+        for (int t = c >> 3; t < NT; t += NP) s += lds[(c & 7) * NT + t];
+        out[mn0 + c] = s;
+    }
     // Byte offset of a piece in a plane.
     static __device__ __forceinline__ int place(int line, int q) {
         if constexpr (L == K_LINES) return line * BK * 2 + 16 * (q ^ ((line / (128 / BK)) & (NP - 1)));
@@ -404,6 +430,9 @@ struct Args {
     int32_t m, n, k;            // C is m x n
     int32_t splits, k_per;      // k of a split (a multiple of the step's depth)
     float* partial;             // splits > 1: [split][m][n rounded up to 8]
+    // both operands MN_LINES: sums over k of A's rows (1) or B's columns (2) besides, [split][m or n]
+    int32_t sums;
+    float* sums_out;
     Finish finish;
 };
 
@@ -414,18 +443,10 @@ struct Shape {
     typedef Operand<T, BL, TN, NT> B;
     static constexpr int STAGE = Kind<T>::kPlanes * (A::PLANE + B::PLANE);
     static constexpr int ROWS = TM / WM, COLS = TN / WN;         // of a wave
-    static constexpr int BLOCKS = ROWS / 16;
-    static constexpr int PITCH = TN + 4;                         // floats of a row on its way out
-    static constexpr int IN = Kind<T>::kStages * STAGE;
-    // blocks of 16 rows of each wave that go out at once
-    static constexpr int out_bytes(int blocks) { return WM * blocks * 16 * PITCH * 4; }
-    static constexpr int most() {
-        int b = BLOCKS;
-        while (b > 1 && out_bytes(b) > (IN > 68 * 1024 ? IN : 68 * 1024)) b /= 2;
-        return b;
-    }
-    static constexpr int OUT = most();
-    static constexpr int LDS = IN > out_bytes(OUT) ? IN : out_bytes(OUT);
+    static constexpr int OUT = ROWS >= 32 ? 2 : 1;               // blocks of 16 rows on their way out
+    static constexpr int PITCH = COLS + 4;                       // floats of a row there
+    static constexpr int IN = Kind<T>::kStages * STAGE, WAY = WM * WN * OUT * 16 * PITCH * 4;
+    static constexpr int LDS = IN > WAY ? IN : WAY;
 };
 
 template <class T, Layout AL, Layout BL, int TM, int TN, int WM, int WN>
@@ -467,8 +488,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
             b.load_edge(n0, g.n, k0, kend);
         }
     };
+    // the sums, in registers, by the work-groups of the first tiles across
+    constexpr bool SUMS = AL == MN_LINES && BL == MN_LINES;
+    const int sums = SUMS && (g.sums == 1 ? n0 == 0 : m0 == 0) ? g.sums : 0;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     auto store = [&](char* stage) {
+        if constexpr (SUMS) {
+            if (sums == 1) a.add_to(sum);
+        }
         a.store(stage);
+        if constexpr (SUMS) {
+            if (sums == 2) b.add_to(sum);
+        }
         b.store(stage + P * A::PLANE);
     };
 
@@ -504,14 +535,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
         }
     };
 
+    // Two stages: while a step is multiplied from one, the next is written to the
+    // other and the one after it is on its way into registers.
     if (steps > 0) load(0);
     if constexpr (STAGES == 2) {
         if (steps > 0) store(lds);
+        if (steps > 1) load(1);
         __syncthreads();
         for (int s = 0; s < steps; ++s) {
-            if (s + 1 < steps) load(s + 1);
-            compute(lds + (s & 1) * S::STAGE);
             if (s + 1 < steps) store(lds + (~s & 1) * S::STAGE);
+            if (s + 2 < steps) load(s + 2);
+            compute(lds + (s & 1) * S::STAGE);
             __syncthreads();
         }
     } else {
@@ -524,57 +558,70 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
         }
     }
 
-    // out: OUT blocks of 16 rows of every wave at a time through the LDS, then
-    // by whole pieces of rows
-    float* buf = reinterpret_cast<float*>(lds);
-    constexpr int OUT = S::OUT, ROWS = WM * OUT * 16, ACROSS = TN / 8, DOWN = S::NT / ACROSS;
-    constexpr int AT = ROWS / DOWN < 4 ? ROWS / DOWN : 4;
-    static_assert(S::NT % ACROSS == 0 && ROWS % (AT * DOWN) == 0, "every thread keeps its columns");
-    const int np = (g.n + 7) / 8 * 8, col = n0 + threadIdx.x % ACROSS * 8;
+    if constexpr (SUMS) {
+        if (sums) {
+            float* to = g.sums_out + (int64_t)split * (sums == 1 ? g.m : g.n);
+            float* scratch = reinterpret_cast<float*>(lds);
+            static_assert(S::LDS >= S::NT * 32, "room for the sums");
+            if (sums == 1) A::sums_out(sum, scratch, to, m0, g.m);
+            else B::sums_out(sum, scratch, to, n0, g.n);
+            __syncthreads();
+        }
+    }
+
+    // out: every wave passes OUT blocks of 16 rows at a time through its own
+    // part of the LDS and finishes them by pieces of rows, AT a lane; the residual's
+    // are loaded a turn ahead.  The turns are not unrolled: they are long code.
+    constexpr int OUT = S::OUT, ROWS = OUT * 16, ACROSS = S::COLS / 8, DOWN = 64 / ACROSS, AT = ROWS / DOWN;
+    float* buf = reinterpret_cast<float*>(lds) + wave * ROWS * S::PITCH;
+    const Finish& f = g.finish;
+    const int np = (g.n + 7) / 8 * 8, col = n0 + wn + lane % ACROSS * 8;
     const bool whole = col + 8 <= g.n;
     float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (g.splits == 1) load_bias(g.finish, col, g.n - col, bias);
+    if (g.splits == 1 && col < g.n) load_bias(f, col, g.n - col, bias);
+    Raw8 more[AT], next[AT];
+    auto load_more = [&](int part, Raw8 (&to)[AT]) {
+        if (!f.residual || !whole || g.splits > 1) return;
+#pragma unroll
+        for (int i = 0; i < AT; ++i) {
+            const int row = m0 + wm + part * ROWS + i * DOWN + lane / ACROSS;
+            if (row < g.m) to[i].load(f.residual, f.residual_bf16, row * f.residual_stride + col);
+        }
+    };
+    load_more(0, next);
 #pragma unroll 1
     for (int part = 0; part < FM / OUT; ++part) {
-        if (part) __syncthreads();
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             if (i / OUT != part) continue;
-            float* to = buf + ((wave / WN * OUT + i % OUT) * 16 + (lane & 15)) * S::PITCH + wn + (lane >> 4) * 4;
 #pragma unroll
-            for (int j = 0; j < FN; ++j) *reinterpret_cast<v4f*>(to + j * 16) = acc[i][j];
+            for (int j = 0; j < FN; ++j)
+                *reinterpret_cast<v4f*>(buf + (i % OUT * 16 + (lane & 15)) * S::PITCH + j * 16 + (lane >> 4) * 4) = acc[i][j];
         }
-        __syncthreads();
-        if (col >= g.n) continue;
-        // this thread's rows: every DOWN-th of the part, AT of them at once
-#pragma unroll 1
-        for (int r0 = threadIdx.x / ACROSS; r0 < ROWS; r0 += AT * DOWN) {
-            int64_t row[AT];
-            Raw8 more[AT];
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int i = 0; i < AT; ++i) {
-                const int r = r0 + i * DOWN;
-                row[i] = m0 + r / (OUT * 16) * S::ROWS + part * OUT * 16 + r % (OUT * 16);
-                if (whole && g.finish.residual && row[i] < g.m)
-                    more[i].load(g.finish.residual, g.finish.residual_bf16, row[i] * g.finish.residual_stride + col);
-            }
+        for (int i = 0; i < AT; ++i) more[i] = next[i];
+        if (part + 1 < FM / OUT) load_more(part + 1, next);
 #pragma unroll
-            for (int i = 0; i < AT; ++i) {
-                if (row[i] >= g.m) continue;
-                const v4f* q = reinterpret_cast<const v4f*>(buf + (r0 + i * DOWN) * S::PITCH + threadIdx.x % ACROSS * 8);
+        for (int i = 0; i < AT; ++i) {
+            const int r = i * DOWN + lane / ACROSS;
+            const int64_t row = m0 + wm + part * ROWS + r;
+            const v4f* q = reinterpret_cast<const v4f*>(buf + r * S::PITCH + lane % ACROSS * 8);
+            if (row < g.m && col < g.n) {
                 if (g.splits > 1) {
-                    v4f* to = reinterpret_cast<v4f*>(g.partial + ((int64_t)split * g.m + row[i]) * np + col);
+                    v4f* to = reinterpret_cast<v4f*>(g.partial + ((int64_t)split * g.m + row) * np + col);
                     to[0] = q[0];
                     to[1] = q[1];
-                    continue;
-                }
-                float v[8];
+                } else {
+                    float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = q[e >> 2][e & 3] + bias[e];
-                if (whole) finish8(g.finish, row[i], col, v, more[i]);
-                else finish_edge(g.finish, row[i], col, g.n - col, v);
+                    for (int e = 0; e < 8; ++e) v[e] = q[e >> 2][e & 3] + bias[e];
+                    if (whole) finish8(f, row, col, v, more[i]);
+                    else finish_edge(f, row, col, g.n - col, v);
+                }
             }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 

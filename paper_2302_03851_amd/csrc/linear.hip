@@ -121,22 +121,53 @@ struct Product {
     int64_t bytes;                // of the partial sums
 };
 
-constexpr int kTile[3][2] = {{128, 128}, {64, 64}, {16, 256}};
+// Tiles of the products, with what a step of k and the way out of a work-group
+// take in us: among as many others as its compute unit holds (busy, a share of
+// the unit's time) and from beginning to end (alone).  Fitted to products from
+// 1 x 512 x 131072 to 8192^3, whose best tile and split they find within 10%, as
+// (bf16, us) 8192^3 256 x 256 907, 256 x 128 1060, 128 x 128 1205; 28629 x 512 x
+// 1536 80, 86, 83; 2048 x 512 x 1536 25, 15, 13.5 and 64 x 64 10.5.
+struct Tile {
+    int32_t rows, cols, held;     // held: work-groups that a compute unit holds
+    double busy, busy_out, alone, alone_out;
+};
+constexpr int kWide = 2;          // the tile of few rows
+constexpr Tile kBf16[5] = {{128, 128, 2, 0.59, 3.3, 0.8, 4.0}, {64, 64, 5, 0.25, 0.2, 0.5, 2.5}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0},
+                           {256, 256, 1, 1.77, 10.0, 1.77, 10.0}, {256, 128, 1, 1.04, 5.8, 1.04, 5.8}};
+constexpr Tile kF32[3] = {{128, 128, 2, 1.39, 2.5, 2.2, 4.0}, {64, 64, 4, 0.43, 0.3, 1.2, 2.5}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0}};
 
 Product product_plan(int32_t m, int32_t n, int32_t k, int32_t dtype) {
-    const int depth = dtype == EDB_BF16 ? 64 : 32;
-    auto tiles = [&](int t) { return (((int64_t)m + kTile[t][0] - 1) / kTile[t][0]) * (((int64_t)n + kTile[t][1] - 1) / kTile[t][1]); };
-    Product p{};
-    p.tile = m <= 16 ? 2 : tiles(0) >= 256 ? 0 : 1;
+    constexpr int32_t kUnits = 256, kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    const int depth = dtype == EDB_BF16 ? 64 : 32, count = dtype == EDB_BF16 ? 5 : 3;
+    const Tile* tiles = dtype == EDB_BF16 ? kBf16 : kF32;
     const int64_t steps = ((int64_t)k + depth - 1) / depth;
-    int64_t splits = 512 / (tiles(p.tile) > 0 ? tiles(p.tile) : 1);
-    if (splits > steps / 4) splits = steps / 4;
-    if (splits > 64) splits = 64;
-    if (splits < 1) splits = 1;
-    const int64_t per = (steps + splits - 1) / splits;
-    p.k_per = (int32_t)((per < 1 ? 1 : per) * depth);
-    p.splits = (int32_t)((steps + (per < 1 ? 1 : per) - 1) / (per < 1 ? 1 : per));
-    if (p.splits < 1) p.splits = 1;
+    const double sums = 8.0 * m * n / 5e6;    // us for a split's sums to be written and read again, at 5 TB/s
+    // Few rows of many columns are read as fast as memory gives them by a tile as
+    // wide as high ones (1 x 512 x 131072 bf16 22.0 us, by 64 x 64 24.4; fp32 44 and
+    // 60), of fewer columns not (16 x 1024 x 1024 fp32 13.6 and 11.9).
+    const bool wide = m <= 16 && n >= 16384;
+    Product p{kWide, 1, 0, 0};
+    double best = 0.0;
+    for (int t = 0; t < count; ++t) {
+        if ((t == kWide) != wide) continue;
+        const Tile& c = tiles[t];
+        const int64_t all = (((int64_t)m + c.rows - 1) / c.rows) * (((int64_t)n + c.cols - 1) / c.cols);
+        for (int32_t splits : kSplits) {
+            if (splits > 1 && (splits > steps || all > 4 * kUnits)) break;
+            const double each = (double)((steps + splits - 1) / splits), unit = (double)((all * splits + kUnits - 1) / kUnits);
+            const double busy = unit * (each * c.busy + c.busy_out),
+                         alone = (double)(((int64_t)unit + c.held - 1) / c.held) * (each * c.alone + c.alone_out);
+            const double us = (busy > alone ? busy : alone) + (splits > 1 ? 4.0 + splits * sums : 0.0);
+            if (best == 0.0 || us < best) {
+                best = us;
+                p.tile = t;
+                p.splits = splits;
+            }
+        }
+    }
+    const int64_t per = steps > 0 ? (steps + p.splits - 1) / p.splits : 1;
+    p.k_per = (int32_t)(per * depth);
+    p.splits = steps > 0 ? (int32_t)((steps + per - 1) / per) : 1;
     p.bytes = p.splits > 1 ? (int64_t)p.splits * m * ((n + 7) / 8 * 8) * 4 : 0;
     return p;
 }
@@ -151,13 +182,16 @@ template <class T, Layout AL, Layout BL>
 void start(const Product& p, const Args& g, hipStream_t st) {
     if (p.tile == 0) start<T, AL, BL, 128, 128, 2, 2>(g, st);
     else if (p.tile == 1) start<T, AL, BL, 64, 64, 2, 2>(g, st);
-    else start<T, AL, BL, 16, 256, 1, 4>(g, st);
+    else if (p.tile == 2) start<T, AL, BL, 16, 256, 1, 4>(g, st);
+    else if constexpr (sizeof(T) == 2) {
+        if (p.tile == 3) start<T, AL, BL, 256, 256, 2, 4>(g, st);
+        else start<T, AL, BL, 256, 128, 4, 2>(g, st);
+    }
 }
 
 // C = A B.  a_lines, b_lines: how the operands lie in memory.
-void multiply(int32_t dtype, Layout a_lines, Layout b_lines, Args g, void* workspace, hipStream_t st) {
+void multiply(const Product& p, int32_t dtype, Layout a_lines, Layout b_lines, Args g, void* workspace, hipStream_t st) {
     if (g.m == 0 || g.n == 0) return;
-    const Product p = product_plan(g.m, g.n, g.k, dtype);
     g.splits = p.splits;
     g.k_per = p.k_per;
     g.partial = static_cast<float*>(workspace);
@@ -177,7 +211,8 @@ void multiply(int32_t dtype, Layout a_lines, Layout b_lines, Args g, void* works
 
 // Scratch memory of the gradients: g, the parts of its columns' sums, the products' partial sums.
 struct GradPlan {
-    bool own_g;
+    bool own_g, summed;           // summed: the weight's product adds up the bias's gradient
+    Product to_dx, to_dw, to_turned;
     int32_t chunks, rows_per;
     int64_t part, partial, bytes;
 };
@@ -185,6 +220,7 @@ struct GradPlan {
 GradPlan grad_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t dout_dtype, int32_t act, bool dx, bool dw, bool db) {
     GradPlan p{};
     p.own_g = (dx || dw) && (act != EDB_ACT_NONE || dtype != dout_dtype);
+    p.summed = db && dw && !p.own_g;
     const int64_t wide = ((int64_t)m + 255) / 256;
     int64_t chunks = (2048 + wide - 1) / wide;
     if (chunks > (n + 31) / 32) chunks = (n + 31) / 32;
@@ -194,16 +230,21 @@ GradPlan grad_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t dout_
     p.chunks = p.rows_per ? (int32_t)(((int64_t)n + p.rows_per - 1) / p.rows_per) : 0;
     int64_t at = p.own_g ? (int64_t)n * ((m + 7) / 8 * 8) * elem_bytes(dtype) : 0;
     p.part = at = (at + 15) / 16 * 16;
-    if (db) at += (int64_t)p.chunks * m * 4;
-    p.partial = at = (at + 15) / 16 * 16;
     int64_t most = 0;
-    if (dx) most = product_plan(n, k, m, dtype).bytes;
+    if (dx) {
+        p.to_dx = product_plan(n, k, m, dtype);
+        most = p.to_dx.bytes;
+    }
     if (dw) {
         // either way round: the weight may be stored output by output
-        const int64_t one = product_plan(k, m, n, dtype).bytes, other = product_plan(m, k, n, dtype).bytes;
-        if (one > most) most = one;
-        if (other > most) most = other;
+        p.to_dw = product_plan(k, m, n, dtype);
+        p.to_turned = product_plan(m, k, n, dtype);
+        if (p.to_dw.bytes > most) most = p.to_dw.bytes;
+        if (p.to_turned.bytes > most) most = p.to_turned.bytes;
+        if (p.summed) p.chunks = p.to_dw.splits > p.to_turned.splits ? p.to_dw.splits : p.to_turned.splits;
     }
+    if (db) at += (int64_t)p.chunks * m * 4;
+    p.partial = at = (at + 15) / 16 * 16;
     p.bytes = at + most;
     return p;
 }
@@ -249,7 +290,8 @@ extern "C" edb_status edb_linear(const void* x, const void* weight, int32_t dtyp
             edb::clear_error();
             return EDB_OK;
         }
-        const int64_t bytes = product_plan(n, m, k, dtype).bytes;
+        const Product p = product_plan(n, m, k, dtype);
+        const int64_t bytes = p.bytes;
         if (workspace_bytes < bytes || (bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
             return fail(EDB_ERR_INVALID, "edb_linear: a 16-byte aligned workspace of " + std::to_string(bytes) + " bytes is needed");
         const Region in = matrix(x, dtype, n, k, x_stride), w = matrix(weight, dtype, lines, line, weight_stride),
@@ -271,7 +313,7 @@ extern "C" edb_status edb_linear(const void* x, const void* weight, int32_t dtyp
         g.k = k;
         g.finish = Finish{bias, residual, residual_stride, out, out_stride, pre, pre_stride, act, bias_dtype == EDB_BF16,
                           residual_dtype == EDB_BF16, out_dtype == EDB_BF16, dtype == EDB_BF16};
-        multiply(dtype, K_LINES, turned ? K_LINES : MN_LINES, g, workspace, reinterpret_cast<hipStream_t>(stream));
+        multiply(p, dtype, K_LINES, turned ? K_LINES : MN_LINES, g, workspace, reinterpret_cast<hipStream_t>(stream));
         return launched(who);
     });
 }
@@ -338,7 +380,7 @@ extern "C" edb_status edb_linear_grad(const void* x, const void* weight, int32_t
         const void* g = p.own_g ? ws : dout;
         const int64_t g_stride = p.own_g ? (m + 7) / 8 * 8 : dout_stride;
         float* part = dbias ? reinterpret_cast<float*>(ws + p.part) : nullptr;
-        if (n && (p.own_g || dbias)) {
+        if (n && (p.own_g || (dbias && !p.summed))) {
             const SlopeArgs s{dout, dout_stride, pre, pre_stride, act, n, m, p.rows_per, p.own_g ? ws : nullptr, part};
             const dim3 grid((unsigned)(((int64_t)m + 255) / 256), (unsigned)p.chunks);
             if (dout_dtype == EDB_F32) {
@@ -349,7 +391,7 @@ extern "C" edb_status edb_linear_grad(const void* x, const void* weight, int32_t
                 else slope_kernel<bf16, bf16><<<grid, 256, 0, st>>>(s);
             }
         }
-        if (dbias) edb::join_columns(part, p.chunks, m, 1, dbias, nullptr, st);
+        if (dbias && !p.summed) edb::join_columns(part, p.chunks, m, 1, dbias, nullptr, st);
         const bool half = dtype == EDB_BF16;
         Args a{};
         a.finish.act = EDB_ACT_NONE;
@@ -364,7 +406,7 @@ extern "C" edb_status edb_linear_grad(const void* x, const void* weight, int32_t
             a.k = m;
             a.finish.out = dx;
             a.finish.out_stride = dx_stride;
-            multiply(dtype, K_LINES, turned ? MN_LINES : K_LINES, a, ws + p.partial, st);
+            multiply(p.to_dx, dtype, K_LINES, turned ? MN_LINES : K_LINES, a, ws + p.partial, st);
         }
         if (dweight) {
             a.a = turned ? g : x;
@@ -376,7 +418,13 @@ extern "C" edb_status edb_linear_grad(const void* x, const void* weight, int32_t
             a.k = n;
             a.finish.out = dweight;
             a.finish.out_stride = dweight_stride;
-            multiply(dtype, MN_LINES, MN_LINES, a, ws + p.partial, st);
+            const Product& q = turned ? p.to_turned : p.to_dw;
+            if (p.summed) {
+                a.sums = turned ? 1 : 2;
+                a.sums_out = q.splits > 1 ? part : dbias;
+            }
+            multiply(q, dtype, MN_LINES, MN_LINES, a, ws + p.partial, st);
+            if (p.summed && q.splits > 1) edb::join_columns(part, q.splits, m, 1, dbias, nullptr, st);
         }
         return launched(who);
     });
