@@ -322,9 +322,9 @@ struct Operand {
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int line = index(j) / NP, q = index(j) % NP * 8;
-            // rows past the end: the last one again, whose results nobody writes
+            // rows (columns) past the end: the last one again, whose results nobody writes
             p[j] = L == K_LINES ? base + (int64_t)min(mn0 + line, mn - 1) * stride + k0 + q
-                                : base + (int64_t)(k0 + line) * stride + mn0 + q;
+                                : base + (int64_t)(k0 + line) * stride + min(mn0 + q, mn - 1);
         }
         step = L == K_LINES ? BK : BK * stride;
     }
@@ -470,7 +470,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
 
     const int kbeg = split * g.k_per, kend = min(kbeg + g.k_per, g.k);
     const int steps = (kend - kbeg + BK - 1) / BK;
+    // a piece that leaves its line's end (MN_LINES) reads on in the next line, if there is one: up to k_fast
     const bool inside = (AL == K_LINES || m0 + TM <= g.m) && (BL == K_LINES || n0 + TN <= g.n);
+    const bool longer = (AL == K_LINES || g.a_stride >= 8) && (BL == K_LINES || g.b_stride >= 8);
+    const int k_fast = inside ? kend : longer ? min(kend, g.k - 1) : 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN * S::ROWS, wn = wave % WN * S::COLS;
 
@@ -480,7 +483,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
     b.start(static_cast<const T*>(g.b), g.b_stride, n0, g.n, kbeg);
     auto load = [&](int s) {
         const int k0 = kbeg + s * BK;
-        if (inside && k0 + BK <= kend) {
+        if (k0 + BK <= k_fast) {
             a.load();
             b.load();
         } else {
@@ -632,6 +635,7 @@ __global__ __launch_bounds__(256) inline void join_kernel(Args g) {
     if (row >= g.m) return;
     const int col = (int)(at - row * pieces) * 8;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int s = 0; s < g.splits; ++s) {
         const v4f* q = reinterpret_cast<const v4f*>(g.partial + (((int64_t)s * g.m + row) * pieces) * 8 + col);
 #pragma unroll

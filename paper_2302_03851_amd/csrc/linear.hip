@@ -132,12 +132,12 @@ struct Tile {
     double busy, busy_out, alone, alone_out;
 };
 constexpr int kWide = 2;          // the tile of few rows
-constexpr Tile kBf16[5] = {{128, 128, 2, 0.59, 3.3, 0.8, 4.0}, {64, 64, 5, 0.25, 0.2, 0.5, 2.5}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0},
+constexpr Tile kBf16[5] = {{128, 128, 2, 0.59, 3.3, 0.8, 4.0}, {64, 64, 5, 0.25, 0.2, 0.35, 2.0}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0},
                            {256, 256, 1, 1.77, 10.0, 1.77, 10.0}, {256, 128, 1, 1.04, 5.8, 1.04, 5.8}};
 constexpr Tile kF32[3] = {{128, 128, 2, 1.39, 2.5, 2.2, 4.0}, {64, 64, 4, 0.43, 0.3, 1.2, 2.5}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0}};
 
 Product product_plan(int32_t m, int32_t n, int32_t k, int32_t dtype) {
-    constexpr int32_t kUnits = 256, kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    constexpr int32_t kUnits = 256;
     const int depth = dtype == EDB_BF16 ? 64 : 32, count = dtype == EDB_BF16 ? 5 : 3;
     const Tile* tiles = dtype == EDB_BF16 ? kBf16 : kF32;
     const int64_t steps = ((int64_t)k + depth - 1) / depth;
@@ -152,16 +152,22 @@ Product product_plan(int32_t m, int32_t n, int32_t k, int32_t dtype) {
         if ((t == kWide) != wide) continue;
         const Tile& c = tiles[t];
         const int64_t all = (((int64_t)m + c.rows - 1) / c.rows) * (((int64_t)n + c.cols - 1) / c.cols);
-        for (int32_t splits : kSplits) {
-            if (splits > 1 && (splits > steps || all > 4 * kUnits)) break;
+        // no splits, or such that fill the units one to four times
+        int64_t last = 0;
+        for (int turns = 0; turns <= 4; ++turns) {
+            int64_t splits = turns && all ? kUnits * turns / all : 1;
+            if (splits > 64) splits = 64;
+            if (turns && splits > steps) splits = steps;
+            if (splits <= last) continue;
+            last = splits;
             const double each = (double)((steps + splits - 1) / splits), unit = (double)((all * splits + kUnits - 1) / kUnits);
             const double busy = unit * (each * c.busy + c.busy_out),
                          alone = (double)(((int64_t)unit + c.held - 1) / c.held) * (each * c.alone + c.alone_out);
-            const double us = (busy > alone ? busy : alone) + (splits > 1 ? 4.0 + splits * sums : 0.0);
+            const double us = (busy > alone ? busy : alone) + (splits > 1 ? 5.0 + splits * sums : 0.0);
             if (best == 0.0 || us < best) {
                 best = us;
                 p.tile = t;
-                p.splits = splits;
+                p.splits = (int32_t)splits;
             }
         }
     }
