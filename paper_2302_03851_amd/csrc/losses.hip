@@ -24,6 +24,7 @@
 #include <string>
 
 #include "edb_internal.h"
+#include "lane_sums.h"
 
 using edb::fail;
 using edb::Region;
@@ -40,11 +41,9 @@ __device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) {
 }
 
 template <int LANES>
-__device__ __forceinline__ Sums lanes_sum(Sums s) {
-#pragma unroll
-    for (int d = LANES / 2; d; d >>= 1)
-        s = s + Sums{__shfl_xor(s.a, d), __shfl_xor(s.b, d), __shfl_xor(s.live, d), __shfl_xor(s.clipped, d)};
-    return s;
+__device__ __forceinline__ Sums lanes_sum(const Sums& s) {
+    using edb::lanes::sum;
+    return {sum<LANES>(s.a), sum<LANES>(s.b), sum<LANES>(s.live), sum<LANES>(s.clipped)};
 }
 
 struct Loss {

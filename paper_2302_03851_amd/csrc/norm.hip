@@ -14,6 +14,7 @@
 
 #include "column_sums.h"
 #include "edb_internal.h"
+#include "lane_sums.h"
 #include "row_access.h"
 
 using edb::fail;
@@ -27,11 +28,12 @@ struct NormArgs {
     int64_t x_stride;
     const void *weight, *bias;
     bool weight_bf16;
-    double eps;
+    double eps, per;          // per: 1 / dim
     void* out;
     int64_t out_stride;
     float* stats;
     int32_t n, dim;
+    bool past;
 };
 
 // K elements of the scale or the shift, `none` where there is no such array.
@@ -47,20 +49,13 @@ __device__ __forceinline__ void load_weight(const void* p, bool half, int col, f
     }
 }
 
-template <int LANES, class V>
-__device__ __forceinline__ V lanes_sum(V v) {
-#pragma unroll
-    for (int d = LANES < 64 ? LANES / 2 : 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-
 // Sums of two values over the LANES threads of a row, in every one of them.
 // Over several waves: `held` has a place for each (the caller's barriers
 // separate its uses).
 template <int LANES, class V>
 __device__ __forceinline__ void row_sums(V& a, V& b, V (*held)[2]) {
-    a = lanes_sum<LANES>(a);
-    b = lanes_sum<LANES>(b);
+    a = edb::lanes::sum<LANES < 64 ? LANES : 64>(a);
+    b = edb::lanes::sum<LANES < 64 ? LANES : 64>(b);
     if constexpr (LANES > 64) {
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) {
@@ -84,17 +79,104 @@ constexpr int threads() {
     return LANES > 256 ? LANES : 256;
 }
 
-// The statistics are sums in 64 bits of the differences from the row's first
-// element: one pass over the row, and no cancellation, since the variance is at
-// least 1/D of that element's own square distance from the mean.  64-bit
-// additions and products run at the rate of 32-bit ones here.
+// K elements as they lie in memory, read once: asked for a turn before they are used.
+template <class T, int K>
+struct RawPiece {
+    static constexpr int kWords = K * (int)sizeof(T) / 16;
+    u32x4 w[kWords > 0 ? kWords : 1];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (K == 1) w[0][0] = __builtin_bit_cast(uint32_t, Elem<T>::get(p));
+        else if constexpr (kWords == 0) {
+            const u32x2 h = Elem<T>::load_half_nt(p);
+            w[0][0] = h[0];
+            w[0][1] = h[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = Elem<T>::load_nt(p + i * Elem<T>::kVec);
+        }
+    }
+    __device__ __forceinline__ void unpack(float* v) const {
+        if constexpr (K == 1) v[0] = __builtin_bit_cast(float, (uint32_t)w[0][0]);
+        else if constexpr (kWords == 0) Elem<T>::unpack_half(u32x2{w[0][0], w[0][1]}, v);
+        else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) Elem<T>::unpack(w[i], v + i * Elem<T>::kVec);
+        }
+    }
+};
+
+// The statistics are sums of differences from a value of the row's own, c: one
+// pass over the row.  By pieces in 32 bits, c being the average of the row's
+// first K elements, and over the pieces in 64, as long as that is safe: squares
+// within fp32's range and c within two deviations of the mean, so that no digits
+// cancel.  Other rows (an outlier at the front, constant, very large or very small
+// ones) are done again in 64 bits with c = the first element, whose own square
+// distance bounds the variance from below.  All rows in 64 bits took 158 us for
+// 262144 x 512 bf16: conversions and 64-bit operations, not memory, bound it.
 struct Moments {
     double mean, rstd;
-    __device__ __forceinline__ Moments(double first, double sum, double squares, int dim, double eps) {
+    bool safe;
+    // per = 1 / dim
+    __device__ __forceinline__ Moments(double c, double sum, double squares, double per, double eps) {
+        const double d = sum * per, all = squares * per, var = all - d * d, v = var + eps;
+        mean = c + d;
+        // one step of Newton's from the hardware's 22 bits and more
+        const double y = (double)__builtin_amdgcn_rsqf((float)v);
+        rstd = y * fma(-0.5 * v * y, y, 1.5);
+        safe = squares >= 1e-25 && squares <= 1e30 && all <= 4.0 * var && v <= 1e37;
+    }
+    // whatever the numbers: the divisions and the root take as long as a row of 512 otherwise
+    __device__ __forceinline__ void wide(double c, double sum, double squares, int dim, double eps) {
         const double d = sum / dim, var = squares / dim - d * d;
-        mean = var == var ? first + d : var;
+        mean = var == var ? c + d : var;
         rstd = 1.0 / sqrt((var > 0.0 ? var : var == var ? 0.0 : var) + eps);
     }
+};
+
+// Sums of the differences of K elements from c, the first `skip` left out, by a tree.
+template <int K>
+__device__ __forceinline__ void piece_sums(const float* e, float c, int skip, float& sum, float& squares) {
+    float s[K], q[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        s[k] = K > 1 && k < skip ? 0.f : e[k] - c;
+        q[k] = s[k] * s[k];
+    }
+#pragma unroll
+    for (int w = K / 2; w; w >>= 1)
+#pragma unroll
+        for (int k = 0; k < w; ++k) {
+            s[k] += s[k + w];
+            q[k] += q[k + w];
+        }
+    sum = s[0];
+    squares = q[0];
+}
+template <int K>
+__device__ __forceinline__ void piece_sums(const float* e, double c, int skip, double& sum, double& squares) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const double d = (double)e[k] - c;
+        if (K > 1 && k < skip) continue;
+        sum += d;
+        squares = fma(d, d, squares);
+    }
+}
+template <int K>
+__device__ __forceinline__ float average(const float* e) {
+    float s = e[0];
+#pragma unroll
+    for (int k = 1; k < K; ++k) s += e[k];
+    return s * (1.f / K);
+}
+
+// (x - mean) rstd: the mean as two floats where the row is safe.
+struct Scaled {
+    float high, low, rstd;
+    const Moments& m;
+    __device__ __forceinline__ explicit Scaled(const Moments& m) : high((float)m.mean), low((float)(m.mean - (double)high)), rstd((float)m.rstd), m(m) {}
+    __device__ __forceinline__ float safe(float x) const { return ((x - high) - low) * rstd; }
+    __device__ __forceinline__ float wide(float x) const { return (float)(((double)x - m.mean) * m.rstd); }
 };
 
 template <class T, class O, int K, int LANES, int V, int ROWS>
@@ -116,20 +198,34 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormArgs a) {
     const T* x = static_cast<const T*>(a.x);
     O* out = static_cast<O*>(a.out);
     int turn = 0;
-    for (int64_t row0 = ((int64_t)blockIdx.x * kGroups + group) * ROWS;; row0 += (int64_t)gridDim.x * kGroups * ROWS) {
-        // the groups of a work-group leave together where they share its barriers: one group then
-        if (row0 >= a.n) break;
-        float e[ROWS][V][K], first[ROWS];
+    const int64_t apart = (int64_t)gridDim.x * kGroups * ROWS;
+    int64_t row0 = ((int64_t)blockIdx.x * kGroups + group) * ROWS;
+    RawPiece<T, K> raw[ROWS][V], front[ROWS];
+    auto load = [&](int64_t from) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const T* row = x + min(row0 + r, (int64_t)a.n - 1) * a.x_stride;
-            first[r] = Elem<T>::get(row);
+            const T* row = x + min(from + r, (int64_t)a.n - 1) * a.x_stride;
+            front[r].load(row);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int nominal = (v * LANES + lane) * K;
-                if (nominal < a.dim) load_k<T, K, true>(row + Piece<K>(nominal, a.dim).col, e[r][v]);
+                if (nominal < a.dim) raw[r][v].load(row + Piece<K>(nominal, a.dim).col);
             }
         }
+    };
+    if (row0 < a.n) load(row0);
+    // (rows that share barriers are a work-group's only ones)
+    for (; row0 < a.n; row0 += apart) {
+        float e[ROWS][V][K], c[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            float f[K];
+            front[r].unpack(f);
+            c[r] = average<K>(f);
+#pragma unroll
+            for (int v = 0; v < V; ++v) raw[r][v].unpack(e[r][v]);
+        }
+        if (row0 + apart < a.n) load(row0 + apart);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             double sum = 0.0, squares = 0.0;
@@ -137,24 +233,33 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormArgs a) {
             for (int v = 0; v < V; ++v) {
                 const int nominal = (v * LANES + lane) * K;
                 if (nominal >= a.dim) continue;
-                const int skip = Piece<K>(nominal, a.dim).skip;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const double d = (double)e[r][v][k] - (double)first[r];
-                    if (K == 1 || k >= skip) {
-                        sum += d;
-                        squares = fma(d, d, squares);
-                    }
-                }
+                float s, q;
+                piece_sums<K>(e[r][v], c[r], Piece<K>(nominal, a.dim).skip, s, q);
+                sum += (double)s;
+                squares += (double)q;
             }
             row_sums<LANES>(sum, squares, held[LANES > 64 ? turn : 0]);
             turn ^= 1;
-            const Moments m(first[r], sum, squares, a.dim, a.eps);
+            Moments m(c[r], sum, squares, a.per, a.eps);
+            const bool safe = m.safe;
+            if (!safe) {
+                const double first = Elem<T>::get(x + min(row0 + r, (int64_t)a.n - 1) * a.x_stride);
+                sum = squares = 0.0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int nominal = (v * LANES + lane) * K;
+                    if (nominal < a.dim) piece_sums<K>(e[r][v], first, Piece<K>(nominal, a.dim).skip, sum, squares);
+                }
+                row_sums<LANES>(sum, squares, held[LANES > 64 ? turn : 0]);
+                turn ^= 1;
+                m.wide(first, sum, squares, a.dim, a.eps);
+            }
             if (row0 + r >= a.n) break;
             if (lane == 0 && a.stats) {
                 a.stats[2 * (row0 + r)] = (float)m.mean;
                 a.stats[2 * (row0 + r) + 1] = (float)m.rstd;
             }
+            const Scaled scaled(m);
             O* to = out + (row0 + r) * a.out_stride;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -166,10 +271,16 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormArgs a) {
                     load_weight<K>(a.bias, a.weight_bf16, p.col, 0.f, b[v]);
                 }
                 float y[K];
+                if (safe) {
 #pragma unroll
-                for (int k = 0; k < K; ++k)
-                    y[k] = fmaf((float)(((double)e[r][v][k] - m.mean) * m.rstd), w[v][k], b[v][k]);
-                store_from<O, K>(to + p.col, y, p.skip);
+                    for (int k = 0; k < K; ++k) y[k] = fmaf(scaled.safe(e[r][v][k]), w[v][k], b[v][k]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) y[k] = fmaf(scaled.wide(e[r][v][k]), w[v][k], b[v][k]);
+                }
+                // results that no cache could hold go past them (30000 x 1024 fp32 45.3 to 41.6 us)
+                if (K == Elem<O>::kVec && a.past && p.skip == 0) Elem<O>::store_nt(to + p.col, Elem<O>::pack(y));
+                else store_from<O, K>(to + p.col, y, p.skip);
             }
         }
     }
@@ -190,22 +301,17 @@ __global__ __launch_bounds__(kLong) void norm_long_kernel(NormArgs a) {
             const Piece<K> p(nominal, a.dim);
             float e[K];
             load_k<T, K>(x + p.col, e);
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const double d = (double)e[k] - first;
-                if (k >= p.skip) {
-                    sum += d;
-                    squares = fma(d, d, squares);
-                }
-            }
+            piece_sums<K>(e, first, p.skip, sum, squares);
         }
         row_sums<kLong>(sum, squares, held[turn]);
         turn ^= 1;
-        const Moments m(first, sum, squares, a.dim, a.eps);
+        Moments m(first, sum, squares, a.per, a.eps);
+        m.wide(first, sum, squares, a.dim, a.eps);
         if (threadIdx.x == 0 && a.stats) {
             a.stats[2 * row] = (float)m.mean;
             a.stats[2 * row + 1] = (float)m.rstd;
         }
+        const Scaled scaled(m);
         O* to = static_cast<O*>(a.out) + row * a.out_stride;
         for (int nominal = threadIdx.x * K; nominal < a.dim; nominal += kLong * K) {
             const Piece<K> p(nominal, a.dim);
@@ -214,7 +320,7 @@ __global__ __launch_bounds__(kLong) void norm_long_kernel(NormArgs a) {
             load_weight<K>(a.weight, a.weight_bf16, p.col, 1.f, w);
             load_weight<K>(a.bias, a.weight_bf16, p.col, 0.f, b);
 #pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = fmaf((float)(((double)e[k] - m.mean) * m.rstd), w[k], b[k]);
+            for (int k = 0; k < K; ++k) e[k] = fmaf(scaled.wide(e[k]), w[k], b[k]);
             store_from<O, K>(to + p.col, e, p.skip);
         }
     }
@@ -255,22 +361,41 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_grad_kernel(GradArgs a)
     }
     const float per = 1.f / (float)a.dim;
     int turn = 0;
-    for (int64_t row0 = ((int64_t)blockIdx.x * kGroups + group) * ROWS; row0 < a.n; row0 += (int64_t)gridDim.x * kGroups * ROWS) {
-        float h[ROWS][V][K], d[ROWS][V][K], mean[ROWS], rstd[ROWS];
+    const int64_t apart = (int64_t)gridDim.x * kGroups * ROWS;
+    int64_t row0 = ((int64_t)blockIdx.x * kGroups + group) * ROWS;
+    RawPiece<T, K> raw_x[ROWS][V];
+    RawPiece<O, K> raw_d[ROWS][V];
+    float raw_mean[ROWS], raw_rstd[ROWS];
+    auto load = [&](int64_t from) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const int64_t row = min(row0 + r, (int64_t)a.n - 1);
-            mean[r] = a.stats[2 * row];
-            rstd[r] = a.stats[2 * row + 1];
+            const int64_t row = min(from + r, (int64_t)a.n - 1);
+            raw_mean[r] = a.stats[2 * row];
+            raw_rstd[r] = a.stats[2 * row + 1];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int nominal = (v * LANES + lane) * K;
                 if (nominal >= a.dim) continue;
                 const int col = Piece<K>(nominal, a.dim).col;
-                load_k<T, K, true>(x + row * a.x_stride + col, h[r][v]);
-                load_k<O, K, true>(dout + row * a.dout_stride + col, d[r][v]);
+                raw_x[r][v].load(x + row * a.x_stride + col);
+                raw_d[r][v].load(dout + row * a.dout_stride + col);
             }
         }
+    };
+    if (row0 < a.n) load(row0);
+    for (; row0 < a.n; row0 += apart) {
+        float h[ROWS][V][K], d[ROWS][V][K], mean[ROWS], rstd[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            mean[r] = raw_mean[r];
+            rstd[r] = raw_rstd[r];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                raw_x[r][v].unpack(h[r][v]);
+                raw_d[r][v].unpack(d[r][v]);
+            }
+        }
+        if (row0 + apart < a.n) load(row0 + apart);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (row0 + r >= a.n) break;
@@ -410,6 +535,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(GradArgs a, int rows_
 
 constexpr int64_t kMaxElems = INT64_C(1) << 48;
 constexpr int32_t kMaxDim = 1 << 20;
+constexpr int64_t kPast = 96 << 20;
 
 int32_t elem_bytes(int32_t dtype) { return dtype == EDB_BF16 ? 2 : 4; }
 bool known(int32_t dtype) { return dtype == EDB_F32 || dtype == EDB_BF16; }
@@ -448,7 +574,8 @@ int64_t pieces_of(int32_t dim, int k) { return ((int64_t)dim + k - 1) / k; }
 template <class T, class O, int K, int LANES, int V, int ROWS>
 void start(const NormArgs& a, hipStream_t st) {
     constexpr int kRows = threads<LANES>() / LANES * ROWS;
-    const int64_t groups = ((int64_t)a.n + kRows - 1) / kRows, most = 2048;
+    // a few turns each at most sizes (262144 x 512 bf16 125 us, with 2048 work-groups 139; 28629 x 512 17.3, 16.7)
+    const int64_t groups = ((int64_t)a.n + kRows - 1) / kRows, most = groups > 8192 ? 8192 : 2048;
     norm_kernel<T, O, K, LANES, V, ROWS><<<(unsigned)(groups < most ? groups : most), threads<LANES>(), 0, st>>>(a);
 }
 
@@ -495,7 +622,9 @@ GradPlan grad_plan(int32_t n, int32_t dim, int k) {
     if (g.lanes) {
         const int rows = (g.lanes > 256 ? 1 : 256 / g.lanes) * g.rows;
         parts = ((int64_t)n + rows - 1) / rows;
-        if (parts > kMostParts) parts = kMostParts;
+        // the parts are a twentieth of what the rows are, but enough to fill the card
+        const int64_t most = n / 32 > kMostParts ? kMostParts : n / 32 > 256 ? n / 32 : 256;
+        if (parts > most) parts = most;
     } else {
         const int64_t wide = (pieces + 255) / 256;
         parts = (2048 + wide - 1) / wide;
@@ -552,7 +681,8 @@ extern "C" edb_status edb_layer_norm(const void* x, int32_t x_dtype, int32_t n, 
         if (edb_status st = edb::apart(who, {matrix(out, out_dtype, n, dim, out_stride), Region::array(stats, n * INT64_C(8))},
                                        {matrix(x, x_dtype, n, dim, x_stride), Region::array(weight, wide), Region::array(bias, wide)}))
             return st;
-        const NormArgs a{x, x_stride, weight, bias, weight_dtype == EDB_BF16, eps, out, out_stride, stats, n, dim};
+        const NormArgs a{x, x_stride, weight, bias, weight_dtype == EDB_BF16, eps, 1.0 / dim, out, out_stride, stats, n, dim,
+                         (int64_t)n * dim * elem_bytes(out_dtype) >= kPast};
         hipStream_t st = reinterpret_cast<hipStream_t>(stream);
         if (x_dtype == EDB_F32) {
             if (out_dtype == EDB_F32) launch_norm<float, float>(a, st);

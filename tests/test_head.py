@@ -3,8 +3,15 @@ gradients also against differences, and their refusals.
 
 Tolerances.  u = 2^-24 is fp32's rounding unit; a result's own rounding adds
 half a unit in its last place, 2^-8 of the value for bf16.
-* Layer norm: the statistics are formed in 64 bits and rounded once, and so is
-  h = (x - mean) rstd; h w + b is one more rounding.
+* Layer norm: differences d from a value of the row are off by u, sums of at
+  most 8 of them (or of their squares, a unit more each) by 3 u, the rest is in
+  64 bits.  So the mean is off by 4 u of the average |d| and its own rounding;
+  the variance by 6 u of the average d^2, which is at most 4 times it where
+  sums are in 32 bits: 24 u, rstd by half of that and its rounding, 13 u.
+  |d| is at most what it is from the farthest element, and its average at most
+  twice the deviation where sums are in 32 bits (average d^2 <= 4 variances).
+  h = (x - mean) rstd takes 4 roundings of itself and what the mean is off,
+  8 u deviations; h w + b one more.
 * Its gradients: h is off by 2 u, g = dy w by u of itself; the row's averages
   add up at most 24 terms a thread (dim / 1024 + 8 for rows past 8192), then a
   tree, waves and a division: DEPTH = dim / 1024 + 56 roundings of sum |term|.
@@ -93,12 +100,13 @@ def _norm_reference(x, w, b, eps):
 
 def _check_norm(x, w, b, eps, r):
     mean, rstd, h, y, wd = _norm_reference(x, w, b, eps)
-    # 64-bit sums of D terms, themselves rounded
     D = x.shape[1]
-    spread = (x.double() - x[:, :1].double()).abs().mean(1, keepdim=True)
-    _close(r.stats[:, :1], mean, _half(mean, F32) + D * 2.0 ** -52 * (spread + mean.abs()))
-    _close(r.stats[:, 1:], rstd, _half(rstd, F32) + D * 2.0 ** -50 * rstd)
-    _close(r.out, y, 1.01 * U * (h * wd).abs() + 1.01 * U * y.abs() + _half(y, r.out.dtype) + D * 2.0 ** -50 * ((h * wd).abs() + wd.abs()))
+    spread = 2 * (x.double() - mean).square().mean(1, keepdim=True).sqrt()
+    # 64-bit sums of D terms, themselves rounded
+    wide = D * 2.0 ** -50
+    _close(r.stats[:, :1], mean, _half(mean, F32) + 4 * U * spread + wide * (spread + mean.abs()))
+    _close(r.stats[:, 1:], rstd, _half(rstd, F32) + (13 * U + wide) * rstd)
+    _close(r.out, y, (18 * U + wide) * (h * wd).abs() + (8 * U + wide) * (spread * rstd * wd).abs() + U * y.abs() + _half(y, r.out.dtype))
 
 
 @gpu
