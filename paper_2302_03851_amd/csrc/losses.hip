@@ -63,7 +63,9 @@ struct Loss {
     int32_t* clipped;
     float* grad;
     // long calls only
+    int32_t* places;                // [chunk]
     Sums *parts, *whole;            // [chunk][2], [sequence]
+    const Sums* counts;             // policy: the parts of policy_counts
     double* slopes;                 // preference: [sequence]
 };
 
@@ -267,101 +269,166 @@ struct Chunk {
     int32_t s0, s1;         // sequences that may have tokens here: s0 <= s < s1
 };
 
-// The numbers of offsets first[0 .. count) that are at most t[0] and t[1], found
-// by the whole work-group, 256 steps at a time.
-__device__ __forceinline__ void upto(const int32_t* first, int count, const int (&t)[2], int (&found)[2], int (*held)[2][kThreads / 64]) {
-    int lo[2] = {0, 0}, hi[2] = {count, count};
-    for (int turn = 0; hi[0] > lo[0] || hi[1] > lo[1]; turn ^= 1) {
-        int step[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            step[i] = (hi[i] - lo[i] + kThreads - 1) / kThreads;
-            const int64_t at = lo[i] + (int64_t)threadIdx.x * step[i];
-            const uint64_t below = __ballot(at < hi[i] && first[at] <= t[i]);
-            if ((threadIdx.x & 63) == 0) held[turn][i][threadIdx.x >> 6] = __popcll(below);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            int k = 0;
-#pragma unroll
-            for (int w = 0; w < kThreads / 64; ++w) k += held[turn][i][w];
-            if (k == 0) {
-                hi[i] = lo[i];
-            } else {
-                const int base = lo[i] + (k - 1) * step[i];
-                hi[i] = (int)min((int64_t)base + step[i], (int64_t)hi[i]);
-                lo[i] = base + 1;
-            }
-        }
-    }
-    found[0] = lo[0];
-    found[1] = lo[1];
+// First of the launches: for every chunk, how many sequences begin up to its
+// first token.  The sequence that holds the token writes it (the one after the
+// last: for chunks before the first sequence).  A search by each work-group of
+// the other launches took 16 of policy_terms' 48 us over 4 M tokens.
+__global__ __launch_bounds__(kThreads) void place_chunks(Loss l, int sequences) {
+    const int s = blockIdx.x * kThreads + threadIdx.x;
+    if (s > sequences) return;
+    const int64_t from = s < sequences ? min(max(l.first[s], 0), l.n) : 0;
+    const int64_t to = s == sequences ? min(max(l.first[0], 0), l.n) : s + 1 < sequences ? min(max(l.first[s + 1], 0), l.n) : l.n;
+    for (int64_t c = (from + kChunk - 1) / kChunk; c * kChunk < to; ++c) l.places[c] = s < sequences ? s + 1 : 0;
 }
 
-typedef int Held[2][2][kThreads / 64];
-__device__ __forceinline__ Chunk chunk_of(const Loss& l, int sequences, Held& held) {
+__device__ __forceinline__ Chunk chunk_of(const Loss& l, int sequences) {
     Chunk c;
     c.from = blockIdx.x * kChunk;
     c.to = (int)min((int64_t)c.from + kChunk, (int64_t)l.n);
-    const int t[2] = {c.from, c.to - 1};
-    int found[2];
-    upto(l.first, sequences, t, found, held);
-    c.s0 = max(found[0] - 1, 0);
-    c.s1 = found[1];
+    // (offsets that fall may leave places unwritten: any number then)
+    c.s0 = min(max(l.places[blockIdx.x] - 1, 0), sequences);
+    c.s1 = blockIdx.x + 1 < gridDim.x ? min(max(l.places[blockIdx.x + 1], 0), sequences) : sequences;
     return c;
 }
 
-// Calls body(s, tokens of s, from, to, lane) with a group of LANES lanes for every
-// sequence of the chunk; from and to count from the chunk's first token.
-template <int LANES, class F>
-__device__ __forceinline__ void by_sequence(const Loss& l, const Chunk& c, F&& body) {
-    for (int s = c.s0 + (int)threadIdx.x / LANES; s < c.s1; s += kThreads / LANES) {
-        const Range r = range_of(l, s);
-        body(s, r, max(r.from, c.from) - c.from, min(r.to, c.to) - c.from, (int)threadIdx.x % LANES);
+// The chunk's sequences that have tokens there, in order.  `from` and `to` count
+// from the chunk's first token; kOn marks one that came in or goes on.
+constexpr uint32_t kOn = 0x8000, kPlace = 0x7fff;
+struct List {
+    int32_t seq[kChunk];
+    uint16_t from[kChunk], to[kChunk];
+    int32_t waves[2][kThreads / 64];
+};
+
+__device__ __forceinline__ int list_sequences(const Loss& l, const Chunk& c, List& list) {
+    int count = 0, turn = 0;
+    for (int base = c.s0; base < c.s1; base += kThreads, turn ^= 1) {
+        const int s = base + (int)threadIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        Range r{0, 0};
+        if (s < c.s1) r = range_of(l, s);
+        const int from = max(r.from, c.from), to = min(r.to, c.to);
+        const uint64_t there = __ballot(from < to);
+        if (lane == 0) list.waves[turn][wave] = __popcll(there);
+        __syncthreads();
+        int at = count + __popcll(there & ((1ull << lane) - 1));
+#pragma unroll
+        for (int w = 0; w < kThreads / 64; ++w) {
+            const int n = list.waves[turn][w];
+            if (w < wave) at += n;
+            count += n;
+        }
+        if (from < to && at < kChunk) {   // offsets that fall could name more
+            list.seq[at] = s;
+            list.from[at] = (uint16_t)((from - c.from) | (r.from < c.from ? kOn : 0));
+            list.to[at] = (uint16_t)((to - c.from) | (r.to > c.to ? kOn : 0));
+        }
     }
+    __syncthreads();
+    return min(count, kChunk);
 }
 
-// The sequence of each token of the chunk (-1: none), into LDS.
-__device__ __forceinline__ void find_sequences(const Loss& l, const Chunk& c, int32_t* of) {
-    for (int i = threadIdx.x; i < kChunk; i += kThreads) of[i] = -1;
-    __syncthreads();
-    auto fill = [&](auto lanes) {
+// Calls body(i, lane) with a group of lanes for every sequence of the list, more
+// lanes where there are fewer (and longer) ones.
+constexpr int kLong = 8;
+template <class F>
+__device__ __forceinline__ void by_sequence(int count, F&& body) {
+    auto go = [&](auto lanes) {
         constexpr int kLanes = decltype(lanes)::value;
-        by_sequence<kLanes>(l, c, [&](int s, Range, int from, int to, int lane) {
-            for (int t = from + lane; t < to; t += kLanes) of[t] = s;
-        });
+        for (int i = (int)threadIdx.x / kLanes; i < count; i += kThreads / kLanes) body(i, (int)threadIdx.x % kLanes, lanes);
     };
-    const int count = c.s1 - c.s0;
-    if (count <= 8) fill(std::integral_constant<int, 64>());
-    else if (count <= 128) fill(std::integral_constant<int, 16>());
-    else fill(std::integral_constant<int, 2>());
-    __syncthreads();
+    if (count <= kLong) go(std::integral_constant<int, 64>());
+    else if (count <= 128) go(std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 2>());
 }
 
-// Adds up what the chunk's tokens left in LDS and hands every sequence's sum on.
-template <class Read>
-__device__ __forceinline__ void sum_sequences(const Loss& l, const Chunk& c, Read&& read) {
-    auto add = [&](auto lanes) {
-        constexpr int kLanes = decltype(lanes)::value;
-        by_sequence<kLanes>(l, c, [&](int s, Range r, int from, int to, int lane) {
+// The places in the list of the sequences of a thread's tokens (kOn: none).
+__device__ __forceinline__ void find_sequences(const List& list, int count, uint16_t* scratch, uint32_t (&of)[kEach]) {
+    if (count <= kLong) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) of[i] = kOn;
+        for (int s = 0; s < count; ++s) {
+            const int from = list.from[s] & kPlace, to = list.to[s] & kPlace;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int t = (int)threadIdx.x + i * kThreads;
+                if (t >= from && t < to) of[i] = s;
+            }
+        }
+        return;
+    }
+    for (int i = threadIdx.x; i < kChunk; i += kThreads) scratch[i] = kOn;
+    __syncthreads();
+    by_sequence(count, [&](int i, int lane, auto lanes) {
+        const int to = list.to[i] & kPlace;
+        for (int t = (list.from[i] & kPlace) + lane; t < to; t += decltype(lanes)::value) scratch[t] = (uint16_t)i;
+    });
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) of[i] = scratch[threadIdx.x + i * kThreads];
+}
+
+// Adds up the sequences' tokens and hands every sum on.  A thread has the tokens
+// threadIdx.x + i kThreads, of the sequences of[] in the list, with terms term[].
+// Few sequences (long ones) are added up from the registers, a sequence after the
+// other by all waves; many one field after the other through LDS, so that it
+// leaves room for more work-groups.  SUMS: doubles that are wanted, 0 to 2.
+template <int SUMS>
+__device__ __forceinline__ void sum_sequences(const Loss& l, const List& list, int count, Sums (&held)[kThreads / 64][kLong],
+                                              double* scratch, const uint32_t (&of)[kEach], const Sums (&term)[kEach]) {
+    auto place = [&](int i) -> Sums& {
+        if (list.from[i] & kOn) return l.parts[2 * blockIdx.x];
+        if (list.to[i] & kOn) return l.parts[2 * blockIdx.x + 1];
+        return l.whole[list.seq[i]];
+    };
+    if (count <= kLong) {
+        for (int s = 0; s < count; ++s) {
             Sums sum{0.0, 0.0, 0, 0};
-            for (int t = from + lane; t < to; t += kLanes) sum = sum + read(t);
-            sum = lanes_sum<kLanes>(sum);
-            if (lane || from >= to) return;
-            if (r.from < c.from) l.parts[2 * blockIdx.x] = sum;
-            else if (r.to > c.to) l.parts[2 * blockIdx.x + 1] = sum;
-            else l.whole[s] = sum;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (of[i] == (uint32_t)s) sum = sum + term[i];
+            const uint32_t counts = edb::lanes::sum<64>((uint32_t)sum.live | (uint32_t)sum.clipped << 16);
+            if (SUMS > 0) sum.a = edb::lanes::sum<64>(sum.a);
+            if (SUMS > 1) sum.b = edb::lanes::sum<64>(sum.b);
+            sum.live = (int)(counts & 0xffff);
+            sum.clipped = (int)(counts >> 16);
+            if ((threadIdx.x & 63) == 0) held[threadIdx.x >> 6][s] = sum;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < count) {
+            Sums sum = held[0][threadIdx.x];
+#pragma unroll
+            for (int w = 1; w < kThreads / 64; ++w) sum = sum + held[w][threadIdx.x];
+            place(threadIdx.x) = sum;
+        }
+        return;
+    }
+    auto field = [&](auto get, auto put) {
+        typedef decltype(get(term[0])) V;
+        V* values = reinterpret_cast<V*>(scratch);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) values[i * kThreads + threadIdx.x] = get(term[i]);
+        __syncthreads();
+        by_sequence(count, [&](int i, int lane, auto lanes) {
+            constexpr int kLanes = decltype(lanes)::value;
+            const int to = list.to[i] & kPlace;
+            V sum = 0;
+            for (int t = (list.from[i] & kPlace) + lane; t < to; t += kLanes) sum += values[t];
+            sum = edb::lanes::sum<kLanes>(sum);
+            if (lane == 0) put(place(i), sum);
         });
     };
-    const int count = c.s1 - c.s0;
-    if (count <= 8) add(std::integral_constant<int, 64>());
-    else if (count <= 128) add(std::integral_constant<int, 16>());
-    else add(std::integral_constant<int, 2>());
+    if (SUMS > 0) field([](const Sums& s) { return s.a; }, [](Sums& to, double v) { to.a = v; });
+    if (SUMS > 1) field([](const Sums& s) { return s.b; }, [](Sums& to, double v) { to.b = v; });
+    field([](const Sums& s) { return (uint32_t)s.live | (uint32_t)s.clipped << 16; },
+          [](Sums& to, uint32_t v) {
+              to.live = (int)(v & 0xffff);
+              to.clipped = (int)(v >> 16);
+          });
 }
 
 // A sequence's sums over its chunks, by a wave.
-__device__ __forceinline__ Sums sequence_sum(const Loss& l, int s) {
+__device__ __forceinline__ Sums sequence_sum(const Loss& l, const Sums* parts, int s) {
     const Range r = range_of(l, s);
     Sums sum{0.0, 0.0, 0, 0};
     if (r.from >= r.to) return sum;
@@ -370,7 +437,7 @@ __device__ __forceinline__ Sums sequence_sum(const Loss& l, int s) {
     for (int c = c0 + (int)(threadIdx.x & 63); c <= c1; c += 64) {
         // the first chunk's share began there, unless the sequence begins right at its start and fills it
         const bool begins = c == c0;
-        sum = sum + l.parts[2 * c + (begins ? 1 : 0)];
+        sum = sum + parts[2 * c + (begins ? 1 : 0)];
     }
     return lanes_sum<64>(sum);
 }
@@ -383,23 +450,23 @@ __device__ __forceinline__ void load_tokens(const T* p, int64_t at, int64_t end,
 
 // Preference 1 of 3: the sequences' sums.
 __global__ __launch_bounds__(kThreads) void preference_sums(Loss l) {
-    __shared__ Held found;
-    __shared__ double ratio[kChunk];
-    __shared__ uint8_t live[kChunk];
+    __shared__ List list;
+    __shared__ Sums held[kThreads / 64][kLong];
+    __shared__ double scratch[kChunk];
     const int64_t at = (int64_t)blockIdx.x * kChunk + threadIdx.x;
     float lp[kEach], ref[kEach];
     int32_t id[kEach];
     load_tokens(l.logprob, at, l.n, 0.f, lp);
     load_tokens(l.other, at, l.n, 0.f, ref);
     load_tokens(l.ids, at, l.n, 0, id);
-    const Chunk c = chunk_of(l, 2 * l.items, found);
+    const Chunk c = chunk_of(l, 2 * l.items);
+    const int count = list_sequences(l, c, list);
+    uint32_t of[kEach];
+    find_sequences(list, count, reinterpret_cast<uint16_t*>(scratch), of);
+    Sums term[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        ratio[i * kThreads + threadIdx.x] = id[i] >= 0 ? (double)lp[i] - (double)ref[i] : 0.0;
-        live[i * kThreads + threadIdx.x] = id[i] >= 0;
-    }
-    __syncthreads();
-    sum_sequences(l, c, [&](int i) { return Sums{ratio[i], 0.0, live[i], 0}; });
+    for (int i = 0; i < kEach; ++i) term[i] = {id[i] >= 0 ? (double)lp[i] - (double)ref[i] : 0.0, 0.0, id[i] >= 0, 0};
+    sum_sequences<1>(l, list, count, held, scratch, of, term);
 }
 
 // 2 of 3: the pairs' losses, a wave each.
@@ -410,7 +477,7 @@ __global__ __launch_bounds__(kThreads) void preference_pairs(Loss l) {
     double mean[2], ratio[2], loss = 0.0, slope = 0.0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        Sums s = sequence_sum(l, 2 * item + i);
+        Sums s = sequence_sum(l, l.parts, 2 * item + i);
         if (weight == 0.0) s = {0.0, 0.0, 0, 0};
         mean[i] = l.mean && s.live ? 1.0 / s.live : 1.0;
         ratio[i] = s.a * mean[i];
@@ -427,85 +494,107 @@ __global__ __launch_bounds__(kThreads) void preference_pairs(Loss l) {
 
 // 3 of 3: the tokens' gradients.
 __global__ __launch_bounds__(kThreads) void preference_grad(Loss l) {
-    __shared__ Held found;
-    __shared__ int32_t of[kChunk];
+    __shared__ List list;
+    __shared__ float slope[kChunk];
+    __shared__ uint16_t scratch[kChunk];
     const int64_t at = (int64_t)blockIdx.x * kChunk + threadIdx.x;
     int32_t id[kEach];
     load_tokens(l.ids, at, l.n, 0, id);
-    const Chunk c = chunk_of(l, 2 * l.items, found);
-    find_sequences(l, c, of);
+    const Chunk c = chunk_of(l, 2 * l.items);
+    const int count = list_sequences(l, c, list);
+    for (int i = threadIdx.x; i < count; i += kThreads) slope[i] = (float)l.slopes[list.seq[i]];
+    uint32_t of[kEach];
+    find_sequences(list, count, scratch, of);
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int s = of[i * kThreads + threadIdx.x];
-        if (at + i * kThreads < c.to) l.grad[at + i * kThreads] = s >= 0 && id[i] >= 0 ? (float)l.slopes[s] : 0.f;
-    }
+    for (int i = 0; i < kEach; ++i)
+        if (at + i * kThreads < c.to) l.grad[at + i * kThreads] = of[i] < kOn && id[i] >= 0 ? slope[of[i] & (kChunk - 1)] : 0.f;
 }
 
 // Policy 1 of 3, for means over the tokens with an id: how many there are.
 __global__ __launch_bounds__(kThreads) void policy_counts(Loss l) {
-    __shared__ Held found;
-    __shared__ uint8_t live[kChunk];
+    __shared__ List list;
+    __shared__ Sums held[kThreads / 64][kLong];
+    __shared__ double scratch[kChunk / 2];
     const int64_t at = (int64_t)blockIdx.x * kChunk + threadIdx.x;
     int32_t id[kEach];
     load_tokens(l.ids, at, l.n, 0, id);
-    const Chunk c = chunk_of(l, l.items, found);
+    const Chunk c = chunk_of(l, l.items);
+    const int count = list_sequences(l, c, list);
+    uint32_t of[kEach];
+    find_sequences(list, count, reinterpret_cast<uint16_t*>(scratch), of);
+    Sums term[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) live[i * kThreads + threadIdx.x] = id[i] >= 0;
-    __syncthreads();
-    sum_sequences(l, c, [&](int i) { return Sums{0.0, 0.0, live[i], 0}; });
-}
-
-// The sequences' weight over their tokens, a wave each.
-__global__ __launch_bounds__(kThreads) void policy_scales(Loss l) {
-    const int s = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    if (s >= l.items) return;
-    const Range r = range_of(l, s);
-    const int live = l.ids ? sequence_sum(l, s).live : r.to - r.from;
-    const double weight = l.weight ? (double)l.weight[s] : 1.0;
-    if ((threadIdx.x & 63) == 0) l.slopes[s] = l.mean && live ? weight / live : weight;
+    for (int i = 0; i < kEach; ++i) term[i] = {0.0, 0.0, id[i] >= 0, 0};
+    sum_sequences<0>(l, list, count, held, scratch, of, term);
 }
 
 // 2 of 3: the tokens' terms and gradients, and the sequences' sums.
 __global__ __launch_bounds__(kThreads) void policy_terms(Loss l) {
-    __shared__ Held found;
-    __shared__ int32_t of[kChunk];
-    __shared__ double gain[kChunk], kl[kChunk];
-    __shared__ uint8_t flags[kChunk];
+    __shared__ List list;
+    __shared__ Sums held[kThreads / 64][kLong];
+    __shared__ double scratch[kChunk];     // a sequence's weight over its tokens, then the tokens' terms
+    __shared__ float advantages[kChunk];
     const int64_t at = (int64_t)blockIdx.x * kChunk + threadIdx.x;
-    float lp[kEach], old[kEach], ref[kEach];
+    float lp[kEach], old[kEach], ref[kEach], each[kEach];
     int32_t id[kEach];
     load_tokens(l.logprob, at, l.n, 0.f, lp);
     load_tokens(l.other, at, l.n, 0.f, old);
     load_tokens(l.reference, at, l.n, 0.f, ref);
     load_tokens(l.ids, at, l.n, 0, id);
-    const Chunk c = chunk_of(l, l.items, found);
-    find_sequences(l, c, of);
+    load_tokens(l.per_token ? l.advantage : nullptr, at, l.n, 0.f, each);
+    const Chunk c = chunk_of(l, l.items);
+    const int count = list_sequences(l, c, list);
+    // means: those of sequences that lie here from their counts, the (two at most) others' by a wave
+    const bool counted = l.mean && l.ids;
+    for (int i = threadIdx.x; i < count; i += kThreads) {
+        const int s = list.seq[i];
+        const double weight = l.weight ? (double)l.weight[s] : 1.0;
+        int live = 1;
+        if (counted) live = (list.from[i] | list.to[i]) & kOn ? 0 : l.whole[s].live;
+        else if (l.mean) {
+            const Range r = range_of(l, s);
+            live = r.to - r.from;
+        }
+        scratch[i] = live ? weight / live : weight;
+        advantages[i] = l.per_token ? 0.f : l.advantage[s];
+    }
+    if (counted) {
+        __syncthreads();
+        const int w = threadIdx.x >> 6, i = w ? count - 1 : 0;
+        if (w < 2 && count > w && ((list.from[i] | list.to[i]) & kOn)) {
+            const int live = sequence_sum(l, l.counts, list.seq[i]).live;
+            if ((threadIdx.x & 63) == 0 && live) scratch[i] /= live;
+        }
+    }
+    __shared__ uint16_t places[kChunk];
+    uint32_t of[kEach];
+    find_sequences(list, count, places, of);
+    __syncthreads();
+    double scale[kEach], a[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        const int j = i * kThreads + threadIdx.x, s = of[j];
-        const int64_t t = at + i * kThreads;
-        Token k{0.0, 0.0, 0.0, false};
-        double scale = 0.0;
-        bool live = false;
-        if (t < c.to && s >= 0 && id[i] >= 0) {
-            scale = l.slopes[s];
-            live = scale != 0.0;
-            if (live) k = policy(l, lp[i], old[i], ref[i], l.advantage[l.per_token ? t : s]);
-        }
-        gain[j] = k.gain;
-        kl[j] = k.kl;
-        flags[j] = (live ? 1 : 0) | (k.clipped ? 2 : 0);
-        if (t < c.to) l.grad[t] = live ? (float)(k.slope * scale) : 0.f;
+        const uint32_t s = of[i];
+        scale[i] = s < kOn && id[i] >= 0 ? scratch[s & (kChunk - 1)] : 0.0;
+        a[i] = l.per_token ? each[i] : advantages[s & (kChunk - 1)];
     }
-    __syncthreads();
-    sum_sequences(l, c, [&](int i) { return Sums{gain[i], kl[i], flags[i] & 1, flags[i] >> 1}; });
+    Sums term[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t t = at + i * kThreads;
+        const bool live = scale[i] != 0.0;
+        const Token k = policy(l, lp[i], old[i], ref[i], a[i]);
+        term[i] = {live ? k.gain : 0.0, live ? k.kl : 0.0, live, live && k.clipped};
+        if (t < c.to) l.grad[t] = live ? (float)(k.slope * scale[i]) : 0.f;
+    }
+    sum_sequences<2>(l, list, count, held, scratch, of, term);
 }
 
 // 3 of 3: the sequences' losses, a wave each.
 __global__ __launch_bounds__(kThreads) void policy_losses(Loss l) {
     const int s = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
     if (s >= l.items) return;
-    const Sums sum = sequence_sum(l, s);
+    const Sums sum = sequence_sum(l, l.parts, s);
     if (threadIdx.x & 63) return;
     const double mean = l.mean && sum.live ? 1.0 / sum.live : 1.0;
     l.loss[s] = (float)(policy_loss(l, sum.a, sum.b) * mean);
@@ -518,15 +607,16 @@ constexpr int32_t kMostItems = 1 << 24;
 
 struct Plan {
     int32_t chunks;          // 0: one launch
-    int64_t whole, slopes, bytes;
+    int64_t places, whole, rest, bytes;      // rest: the pairs' slopes or the chunks' counts
 };
-Plan plan_of(int32_t n, int32_t sequences) {
+Plan plan_of(int32_t n, int32_t sequences, bool pairs) {
     Plan p{};
     if (n <= kFew) return p;
     p.chunks = (int32_t)(((int64_t)n + kChunk - 1) / kChunk);
-    p.whole = (int64_t)p.chunks * 2 * sizeof(Sums);
-    p.slopes = p.whole + (int64_t)sequences * sizeof(Sums);
-    p.bytes = p.slopes + (int64_t)sequences * 8;
+    p.places = (int64_t)p.chunks * 2 * sizeof(Sums);
+    p.whole = p.places + ((int64_t)p.chunks * 4 + 15) / 16 * 16;
+    p.rest = p.whole + (int64_t)sequences * sizeof(Sums);
+    p.bytes = p.rest + (pairs ? (int64_t)sequences * 8 : (int64_t)p.chunks * 2 * sizeof(Sums));
     return p;
 }
 
@@ -561,7 +651,7 @@ extern "C" edb_status edb_preference_loss_bytes(int32_t n, int32_t pairs, int64_
     return edb::guarded([&]() -> edb_status {
         if (!bytes) return fail(EDB_ERR_INVALID, "edb_preference_loss_bytes: NULL argument");
         if (edb_status st = check_items("edb_preference_loss_bytes", n, pairs, "pairs")) return st;
-        *bytes = plan_of(n, 2 * pairs).bytes;
+        *bytes = plan_of(n, 2 * pairs, true).bytes;
         edb::clear_error();
         return EDB_OK;
     });
@@ -581,7 +671,7 @@ extern "C" edb_status edb_preference_loss(const float* logprob, const float* ref
             return fail(EDB_ERR_INVALID, "edb_preference_loss: smoothing must be in [0, 1], and 0 but for the logistic loss");
         if ((n && (!logprob || !g_logprob)) || (pairs && (!first || !loss || !reward)))
             return fail(EDB_ERR_INVALID, "edb_preference_loss: NULL argument");
-        const Plan p = plan_of(n, 2 * pairs);
+        const Plan p = plan_of(n, 2 * pairs, true);
         if (workspace_bytes < p.bytes || (p.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
             return fail(EDB_ERR_INVALID, "edb_preference_loss: a 16-byte aligned workspace of " + std::to_string(p.bytes) +
                                              " bytes is needed");
@@ -622,8 +712,10 @@ extern "C" edb_status edb_preference_loss(const float* logprob, const float* ref
         } else {
             char* ws = static_cast<char*>(workspace);
             l.parts = reinterpret_cast<Sums*>(ws);
+            l.places = reinterpret_cast<int32_t*>(ws + p.places);
             l.whole = reinterpret_cast<Sums*>(ws + p.whole);
-            l.slopes = reinterpret_cast<double*>(ws + p.slopes);
+            place_chunks<<<groups(2 * (int64_t)pairs + 1, kThreads), kThreads, 0, st>>>(l, 2 * pairs);
+            l.slopes = reinterpret_cast<double*>(ws + p.rest);
             preference_sums<<<p.chunks, kThreads, 0, st>>>(l);
             preference_pairs<<<groups(pairs, kThreads / 64), kThreads, 0, st>>>(l);
             preference_grad<<<p.chunks, kThreads, 0, st>>>(l);
@@ -636,7 +728,7 @@ extern "C" edb_status edb_policy_loss_bytes(int32_t n, int32_t sequences, int64_
     return edb::guarded([&]() -> edb_status {
         if (!bytes) return fail(EDB_ERR_INVALID, "edb_policy_loss_bytes: NULL argument");
         if (edb_status st = check_items("edb_policy_loss_bytes", n, sequences, "sequences")) return st;
-        *bytes = plan_of(n, sequences).bytes;
+        *bytes = plan_of(n, sequences, false).bytes;
         edb::clear_error();
         return EDB_OK;
     });
@@ -657,7 +749,7 @@ extern "C" edb_status edb_policy_loss(const float* logprob, const float* old_log
         if ((n && (!logprob || !old_logprob || !g_logprob)) || (sequences && (!first || !loss || !divergence || !clipped)) ||
             ((per_token ? n : sequences) && !advantage))
             return fail(EDB_ERR_INVALID, "edb_policy_loss: NULL argument");
-        const Plan p = plan_of(n, sequences);
+        const Plan p = plan_of(n, sequences, false);
         if (workspace_bytes < p.bytes || (p.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
             return fail(EDB_ERR_INVALID, "edb_policy_loss: a 16-byte aligned workspace of " + std::to_string(p.bytes) +
                                              " bytes is needed");
@@ -704,11 +796,13 @@ extern "C" edb_status edb_policy_loss(const float* logprob, const float* old_log
             else policy_kernel<1024><<<sequences, 1024, 0, st>>>(l);
         } else {
             char* ws = static_cast<char*>(workspace);
-            l.parts = reinterpret_cast<Sums*>(ws);
+            l.parts = reinterpret_cast<Sums*>(ws + p.rest);
+            l.counts = l.parts;
+            l.places = reinterpret_cast<int32_t*>(ws + p.places);
+            place_chunks<<<groups((int64_t)sequences + 1, kThreads), kThreads, 0, st>>>(l, sequences);
             l.whole = reinterpret_cast<Sums*>(ws + p.whole);
-            l.slopes = reinterpret_cast<double*>(ws + p.slopes);
             if (l.mean && ids) policy_counts<<<p.chunks, kThreads, 0, st>>>(l);
-            policy_scales<<<groups(sequences, kThreads / 64), kThreads, 0, st>>>(l);
+            l.parts = reinterpret_cast<Sums*>(ws);
             policy_terms<<<p.chunks, kThreads, 0, st>>>(l);
             policy_losses<<<groups(sequences, kThreads / 64), kThreads, 0, st>>>(l);
         }
