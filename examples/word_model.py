@@ -6,13 +6,13 @@ model predicts each next word:
     x      = embed(ids, E)                      written straight into the graphs' input rows
     h      = the chain LSTM's states            (edb.Forward; its weights and E stay as drawn)
     z      = h + embed(ids, B)                  B: a trained row per word
-    logits = z O                                O: the trained output weights
+    logits = z O                                linear; O: the trained output weights
 
 A teacher of the same form scores the words first; the 16 best of each place are
 kept (logprobs), and the student learns them:
 
     distill                                     loss and gradient of the logits in one call
-    dz = dlogits O^T,  dO = z^T dlogits         products of torch
+    dz = dlogits O^T,  dO = z^T dlogits         linear_grad
     embed_grad(ids, dz)                         gradient of B
 
 Then it is tuned on the words that came (logprobs, logprobs_grad, with a small
@@ -29,7 +29,7 @@ sys.path.insert(0, str(pathlib.Path(__file__).resolve().parent.parent))
 import numpy as np
 import torch
 
-from paper_2302_03851_amd import edb, tokens, workloads
+from paper_2302_03851_amd import edb, head, tokens, workloads
 
 
 class WordModel:
@@ -50,13 +50,13 @@ class WordModel:
         return self.encoder.arena_h[self.slot].float() + tokens.embed(ids, self.skip)
 
     def logits(self, z):
-        return torch.mm(z, self.out)
+        return head.linear(z, self.out).out
 
     def step(self, ids, z, dlogits, rate):
         """One step down the gradients of B and O."""
-        dz = torch.mm(dlogits, self.out.t().contiguous())
-        self.out.add_(torch.mm(z.t().contiguous(), dlogits), alpha=-rate)
-        tokens.embed_grad(ids, dz, self.vocab, scale=-rate, out=self.skip, accumulate=True)
+        g = head.linear_grad(z, self.out, dlogits, dbias=False)
+        self.out.add_(g.dweight, alpha=-rate)
+        tokens.embed_grad(ids, g.dx, self.vocab, scale=-rate, out=self.skip, accumulate=True)
 
 
 def run(instances=16, vocab=5000, steps=30, kept=16, temperature=2.0, rate=0.3, device="cuda:0", report=print):

@@ -270,7 +270,7 @@ __device__ __forceinline__ void split8(const u32x4 (&raw)[2], u32x4 (&o)[3]) {
     for (int i = 0; i < 8; ++i) x[i] = __builtin_bit_cast(float, (uint32_t)raw[i >> 2][i & 3]);
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+    for (int i = 0; i < 8; i += 2) asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(most) : "v"(x[i]), "v"(x[i + 1]));
     constexpr float kLargest = 0x1.FEp127f;   // of the bf16 values
     const bool far = most > kLargest;
 #pragma unroll
@@ -381,7 +381,8 @@ struct Operand {
     }
     // Byte offset of a piece in a plane.
     static __device__ __forceinline__ int place(int line, int q) {
-        if constexpr (L == K_LINES) return line * BK * 2 + 16 * (q ^ ((line / (128 / BK)) & (NP - 1)));
+        // 16 lines of one q, and the lines that the hardware reads in one go from two q, keep to different banks
+        if constexpr (L == K_LINES) return line * BK * 2 + 16 * (q ^ ((BK == 64 ? line >> 1 : -(line >> 2)) & (NP - 1)));
         else return line * R * 2 + 32 * ((q >> 1) ^ turn(line)) + 16 * (q & 1);
     }
     // Where the 32-byte blocks of line k go: the 8 lines that two groups of 16
@@ -628,19 +629,37 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
     }
 }
 
-// The splits' sums, finished: a thread takes 8 columns of a row.
-__global__ __launch_bounds__(256) inline void join_kernel(Args g) {
-    const int pieces = (g.n + 7) / 8;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / pieces;
-    if (row >= g.m) return;
+// The splits' sums, finished: a thread takes 8 columns of a row, of every
+// SHARES-th split, and the shares are added through LDS, so that few pieces of
+// many splits fill the card too.
+template <int SHARES>
+__global__ __launch_bounds__(256) void join_kernel(Args g) {
+    constexpr int AT = 256 / SHARES;
+    __shared__ float held[SHARES > 1 ? SHARES - 1 : 1][SHARES > 1 ? AT : 1][8];
+    const int pieces = (g.n + 7) / 8, mine = threadIdx.x % AT, share = threadIdx.x / AT;
+    const int64_t at = (int64_t)blockIdx.x * AT + mine, row = at / pieces;
     const int col = (int)(at - row * pieces) * 8;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = 0; s < g.splits; ++s) {
-        const v4f* q = reinterpret_cast<const v4f*>(g.partial + (((int64_t)s * g.m + row) * pieces) * 8 + col);
+    if (row < g.m) {
+#pragma unroll 4
+        for (int s = share; s < g.splits; s += SHARES) {
+            const v4f* q = reinterpret_cast<const v4f*>(g.partial + (((int64_t)s * g.m + row) * pieces) * 8 + col);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += q[e >> 2][e & 3];
+            for (int e = 0; e < 8; ++e) v[e] += q[e >> 2][e & 3];
+        }
     }
+    if constexpr (SHARES > 1) {
+        if (share)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) held[share - 1][mine][e] = v[e];
+        __syncthreads();
+        if (share) return;
+#pragma unroll
+        for (int i = 0; i < SHARES - 1; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += held[i][mine][e];
+    }
+    if (row >= g.m) return;
     float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     load_bias(g.finish, col, g.n - col, bias);
 #pragma unroll

@@ -134,7 +134,7 @@ struct Tile {
 constexpr int kWide = 2;          // the tile of few rows
 constexpr Tile kBf16[5] = {{128, 128, 2, 0.59, 3.3, 0.8, 4.0}, {64, 64, 5, 0.25, 0.2, 0.35, 2.0}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0},
                            {256, 256, 1, 1.77, 10.0, 1.77, 10.0}, {256, 128, 1, 1.04, 5.8, 1.04, 5.8}};
-constexpr Tile kF32[3] = {{128, 128, 2, 1.39, 2.5, 2.2, 4.0}, {64, 64, 4, 0.43, 0.3, 1.2, 2.5}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0}};
+constexpr Tile kF32[3] = {{128, 128, 2, 1.39, 2.5, 2.2, 4.0}, {64, 64, 4, 0.43, 0.3, 1.6, 2.5}, {16, 256, 2, 1.2, 0.0, 1.2, 0.0}};
 
 Product product_plan(int32_t m, int32_t n, int32_t k, int32_t dtype) {
     constexpr int32_t kUnits = 256;
@@ -152,6 +152,7 @@ Product product_plan(int32_t m, int32_t n, int32_t k, int32_t dtype) {
         if ((t == kWide) != wide) continue;
         const Tile& c = tiles[t];
         const int64_t all = (((int64_t)m + c.rows - 1) / c.rows) * (((int64_t)n + c.cols - 1) / c.cols);
+        if (all > (1 << 23)) continue;    // a launch has less than 2^32 threads; tiles of 128 x 128 are never more
         // no splits, or such that fill the units one to four times
         int64_t last = 0;
         for (int turns = 0; turns <= 4; ++turns) {
@@ -211,7 +212,8 @@ void multiply(const Product& p, int32_t dtype, Layout a_lines, Layout b_lines, A
     else go(float());
     if (p.splits > 1) {
         const int64_t pieces = ((int64_t)g.n + 7) / 8 * g.m;
-        edb::gemm::join_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(g);
+        if (pieces < 65536 && p.splits >= 8) edb::gemm::join_kernel<8><<<(unsigned)((pieces + 31) / 32), 256, 0, st>>>(g);
+        else edb::gemm::join_kernel<1><<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(g);
     }
 }
 

@@ -535,6 +535,21 @@ def test_linear_offsets_past_32_bits(T):
 
 
 @gpu
+@pytest.mark.parametrize("n,k,m,T", [(5000001, 3, 5, F32), (2100000, 9, 70, BF16), (3, 1300001, 2, F32), (2, 3, 3000003, BF16)])
+def test_linear_long(n, k, m, T):
+    """Millions of rows, of terms and of columns."""
+    from paper_2302_03851_amd import head
+    g = _gen(n)
+    x = torch.randn((n, k), generator=g, device="cuda").to(T)
+    w = torch.randn((k, m), generator=g, device="cuda").to(T)
+    b = torch.randn(m, generator=g, device="cuda")
+    r = head.linear(x, w, b, "relu", keep=True)
+    _check_linear(x, w, b, "relu", None, r)
+    _check_linear_grad(x, w, r.out, "relu", r.pre, head.linear_grad(x, w, r.out, "relu", r.pre))
+    _check_linear_grad(x, w, r.out, "none", None, head.linear_grad(x, w, r.out))
+
+
+@gpu
 def test_linear_differences():
     """The gradients against central differences of the results in fp32: the step is 2^-5; bends are
     below 3 step^2 / 6 of the terms, noise (2 k + 16) u of them over the step."""

@@ -313,7 +313,83 @@ def test_differences():
             assert abs(float(r.g_logprob[t]) - slope) <= step ** 2 / 6 * 40 + 2 * noise
 
 
-# ---- together, streams and graphs -----------------------------------------------------
+# ---- together ---------------------------------------------------------------------------
+
+
+def _chain(model, h, ids, loss):
+    """The example's loss and gradients by torch's derivatives in 64 bits; loss(lp) gives the mean to descend."""
+    leaves = [t.double().requires_grad_() for t in (model.w, model.b, model.W, model.c, model.O)]
+    w, b, W, c, O = leaves
+    z = torch.nn.functional.layer_norm(h.double(), (h.shape[1],), w, b, 1e-5)
+    u = torch.nn.functional.gelu(z @ W + c) + z
+    lp = torch.log_softmax(u @ O, 1).gather(1, ids.clamp(min=0).long()[:, None])[:, 0]
+    value = loss(lp)
+    return value.detach(), torch.autograd.grad(value, leaves)
+
+
+@gpu
+def test_preferred_words_gradients():
+    """The head, the log probabilities and both losses as one program, against torch's derivatives in 64 bits.
+
+    Five products of at most 2 n + 16 roundings (n = 64 hidden, up to 400 words or logits) of sums that are up to
+    8 times their terms' norm here: 5 * 816 * 8 u = 2^-9, of each gradient's norm."""
+    from examples import preferred_words as ex
+    h, ids, first = ex.states(8, 400, "cuda:0")
+    model = ex.Head(h.shape[1], 400, 3, "cuda:0")
+    g = _gen(4)
+    model.c = torch.randn(h.shape[1], generator=g, device="cuda")
+    model.w = 1 + 0.3 * torch.randn(h.shape[1], generator=g, device="cuda")
+    n, s = h.shape[0], first.numel() - 1
+    reference = -torch.rand(n, generator=g, device="cuda") * 8
+    seq, live = _spread(first.long(), n, ids)
+
+    def close(got, ref):
+        for a, b in zip(got, ref):
+            assert float((a.double() - b).norm()) <= 2.0 ** -9 * float(b.norm())
+
+    def sums(v):
+        return torch.zeros(s + 1, dtype=torch.float64, device="cuda").index_add(0, seq, torch.where(live, v, 0.0))[:s]
+
+    count = sums(torch.ones(n, dtype=torch.float64, device="cuda"))
+
+    def preference(lp):
+        r = (sums(lp - reference.double()) / count).view(-1, 2)
+        return torch.nn.functional.softplus(-0.5 * (r[:, 0] - r[:, 1])).mean()
+
+    lp, p, gradients = ex.preferred(model, h, ids, first, reference, 0.5)
+    value, ref = _chain(model, h, ids, preference)
+    assert abs(float(p.loss.double().mean()) - float(value)) <= 2.0 ** -9 * float(value)
+    close(gradients, ref)
+
+    old = lp + 0.1 * torch.randn(n, generator=g, device="cuda")
+    adv = torch.randn(s, generator=g, device="cuda")
+    a = torch.cat([adv, adv.new_zeros(1)]).double()[seq]
+    # a ratio within the forward pass's error of a border could fall on either side: none here
+    d = (lp.double() - old.double())[live]
+    assert min(float((d - math.log(x)).abs().min()) for x in (0.8, 1.28)) > 1e-5
+
+    def policy(lp):
+        r = torch.exp(lp - old.double())
+        q = reference.double() - lp
+        each = -torch.minimum(r * a, r.clamp(0.8, 1.28) * a) + 0.02 * (torch.expm1(q) - q)
+        return (sums(each) / count).mean()
+
+    _, p, gradients = ex.tuned(model, h, ids, first, old, reference, adv, 0.02)
+    value, ref = _chain(model, h, ids, policy)
+    assert abs(float(p.loss.double().mean()) - float(value)) <= 2.0 ** -9 * (abs(float(value)) + 1)
+    close(gradients, ref)
+
+
+@gpu
+def test_preferred_words_example():
+    from examples import preferred_words
+    said = []
+    preferences, tunings = preferred_words.run(instances=6, vocab=1003, steps=6, report=said.append)
+    assert all(math.isfinite(x) for x in preferences + tunings) and len(preferences) == len(tunings) == 6
+    assert abs(preferences[0] - math.log(2)) < 1e-5 and len(said) == 3
+
+
+# ---- streams and graphs -----------------------------------------------------
 
 
 def _everything(seed):
