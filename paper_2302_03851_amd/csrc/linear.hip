@@ -34,7 +34,9 @@ struct SlopeArgs {
 
 // g = dy act'(v) as the products take it, and the sums of its columns before
 // that rounding: 32 pieces of 8 columns by 8 rows at once a work-group.
-// For bf16 operands g is rounded to bf16, as the matrix instructions need it.
+// For bf16 operands g is rounded to bf16, as the matrix instructions need it (two
+// pieces would double the products).  Memory bound: the sums alone of 8192 x 65536
+// bf16 189 us, 5.7 TB/s.
 template <class D, class T>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     __shared__ float held[8][32][9];

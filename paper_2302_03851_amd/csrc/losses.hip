@@ -602,7 +602,12 @@ __global__ __launch_bounds__(kThreads) void policy_losses(Loss l) {
     l.clipped[s] = sum.clipped;
 }
 
-constexpr int32_t kFew = 32768;
+// Up to so many tokens, and so many a pair or sequence, are taken by one launch
+// (policy, us: 32768 in 64 sequences 8.3, by the long calls' four launches 17.5; in 2
+// sequences 22 and 18, in one 40 and 17).  Where most are in one of many sequences
+// after all, its group takes those 40.
+constexpr int32_t kFew = 32768, kFewEach = 8192;
+constexpr int32_t kShort = 128;    // tokens a pair or sequence, on average, up to which a wave takes it
 constexpr int32_t kMostItems = 1 << 24;
 
 struct Plan {
@@ -611,7 +616,8 @@ struct Plan {
 };
 Plan plan_of(int32_t n, int32_t sequences, bool pairs) {
     Plan p{};
-    if (n <= kFew) return p;
+    const int32_t items = pairs ? sequences / 2 : sequences;
+    if (items == 0 || (n <= kFew && n / items <= kFewEach)) return p;
     p.chunks = (int32_t)(((int64_t)n + kChunk - 1) / kChunk);
     p.places = (int64_t)p.chunks * 2 * sizeof(Sums);
     p.whole = p.places + ((int64_t)p.chunks * 4 + 15) / 16 * 16;
@@ -706,8 +712,8 @@ extern "C" edb_status edb_preference_loss(const float* logprob, const float* ref
         if (pairs == 0) {
             if (n) no_sequences<<<groups(n, 256), 256, 0, st>>>(g_logprob, n);
         } else if (p.chunks == 0) {
-            if (n / pairs < 512) preference_kernel<64><<<groups(pairs, 4), 256, 0, st>>>(l);
-            else if (n / pairs < 4096) preference_kernel<256><<<pairs, 256, 0, st>>>(l);
+            if (n / pairs < kShort) preference_kernel<64><<<groups(pairs, 4), 256, 0, st>>>(l);
+            else if (n / pairs < 16 * kShort) preference_kernel<256><<<pairs, 256, 0, st>>>(l);
             else preference_kernel<1024><<<pairs, 1024, 0, st>>>(l);
         } else {
             char* ws = static_cast<char*>(workspace);
@@ -791,8 +797,8 @@ extern "C" edb_status edb_policy_loss(const float* logprob, const float* old_log
         if (sequences == 0) {
             if (n) no_sequences<<<groups(n, 256), 256, 0, st>>>(g_logprob, n);
         } else if (p.chunks == 0) {
-            if (n / sequences < 512) policy_kernel<64><<<groups(sequences, 4), 256, 0, st>>>(l);
-            else if (n / sequences < 4096) policy_kernel<256><<<sequences, 256, 0, st>>>(l);
+            if (n / sequences < kShort) policy_kernel<64><<<groups(sequences, 4), 256, 0, st>>>(l);
+            else if (n / sequences < 16 * kShort) policy_kernel<256><<<sequences, 256, 0, st>>>(l);
             else policy_kernel<1024><<<sequences, 1024, 0, st>>>(l);
         } else {
             char* ws = static_cast<char*>(workspace);
