@@ -8,7 +8,8 @@
 //   * fp32 as three bf16 values that add up to it to the last bit (8 + 8 + 8
 //     significant bits), 32 k a step.  Of the nine products the six largest are
 //     formed, which leaves out less than 2^-24 of a term; they take 6/16 of the
-//     time of the fp32 matrix instructions.
+//     time of the fp32 matrix instructions.  (The last piece is a multiple of
+//     2^-133, bf16's least number: factors below 2^-109 lose digits.)
 // v_mfma_f32_16x16x32_bf16 wants 8 consecutive k of one row (or column) a lane.
 // An operand whose k are contiguous in memory (K_LINES) is kept line by line and
 // read 16 bytes at a time; one whose rows (columns) are (MN_LINES) is kept as it

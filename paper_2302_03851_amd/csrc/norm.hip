@@ -597,8 +597,12 @@ void launch_norm(const NormArgs& a, hipStream_t st) {
     else if (pieces <= 512) start<T, O, K, 256, 2, 1>(a, st);
     else if (pieces <= 1024) start<T, O, K, 256, 4, 1>(a, st);
     else if (pieces <= 2048) start<T, O, K, 1024, 2, 1>(a, st);
-    else if (K == 4 && pieces <= 4096) start<T, O, 4, 1024, 4, 1>(a, st);   // 8 elements a piece: no registers for it
-    else norm_long_kernel<T, O><<<(unsigned)(a.n < 2048 ? a.n : 2048), kLong, 0, st>>>(a);
+    else {
+        if constexpr (K == 4) {   // 8 elements a piece: no registers for it
+            if (pieces <= 4096) return start<T, O, K, 1024, 4, 1>(a, st);
+        }
+        norm_long_kernel<T, O><<<(unsigned)(a.n < 2048 ? a.n : 2048), kLong, 0, st>>>(a);
+    }
 }
 
 constexpr int64_t kMostParts = 1024;

@@ -483,6 +483,23 @@ def test_linear_values(T):
 
 
 @gpu
+@pytest.mark.parametrize("scale", [1e-30, 1e-33, 1e-35, 1e-37, 1e-39])
+@pytest.mark.parametrize("T", [F32, BF16])
+def test_linear_small(T, scale):
+    """Factors down to below the normal numbers: fp32 ones are off by 2^-134 each (half of bf16's least number)."""
+    from paper_2302_03851_amd import head
+    g = _gen(11)
+    x = (torch.randn((70, 96), generator=g, device="cuda").double() * scale).to(T)
+    w = (torch.randn((96, 130), generator=g, device="cuda") * 1e4).to(T)
+    for a, b in ((x, w), (w.t().contiguous(), x.t().contiguous())):
+        v, size = torch.mm(a.double(), b.double()), torch.mm(a.double().abs(), b.double().abs())
+        tol = (2 * 96 + 16) * U * size + _half(v, F32)
+        if T == F32:
+            tol = tol + 2.0 ** -134 * (a.double().abs().sum(1, keepdim=True) + b.double().abs().sum(0, keepdim=True))
+        _close(head.linear(a, b, dtype=F32).out, v, tol)
+
+
+@gpu
 def test_linear_in_place():
     """The residual's place may take the result; columns of one buffer; nothing to do."""
     from paper_2302_03851_amd import head
