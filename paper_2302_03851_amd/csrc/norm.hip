@@ -342,6 +342,9 @@ struct GradArgs {
     int32_t n, dim;
 };
 
+// (x - mean) rstd, by halves: the difference itself could leave fp32's range.
+__device__ __forceinline__ float scaled(float x, float mean, float rstd) { return fmaf(x, 0.5f, -0.5f * mean) * (2.f * rstd); }
+
 // A work-group's rows give their gradients and, in registers, their share of
 // dw and db, which it writes once; a second launch adds up the shares.  Memory
 // bound: 262144 x 512 bf16 151 us with the second launch's 5 (5.2 TB/s), 8000 x 8192 85
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_grad_kernel(GradArgs a)
                 const int skip = Piece<K>(nominal, a.dim).skip;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    h[r][v][k] = (h[r][v][k] - mean[r]) * rstd[r];
+                    h[r][v][k] = scaled(h[r][v][k], mean[r], rstd[r]);
                     if (K > 1 && k < skip) continue;
                     const float g = d[r][v][k] * w[v][k];
                     c1 += g;
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(kLong) void norm_grad_long_kernel(GradArgs a) {
                 if (k < p.skip) continue;
                 const float g = d[k] * w[k];
                 c1 += g;
-                c2 = fmaf(g, (e[k] - mean) * rstd, c2);
+                c2 = fmaf(g, scaled(e[k], mean, rstd), c2);
             }
         }
         row_sums<kLong>(c1, c2, held[turn]);
@@ -504,7 +507,7 @@ __global__ __launch_bounds__(kLong) void norm_grad_long_kernel(GradArgs a) {
             load_k<O, K>(dout + p.col, d);
             load_weight<K>(a.weight, a.weight_bf16, p.col, 1.f, w);
 #pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = rstd * (fmaf(d[k], w[k], -c1) - (e[k] - mean) * rstd * c2);
+            for (int k = 0; k < K; ++k) e[k] = rstd * (fmaf(d[k], w[k], -c1) - scaled(e[k], mean, rstd) * c2);
             store_from<T, K>(dx + p.col, e, p.skip);
         }
     }
@@ -528,7 +531,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(GradArgs a, int rows_
         load_k<O, K>(static_cast<const O*>(a.dout) + row * a.dout_stride + p.col, d);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            dw[k] = fmaf(d[k], (e[k] - mean) * rstd, dw[k]);
+            dw[k] = fmaf(d[k], scaled(e[k], mean, rstd), dw[k]);
             db[k] += d[k];
         }
     }

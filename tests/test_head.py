@@ -151,6 +151,15 @@ def test_layer_norm_values(dim, T):
         r = head.layer_norm(x, None, None, eps, dtype=F32)
         _check_norm(x, None, None, eps, r)
         assert torch.isnan(r.out[6:9]).all() and not r.out[2].any() and not r.out[9].any()
+        if eps == 1e-5:
+            good = [0, 1, 2, 3, 4, 5, 9, 10, 11]
+            dy = torch.randn((9, dim), generator=g, device="cuda").to(T)
+            xs = x[good].contiguous()
+            xs[5, 0], xs[5, 1:] = -3.3e38, 3.3e38      # differences past fp32's range
+            st = head.layer_norm(xs).stats
+            _check_norm_grad(xs, st, dy, None, head.layer_norm_grad(xs, st, dy))
+            q = head.layer_norm_grad(x, r.stats, torch.ones_like(x))
+            assert torch.isnan(q.dx[6:9]).all() and torch.isnan(q.dweight).all() and (q.dbias == 12).all()
     assert torch.isnan(head.layer_norm(x[2:3], eps=0.0).out).all()
 
 
