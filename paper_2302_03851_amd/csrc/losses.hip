@@ -87,10 +87,13 @@ __device__ __forceinline__ double log_ratio(const Loss& l, int64_t t) {
 __device__ __forceinline__ void preference(const Loss& l, double diff, double& loss, double& slope) {
     const double y = l.beta * diff;
     if (l.kind == EDB_PREFERENCE_LOGISTIC) {
-        const double near = log1p(exp(-fabs(y))), won = (y < 0.0 ? -y : 0.0) + near, lost = (y > 0.0 ? y : 0.0) + near;
-        const double p = y > 0.0 ? exp(-y) / (1.0 + exp(-y)) : 1.0 / (1.0 + exp(y));   // of the other being preferred
-        loss = l.smoothing != 0.0 ? (1.0 - l.smoothing) * won + l.smoothing * lost : won;
-        slope = l.beta * (l.smoothing - p);
+        // a term of factor 0 is left out: the other's limit stands where it is infinite
+        const double small = exp(-fabs(y)), near = log1p(small), won = (y < 0.0 ? -y : 0.0) + near, lost = (y > 0.0 ? y : 0.0) + near;
+        const double few = small / (1.0 + small), most = 1.0 / (1.0 + small);
+        const double p = y > 0.0 ? few : most, q = y > 0.0 ? most : few;   // of the other being preferred, and of this one
+        const double e = l.smoothing;
+        loss = e == 0.0 ? won : e == 1.0 ? lost : (1.0 - e) * won + e * lost;
+        slope = l.beta * (e == 0.0 ? -p : e * q - (1.0 - e) * p);
     } else if (l.kind == EDB_PREFERENCE_HINGE) {
         loss = y < 1.0 ? 1.0 - y : y != y ? y : 0.0;
         slope = y < 1.0 ? -l.beta : y != y ? y : 0.0;

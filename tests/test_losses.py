@@ -256,6 +256,41 @@ def test_limits(n):
 
 
 @gpu
+@pytest.mark.parametrize("n", [640, 70000])
+@pytest.mark.parametrize("mean", [False, True])
+def test_smoothing_of_one(n, mean):
+    """All of the weight on the other one: the loss and its gradient of the swapped pair, the limits at infinite
+    ratios, and gradients that keep their digits where the loss is next to 0."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(n)
+    s, beta = 32, 0.5
+    first = _offsets("even", n, s, g)
+    lp = -torch.rand(n, generator=g, device="cuda")
+    ref = lp + 0.01 * torch.randn(n, generator=g, device="cuda")
+    at = first[:-1] + 1
+    lp[at[0]], lp[at[3]], ref[at[4]], ref[at[7]], lp[at[8]] = -INF, -INF, -INF, -INF, NAN
+    per = int(first[1] - first[0]) if mean else 1
+    for i, margin in ((10, -130.0), (12, 130.0), (14, -60.0), (16, -1400.0), (18, 1400.0)):
+        lp[at[i]] += margin * per
+    r = tokens.preference_loss(lp, ref, first.to(torch.int32), "logistic", beta, 1.0, mean)
+    ratio = _total(lp.double() - ref.double(), *_spread(first, n, None), s)
+    live = _total(torch.ones(n, dtype=torch.float64, device="cuda"), *_spread(first, n, None), s)
+    scale = 1 / live if mean else torch.ones_like(live)
+    y = beta * (ratio * scale).view(-1, 2).diff(dim=1)[:, 0].neg()
+    loss = torch.nn.functional.softplus(y, threshold=1e9)
+    slope = torch.stack([beta * torch.sigmoid(y), -beta * torch.sigmoid(y)], 1).view(-1) * scale
+    # y is off by 2^-40 of its terms, which the exponentials hand on relative to their own size
+    terms = beta * (_total((lp.double() - ref.double()).abs(), *_spread(first, n, None), s) * scale).view(-1, 2).sum(1)
+    _close(r.loss, loss, terms * torch.sigmoid(y).nan_to_num(0.0))
+    seq = _spread(first, n, None)[0]
+    _close(r.g_logprob, slope[seq], (slope.abs() * terms.nan_to_num(0.0, 0.0, 0.0).repeat_interleave(2))[seq])
+    # -inf: no loss; inf: all of it; NaN stays
+    assert r.loss[0] == 0 and r.loss[1] == INF and r.loss[2] == INF and r.loss[3] == 0 and torch.isnan(r.loss[4])
+    assert not r.g_logprob[first[0]:first[2]].any() and (r.g_logprob[first[2]:first[3]] > 0).all()
+    assert (r.g_logprob[first[10]:first[11]] > 0).all() and (r.g_logprob[first[14]:first[15]] > 0).all()
+
+
+@gpu
 def test_empty_calls():
     from paper_2302_03851_amd import tokens
     none, zero = torch.zeros(0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
