@@ -65,7 +65,7 @@ struct Loss {
     // long calls only
     int32_t* places;                // [chunk]
     Sums *parts, *whole;            // [chunk][2], [sequence]
-    const Sums* counts;             // policy: the parts of policy_counts
+    bool counted;                   // policy, means over the tokens with an id: whole's live come before all else
     double* slopes;                 // preference: [sequence]
 };
 
@@ -279,6 +279,7 @@ struct Chunk {
 __global__ __launch_bounds__(kThreads) void place_chunks(Loss l, int sequences) {
     const int s = blockIdx.x * kThreads + threadIdx.x;
     if (s > sequences) return;
+    if (l.counted && s < sequences) l.whole[s].live = 0;
     const int64_t from = s < sequences ? min(max(l.first[s], 0), l.n) : 0;
     const int64_t to = s == sequences ? min(max(l.first[0], 0), l.n) : s + 1 < sequences ? min(max(l.first[s + 1], 0), l.n) : l.n;
     for (int64_t c = (from + kChunk - 1) / kChunk; c * kChunk < to; ++c) l.places[c] = s < sequences ? s + 1 : 0;
@@ -378,6 +379,12 @@ __device__ __forceinline__ void find_sequences(const List& list, int count, uint
 template <int SUMS>
 __device__ __forceinline__ void sum_sequences(const Loss& l, const List& list, int count, Sums (&held)[kThreads / 64][kLong],
                                               double* scratch, const uint32_t (&of)[kEach], const Sums (&term)[kEach]) {
+    // the counts alone are whole numbers, and added up right there, in whatever order
+    auto count_to = [&](int i, int32_t live) {
+        int32_t& to = l.whole[list.seq[i]].live;
+        if ((list.from[i] | list.to[i]) & kOn) atomicAdd(&to, live);
+        else to = live;
+    };
     auto place = [&](int i) -> Sums& {
         if (list.from[i] & kOn) return l.parts[2 * blockIdx.x];
         if (list.to[i] & kOn) return l.parts[2 * blockIdx.x + 1];
@@ -401,7 +408,8 @@ __device__ __forceinline__ void sum_sequences(const Loss& l, const List& list, i
             Sums sum = held[0][threadIdx.x];
 #pragma unroll
             for (int w = 1; w < kThreads / 64; ++w) sum = sum + held[w][threadIdx.x];
-            place(threadIdx.x) = sum;
+            if (SUMS) place(threadIdx.x) = sum;
+            else count_to(threadIdx.x, sum.live);
         }
         return;
     }
@@ -418,20 +426,25 @@ __device__ __forceinline__ void sum_sequences(const Loss& l, const List& list, i
             V sum = 0;
             for (int t = (list.from[i] & kPlace) + lane; t < to; t += kLanes) sum += values[t];
             sum = edb::lanes::sum<kLanes>(sum);
-            if (lane == 0) put(place(i), sum);
+            if (lane == 0) put(i, sum);
         });
     };
-    if (SUMS > 0) field([](const Sums& s) { return s.a; }, [](Sums& to, double v) { to.a = v; });
-    if (SUMS > 1) field([](const Sums& s) { return s.b; }, [](Sums& to, double v) { to.b = v; });
+    if (SUMS > 0) field([](const Sums& s) { return s.a; }, [&](int i, double v) { place(i).a = v; });
+    if (SUMS > 1) field([](const Sums& s) { return s.b; }, [&](int i, double v) { place(i).b = v; });
     field([](const Sums& s) { return (uint32_t)s.live | (uint32_t)s.clipped << 16; },
-          [](Sums& to, uint32_t v) {
-              to.live = (int)(v & 0xffff);
-              to.clipped = (int)(v >> 16);
+          [&](int i, uint32_t v) {
+              if (SUMS) {
+                  Sums& to = place(i);
+                  to.live = (int)(v & 0xffff);
+                  to.clipped = (int)(v >> 16);
+              } else {
+                  count_to(i, (int)v);
+              }
           });
 }
 
 // A sequence's sums over its chunks, by a wave.
-__device__ __forceinline__ Sums sequence_sum(const Loss& l, const Sums* parts, int s) {
+__device__ __forceinline__ Sums sequence_sum(const Loss& l, int s) {
     const Range r = range_of(l, s);
     Sums sum{0.0, 0.0, 0, 0};
     if (r.from >= r.to) return sum;
@@ -440,7 +453,7 @@ __device__ __forceinline__ Sums sequence_sum(const Loss& l, const Sums* parts, i
     for (int c = c0 + (int)(threadIdx.x & 63); c <= c1; c += 64) {
         // the first chunk's share began there, unless the sequence begins right at its start and fills it
         const bool begins = c == c0;
-        sum = sum + parts[2 * c + (begins ? 1 : 0)];
+        sum = sum + l.parts[2 * c + (begins ? 1 : 0)];
     }
     return lanes_sum<64>(sum);
 }
@@ -480,7 +493,7 @@ __global__ __launch_bounds__(kThreads) void preference_pairs(Loss l) {
     double mean[2], ratio[2], loss = 0.0, slope = 0.0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        Sums s = sequence_sum(l, l.parts, 2 * item + i);
+        Sums s = sequence_sum(l, 2 * item + i);
         if (weight == 0.0) s = {0.0, 0.0, 0, 0};
         mean[i] = l.mean && s.live ? 1.0 / s.live : 1.0;
         ratio[i] = s.a * mean[i];
@@ -548,27 +561,17 @@ __global__ __launch_bounds__(kThreads) void policy_terms(Loss l) {
     load_tokens(l.per_token ? l.advantage : nullptr, at, l.n, 0.f, each);
     const Chunk c = chunk_of(l, l.items);
     const int count = list_sequences(l, c, list);
-    // means: those of sequences that lie here from their counts, the (two at most) others' by a wave
-    const bool counted = l.mean && l.ids;
     for (int i = threadIdx.x; i < count; i += kThreads) {
         const int s = list.seq[i];
         const double weight = l.weight ? (double)l.weight[s] : 1.0;
         int live = 1;
-        if (counted) live = (list.from[i] | list.to[i]) & kOn ? 0 : l.whole[s].live;
+        if (l.counted) live = l.whole[s].live;
         else if (l.mean) {
             const Range r = range_of(l, s);
             live = r.to - r.from;
         }
         scratch[i] = live ? weight / live : weight;
         advantages[i] = l.per_token ? 0.f : l.advantage[s];
-    }
-    if (counted) {
-        __syncthreads();
-        const int w = threadIdx.x >> 6, i = w ? count - 1 : 0;
-        if (w < 2 && count > w && ((list.from[i] | list.to[i]) & kOn)) {
-            const int live = sequence_sum(l, l.counts, list.seq[i]).live;
-            if ((threadIdx.x & 63) == 0 && live) scratch[i] /= live;
-        }
     }
     __shared__ uint16_t places[kChunk];
     uint32_t of[kEach];
@@ -597,7 +600,7 @@ __global__ __launch_bounds__(kThreads) void policy_terms(Loss l) {
 __global__ __launch_bounds__(kThreads) void policy_losses(Loss l) {
     const int s = blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
     if (s >= l.items) return;
-    const Sums sum = sequence_sum(l, l.parts, s);
+    const Sums sum = sequence_sum(l, s);
     if (threadIdx.x & 63) return;
     const double mean = l.mean && sum.live ? 1.0 / sum.live : 1.0;
     l.loss[s] = (float)(policy_loss(l, sum.a, sum.b) * mean);
@@ -615,7 +618,7 @@ constexpr int32_t kMostItems = 1 << 24;
 
 struct Plan {
     int32_t chunks;          // 0: one launch
-    int64_t places, whole, rest, bytes;      // rest: the pairs' slopes or the chunks' counts
+    int64_t places, whole, slopes, bytes;
 };
 Plan plan_of(int32_t n, int32_t sequences, bool pairs) {
     Plan p{};
@@ -624,8 +627,8 @@ Plan plan_of(int32_t n, int32_t sequences, bool pairs) {
     p.chunks = (int32_t)(((int64_t)n + kChunk - 1) / kChunk);
     p.places = (int64_t)p.chunks * 2 * sizeof(Sums);
     p.whole = p.places + ((int64_t)p.chunks * 4 + 15) / 16 * 16;
-    p.rest = p.whole + (int64_t)sequences * sizeof(Sums);
-    p.bytes = p.rest + (pairs ? (int64_t)sequences * 8 : (int64_t)p.chunks * 2 * sizeof(Sums));
+    p.slopes = p.whole + (int64_t)sequences * sizeof(Sums);
+    p.bytes = p.slopes + (pairs ? (int64_t)sequences * 8 : 0);
     return p;
 }
 
@@ -724,7 +727,7 @@ extern "C" edb_status edb_preference_loss(const float* logprob, const float* ref
             l.places = reinterpret_cast<int32_t*>(ws + p.places);
             l.whole = reinterpret_cast<Sums*>(ws + p.whole);
             place_chunks<<<groups(2 * (int64_t)pairs + 1, kThreads), kThreads, 0, st>>>(l, 2 * pairs);
-            l.slopes = reinterpret_cast<double*>(ws + p.rest);
+            l.slopes = reinterpret_cast<double*>(ws + p.slopes);
             preference_sums<<<p.chunks, kThreads, 0, st>>>(l);
             preference_pairs<<<groups(pairs, kThreads / 64), kThreads, 0, st>>>(l);
             preference_grad<<<p.chunks, kThreads, 0, st>>>(l);
@@ -805,13 +808,12 @@ extern "C" edb_status edb_policy_loss(const float* logprob, const float* old_log
             else policy_kernel<1024><<<sequences, 1024, 0, st>>>(l);
         } else {
             char* ws = static_cast<char*>(workspace);
-            l.parts = reinterpret_cast<Sums*>(ws + p.rest);
-            l.counts = l.parts;
-            l.places = reinterpret_cast<int32_t*>(ws + p.places);
-            place_chunks<<<groups((int64_t)sequences + 1, kThreads), kThreads, 0, st>>>(l, sequences);
-            l.whole = reinterpret_cast<Sums*>(ws + p.whole);
-            if (l.mean && ids) policy_counts<<<p.chunks, kThreads, 0, st>>>(l);
             l.parts = reinterpret_cast<Sums*>(ws);
+            l.places = reinterpret_cast<int32_t*>(ws + p.places);
+            l.whole = reinterpret_cast<Sums*>(ws + p.whole);
+            l.counted = l.mean && ids;
+            place_chunks<<<groups((int64_t)sequences + 1, kThreads), kThreads, 0, st>>>(l, sequences);
+            if (l.counted) policy_counts<<<p.chunks, kThreads, 0, st>>>(l);
             policy_terms<<<p.chunks, kThreads, 0, st>>>(l);
             policy_losses<<<groups(sequences, kThreads / 64), kThreads, 0, st>>>(l);
         }

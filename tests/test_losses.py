@@ -223,6 +223,47 @@ def test_long_sums():
         _check_policy(lp, lp, ref, first, torch.ones(2, device="cuda"), 0.2, 0.2, 0.1, False, mean, None, None)
 
 
+def _median_us(f, calls=5):
+    f()
+    times = []
+    for _ in range(calls):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b) * 1e3)
+    return sorted(times)[calls // 2]
+
+
+def _one_long(n):
+    """Log probabilities, old and reference ones, and ids, three of four tokens with one."""
+    lp = -torch.rand(n, generator=_gen(n), device="cuda")
+    return lp, lp + 0.1, lp - 0.1, (torch.arange(n, device="cuda") % 4 - 1).to(torch.int32)
+
+
+@gpu
+def test_long_sequence_counts():
+    """Means over the tokens with an id cost a look at the ids, however long a sequence is (where every chunk added up
+    all of its sequence's chunks, 2^26 tokens in one took six times as long as for their sum)."""
+    from paper_2302_03851_amd import tokens
+    n = 1 << 26
+    lp, old, ref, ids = _one_long(n)
+    first = torch.tensor([0, 5, n - 3, n], dtype=torch.int32, device="cuda")
+    adv = torch.tensor([1.0, 2.0, 3.0], device="cuda")
+    r = tokens.policy_loss(lp, old, first, adv, reference=ref, kl=0.1, ids=ids)
+    count = (ids[5:n - 3] >= 0).sum().double()
+    gain, q = torch.exp(lp.double() - old.double()), ref.double() - lp.double()
+    each = torch.where(ids >= 0, 0.1 * (torch.expm1(q) - q) - 2.0 * gain, 0.0)
+    _close(r.loss[1], each[5:n - 3].sum() / count, 2.0)
+    slope = torch.where(ids >= 0, -2.0 * gain - 0.1 * torch.expm1(q), 0.0)
+    _close(r.g_logprob[5:n - 3], slope[5:n - 3] / count, 2.0 / n)
+
+    def run(mean):
+        return lambda: tokens.policy_loss(lp, old, first, adv, reference=ref, kl=0.1, mean=mean, ids=ids, out=r)
+    assert _median_us(run(True)) <= 3 * _median_us(run(False))
+
+
 @gpu
 @pytest.mark.parametrize("n", [400, 70000])
 def test_limits(n):
