@@ -275,23 +275,36 @@ struct Chunk {
 // First of the launches: for every chunk, how many sequences begin up to its
 // first token.  The sequence that holds the token writes it (the one after the
 // last: for chunks before the first sequence).  A search by each work-group of
-// the other launches took 16 of policy_terms' 48 us over 4 M tokens.
+// the other launches took 16 of policy_terms' 48 us over 4 M tokens.  A long
+// sequence's chunks are the whole wave's: one thread's stores, one after the
+// other, took 1.0 ms for the 65536 chunks of 2^26 tokens.
 __global__ __launch_bounds__(kThreads) void place_chunks(Loss l, int sequences) {
     const int s = blockIdx.x * kThreads + threadIdx.x;
-    if (s > sequences) return;
+    constexpr int kOwn = 4;
     if (l.counted && s < sequences) l.whole[s].live = 0;
-    const int64_t from = s < sequences ? min(max(l.first[s], 0), l.n) : 0;
-    const int64_t to = s == sequences ? min(max(l.first[0], 0), l.n) : s + 1 < sequences ? min(max(l.first[s + 1], 0), l.n) : l.n;
-    for (int64_t c = (from + kChunk - 1) / kChunk; c * kChunk < to; ++c) l.places[c] = s < sequences ? s + 1 : 0;
+    int c0 = 0, c1 = 0;
+    if (s <= sequences) {
+        const int64_t from = s < sequences ? min(max(l.first[s], 0), l.n) : 0;
+        const int64_t to = s == sequences ? min(max(l.first[0], 0), l.n) : s + 1 < sequences ? min(max(l.first[s + 1], 0), l.n) : l.n;
+        c0 = (int)((from + kChunk - 1) / kChunk);
+        c1 = (int)((to + kChunk - 1) / kChunk);
+    }
+    const int begun = s < sequences ? s + 1 : 0;
+    if (c1 - c0 <= kOwn)
+        for (int c = c0; c < c1; ++c) l.places[c] = begun;
+    for (uint64_t left = __ballot(c1 - c0 > kOwn); left; left &= left - 1) {
+        const int lane = __ffsll((unsigned long long)left) - 1, of = __shfl(begun, lane), end = __shfl(c1, lane);
+        for (int c = __shfl(c0, lane) + (int)(threadIdx.x & 63); c < end; c += 64) l.places[c] = of;
+    }
 }
 
-__device__ __forceinline__ Chunk chunk_of(const Loss& l, int sequences) {
+__device__ __forceinline__ Chunk chunk_of(const Loss& l, int sequences, int chunk) {
     Chunk c;
-    c.from = blockIdx.x * kChunk;
+    c.from = chunk * kChunk;
     c.to = (int)min((int64_t)c.from + kChunk, (int64_t)l.n);
     // (offsets that fall may leave places unwritten: any number then)
-    c.s0 = min(max(l.places[blockIdx.x] - 1, 0), sequences);
-    c.s1 = blockIdx.x + 1 < gridDim.x ? min(max(l.places[blockIdx.x + 1], 0), sequences) : sequences;
+    c.s0 = min(max(l.places[chunk] - 1, 0), sequences);
+    c.s1 = c.to < l.n ? min(max(l.places[chunk + 1], 0), sequences) : sequences;
     return c;
 }
 
@@ -450,11 +463,17 @@ __device__ __forceinline__ Sums sequence_sum(const Loss& l, int s) {
     if (r.from >= r.to) return sum;
     const int c0 = r.from / kChunk, c1 = (r.to - 1) / kChunk;
     if (c0 == c1) return l.whole[s];
-    for (int c = c0 + (int)(threadIdx.x & 63); c <= c1; c += 64) {
-        // the first chunk's share began there, unless the sequence begins right at its start and fills it
-        const bool begins = c == c0;
-        sum = sum + l.parts[2 * c + (begins ? 1 : 0)];
+    // the first chunk's share began there, the others' came in; eight asked for at once
+    constexpr int kOnce = 8;
+    int c = c0 + (int)(threadIdx.x & 63);
+    for (; c + (kOnce - 1) * 64 <= c1; c += kOnce * 64) {
+        Sums part[kOnce];
+#pragma unroll
+        for (int i = 0; i < kOnce; ++i) part[i] = l.parts[2 * (c + i * 64) + (c + i * 64 == c0 ? 1 : 0)];
+#pragma unroll
+        for (int i = 0; i < kOnce; ++i) sum = sum + part[i];
     }
+    for (; c <= c1; c += 64) sum = sum + l.parts[2 * c + (c == c0 ? 1 : 0)];
     return lanes_sum<64>(sum);
 }
 
@@ -475,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void preference_sums(Loss l) {
     load_tokens(l.logprob, at, l.n, 0.f, lp);
     load_tokens(l.other, at, l.n, 0.f, ref);
     load_tokens(l.ids, at, l.n, 0, id);
-    const Chunk c = chunk_of(l, 2 * l.items);
+    const Chunk c = chunk_of(l, 2 * l.items, blockIdx.x);
     const int count = list_sequences(l, c, list);
     uint32_t of[kEach];
     find_sequences(list, count, reinterpret_cast<uint16_t*>(scratch), of);
@@ -516,7 +535,7 @@ __global__ __launch_bounds__(kThreads) void preference_grad(Loss l) {
     const int64_t at = (int64_t)blockIdx.x * kChunk + threadIdx.x;
     int32_t id[kEach];
     load_tokens(l.ids, at, l.n, 0, id);
-    const Chunk c = chunk_of(l, 2 * l.items);
+    const Chunk c = chunk_of(l, 2 * l.items, blockIdx.x);
     const int count = list_sequences(l, c, list);
     for (int i = threadIdx.x; i < count; i += kThreads) slope[i] = (float)l.slopes[list.seq[i]];
     uint32_t of[kEach];
@@ -527,22 +546,57 @@ __global__ __launch_bounds__(kThreads) void preference_grad(Loss l) {
         if (at + i * kThreads < c.to) l.grad[at + i * kThreads] = of[i] < kOn && id[i] >= 0 ? slope[of[i] & (kChunk - 1)] : 0.f;
 }
 
-// Policy 1 of 3, for means over the tokens with an id: how many there are.
-__global__ __launch_bounds__(kThreads) void policy_counts(Loss l) {
+// Policy 1 of 3, for means over the tokens with an id: how many there are.  A
+// work-group takes up to kCounted chunks one after the other; where one sequence
+// covers several of them, it adds to that one's number once (65536 additions to
+// one place took 0.7 ms).
+constexpr int kCounted = 32;
+__global__ __launch_bounds__(kThreads) void policy_counts(Loss l, int chunks, int each) {
     __shared__ List list;
     __shared__ Sums held[kThreads / 64][kLong];
     __shared__ double scratch[kChunk / 2];
-    const int64_t at = (int64_t)blockIdx.x * kChunk + threadIdx.x;
-    int32_t id[kEach];
-    load_tokens(l.ids, at, l.n, 0, id);
-    const Chunk c = chunk_of(l, l.items);
-    const int count = list_sequences(l, c, list);
-    uint32_t of[kEach];
-    find_sequences(list, count, reinterpret_cast<uint16_t*>(scratch), of);
-    Sums term[kEach];
+    __shared__ int32_t counts[kThreads / 64];
+    const int begin = blockIdx.x * each, end = min(begin + each, chunks);
+    int32_t mine = 0, whose = -1;     // this thread's tokens of the sequence that covers the chunks
+    auto hand_over = [&]() {
+        if (whose < 0) return;
+        const int32_t n = edb::lanes::sum<64>(mine);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = n;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            int32_t all = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) term[i] = {0.0, 0.0, id[i] >= 0, 0};
-    sum_sequences<0>(l, list, count, held, scratch, of, term);
+            for (int w = 0; w < kThreads / 64; ++w) all += counts[w];
+            atomicAdd(&l.whole[whose].live, all);
+        }
+        mine = 0;
+        whose = -1;
+    };
+    for (int chunk = begin; chunk < end; ++chunk) {
+        const int64_t at = (int64_t)chunk * kChunk + threadIdx.x;
+        int32_t id[kEach];
+        load_tokens(l.ids, at, l.n, 0, id);
+        const Chunk c = chunk_of(l, l.items, chunk);
+        __syncthreads();              // the list of the chunk before is done with
+        const int count = list_sequences(l, c, list);
+        if (count == 1 && (list.from[0] & list.to[0] & kOn)) {
+            const int seq = list.seq[0];
+            if (seq != whose) hand_over();
+            whose = seq;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) mine += id[i] >= 0;
+            continue;
+        }
+        hand_over();
+        uint32_t of[kEach];
+        find_sequences(list, count, reinterpret_cast<uint16_t*>(scratch), of);
+        Sums term[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) term[i] = {0.0, 0.0, id[i] >= 0, 0};
+        sum_sequences<0>(l, list, count, held, scratch, of, term);
+    }
+    hand_over();
 }
 
 // 2 of 3: the tokens' terms and gradients, and the sequences' sums.
@@ -559,7 +613,7 @@ __global__ __launch_bounds__(kThreads) void policy_terms(Loss l) {
     load_tokens(l.reference, at, l.n, 0.f, ref);
     load_tokens(l.ids, at, l.n, 0, id);
     load_tokens(l.per_token ? l.advantage : nullptr, at, l.n, 0.f, each);
-    const Chunk c = chunk_of(l, l.items);
+    const Chunk c = chunk_of(l, l.items, blockIdx.x);
     const int count = list_sequences(l, c, list);
     for (int i = threadIdx.x; i < count; i += kThreads) {
         const int s = list.seq[i];
@@ -813,7 +867,11 @@ extern "C" edb_status edb_policy_loss(const float* logprob, const float* old_log
             l.whole = reinterpret_cast<Sums*>(ws + p.whole);
             l.counted = l.mean && ids;
             place_chunks<<<groups((int64_t)sequences + 1, kThreads), kThreads, 0, st>>>(l, sequences);
-            if (l.counted) policy_counts<<<p.chunks, kThreads, 0, st>>>(l);
+            if (l.counted) {
+                // (2048 work-groups fill the card)
+                const int each = p.chunks >= 2048 * kCounted ? kCounted : (p.chunks + 2047) / 2048;
+                policy_counts<<<groups(p.chunks, each), kThreads, 0, st>>>(l, p.chunks, each);
+            }
             policy_terms<<<p.chunks, kThreads, 0, st>>>(l);
             policy_losses<<<groups(sequences, kThreads / 64), kThreads, 0, st>>>(l);
         }

@@ -265,6 +265,36 @@ def test_long_sequence_counts():
 
 
 @gpu
+def test_long_sequence_time():
+    """One sequence of 2^26 tokens costs about what 4096 of 2^14 do (where one thread wrote its 65536 places and one
+    wave asked for its sums one by one, six times as much)."""
+    from paper_2302_03851_amd import tokens
+    n = 1 << 26
+    lp, old, ref, ids = _one_long(n)
+
+    def times(first):
+        adv = torch.ones(first.numel() - 1, device="cuda")
+        q = tokens.preference_loss(lp, ref, first, mean=True, ids=ids)
+        r = tokens.policy_loss(lp, old, first, adv, reference=ref, kl=0.1, mean=False, ids=ids)
+        return (_median_us(lambda: tokens.preference_loss(lp, ref, first, mean=True, ids=ids, out=q)),
+                _median_us(lambda: tokens.policy_loss(lp, old, first, adv, reference=ref, kl=0.1, mean=False, ids=ids, out=r)))
+    many = times((torch.arange(4097, device="cuda") << 14).to(torch.int32))
+    one = times(torch.tensor([0, n, n], dtype=torch.int32, device="cuda"))
+    assert one[0] <= 3 * many[0] and one[1] <= 3 * many[1], (one, many)
+
+
+@gpu
+@pytest.mark.parametrize("layout,s", [("cuts", 300), ("cuts", 20000), ("gaps", 40), ("one", 6), ("short", 3000), ("even", 5000)])
+def test_many_chunks(layout, s):
+    """Enough tokens for work-groups that count several chunks: sequences that cover some of them, begin, end or lie
+    within one."""
+    n = 5 * (1 << 20) + 77
+    g, first, lp, old, ref, i = _tokens(n, s, layout, True, s)
+    _check_policy(lp, old, ref, first, torch.randn(s, generator=g, device="cuda"), 0.2, 0.28, 0.04, False, True, i, None)
+    _check_preference(lp, ref, first, "logistic", 0.1, 0.0, True, i, None)
+
+
+@gpu
 @pytest.mark.parametrize("n", [400, 70000])
 def test_limits(n):
     """Infinite log probabilities, ratios past the range, no advantage, ratios of exactly 1."""
