@@ -317,14 +317,36 @@ struct List {
     int32_t waves[2][kThreads / 64];
 };
 
+// Where more sequences than kWalk may lie here, most of them are empty: then every
+// token looks for its own by halving, and those that are their sequence's first
+// here name it (2^20 empty ones one after the other took the chunk 1.0 ms).
+constexpr int kWalk = 2 * kChunk;
 __device__ __forceinline__ int list_sequences(const Loss& l, const Chunk& c, List& list) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const bool search = c.s1 - c.s0 > kWalk;
+    int of[kEach];
+    if (search) {
+        int high[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            of[i] = c.s0;
+            high[i] = c.s1;
+        }
+        // the last that begins up to the token, all steps for all tokens (a span of 1 stays)
+        for (int span = c.s1 - c.s0; span > 1; span -= span / 2) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int middle = of[i] + (high[i] - of[i]) / 2;
+                if (l.first[middle] <= c.from + (int)threadIdx.x + i * kThreads) of[i] = middle;
+                else high[i] = middle;
+            }
+        }
+    }
     int count = 0, turn = 0;
-    for (int base = c.s0; base < c.s1; base += kThreads, turn ^= 1) {
-        const int s = base + (int)threadIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        Range r{0, 0};
-        if (s < c.s1) r = range_of(l, s);
+    auto add = [&](int s, const Range& r, bool mine) {
         const int from = max(r.from, c.from), to = min(r.to, c.to);
-        const uint64_t there = __ballot(from < to);
+        const bool listed = mine && from < to;
+        const uint64_t there = __ballot(listed);
         if (lane == 0) list.waves[turn][wave] = __popcll(there);
         __syncthreads();
         int at = count + __popcll(there & ((1ull << lane) - 1));
@@ -334,10 +356,26 @@ __device__ __forceinline__ int list_sequences(const Loss& l, const Chunk& c, Lis
             if (w < wave) at += n;
             count += n;
         }
-        if (from < to && at < kChunk) {   // offsets that fall could name more
+        if (listed && at < kChunk) {   // offsets that fall could name more
             list.seq[at] = s;
             list.from[at] = (uint16_t)((from - c.from) | (r.from < c.from ? kOn : 0));
             list.to[at] = (uint16_t)((to - c.from) | (r.to > c.to ? kOn : 0));
+        }
+        turn ^= 1;
+    };
+    if (search) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int64_t t = (int64_t)c.from + threadIdx.x + i * kThreads;
+            const Range r = range_of(l, of[i]);
+            add(of[i], r, t < c.to && t == max(r.from, c.from));
+        }
+    } else {
+        for (int base = c.s0; base < c.s1; base += kThreads) {
+            const int s = base + (int)threadIdx.x;
+            Range r{0, 0};
+            if (s < c.s1) r = range_of(l, s);
+            add(s, r, true);
         }
     }
     __syncthreads();

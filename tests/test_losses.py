@@ -295,6 +295,32 @@ def test_many_chunks(layout, s):
 
 
 @gpu
+def test_empty_sequences_time():
+    """A million empty sequences behind the last token, before the first or at one place in the middle cost a look at
+    each (where the chunk there went through all of them by itself, 4 ms for the calls that take 0.15 and 0.26)."""
+    from paper_2302_03851_amd import tokens
+    n, many = 1 << 20, 1 << 20
+    lp, old, ref, ids = _one_long(n)
+    some = (torch.arange(1025, device="cuda") << 10) - 3
+    some[0], some[-1] = 0, n
+    for at in (0, 513, 1025):
+        first = torch.cat([some[:at], some.new_full((many - 1024,), int(some[min(at, 1024)])), some[at:]])
+        assert first.numel() == many + 1
+        adv = torch.randn(many, generator=_gen(at), device="cuda")
+        _check_policy(lp, old, ref, first, adv, 0.2, 0.28, 0.04, False, True, ids, None)
+        _check_preference(lp, ref, first, "logistic", 0.1, 0.0, True, ids, None)
+        # the same tokens in as many sequences of one each
+        each = torch.arange(many + 1, device="cuda")
+        took = []
+        for f in (first.to(torch.int32), each.to(torch.int32)):
+            q = tokens.preference_loss(lp, ref, f, mean=True, ids=ids)
+            r = tokens.policy_loss(lp, old, f, adv, reference=ref, kl=0.1, ids=ids)
+            took.append((_median_us(lambda: tokens.preference_loss(lp, ref, f, mean=True, ids=ids, out=q)),
+                         _median_us(lambda: tokens.policy_loss(lp, old, f, adv, reference=ref, kl=0.1, ids=ids, out=r))))
+        assert took[0][0] <= 3 * took[1][0] and took[0][1] <= 3 * took[1][1], took
+
+
+@gpu
 @pytest.mark.parametrize("n", [400, 70000])
 def test_limits(n):
     """Infinite log probabilities, ratios past the range, no advantage, ratios of exactly 1."""
