@@ -813,8 +813,9 @@ edb_status edb_linear(const void* x, const void* weight, int32_t dtype, int32_t 
  *   dbias = sum_i g[i][:]               float[m]
  * (the residual's gradient is dout).  dx, dweight and dbias are each NULL where
  * not wanted; x is read for dweight only, weight for dx only.  For bf16 operands
- * dx and dweight are formed from g rounded to bf16.  results: the sum of the
- * EDB_LINEAR_D* that are wanted. */
+ * dx and dweight are formed from g rounded to bf16.  dbias is added up in another
+ * order with dweight than without, and may differ in its last bits then.
+ * results: the sum of the EDB_LINEAR_D* that are wanted. */
 edb_status edb_linear_grad_bytes(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t dout_dtype, int32_t act,
                                  int32_t results, int64_t* bytes);
 edb_status edb_linear_grad(const void* x, const void* weight, int32_t dtype, int32_t n, int32_t k, int32_t m,

@@ -501,11 +501,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
             b.load_edge(n0, g.n, k0, kend);
         }
     };
-    // the sums, in registers, by the work-groups of the first tiles across
+    // the sums, in registers, by the work-groups of the first tiles across; every kFold
+    // steps they go on in other registers, so that long ones are no chains of additions
+    // (262144 numbers of one sign, of the worst size: 1968 units off in one chain, 46 so)
+    constexpr int kFold = 64;
     constexpr bool SUMS = AL == MN_LINES && BL == MN_LINES;
     const int sums = SUMS && (g.sums == 1 ? n0 == 0 : m0 == 0) ? g.sums : 0;
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    auto store = [&](char* stage) {
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, folded[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto store = [&](char* stage, int step) {
         if constexpr (SUMS) {
             if (sums == 1) a.add_to(sum);
         }
@@ -514,6 +517,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
             if (sums == 2) b.add_to(sum);
         }
         b.store(stage + P * A::PLANE);
+        if constexpr (SUMS) {
+            if (sums && (step & (kFold - 1)) == kFold - 1) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    folded[i] += sum[i];
+                    sum[i] = 0.f;
+                }
+            }
+        }
     };
 
     v4f acc[FM][FN];
@@ -552,18 +564,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
     // other and the one after it is on its way into registers.
     if (steps > 0) load(0);
     if constexpr (STAGES == 2) {
-        if (steps > 0) store(lds);
+        if (steps > 0) store(lds, 0);
         if (steps > 1) load(1);
         __syncthreads();
         for (int s = 0; s < steps; ++s) {
-            if (s + 1 < steps) store(lds + (~s & 1) * S::STAGE);
+            if (s + 1 < steps) store(lds + (~s & 1) * S::STAGE, s + 1);
             if (s + 2 < steps) load(s + 2);
             compute(lds + (s & 1) * S::STAGE);
             __syncthreads();
         }
     } else {
         for (int s = 0; s < steps; ++s) {
-            store(lds);
+            store(lds, s);
             __syncthreads();
             if (s + 1 < steps) load(s + 1);
             compute(lds);
@@ -576,6 +588,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
             float* to = g.sums_out + (int64_t)split * (sums == 1 ? g.m : g.n);
             float* scratch = reinterpret_cast<float*>(lds);
             static_assert(S::LDS >= S::NT * 32, "room for the sums");
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += folded[i];
             if (sums == 1) A::sums_out(sum, scratch, to, m0, g.m);
             else B::sums_out(sum, scratch, to, n0, g.n);
             __syncthreads();

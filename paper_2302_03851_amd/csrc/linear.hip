@@ -35,8 +35,9 @@ struct SlopeArgs {
 // g = dy act'(v) as the products take it, and the sums of its columns before
 // that rounding: 32 pieces of 8 columns by 8 rows at once a work-group.
 // For bf16 operands g is rounded to bf16, as the matrix instructions need it (two
-// pieces would double the products).  Memory bound: the sums alone of 8192 x 65536
-// bf16 189 us, 5.7 TB/s.
+// pieces would double the products).  Sums over more than 64 rows of a thread's go
+// on in a second register, so that long columns are no chains of additions.
+// Memory bound: the sums alone of 8192 x 65536 bf16 189 us, 5.7 TB/s.
 template <class D, class T>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     __shared__ float held[8][32][9];
@@ -44,7 +45,8 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     const int col = (blockIdx.x * 32 + piece) * 8, left = min(a.m - col, 8);
     const int64_t gm = (a.m + 7) / 8 * 8;
     const int64_t first = (int64_t)blockIdx.y * a.rows_per, end = min(first + a.rows_per, (int64_t)a.n);
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, folded[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    int turn = 0;
     if (left > 0)
         for (int64_t row = first + line; row < end; row += 8) {
             const D* d = static_cast<const D*>(a.dout) + row * a.dout_stride + col;
@@ -63,11 +65,18 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
             edb::gemm::slope8(a.act, y, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += x[i];
+            if ((++turn & 63) == 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    folded[i] += sum[i];
+                    sum[i] = 0.f;
+                }
+            }
             if (a.g) store_k<T, 8>(static_cast<T*>(a.g) + row * gm + col, x);
         }
     if (!a.part) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) held[line][piece][i] = sum[i];
+    for (int i = 0; i < 8; ++i) held[line][piece][i] = folded[i] + sum[i];
     __syncthreads();
     const int c = threadIdx.x, to = blockIdx.x * 256 + c;
     if (to >= a.m) return;

@@ -601,6 +601,32 @@ def test_linear_differences():
             assert abs(float(got[at]) - slope) <= step ** 2 / 2 * size + (2 * k + 16) * U * size / step
 
 
+@gpu
+@pytest.mark.parametrize("n,k,m,T", [(262144, 2048, 2048, F32), (262144, 512, 1024, BF16), (300001, 40, 72, F32), (40000, 300, 20000, BF16),
+                                     (70001, 515, 4104, BF16)])
+@pytest.mark.parametrize("turned", [False, True])
+def test_linear_grad_bias_of_one_sign(n, k, m, T, turned):
+    """The bias's gradient of numbers of one sign, with the weight's and alone: column c adds up numbers whose sum loses
+    nearly half a place at every addition while it is between 2^(c % 18) and twice that.  Summed with the weight's
+    gradient, a thread adds up at most 256 pieces at a time and n / 2048 such sums, then come 32 threads and 64 parts;
+    alone, 64 rows at a time, n m / 2^28 such sums and the rest of it."""
+    from paper_2302_03851_amd import head
+    x, w = torch.zeros((n, k), device="cuda", dtype=T), torch.zeros((m, k) if turned else (k, m), device="cuda", dtype=T)
+    w = w.t() if turned else w
+    column = 1 + 0.49 * 2.0 ** (torch.arange(m, device="cuda", dtype=torch.float64) % 18 - 23)
+    if T == BF16:
+        column = 0.5 + torch.rand(m, generator=_gen(m), device="cuda")
+    dy = column.to(T).expand(n, m).contiguous()
+    if T == BF16:
+        dy *= torch.rand((n, 1), generator=_gen(n), device="cuda").to(T) + 0.5
+    ref = torch.zeros(m, dtype=torch.float64, device="cuda")
+    for part in dy.split(65536):
+        ref += part.double().sum(0)
+    for adds, got in ((n / 2048 + 360, head.linear_grad(x, w, dy).dbias), (n / 2048 + 360, head.linear_grad(x, w, dy, dx=False).dbias),
+                      (n * m / 2.0 ** 28 + 360, head.linear_grad(x, w, dy, dx=False, dweight=False).dbias)):
+        _close(got, ref, adds * U * ref + _half(ref, F32))
+
+
 # ---- streams and graphs ------------------------------------------------------------
 
 
