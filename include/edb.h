@@ -803,6 +803,12 @@ edb_status edb_linear(const void* x, const void* weight, int32_t dtype, int32_t 
                       int32_t out_dtype, int64_t out_stride, void* pre, int64_t pre_stride, void* workspace,
                       int64_t workspace_bytes, void* stream);
 
+/* How edb_linear forms a product of these sizes, for tests and profiles: tiles of
+ * rows x cols results, k in `splits` parts.  edb_linear_grad takes dx for a product
+ * of n x m by m x k, dweight for one of k x n by n x m, or of m x n by n x k where it
+ * is stored turned. */
+edb_status edb_linear_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t* rows, int32_t* cols, int32_t* splits);
+
 #define EDB_LINEAR_DX 1
 #define EDB_LINEAR_DWEIGHT 2
 #define EDB_LINEAR_DBIAS 4

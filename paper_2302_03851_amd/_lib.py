@@ -55,7 +55,7 @@ EXPORTS = [
     "edb_embed", "edb_embed_grad_bytes", "edb_embed_grad",
     "edb_logprobs_bytes", "edb_logprobs", "edb_logprobs_grad", "edb_distill_bytes", "edb_distill",
     "edb_layer_norm", "edb_layer_norm_grad_bytes", "edb_layer_norm_grad",
-    "edb_linear_bytes", "edb_linear", "edb_linear_grad_bytes", "edb_linear_grad",
+    "edb_linear_bytes", "edb_linear_plan", "edb_linear", "edb_linear_grad_bytes", "edb_linear_grad",
     "edb_preference_loss_bytes", "edb_preference_loss", "edb_policy_loss_bytes", "edb_policy_loss",
 ]
 
@@ -187,6 +187,7 @@ def load():
         "edb_layer_norm_grad": (C.c_int32, [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, vp, vp, C.c_int32, C.c_int64,
                                             vp, C.c_int32, vp, C.c_int64, vp, vp, vp, C.c_int64, vp]),
         "edb_linear_bytes": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, P(C.c_int64)]),
+        "edb_linear_plan": (C.c_int32, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, P(C.c_int32), P(C.c_int32), P(C.c_int32)]),
         "edb_linear": (C.c_int32, [vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_int32,
                                    vp, C.c_int32, C.c_int32, vp, C.c_int32, C.c_int64, vp, C.c_int32, C.c_int64, vp,
                                    C.c_int64, vp, C.c_int64, vp]),

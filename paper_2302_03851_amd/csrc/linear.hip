@@ -286,6 +286,21 @@ extern "C" edb_status edb_linear_bytes(int32_t n, int32_t k, int32_t m, int32_t 
     });
 }
 
+extern "C" edb_status edb_linear_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t* rows, int32_t* cols, int32_t* splits) {
+    return edb::guarded([&]() -> edb_status {
+        if (!rows || !cols || !splits) return fail(EDB_ERR_INVALID, "edb_linear_plan: NULL argument");
+        if (!known(dtype)) return fail(EDB_ERR_INVALID, "edb_linear_plan: dtype must be F32 or BF16");
+        if (edb_status st = check_sizes("edb_linear_plan", n, k, m)) return st;
+        const Product p = product_plan(n, m, k, dtype);
+        const Tile& t = dtype == EDB_BF16 ? kBf16[p.tile] : kF32[p.tile];
+        *rows = t.rows;
+        *cols = t.cols;
+        *splits = p.splits;
+        edb::clear_error();
+        return EDB_OK;
+    });
+}
+
 extern "C" edb_status edb_linear(const void* x, const void* weight, int32_t dtype, int32_t n, int32_t k, int32_t m,
                                  int64_t x_stride, int64_t weight_stride, int32_t turned, const void* bias,
                                  int32_t bias_dtype, int32_t act, const void* residual, int32_t residual_dtype,
