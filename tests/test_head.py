@@ -492,6 +492,45 @@ def test_linear_values(T):
 
 
 @gpu
+@pytest.mark.parametrize("T", [F32, BF16])
+@pytest.mark.parametrize("turned", [False, True])
+@pytest.mark.parametrize("n,k,m", [(40, 70, 50), (700, 33, 300), (9001, 1000, 1000)])
+def test_linear_grad_values(n, k, m, T, turned):
+    """Infinities, NaN and large numbers of dout reach the sums of their own columns only, with the weight's gradient and
+    alone, and a NaN row of x all of the weight's gradient; the product of the transposes has the same values."""
+    from paper_2302_03851_amd import head
+    g = _gen(n)
+    x, w = torch.randn((n, k), generator=g, device="cuda").to(T), torch.randn((k, m), generator=g, device="cuda").to(T)
+    wt = w.t().contiguous().t() if turned else w
+    dy = torch.randn((n, m), generator=g, device="cuda")
+    dy[3, 0], dy[n - 1, 1], dy[7, 2], dy[8, 2] = INF, -INF, INF, -INF
+    dy[n // 2, 4] = float("nan")
+    dy[:, 5] *= 1e30
+    dy[5, m - 1] = INF
+    dy = dy.to(T)
+    inner = [c for c in range(m) if c not in (0, 1, 2, 4, m - 1)]
+    for want in (dict(), dict(dx=False), dict(dx=False, dweight=False)):
+        q = head.linear_grad(x, wt, dy, **want)
+        _check_linear_grad(x, w, dy, "none", None, head.LinearGrad(None, None, q.dbias))
+        assert q.dbias[0] == INF and q.dbias[1] == -INF and torch.isnan(q.dbias[2]) and torch.isnan(q.dbias[4]) and q.dbias[m - 1] == INF
+        if q.dweight is not None:      # the other columns know nothing of it
+            _check_linear_grad(x, w[:, inner], dy[:, inner], "none", None, head.LinearGrad(None, q.dweight[:, inner], None))
+            assert not torch.isfinite(q.dweight[:, [0, 1, 2, 4, m - 1]]).any()
+    bad = x.clone()
+    bad[n // 3] = float("nan")
+    q = head.linear_grad(bad, wt, dy, dx=False)
+    assert torch.isnan(q.dweight).all()
+    _check_linear_grad(bad, w, dy, "none", None, head.LinearGrad(None, None, q.dbias))
+    # as the right operand: a column of the results each
+    s = head.linear(wt.t().contiguous(), x.t().contiguous() if turned else x.t(), dtype=F32)
+    _check_linear(w.t(), x.t(), None, "none", None, s)
+    far = x.clone()
+    far[1, 3], far[2, k - 1], far[4, 0], far[4, 1], far[6, 2] = INF, -INF, INF, -INF, float("nan")
+    s = head.linear(wt.t().contiguous(), far.t().contiguous() if turned else far.t(), dtype=F32)
+    _check_linear(w.t(), far.t(), None, "none", None, s)
+
+
+@gpu
 @pytest.mark.parametrize("scale", [1e-30, 1e-33, 1e-35, 1e-37, 1e-39])
 @pytest.mark.parametrize("T", [F32, BF16])
 def test_linear_small(T, scale):
