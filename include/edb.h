@@ -793,7 +793,9 @@ enum { EDB_ACT_NONE = 0, EDB_ACT_RELU = 1, EDB_ACT_GELU = 2, EDB_ACT_SILU = 3, E
  *   pre       [n x m] of dtype, or NULL: v, for edb_linear_grad
  * gelu is v Phi(v) with the normal distribution's Phi.  fp32 products are
  * formed from three bf16 pieces of either factor, to 2^-24 of the terms; a factor
- * below 2^-109, whose last piece is not a multiple of 2^-133, is off by 2^-134.
+ * below 2^-109, whose last piece is not a multiple of 2^-133, is off by 2^-134 (so
+ * one of 2^-134 or less counts as 0, beside an infinity too: NaN), and a term above
+ * 2^128 - 2^121 in magnitude may count as infinite.
  * k, m <= 2^24; no matrix of more than 2^23 tiles of 128 x 128.  A row of x with an
  * infinity or NaN affects its own row of results only. */
 edb_status edb_linear_bytes(int32_t n, int32_t k, int32_t m, int32_t dtype, int64_t* bytes);

@@ -9,7 +9,9 @@
 //     significant bits), 32 k a step.  Of the nine products the six largest are
 //     formed, which leaves out less than 2^-24 of a term; they take 6/16 of the
 //     time of the fp32 matrix instructions.  (The last piece is a multiple of
-//     2^-133, bf16's least number: factors below 2^-109 lose digits.)
+//     2^-133, bf16's least number: factors below 2^-109 lose digits.  First pieces
+//     are rounded up by 2^-8 of them at most, and their product by 2^-7: it may
+//     leave fp32's range where the term does not.)
 // v_mfma_f32_16x16x32_bf16 wants 8 consecutive k of one row (or column) a lane.
 // An operand whose k are contiguous in memory (K_LINES) is kept line by line and
 // read 16 bytes at a time; one whose rows (columns) are (MN_LINES) is kept as it

@@ -531,6 +531,30 @@ def test_linear_grad_values(n, k, m, T, turned):
 
 
 @gpu
+@pytest.mark.parametrize("n,k,m", [(6, 40, 30), (600, 3000, 520)])
+def test_linear_ends_of_the_range(n, k, m):
+    """fp32 terms up to 2^128 - 2^121, whose first pieces' product is the largest (1 + 2^-8)^2 of it, and infinities
+    times the smallest numbers that are not taken for zeros."""
+    from paper_2302_03851_amd import head
+    g = _gen(k)
+    x, w = torch.zeros((n, k), device="cuda"), torch.zeros((k, m), device="cuda")
+    # mantissas just above the middle between two bf16 values: their first pieces are rounded up by the most
+    up = 1 + 2.0 ** -8 + 2.0 ** -23
+    x[0, 3], w[3, 0], w[3, 1] = up * 2.0 ** 64, 2.0 ** 63 * 1.976, -(2.0 ** 63) * 1.976
+    x[1, 4], w[4, 0], w[4, 1] = up * 2.0 ** 100, up * 2.0 ** 27, -up * 2.0 ** 27
+    x[2, 5], w[5, 0], w[5, 1] = 1.98 * 2.0 ** 127, 1.0, -1.0
+    assert float((x.double() @ w.double()).abs().max()) <= 2.0 ** 128 - 2.0 ** 121
+    r = head.linear(x, w)
+    _check_linear(x, w, None, "none", None, r)
+    assert torch.isfinite(r.out).all()
+    x, w = torch.zeros((n, k), device="cuda"), torch.zeros((k, m), device="cuda")
+    x[0, 7], x[1, 7] = INF, -INF
+    w[7, :4] = torch.tensor([2.0 ** -133, -(2.0 ** -133), 2.0 ** -126, 1.5 * 2.0 ** -133], device="cuda")
+    for a, b in ((x, w), (w.t().contiguous(), x.t().contiguous())):
+        _check_linear(a, b, None, "none", None, head.linear(a, b))
+
+
+@gpu
 @pytest.mark.parametrize("scale", [1e-30, 1e-33, 1e-35, 1e-37, 1e-39])
 @pytest.mark.parametrize("T", [F32, BF16])
 def test_linear_small(T, scale):
