@@ -422,6 +422,36 @@ def test_wild_offsets(n):
 
 
 @gpu
+@pytest.mark.parametrize("n,s", [(40000, 9000), (5 * (1 << 20) + 77, 6000)])
+def test_wild_offsets_of_many(n, s):
+    """The same where tokens look for their sequences by halving, and work-groups count several chunks."""
+    from paper_2302_03851_amd import tokens
+    g = _gen(n)
+    first = torch.randint(-2 ** 31, 2 ** 31 - 1, (s + 1,), generator=g, device="cuda").to(torch.int32)
+    first[::3] = torch.randint(0, n, (first[::3].numel(),), generator=g, device="cuda").to(torch.int32)
+    sorted_half = first.clone()
+    sorted_half[: s // 2] = torch.randint(0, n, (s // 2,), generator=g, device="cuda").sort().values.to(torch.int32)
+    same = torch.full_like(first, n // 3)
+    same[0], same[s // 2:s // 2 + 2] = 0, torch.tensor([n, n // 2], dtype=torch.int32, device="cuda")
+    lp = -torch.rand(n, generator=g, device="cuda")
+    ids = (torch.arange(n, device="cuda") % 3 - 1).to(torch.int32)
+    adv = torch.randn(s, generator=g, device="cuda")
+    for f in (first, sorted_half, same):
+        mem = torch.full((n + 64,), 7.0, device="cuda")
+        small = torch.full((3 * s + 160,), 7.0, device="cuda")
+        tokens.preference_loss(lp, lp, f, mean=True, ids=ids,
+                               out=tokens.Preference(small[32:32 + s // 2], small[64 + s:64 + 2 * s].view(-1, 2), mem[32:32 + n]))
+        torch.cuda.synchronize()
+        assert (mem[:32] == 7).all() and (mem[32 + n:] == 7).all() and (small[:32] == 7).all() and (small[64 + 2 * s:] == 7).all()
+        small.fill_(7.0)
+        tokens.policy_loss(lp, lp, f, adv, ids=ids, out=tokens.Policy(
+            small[32:32 + s], small[64 + s:64 + 2 * s], small[96 + 2 * s:96 + 3 * s].view(torch.int32), mem[32:32 + n]))
+        torch.cuda.synchronize()
+        assert (mem[:32] == 7).all() and (mem[32 + n:] == 7).all() and (small[:32] == 7).all() and (small[96 + 3 * s:] == 7).all()
+        assert (small[32 + s:64 + s] == 7).all() and (small[64 + 2 * s:96 + 2 * s] == 7).all()
+
+
+@gpu
 def test_differences():
     """The gradients against central differences of the losses: steps of 2^-5; the third derivatives stay
     below 40 here, the losses' own roundings give u |loss| / step."""
