@@ -774,7 +774,8 @@ edb_status edb_layer_norm(const void* x, int32_t x_dtype, int32_t n, int32_t dim
  * h = (x - mean) rstd, g = dout weight,
  *   dx[i][:]   = rstd_i (g - average of g - h average of g h)   of x's dtype
  *   dweight[:] = sum_i dout[i][:] h[i][:],  dbias[:] = sum_i dout[i][:]   float[dim]
- * dx, dweight and dbias are each NULL where not wanted. */
+ * dx, dweight and dbias are each NULL where not wanted.  (stats are fp32: where the
+ * mean is far above the spread, h is off by 2^-24 |mean| rstd.) */
 edb_status edb_layer_norm_grad_bytes(int32_t n, int32_t dim, int32_t x_dtype, int64_t* bytes);
 edb_status edb_layer_norm_grad(const void* x, int32_t x_dtype, int32_t n, int32_t dim, int64_t x_stride,
                                const float* stats, const void* dout, int32_t dout_dtype, int64_t dout_stride,

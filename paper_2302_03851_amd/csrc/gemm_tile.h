@@ -73,7 +73,7 @@ struct Power {
 };
 
 // erfc(z) exp(z^2) / 2 of z = a / sqrt(2) >= 0, as t Q(t) with t = 1 / (1 + z / 2)
-// and Q fitted for the least largest relative error up to z = 10.6 (4.4e-8; in
+// and Q fitted for the least largest relative error up to z = 10.6 (6.0e-8; in
 // fp32 3.2e-7).
 __device__ __forceinline__ float tail(float a) {
     const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.35355339059327376f, 1.f));
@@ -454,13 +454,13 @@ struct Shape {
 };
 
 // Bound by what a compute unit's waves wait for each other: 8192^3 bf16 907 us
-// (1212 TFLOP/s; a library product 900), the matrix cores busy 60% of it, LDS 40%,
-// without bank conflicts; with 128 x 128 tiles, whose operands pass through LDS
-// half as often again, 1205.  fp32 4096^3 713 us (193 TFLOP/s of fp32; a library
-// product 910), where splitting the operands takes the vector units half as long
+// (1212 TFLOP/s; a library product, in turn with it, 668), the matrix cores busy 60%
+// of it, LDS 40%, without bank conflicts; with 128 x 128 tiles, whose operands pass
+// through LDS half as often again, 1165.  fp32 4096^3 683 us (201 TFLOP/s of fp32; a
+// library product 922), where splitting the operands takes the vector units half as long
 // as the products take the matrix cores and two work-groups of a unit overlap
 // the two only in part.  B by its columns (MN_LINES) from row-major memory takes
-// 15% longer than by K_LINES (8192^3 1038 us): twice the LDS reads.
+// 6% longer than by K_LINES (8192^3 964 us; a library product 770): twice the LDS reads.
 template <class T, Layout AL, Layout BL, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Args g) {
     using S = Shape<T, AL, BL, TM, TN, WM, WN>;

@@ -136,8 +136,8 @@ struct Product {
 // take in us: among as many others as its compute unit holds (busy, a share of
 // the unit's time) and from beginning to end (alone).  Fitted to products from
 // 1 x 512 x 131072 to 8192^3, whose best tile and split they find within 10%, as
-// (bf16, us) 8192^3 256 x 256 907, 256 x 128 1060, 128 x 128 1205; 28629 x 512 x
-// 1536 80, 86, 83; 2048 x 512 x 1536 25, 15, 13.5 and 64 x 64 10.5.
+// (bf16, us) 8192^3 256 x 256 907, 256 x 128 1097, 128 x 128 1165; 28629 x 512 x
+// 1536 68, 80, 75; 2048 x 512 x 1536 23, 15, 13 and 64 x 64 9.8.
 struct Tile {
     int32_t rows, cols, held;     // held: work-groups that a compute unit holds
     double busy, busy_out, alone, alone_out;

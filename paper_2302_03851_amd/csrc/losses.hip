@@ -701,9 +701,10 @@ __global__ __launch_bounds__(kThreads) void policy_losses(Loss l) {
 }
 
 // Up to so many tokens, and so many a pair or sequence, are taken by one launch
-// (policy, us: 32768 in 64 sequences 8.3, by the long calls' four launches 17.5; in 2
-// sequences 22 and 18, in one 40 and 17).  Where most are in one of many sequences
-// after all, its group takes those 40.
+// (policy, us: 32768 in 64 sequences 8.0, by the long calls' four launches 17; in 2
+// sequences 22 and 17, in one 40 and 17).  Where most are in one of many sequences
+// after all, its group is alone with them: 32768 in one of 64 take 95, in one of 4096,
+// where a group is a wave, 340.
 constexpr int32_t kFew = 32768, kFewEach = 8192;
 constexpr int32_t kShort = 128;    // tokens a pair or sequence, on average, up to which a wave takes it
 constexpr int32_t kMostItems = 1 << 24;

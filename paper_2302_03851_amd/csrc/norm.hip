@@ -581,7 +581,8 @@ int64_t pieces_of(int32_t dim, int k) { return ((int64_t)dim + k - 1) / k; }
 template <class T, class O, int K, int LANES, int V, int ROWS>
 void start(const NormArgs& a, hipStream_t st) {
     constexpr int kRows = threads<LANES>() / LANES * ROWS;
-    // a few turns each at most sizes (262144 x 512 bf16 125 us, with 2048 work-groups 139; 28629 x 512 17.3, 16.7)
+    // a few turns each at most sizes (262144 x 512 bf16 109 us, with 2048 work-groups 112; 28629 x 512 16.3, with one
+    // turn each, of 3579, 17.2)
     const int64_t groups = ((int64_t)a.n + kRows - 1) / kRows, most = groups > 8192 ? 8192 : 2048;
     norm_kernel<T, O, K, LANES, V, ROWS><<<(unsigned)(groups < most ? groups : most), threads<LANES>(), 0, st>>>(a);
 }
